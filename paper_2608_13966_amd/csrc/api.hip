@@ -60,7 +60,7 @@ int check_desc(const quasar_desc* d) {
 
 extern "C" {
 
-const char* quasar_version(void) { return "0.1.0"; }
+const char* quasar_version(void) { return "0.2.0"; }
 
 const char* quasar_status_string(int s) {
   switch (s) {

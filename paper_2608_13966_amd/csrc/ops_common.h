@@ -1,0 +1,163 @@
+// ops_common.h -- device helpers of the operators of quasar_ops.h: pieces of
+// eight elements at any alignment, reductions over a wavefront and a workgroup.
+#pragma once
+
+#include "device_common.h"
+
+namespace quasar {
+
+// element types of a tensor operand; kNone: no operand
+enum ElemType : int { kElemF32 = 0, kElemBF16 = 1, kElemNone = 2, kElemE4M3 = 3 };
+template <int T>
+constexpr int elem_size() { return T == kElemF32 ? 4 : T == kElemE4M3 ? 1 : 2; }
+
+// 16 bytes from or to an address of any alignment: one instruction
+// (unaligned accesses to global memory are on under HSA), so rows whose
+// stride or base is not a multiple of 16 bytes take the same code.
+__device__ __forceinline__ uint4 ld16_any(const void* p) {
+  uint4 v;
+  __builtin_memcpy(&v, p, 16);
+  return v;
+}
+__device__ __forceinline__ void st16_any(void* p, uint4 v) { __builtin_memcpy(p, &v, 16); }
+__device__ __forceinline__ uint2 ld8_any(const void* p) {
+  uint2 v;
+  __builtin_memcpy(&v, p, 8);
+  return v;
+}
+__device__ __forceinline__ void st8_any(void* p, uint2 v) { __builtin_memcpy(p, &v, 8); }
+
+// Element i of a tensor of run-time type (F32 or BF16).
+__device__ __forceinline__ float elem(const void* p, int64_t i, bool bf16) {
+  return bf16 ? as_f32((uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16) : reinterpret_cast<const float*>(p)[i];
+}
+__device__ __forceinline__ uint16_t bf16_bits(float x) { return (uint16_t)pack_bf16x2(x, 0.0f); }
+__device__ __forceinline__ void put_elem(void* p, int64_t i, float v, bool bf16) {
+  if (bf16)
+    reinterpret_cast<uint16_t*>(p)[i] = bf16_bits(v);
+  else
+    reinterpret_cast<float*>(p)[i] = v;
+}
+
+// Eight consecutive elements in their storage form; n of them exist (n >= 8:
+// all), the rest read as `fill` bits.
+template <int T>
+struct Piece;
+template <>
+struct Piece<kElemBF16> {
+  uint32_t d[4];
+  __device__ __forceinline__ void load(const void* base, int64_t e, int n, uint16_t fill = 0) {
+    const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + e;
+    if (n >= 8) {
+      const uint4 t = ld16_any(p);
+      d[0] = t.x; d[1] = t.y; d[2] = t.z; d[3] = t.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const uint32_t lo = 2 * i < n ? p[2 * i] : fill, hi = 2 * i + 1 < n ? p[2 * i + 1] : fill;
+        d[i] = lo | (hi << 16);
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    return (i & 1) ? as_f32(d[i >> 1] & 0xffff0000u) : as_f32(d[i >> 1] << 16);
+  }
+};
+template <>
+struct Piece<kElemF32> {
+  float f[8];
+  __device__ __forceinline__ void load(const void* base, int64_t e, int n, uint16_t fill = 0) {
+    const float* p = reinterpret_cast<const float*>(base) + e;
+    if (n >= 8) {
+      const uint4 a = ld16_any(p), b = ld16_any(p + 4);
+      f[0] = as_f32(a.x); f[1] = as_f32(a.y); f[2] = as_f32(a.z); f[3] = as_f32(a.w);
+      f[4] = as_f32(b.x); f[5] = as_f32(b.y); f[6] = as_f32(b.z); f[7] = as_f32(b.w);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) f[i] = i < n ? p[i] : as_f32((uint32_t)fill << 16);
+    }
+  }
+  __device__ __forceinline__ float get(int i) const { return f[i]; }
+};
+
+// Eight values to a tensor of fp32 or bf16 elements (nearest even), the first n of them.
+template <bool BF16>
+__device__ __forceinline__ void store_piece(void* base, int64_t e, const float (&v)[8], int n) {
+  if constexpr (BF16) {
+    uint16_t* p = reinterpret_cast<uint16_t*>(base) + e;
+    if (n >= 8) {
+      st16_any(p, make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                             pack_bf16x2(v[6], v[7])));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (i < n) p[i] = bf16_bits(v[i]);
+    }
+  } else {
+    float* p = reinterpret_cast<float*>(base) + e;
+    if (n >= 8) {
+      st16_any(p, make_uint4(as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])));
+      st16_any(p + 4, make_uint4(as_u32(v[4]), as_u32(v[5]), as_u32(v[6]), as_u32(v[7])));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (i < n) p[i] = v[i];
+    }
+  }
+}
+__device__ __forceinline__ void store_piece(void* base, int64_t e, const float (&v)[8], int n, bool bf16) {
+  if (bf16)
+    store_piece<true>(base, e, v, n);
+  else
+    store_piece<false>(base, e, v, n);
+}
+
+// Eight values as E4M3 bytes (nearest even; |v| <= 448 (1 + 2^-4) rounds
+// inside the format, NaN gives its NaN).
+__device__ __forceinline__ uint2 pack_e4m3x8(const float (&v)[8]) {
+  int a = 0, b = 0;
+  a = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], a, false);
+  a = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], a, true);
+  b = __builtin_amdgcn_cvt_pk_fp8_f32(v[4], v[5], b, false);
+  b = __builtin_amdgcn_cvt_pk_fp8_f32(v[6], v[7], b, true);
+  return make_uint2((uint32_t)a, (uint32_t)b);
+}
+
+// ---- reductions -------------------------------------------------------------
+// Over the wavefront's 64 lanes, every lane gets the same bits (the pairing
+// of lanes is symmetric); no LDS.  A NaN is not kept by the maximum.
+struct SumOp {
+  __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+struct MaxOp {
+  __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); }
+};
+template <typename Op>
+__device__ __forceinline__ float wave_reduce(float x, Op op) {
+  x = op(x, dpp_f32<kDppXor1>(x));
+  x = op(x, dpp_f32<kDppXor2>(x));
+  x = op(x, dpp_f32<kDppHalfMirror>(x));
+  x = op(x, dpp_f32<kDppMirror>(x));
+  x = pair_rows<16>(x, op);
+  return pair_rows<32>(x, op);
+}
+
+// Over a workgroup of WAVES wavefronts; `s`: WAVES floats of LDS that nothing
+// else uses and that the previous reduction through them is done with (one
+// barrier in between is enough: each call has one of its own).
+template <int WAVES, typename Op>
+__device__ __forceinline__ float group_reduce(float x, float* s, Op op) {
+  x = wave_reduce(x, op);
+  if constexpr (WAVES == 1) return x;
+  if ((threadIdx.x & 63) == 0) s[wave_index()] = x;
+  __syncthreads();
+  x = s[0];
+#pragma unroll
+  for (int i = 1; i < WAVES; i++) x = op(x, s[i]);
+  return x;
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+}  // namespace quasar
