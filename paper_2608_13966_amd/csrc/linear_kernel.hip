@@ -19,9 +19,28 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 v) { return __builtin_bit_cast(bf16x8, v); }
+
+// fma(s, v, z) in fp32, v the fp16 number in the low or high half of x.  A code
+// q at bit o of a half (q 2^o < 2^10) is the subnormal q 2^(o - 24), which the
+// instruction takes exactly: with s 2^(24 - o) in s's place it is fma(s, q, z)
+// without a conversion.
+template <bool HIGH>
+__device__ __forceinline__ float fma_half(float s, uint32_t x, float z) {
+  float r;
+  if constexpr (HIGH)
+    asm("v_fma_mix_f32 %0, %1, %2, %3 op_sel:[0,1,0] op_sel_hi:[0,1,0]" : "=v"(r) : "v"(s), "v"(x), "v"(z));
+  else
+    asm("v_fma_mix_f32 %0, %1, %2, %3 op_sel_hi:[0,1,0]" : "=v"(r) : "v"(s), "v"(x), "v"(z));
+  return r;
+}
+
+// Two E4M3 bytes (of the low or the high half of x) as packed bf16; exact.
+template <bool HIGH>
+__device__ __forceinline__ uint32_t e4m3_bf16(uint32_t x) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, HIGH));
+}
 
 struct Weights {  // what r is made from
   const uint8_t* codes;
@@ -29,50 +48,88 @@ struct Weights {  // what r is made from
   const float* zeros;
   const float* tensor_scale;
   int64_t rows, cols;
-  int group;
+  int shift;  // a group is 2^shift columns (INT)
+};
+
+// Where one row's codes and parameters lie.
+template <int FMT, int BITS>
+struct WeightRow {
+  const uint8_t* codes;
+  const uint8_t* scales;
+  const float* zeros;
+  float tensor_scale;
+  int shift;
+
+  __device__ __forceinline__ WeightRow(const Weights& w, int64_t row) {
+    shift = w.shift;
+    if constexpr (FMT == QUASAR_RUBIN_INT3) {
+      const int64_t block = (row >> 3) * (w.cols >> 6);
+      codes = w.codes + block * 192 + (row & 7) * 24;
+      scales = reinterpret_cast<const uint8_t*>(w.scales) + block * 8;
+    } else if constexpr (FMT == QUASAR_NVFP4) {
+      codes = w.codes + row * (w.cols >> 1);
+      scales = reinterpret_cast<const uint8_t*>(w.scales) + row * (w.cols >> 4);
+      tensor_scale = w.tensor_scale[0];
+    } else {
+      const int64_t g = row * (w.cols >> w.shift);
+      codes = w.codes + row * (w.cols >> 3) * BITS;
+      scales = reinterpret_cast<const uint8_t*>(w.scales) + 4 * g;
+      if constexpr (FMT == QUASAR_INT) zeros = w.zeros + g;
+    }
+  }
 };
 
 // 32 consecutive weights of one row from element k on (k % 32 == 0), n of
 // which exist (n >= 32: all; less only at a row's end: 16 for NVFP4, or <= 0,
-// none).  load() issues the loads, chunk(i) gives weights 8i .. 8i+7 in bf16,
-// 0 where none exists.
+// none).  load() issues the loads, ready() follows before the first chunk();
+// chunk(i) gives weights 8i .. 8i+7 in bf16, 0 where none exists.
 template <int FMT, int BITS>
 struct Strip {
+  static constexpr int kOffsets = 10 / BITS;  // codes of a half that are subnormals where they are
   uint32_t d[BITS];    // the codes: 32 * BITS bits
-  float s[2], z;       // NVFP4: the scales of the two blocks
-  uint32_t book[2];    // RUBIN: the eight E4M3 entries
-  int n;
+  uint32_t p[2];       // the parameters as loaded: s and z, the two E4M3 scales, or the eight E4M3 entries
+  float s[5], z;       // INT: s 2^(24 - BITS i) and z; NVFP4: the blocks' scales
 
-  __device__ __forceinline__ void load(const Weights& w, int64_t row, int k, int left) {
-    n = left;
-    s[0] = s[1] = z = 0.0f;
+  // all 32 exist
+  __device__ __forceinline__ void load(const WeightRow<FMT, BITS>& w, int k) {
+    if constexpr (FMT == QUASAR_RUBIN_INT3) {
+      __builtin_memcpy(d, w.codes + (k >> 6) * 192 + ((k >> 5) & 1) * 12, 12);
+      __builtin_memcpy(p, w.scales + (k >> 6) * 8, 8);
+    } else {
+      __builtin_memcpy(d, w.codes + (k >> 3) * BITS, 4 * BITS);
+      if constexpr (FMT == QUASAR_NVFP4) {
+        uint16_t e;
+        __builtin_memcpy(&e, w.scales + (k >> 4), 2);
+        p[0] = e;
+      } else {
+        const int g = k >> w.shift;
+        p[0] = reinterpret_cast<const uint32_t*>(w.scales)[g];
+        p[1] = FMT == QUASAR_INT ? as_u32(w.zeros[g]) : 0u;
+      }
+    }
+  }
+  __device__ __forceinline__ void load(const WeightRow<FMT, BITS>& w, int k, int n) {
+    p[0] = p[1] = 0u;
 #pragma unroll
     for (int i = 0; i < BITS; i++) d[i] = 0u;
-    if (n <= 0) return;
-    if constexpr (FMT == QUASAR_RUBIN_INT3) {
-      const int64_t block = (row >> 3) * (w.cols >> 6) + (k >> 6);
-      const uint8_t* p = w.codes + block * 192 + (row & 7) * 24 + ((k & 63) >> 5) * 12;
-      __builtin_memcpy(d, p, 12);
-      const uint2 b = ld8_any(reinterpret_cast<const uint8_t*>(w.scales) + block * 8);
-      book[0] = b.x;
-      book[1] = b.y;
-    } else {
-      const uint8_t* p = w.codes + (row * w.cols + k) * BITS / 8;
-      if (FMT != QUASAR_NVFP4 || n >= 32)
-        __builtin_memcpy(d, p, 4 * BITS);
-      else
-        __builtin_memcpy(d, p, 8);
-      if constexpr (FMT == QUASAR_NVFP4) {
-        const uint8_t* e = reinterpret_cast<const uint8_t*>(w.scales) + row * (w.cols >> 4) + (k >> 4);
-        const float st = w.tensor_scale[0];
-        s[0] = st * __builtin_amdgcn_cvt_f32_fp8((int)e[0], 0);
-        if (n >= 32) s[1] = st * __builtin_amdgcn_cvt_f32_fp8((int)e[1], 0);
-      } else {
-        const int64_t g = row * (w.cols / w.group) + k / w.group;
-        s[0] = reinterpret_cast<const float*>(w.scales)[g];
-        // symmetric codes are offset by 2^(b-1): s q = fma(s, q + 2^(b-1), -2^(b-1) s), rounded once either way
-        z = FMT == QUASAR_INT ? w.zeros[g] : s[0] * (float)-(1 << (BITS - 1));
-      }
+    if (n >= 32) {
+      load(w, k);
+    } else if (FMT == QUASAR_NVFP4 && n > 0) {
+      __builtin_memcpy(d, w.codes + (k >> 1), 8);
+      p[0] = w.scales[k >> 4];
+    }
+  }
+
+  __device__ __forceinline__ void ready(float tensor_scale) {
+    if constexpr (FMT == QUASAR_NVFP4) {
+      s[0] = tensor_scale * __builtin_amdgcn_cvt_f32_fp8((int)p[0], 0);
+      s[1] = tensor_scale * __builtin_amdgcn_cvt_f32_fp8((int)p[0], 1);
+    } else if constexpr (FMT != QUASAR_RUBIN_INT3) {
+      const float f = as_f32(p[0]);
+      // symmetric codes are offset by 2^(b-1): s q = fma(s, q + 2^(b-1), -2^(b-1) s), rounded once either way
+      z = FMT == QUASAR_INT_SYM ? f * (float)-(1 << (BITS - 1)) : as_f32(p[1]);
+#pragma unroll
+      for (int i = 0; i < kOffsets; i++) s[i] = f * (float)(1 << (24 - BITS * i));
     }
   }
 
@@ -93,40 +150,54 @@ struct Strip {
       for (int h = 0; h < 2; h++) {
         const uint32_t u = v >> (12 * h);
         const uint32_t sel = (u & 7u) | ((u << 5) & 0x700u) | ((u << 10) & 0x70000u) | ((u << 15) & 0x7000000u);
-        const int b = (int)__builtin_amdgcn_perm(book[1], book[0], sel);
-        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(b, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(b, true);
-        o[2 * h] = pack_bf16x2(lo[0], lo[1]);
-        o[2 * h + 1] = pack_bf16x2(hi[0], hi[1]);
+        const uint32_t b = __builtin_amdgcn_perm(p[1], p[0], sel);
+        o[2 * h] = e4m3_bf16<false>(b);
+        o[2 * h + 1] = e4m3_bf16<true>(b);
       }
-      if (n <= 0) o[0] = o[1] = o[2] = o[3] = 0u;
     } else {
-      float q[8];
+      float v[8];
       if constexpr (BITS == 4) {
         const uint32_t c = FMT == QUASAR_INT ? d[i] : d[i] ^ 0x88888888u;
-        const uint32_t e = c & 0x0f0f0f0fu, f = (c >> 4) & 0x0f0f0f0fu;
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          q[2 * j] = (float)((e >> (8 * j)) & 0xffu);
-          q[2 * j + 1] = (float)((f >> (8 * j)) & 0xffu);
-        }
+        pair<0>(c, v[0], v[4]);
+        pair<1>(c, v[1], v[5]);
+        pair<0>(c >> 8, v[2], v[6]);
+        pair<1>(c >> 8, v[3], v[7]);
       } else if constexpr (BITS == 2) {
-        const uint32_t c = (FMT == QUASAR_INT ? d[i >> 1] : d[i >> 1] ^ 0xaaaaaaaau);
-#pragma unroll
-        for (int j = 0; j < 4; j++) {
-          const uint32_t m = (c >> (2 * j)) & 0x03030303u;
-          q[j] = (float)((m >> (16 * (i & 1))) & 0xffu);
-          q[4 + j] = (float)((m >> (16 * (i & 1) + 8)) & 0xffu);
+        // chunk 2 j is the low halves of dword j's, chunk 2 j + 1 the high ones
+        const uint32_t c = FMT == QUASAR_INT ? d[i >> 1] : d[i >> 1] ^ 0xaaaaaaaau;
+        if (i & 1) {
+          half<0, true>(c, v[0]); half<1, true>(c, v[1]); half<2, true>(c, v[2]); half<3, true>(c, v[3]);
+          half<4, true>(c, v[4]); half<0, true>(c >> 10, v[5]); half<1, true>(c >> 10, v[6]); half<2, true>(c >> 10, v[7]);
+        } else {
+          half<0, false>(c, v[0]); half<1, false>(c, v[1]); half<2, false>(c, v[2]); half<3, false>(c, v[3]);
+          half<4, false>(c, v[4]); half<0, false>(c >> 10, v[5]); half<1, false>(c >> 10, v[6]); half<2, false>(c >> 10, v[7]);
         }
       } else {
         const uint32_t c = FMT == QUASAR_INT ? bits24(i) : bits24(i) ^ 0x924924u;
-#pragma unroll
-        for (int j = 0; j < 8; j++) q[j] = (float)((c >> (3 * j)) & 7u);
+        const uint32_t e = (c & 0x7fffu) | ((c >> 15) << 16);  // codes 0 .. 4, and 5 .. 7 from bit 16 on
+        pair<0>(e, v[0], v[5]);
+        pair<1>(e, v[1], v[6]);
+        pair<2>(e, v[2], v[7]);
+        half<0, false>(e >> 9, v[3]);
+        half<1, false>(e >> 9, v[4]);
       }
 #pragma unroll
-      for (int j = 0; j < 4; j++)
-        o[j] = pack_bf16x2(__builtin_fmaf(s[0], q[2 * j], z), __builtin_fmaf(s[0], q[2 * j + 1], z));
+      for (int j = 0; j < 4; j++) o[j] = pack_bf16x2(v[2 * j], v[2 * j + 1]);
     }
     return make_uint4(o[0], o[1], o[2], o[3]);
+  }
+
+  // the weights of the codes that lie J codes from bit 0 of the halves of c
+  template <int J>
+  static constexpr uint32_t kMask = ((1u << BITS) - 1u) << (BITS * J) | ((1u << BITS) - 1u) << (BITS * J + 16);
+  template <int J>
+  __device__ __forceinline__ void pair(uint32_t c, float& lo, float& hi) const {
+    lo = fma_half<false>(s[J], c & kMask<J>, z);
+    hi = fma_half<true>(s[J], c & kMask<J>, z);
+  }
+  template <int J, bool HIGH>
+  __device__ __forceinline__ void half(uint32_t c, float& v) const {
+    v = fma_half<HIGH>(s[J], c & kMask<J>, z);
   }
 
   // bits 24 i .. 24 i + 23 of a 3-bit strip
@@ -138,19 +209,32 @@ struct Strip {
   }
 };
 
-// Eight activations from element e of x in bf16.
+// Eight activations as fetched, and in bf16; all 0 where `has` is false.
 template <int XT>
-__device__ __forceinline__ uint4 load_x8(const void* x, int64_t e) {
-  if constexpr (XT == kElemBF16) {
-    return ld16_any(reinterpret_cast<const uint16_t*>(x) + e);
-  } else {
-    const uint2 b = ld8_any(reinterpret_cast<const uint8_t*>(x) + e);
-    const auto p = __builtin_amdgcn_cvt_pk_f32_fp8((int)b.x, false), q = __builtin_amdgcn_cvt_pk_f32_fp8((int)b.x, true);
-    const auto r = __builtin_amdgcn_cvt_pk_f32_fp8((int)b.y, false), t = __builtin_amdgcn_cvt_pk_f32_fp8((int)b.y, true);
-    return make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(q[0], q[1]), pack_bf16x2(r[0], r[1]),
-                      pack_bf16x2(t[0], t[1]));
+struct XChunk {
+  uint32_t d[XT == kElemBF16 ? 4 : 2];
+  __device__ __forceinline__ void load(const void* x, int64_t e) {
+    if constexpr (XT == kElemBF16) {
+      const uint4 t = ld16_any(reinterpret_cast<const uint16_t*>(x) + e);
+      d[0] = t.x; d[1] = t.y; d[2] = t.z; d[3] = t.w;
+    } else {
+      const uint2 t = ld8_any(reinterpret_cast<const uint8_t*>(x) + e);
+      d[0] = t.x; d[1] = t.y;
+    }
   }
-}
+  __device__ __forceinline__ void load(const void* x, int64_t e, bool has) {
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(d) / 4); i++) d[i] = 0u;
+    if (has) load(x, e);
+  }
+  __device__ __forceinline__ uint4 bf16() const {
+    if constexpr (XT == kElemBF16) {
+      return make_uint4(d[0], d[1], d[2], d[3]);
+    } else {
+      return make_uint4(e4m3_bf16<false>(d[0]), e4m3_bf16<true>(d[0]), e4m3_bf16<false>(d[1]), e4m3_bf16<true>(d[1]));
+    }
+  }
+};
 
 __device__ __forceinline__ float activate(float v, int act) {
   if (act == QUASAR_ACT_RELU) return v < 0.0f ? 0.0f : v;  // NaN stays
@@ -160,75 +244,429 @@ __device__ __forceinline__ float activate(float v, int act) {
 }
 
 // ---- few tokens ---------------------------------------------------------------
-// A workgroup makes 16 outputs of r's rows for TT * 16 tokens; its wavefronts
-// split the columns in steps of 128 and meet in LDS.  The lane of row l % 16
-// and quarter l / 16 decodes the 32 weights of its quarter of a step; matrix
-// instruction i takes the eighths i of all four quarters, x likewise (the
-// order of the columns inside a sum is free).
+// The codes and parameters of 16 rows x 128 columns in LDS, and how a
+// wavefront brings them there: a lane's load is a 16-byte piece whose
+// neighbours in memory are its neighbours' (loaded in the order in which the
+// matrix instruction wants them, every lane's would be a cache access of its
+// own: that took twice as long at one token).
+template <int FMT, int BITS>
+struct Block16 {
+  static constexpr bool kRubin = FMT == QUASAR_RUBIN_INT3, kNv = FMT == QUASAR_NVFP4;
+  static constexpr int kPieces = 16 * BITS;  // 16-byte pieces of codes
+  static constexpr int kBytes = 16 * kPieces + 256;
+
+  // Of the 16 rows from n0 on: where they lie (the same in every lane), and
+  // this lane's piece and parameters from there.
+  struct Place {
+    const uint8_t *codes, *par, *zero;
+    uint32_t piece, first;  // bytes
+    int at;                 // LDS offset of the piece
+    int shift;              // a group is 2^shift columns (INT)
+    float tensor_scale;
+
+    __device__ __forceinline__ Place(const Weights& w, int64_t n0, int lane) {
+      shift = w.shift;
+      const int last = (int)(w.rows - 1 - n0 < 15 ? w.rows - 1 - n0 : 15);  // rows past the matrix: its last one's
+      if constexpr (kRubin) {
+        const int b = lane / 12, i = lane - 12 * b;
+        const uint32_t wide = (uint32_t)(w.cols >> 6);
+        codes = w.codes + (n0 >> 3) * (w.cols >> 6) * 192;
+        par = reinterpret_cast<const uint8_t*>(w.scales) + (n0 >> 3) * (w.cols >> 6) * 8;
+        piece = (((b >> 1) & (last >> 3)) * wide + (b & 1)) * 192 + 16 * i;
+        first = (((lane >> 1) & (last >> 3)) * wide + (lane & 1)) * 8;
+        at = b * 192 + 16 * i;
+      } else {
+        const int r = BITS == 4 ? lane >> 2 : BITS == 2 ? lane >> 1 : lane / 3, i = lane - r * BITS;
+        codes = w.codes + n0 * (w.cols >> 3) * BITS;
+        piece = (uint32_t)(r < last ? r : last) * (uint32_t)(w.cols >> 3) * BITS + 16 * i;
+        // four pieces a row: rows 4 apart use other banks
+        at = BITS == 4 ? 64 * r + 16 * (i ^ ((r >> 2) & 3)) : (r * BITS + i) * 16;
+        if constexpr (kNv) {
+          par = reinterpret_cast<const uint8_t*>(w.scales) + n0 * (w.cols >> 4);
+          first = (uint32_t)((lane & 15) < last ? lane & 15 : last) * (uint32_t)(w.cols >> 4);
+          tensor_scale = w.tensor_scale[0];
+        } else {
+          const int per = 7 - shift, pr = (lane >> per) & 15;
+          const int64_t e = n0 * (w.cols >> shift);
+          par = reinterpret_cast<const uint8_t*>(w.scales) + 4 * e;
+          first = 4 * ((uint32_t)(pr < last ? pr : last) * (uint32_t)(w.cols >> shift) + (lane & per));
+          if constexpr (FMT == QUASAR_INT) zero = reinterpret_cast<const uint8_t*>(w.zeros + e);
+        }
+      }
+    }
+  };
+  uint4 c;
+  uint32_t p[2];
+
+  // columns k .. k + 127
+  __device__ __forceinline__ void load(const Place& w, int k, int lane) {
+    if (kPieces == 64 || lane < kPieces) c = ld16_any(w.codes + (kRubin ? (k >> 6) * 192 : (k >> 3) * BITS) + w.piece);
+    if constexpr (kRubin || kNv) {
+      if (lane < (kRubin ? 4 : 16)) {
+        const uint2 t = ld8_any(w.par + (kRubin ? (k >> 6) * 8 : k >> 4) + w.first);
+        p[0] = t.x;
+        p[1] = t.y;
+      }
+    } else if (lane < (16 << (7 - w.shift))) {
+      p[0] = *reinterpret_cast<const uint32_t*>(w.par + 4 * (k >> w.shift) + w.first);
+      if constexpr (FMT == QUASAR_INT) p[1] = *reinterpret_cast<const uint32_t*>(w.zero + 4 * (k >> w.shift) + w.first);
+    }
+  }
+
+  __device__ __forceinline__ void put(const Place& w, char* lds, int lane) const {
+    if (kPieces == 64 || lane < kPieces) *reinterpret_cast<uint4*>(lds + w.at) = c;
+    uint32_t* q = reinterpret_cast<uint32_t*>(lds + 16 * kPieces);
+    if constexpr (kRubin || kNv) {
+      if (lane < (kRubin ? 4 : 16)) *reinterpret_cast<uint2*>(q + 2 * lane) = make_uint2(p[0], p[1]);
+    } else if (lane < (16 << (7 - w.shift))) {
+      q[lane] = p[0];
+      if constexpr (FMT == QUASAR_INT) q[32 + lane] = p[1];
+    }
+  }
+
+  // the 32 weights of row r and quarter q
+  static __device__ __forceinline__ void get(const Place& w, const char* lds, int r, int q, Strip<FMT, BITS>& o) {
+    const char* par = lds + 16 * kPieces;
+    if constexpr (kRubin) {
+      const int b = (r >> 3) * 2 + (q >> 1);
+      const uint32_t* d = reinterpret_cast<const uint32_t*>(lds + b * 192 + (r & 7) * 24 + (q & 1) * 12);
+      o.d[0] = d[0]; o.d[1] = d[1]; o.d[2] = d[2];
+      const uint2 t = *reinterpret_cast<const uint2*>(par + 8 * b);
+      o.p[0] = t.x;
+      o.p[1] = t.y;
+      o.ready(0.0f);
+    } else {
+      if constexpr (BITS == 4) {
+        const uint4 t = *reinterpret_cast<const uint4*>(lds + 64 * r + 16 * (q ^ ((r >> 2) & 3)));
+        o.d[0] = t.x; o.d[1] = t.y; o.d[2] = t.z; o.d[3] = t.w;
+      } else if constexpr (BITS == 2) {
+        const uint2 t = *reinterpret_cast<const uint2*>(lds + 32 * r + 8 * q);
+        o.d[0] = t.x; o.d[1] = t.y;
+      } else {
+        const uint32_t* d = reinterpret_cast<const uint32_t*>(lds + 48 * r + 12 * q);
+        o.d[0] = d[0]; o.d[1] = d[1]; o.d[2] = d[2];
+      }
+      if constexpr (kNv) {
+        o.p[0] = *reinterpret_cast<const uint16_t*>(par + 8 * r + 2 * q);
+        o.ready(w.tensor_scale);
+      } else {
+        const int per = 7 - w.shift, e = (r << per) + ((32 * q) >> w.shift);
+        o.p[0] = reinterpret_cast<const uint32_t*>(par)[e];
+        o.p[1] = FMT == QUASAR_INT ? reinterpret_cast<const uint32_t*>(par)[32 + e] : 0u;
+        o.ready(0.0f);
+      }
+    }
+  }
+};
+
+// A workgroup makes 16 outputs for up to 4 NX tokens (NX 1, 2, 4, or 8 for 32);
+// its wavefronts split the columns in steps of 128 and meet in LDS.  The lane
+// of row l % 16 and quarter l / 16 decodes the 32 weights of its quarter of a
+// step; matrix instruction i takes the eighths i of all four quarters, x
+// likewise (the order of the columns inside a sum is free).  Both operands go
+// through the wavefront's own part of LDS; the next step's loads are in flight
+// meanwhile.  (Two or four steps in flight, or 4 or 16 wavefronts, were up to
+// 25% slower at 4096 x 4096 to 14336 x 4096 and 1 to 32 tokens: registers and
+// LDS then hold fewer wavefronts.)
 constexpr int kStripWaves = 8;
-template <int FMT, int BITS, int XT, int TT>
+template <int FMT, int BITS, int XT, int NX>
 __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quasar_linear a) {
-  __shared__ float red[kStripWaves][TT][4][64];
+  constexpr int kTokens = 4 * NX, TT = kTokens > 16 ? 2 : 1;
+  constexpr int kPart = Block16<FMT, BITS>::kBytes + kTokens * 256;
+  __shared__ __align__(16) char lds[kStripWaves * kPart];
+  static_assert(kPart >= TT * 1024, "the partial sums fit");
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int r16 = lane & 15, quarter = lane >> 4;
+  char* const mine = lds + wave * kPart;
+  char* const xs = mine + Block16<FMT, BITS>::kBytes;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  const int64_t t0 = (int64_t)blockIdx.y * (16 * TT);
-  const int64_t row = n0 + r16 < w.rows ? n0 + r16 : w.rows - 1;
-  const int K = (int)w.cols, steps = (K + 127) / 128, per = (steps + kStripWaves - 1) / kStripWaves;
-  const int s0 = wave * per, s1 = s0 + per < steps ? s0 + per : steps;
-  int64_t xe[TT];
+  // whole steps, in shares that differ by one at the most; the columns past them are the last wavefront's
+  const int K = (int)w.cols, steps = K / 128;
+  const int s0 = steps * wave / kStripWaves, s1 = steps * (wave + 1) / kStripWaves;
+  const typename Block16<FMT, BITS>::Place place(w, n0, lane);
+  struct Fetched {
+    Block16<FMT, BITS> w;
+    XChunk<XT> x[NX];
+  } f = {};
+  // x: 8 columns a lane, 16 lanes a token; NX times 4 tokens
+  const int kk = lane & 15, tokens = (int)a.tokens;
+  int64_t xe[NX];  // tokens past the last are not read: they only reach outputs that are not stored
 #pragma unroll
-  for (int t = 0; t < TT; t++) {
-    const int64_t token = t0 + 16 * t + r16;
-    xe[t] = (token < a.tokens ? token : a.tokens - 1) * a.x_stride;
-  }
+  for (int i = 0; i < NX; i++) xe[i] = (4 * i + (lane >> 4)) * a.x_stride + 8 * kk;
+  const auto fetch = [&](Fetched& o, int s) {
+    o.w.load(place, s * 128, lane);
+#pragma unroll
+    for (int i = 0; i < NX; i++)
+      if (4 * i + (lane >> 4) < tokens) o.x[i].load(a.x, xe[i] + s * 128);
+  };
   f32x4 acc[TT];
 #pragma unroll
   for (int t = 0; t < TT; t++) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 2
-  for (int s = s0; s < s1; s++) {
-    const int k = s * 128 + quarter * 32;
-    Strip<FMT, BITS> strip;
-    strip.load(w, row, k, K - k);
-    uint4 x[TT][4];
-#pragma unroll
-    for (int t = 0; t < TT; t++)
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        x[t][i] = make_uint4(0u, 0u, 0u, 0u);
-        if (k + 8 * i < K) x[t][i] = load_x8<XT>(a.x, xe[t] + k + 8 * i);
-      }
+  // token t's eighth e of a step lies at chunk e * kTokens + (t ^ e % kTokens): both sides without bank conflicts
+  const auto multiply = [&](Strip<FMT, BITS>& strip) {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
       const bf16x8 r = as_bf16x8(strip.chunk(i));
 #pragma unroll
-      for (int t = 0; t < TT; t++)
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r, as_bf16x8(x[t][i]), acc[t], 0, 0, 0);
+      for (int t = 0; t < TT; t++) {
+        const int e = 4 * quarter + i, col = (16 * t + r16) & (kTokens - 1);
+        const uint4 x = *reinterpret_cast<const uint4*>(xs + 16 * (e * kTokens + (col ^ (e & (kTokens - 1)))));
+        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r, as_bf16x8(x), acc[t], 0, 0, 0);
+      }
     }
+  };
+  const auto put_x = [&](int i, const XChunk<XT>& x) {
+    const int t = 4 * i + (lane >> 4);
+    *reinterpret_cast<uint4*>(xs + 16 * (kk * kTokens + (t ^ (kk & (kTokens - 1))))) = x.bf16();
+  };
+  if (s0 < s1) fetch(f, s0);
+  for (int s = s0; s < s1; s++) {
+    wave_lds_fence();
+    f.w.put(place, mine, lane);
+#pragma unroll
+    for (int i = 0; i < NX; i++) put_x(i, f.x[i]);
+    if (s + 1 < s1) fetch(f, s + 1);
+    wave_lds_fence();
+    Strip<FMT, BITS> strip;
+    Block16<FMT, BITS>::get(place, mine, r16, quarter, strip);
+    multiply(strip);
   }
+  if (wave == kStripWaves - 1 && steps * 128 < K) {
+    const int k = steps * 128 + quarter * 32;
+    const WeightRow<FMT, BITS> row(w, n0 + r16 < w.rows ? n0 + r16 : w.rows - 1);
+    Strip<FMT, BITS> strip;
+    strip.load(row, k, K - k);
+    strip.ready(row.tensor_scale);
+    wave_lds_fence();
+#pragma unroll
+    for (int i = 0; i < NX; i++) {
+      const int t = 4 * i + (lane >> 4);
+      XChunk<XT> x;
+      x.load(a.x, t * a.x_stride + steps * 128 + 8 * kk, t < tokens && steps * 128 + 8 * kk < K);
+      put_x(i, x);
+    }
+    wave_lds_fence();
+    multiply(strip);
+  }
+  wave_lds_fence();
+  float* const sums = reinterpret_cast<float*>(mine);
 #pragma unroll
   for (int t = 0; t < TT; t++)
 #pragma unroll
-    for (int i = 0; i < 4; i++) red[wave][t][i][lane] = acc[t][i];
+    for (int i = 0; i < 4; i++) sums[(4 * t + i) * 64 + lane] = acc[t][i];
   __syncthreads();
   for (int o = threadIdx.x; o < 256 * TT; o += 64 * kStripWaves) {
     const int n = o & 15, t = o >> 4;
-    const int64_t token = t0 + t;
-    if (n0 + n >= w.rows || token >= a.tokens) continue;
+    if (n0 + n >= w.rows || t >= tokens) continue;
     float v = 0.0f;
 #pragma unroll
-    for (int q = 0; q < kStripWaves; q++) v += red[q][t >> 4][n & 3][(n >> 2) * 16 + (t & 15)];
-    if (a.x_scale) v *= a.x_scale[token];
+    for (int q = 0; q < kStripWaves; q++)
+      v += reinterpret_cast<const float*>(lds + q * kPart)[(4 * (t >> 4) + (n & 3)) * 64 + (n >> 2) * 16 + (t & 15)];
+    if (a.x_scale) v *= a.x_scale[t];
     if (a.bias) v += elem(a.bias, n0 + n, a.bias_dtype == QUASAR_BF16);
     v = activate(v, a.act);
-    if (a.residual) v += elem(a.residual, token * a.residual_stride + n0 + n, a.residual_dtype == QUASAR_BF16);
-    put_elem(a.y, token * a.y_stride + n0 + n, v, a.y_dtype == QUASAR_BF16);
+    if (a.residual) v += elem(a.residual, t * a.residual_stride + n0 + n, a.residual_dtype == QUASAR_BF16);
+    put_elem(a.y, t * a.y_stride + n0 + n, v, a.y_dtype == QUASAR_BF16);
   }
 }
 
-// ---- many tokens --------------------------------------------------------------
-constexpr int kTileK = 64;  // columns a tile step takes: 128 bytes of a row
+// ---- tiles ----------------------------------------------------------------------
+constexpr int kTileK = 64;  // columns a tile step takes: 128 bytes of a row in bf16
 
+// In LDS, 16-byte chunk c of row m of a step lies at chunk c ^ (m / 2 % 8) of
+// the row's 128 bytes: the 16 rows that an operand read or a store touches at
+// one chunk then lie in 16 different groups of four banks.
+__device__ __forceinline__ int chunk_at(int m, int c) { return m * kTileK + 8 * (c ^ ((m >> 1) & 7)); }
+
+// Eight neighbouring outputs (`left` of them exist) of token `token`, from
+// output n on: scale, bias, activation, residual, store.
+__device__ __forceinline__ void finish8(const quasar_linear& a, int64_t token, int64_t n, int left, float (&v)[8]) {
+  if (a.x_scale) {
+    const float f = a.x_scale[token];
+#pragma unroll
+    for (int q = 0; q < 8; q++) v[q] *= f;
+  }
+  const auto add = [&](const void* p, int64_t e, bool bf16) {
+    if (bf16) {
+      Piece<kElemBF16> b;
+      b.load(p, e, left);
+#pragma unroll
+      for (int q = 0; q < 8; q++) v[q] += b.get(q);
+    } else {
+      Piece<kElemF32> b;
+      b.load(p, e, left);
+#pragma unroll
+      for (int q = 0; q < 8; q++) v[q] += b.get(q);
+    }
+  };
+  if (a.bias) add(a.bias, n, a.bias_dtype == QUASAR_BF16);
+  if (a.act != QUASAR_ACT_NONE) {
+#pragma unroll
+    for (int q = 0; q < 8; q++) v[q] = activate(v[q], a.act);
+  }
+  if (a.residual) add(a.residual, token * a.residual_stride + n, a.residual_dtype == QUASAR_BF16);
+  store_piece(a.y, token * a.y_stride + n, v, left, a.y_dtype == QUASAR_BF16);
+}
+
+// A wavefront's tile of 16 TM tokens x 64 outputs from its accumulators
+// (acc[i][j][e]: token 16 i + 4 (lane / 16) + e, output 16 j + lane % 16), 32
+// tokens at a time through its part `st` of LDS (kSlab floats), so that y is
+// written 16 bytes a lane.  part: the sums go there [tokens, rows] instead.
+constexpr int kSlabPitch = 64 + 4, kSlab = 32 * kSlabPitch;
+template <int TM>
+__device__ __forceinline__ void store_tile(const quasar_linear& a, int64_t rows, const f32x4 (&acc)[TM][4], int64_t m0,
+                                           int64_t n0, float* st, float* part) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int s = 0; s < TM / 2; s++) {
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+          st[(16 * i + 4 * (lane >> 4) + e) * kSlabPitch + 16 * j + (lane & 15)] = acc[2 * s + i][j][e];
+    wave_lds_fence();
+#pragma unroll 1
+    for (int p = 0; p < 32; p += 8) {
+      const int tr = p + (lane >> 3), c = (lane & 7) * 8;
+      const int64_t token = m0 + 32 * s + tr, n = n0 + c;
+      if (token < a.tokens && n < rows) {
+        const int left = (int)(rows - n < 8 ? rows - n : 8);
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; q++) v[q] = st[tr * kSlabPitch + c + q];
+        if (part)
+          store_piece<false>(part, token * rows + n, v, left);
+        else
+          finish8(a, token, n, left, v);
+      }
+    }
+    wave_lds_fence();
+  }
+}
+
+// ---- a middling number of tokens -------------------------------------------------
+// A workgroup makes BM tokens x 128 outputs over its share of the columns
+// (split of splits), in steps of 128.  Each thread fetches its weights and
+// activations of the next two steps into registers while this one is
+// multiplied, and turns them into bf16 in LDS after it, so r is never written to memory.
+// LDS holds one step: another workgroup of the CU multiplies meanwhile.
+// Chunk c of row m of a step lies at chunk c ^ m % 16 of the row's 256 bytes.
+constexpr int kFusedK = 128;
+__device__ __forceinline__ int wide_at(int m, int c) { return m * kFusedK + 8 * (c ^ (m & 15)); }
+
+template <int FMT, int BITS, int XT, int BM>
+__global__ __launch_bounds__(256, BM == 64 ? 3 : 2) void fused_kernel(Weights w, quasar_linear a, int tiles_m, int splits,
+                                                                      int steps_per, float* part) {
+  constexpr int TM = BM / 32, NX = BM / 16;  // 16-token tiles of a wavefront; chunks of x a thread fetches
+  __shared__ __align__(16) uint16_t lds[(BM + 128) * kFusedK];
+  static_assert(4 * kSlab * 4 <= (int)sizeof(lds), "the epilogue's stage fits");
+  uint16_t* const xs = lds;
+  uint16_t* const rs = lds + BM * kFusedK;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
+  const int split = blockIdx.x % (unsigned)splits, tile = blockIdx.x / (unsigned)splits;
+  const int64_t m0 = (int64_t)(tile % tiles_m) * BM, n0 = (int64_t)(tile / tiles_m) * 128;
+  const int K = (int)w.cols, all = (K + kFusedK - 1) / kFusedK;
+  const int s0 = split * steps_per, s1 = s0 + steps_per < all ? s0 + steps_per : all;
+
+  // this thread's quarter of the step in rows tid / 4 and 64 + tid / 4 of r; its chunk of x in rows tid / 16 + 16 i
+  const int wr = tid >> 2, wq = tid & 3, xr = tid >> 4, xc = tid & 15;
+  const WeightRow<FMT, BITS> row0(w, n0 + wr < w.rows ? n0 + wr : w.rows - 1);
+  const WeightRow<FMT, BITS> row1(w, n0 + 64 + wr < w.rows ? n0 + 64 + wr : w.rows - 1);
+  const char* xp[NX];
+#pragma unroll
+  for (int i = 0; i < NX; i++) {
+    const int64_t m = m0 + xr + 16 * i;
+    xp[i] = reinterpret_cast<const char*>(a.x) + ((m < a.tokens ? m : a.tokens - 1) * a.x_stride + 8 * xc) * elem_size<XT>();
+  }
+  struct Fetched {
+    Strip<FMT, BITS> w[2];
+    XChunk<XT> x[NX];
+  } f[2];
+  const auto fetch = [&](Fetched& o, int s) {
+    const int k = s * kFusedK;
+    if (k + kFusedK <= K) {
+      o.w[0].load(row0, k + 32 * wq);
+      o.w[1].load(row1, k + 32 * wq);
+#pragma unroll
+      for (int i = 0; i < NX; i++) o.x[i].load(xp[i], k);
+    } else {
+      o.w[0].load(row0, k + 32 * wq, K - k - 32 * wq);
+      o.w[1].load(row1, k + 32 * wq, K - k - 32 * wq);
+#pragma unroll
+      for (int i = 0; i < NX; i++) o.x[i].load(xp[i], k, k + 8 * xc < K);
+    }
+  };
+  const auto stage = [&](Fetched& o) {
+#pragma unroll
+    for (int i = 0; i < NX; i++) *reinterpret_cast<uint4*>(xs + wide_at(xr + 16 * i, xc)) = o.x[i].bf16();
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+      o.w[h].ready(row0.tensor_scale);
+#pragma unroll
+      for (int i = 0; i < 4; i++) *reinterpret_cast<uint4*>(rs + wide_at(wr + 64 * h, 4 * wq + i)) = o.w[h].chunk(i);
+    }
+  };
+  const int wm = wave >> 1, wn = wave & 1;
+  f32x4 acc[TM][4];
+#pragma unroll
+  for (int i = 0; i < TM; i++)
+#pragma unroll
+    for (int j = 0; j < 4; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const auto meet = [&] {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  const auto step = [&](Fetched& o, int s) {
+    meet();  // every wavefront is done with the step before
+    stage(o);
+    if (s + 2 < s1) fetch(o, s + 2);
+    meet();
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      bf16x8 mx[TM], mr[4];
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+        mx[i] = as_bf16x8(*reinterpret_cast<const uint4*>(xs + wide_at(wm * (BM / 2) + 16 * i + (lane & 15), 4 * k + (lane >> 4))));
+#pragma unroll
+      for (int j = 0; j < 4; j++)
+        mr[j] = as_bf16x8(*reinterpret_cast<const uint4*>(rs + wide_at(wn * 64 + 16 * j + (lane & 15), 4 * k + (lane >> 4))));
+#pragma unroll
+      for (int i = 0; i < TM; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx[i], mr[j], acc[i][j], 0, 0, 0);
+    }
+  };
+  fetch(f[0], s0);
+  if (s0 + 1 < s1) fetch(f[1], s0 + 1);
+  for (int s = s0; s < s1; s += 2) {
+    step(f[0], s);
+    if (s + 1 < s1) step(f[1], s + 1);
+  }
+  meet();
+  store_tile<TM>(a, w.rows, acc, m0 + wm * (BM / 2), n0 + wn * 64, reinterpret_cast<float*>(lds) + wave * kSlab,
+                 part ? part + (int64_t)split * a.tokens * w.rows : nullptr);
+}
+
+// y from the sums of `splits` shares of the columns, eight outputs a thread.
+__global__ __launch_bounds__(256) void join_kernel(quasar_linear a, int64_t rows, const float* part, int splits) {
+  const int64_t per = (rows + 7) / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t token = i / per, n = (i - token * per) * 8;
+  if (token >= a.tokens) return;
+  const int left = (int)(rows - n < 8 ? rows - n : 8);
+  float v[8] = {};
+  for (int s = 0; s < splits; s++) {
+    Piece<kElemF32> p;
+    p.load(part, ((int64_t)s * a.tokens + token) * rows + n, left);
+#pragma unroll
+    for (int q = 0; q < 8; q++) v[q] += p.get(q);
+  }
+  finish8(a, token, n, left, v);
+}
+
+// ---- many tokens --------------------------------------------------------------
 // r in bf16 [rows, kp], columns past the last zero; then (workgroups from
 // weight_blocks on) x in bf16 [tokens, kp] likewise, where it is not used as
 // it is.  A thread makes 32 weights, or 8 activations.
@@ -241,9 +679,11 @@ __global__ __launch_bounds__(256) void unpack_kernel(Weights w, quasar_linear a,
     const int64_t row = i / per;
     if (row >= w.rows) return;
     const int k = (int)(i - row * per) * 32;
+    const WeightRow<FMT, BITS> at(w, row);
     Strip<FMT, BITS> strip;
     const int left = (int)w.cols - k;
-    strip.load(w, row, k, left);
+    strip.load(at, k, left);
+    strip.ready(at.tensor_scale);
 #pragma unroll
     for (int c = 0; c < 4; c++) st128(r + row * kp + k + 8 * c, 8 * c < left ? strip.chunk(c) : make_uint4(0u, 0u, 0u, 0u));
   } else {
@@ -252,180 +692,271 @@ __global__ __launch_bounds__(256) void unpack_kernel(Weights w, quasar_linear a,
     const int64_t t = i / per;
     if (t >= a.tokens) return;
     const int k = (int)(i - t * per) * 8;
-    st128(xo + t * kp + k, k < w.cols ? load_x8<XT>(a.x, t * a.x_stride + k) : make_uint4(0u, 0u, 0u, 0u));
+    XChunk<XT> c;
+    c.load(a.x, t * a.x_stride + k, k < w.cols);
+    st128(xo + t * kp + k, c.bf16());
   }
 }
 
-// 16 bytes per lane from global memory straight into LDS: lane l's go to
-// to + 16 l (to: the same in every lane).
-__device__ __forceinline__ void load_lds16(const void* from, void* to) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
-                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+// 16 bytes per lane from global memory straight into LDS: lane l's go from
+// from + off to to + 16 l (from and to: the same in every lane).  In assembly
+// because the compiler makes every later LDS read wait for all such loads in
+// flight; the kernel counts them itself (no register is written by them).
+__device__ __forceinline__ void load_lds16(const char* from, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory");
 }
 
-// A workgroup makes BM tokens x BN outputs, WM x WN wavefronts of 32x32x16
-// matrix instructions; LDS holds two steps of both operands, one filled while
-// the other is used.  Row m's 16-byte chunk c of a step lies at chunk
-// c ^ (m / 2 % 8) of its 128 bytes: the 32 rows that an operand read touches
-// then spread over all banks.
-template <int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void tile_kernel(quasar_linear a, const uint16_t* x, int64_t x_stride,
-                                                            const uint16_t* r, int64_t rows, int kp, int tiles_m,
-                                                            int tiles_n) {
-  constexpr int kWavesT = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
-  constexpr int kStage = (BM + BN) * kTileK;  // bf16 elements
-  extern __shared__ __align__(16) uint16_t lds[];
+// Tile `b` of a grid as (tm, tn): each of the eight XCDs (workgroup b runs on
+// XCD b % 8) takes a stretch of the tiles, eight tiles of tokens wide, so that
+// what its workgroups read together fits its L2.
+__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int total = tiles_m * tiles_n, q = total >> 3, r = total & 7, xcd = b & 7;
+  const int t = xcd * q + (xcd < r ? xcd : r) + (b >> 3);
+  const int per = 8 * tiles_n, g = t / per, first = g * 8, wide = tiles_m - first < 8 ? tiles_m - first : 8;
+  const int in = t - g * per;
+  tm = first + in % wide;
+  tn = in / wide;
+}
+
+// A workgroup makes 256 tokens x 256 outputs with 8 wavefronts of 128 x 64.
+// Both operands of a step lie in LDS as two halves each (x0: the first 64
+// tokens of every wavefront's 128, r0: the first 32 outputs of its 64, x1 and
+// r1 the rest), and a step has four phases, each with 16 matrix instructions a
+// wavefront: (x0 r0), (x0 r1), (x1 r1), (x1 r0).  Two stages; a half is
+// filled again as soon as both halves of the workgroup are done with it.
+//
+// The wavefronts of a SIMD work in turn: those of wm = 1 run one barrier
+// behind, so that while one multiplies the other reads its next operands.
+// Barriers 2p and 2p + 1 end the reading and the multiplying of phase p for
+// wm = 0, 2p + 1 and 2p + 2 for wm = 1.  Hence
+//  - a half filled in phase p may be one whose last reads were in phase p - 2
+//    or before (x0: filled in phase 2 of a step, read in 0; r0: 3, 0; r1: 4, 1;
+//    x1: 5, 2);
+//  - what phase p reads has to have landed for every wavefront's own loads
+//    before the barrier that ends its reading of phase p - 1: with two loads a
+//    phase and at least four phases in between, "at most 8 outstanding" then.
+// Past the last step the loads repeat it, so that the counts hold.
+__global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uint16_t* x, int64_t x_stride,
+                                                      const uint16_t* r, int64_t rows, int kp, int tiles_m, int tiles_n,
+                                                      int steps_per, float* part) {
+  constexpr int kHalf = 128 * kTileK, kStage = 4 * kHalf;  // elements; halves x0, r0, r1, x1
+  __shared__ __align__(16) uint16_t lds[2 * kStage];
+  static_assert(8 * kSlab * 4 <= (int)sizeof(lds), "the epilogue's stage fits");
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
   const int lane = threadIdx.x & 63, wave = wave_index();
-  const int wm = wave / WN, wn = wave % WN;
-  const int tm = blockIdx.x % (unsigned)tiles_m, tn = blockIdx.x / (unsigned)tiles_m;
-  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+  const int wm = wave >> 2, wn = wave & 3;
+  int tm, tn;
+  const int split = blockIdx.x / (unsigned)(tiles_m * tiles_n);
+  tile_of(blockIdx.x - split * tiles_m * tiles_n, tiles_m, tiles_n, tm, tn);
+  const int64_t m0 = (int64_t)tm * 256, n0 = (int64_t)tn * 256;
+  const int ms = (int)(a.tokens - m0 < 256 ? a.tokens - m0 : 256), ns = (int)(rows - n0 < 256 ? rows - n0 : 256);
+  const int first = split * steps_per, left = kp / kTileK - first, steps = left < steps_per ? left : steps_per;
 
-  // this lane's rows of the loads: 8 rows of 128 bytes a wavefront and instruction
-  constexpr int kLoads = (BM + BN) / 8 / kWavesT;
-  const char* src[kLoads];
+  // each wavefront loads 16 rows of a half, 8 an instruction; rows past the matrix repeat its last
+  uint32_t off[4][2];
 #pragma unroll
-  for (int i = 0; i < kLoads; i++) {
-    const int lr = (wave * kLoads + i) * 8 + (lane >> 3);
-    const int c = (lane & 7) ^ ((lr >> 1) & 7);
-    const int64_t m = m0 + lr, n = n0 + lr - BM;
-    src[i] = lr < BM ? reinterpret_cast<const char*>(x + (m < a.tokens ? m : a.tokens - 1) * x_stride) + 16 * c
-                     : reinterpret_cast<const char*>(r + (n < rows ? n : rows - 1) * kp) + 16 * c;
-  }
-  const auto fill = [&](int stage) {
+  for (int i = 0; i < 2; i++) {
+    const int lr = wave * 16 + i * 8 + (lane >> 3);
+    const uint32_t c = 16u * ((lane & 7) ^ ((lr >> 1) & 7));
 #pragma unroll
-    for (int i = 0; i < kLoads; i++) {
-      load_lds16(src[i], lds + stage * kStage + (wave * kLoads + i) * 8 * kTileK);
-      src[i] += 2 * kTileK;
+    for (int h = 0; h < 2; h++) {
+      const int m = (lr >> 6) * 128 + h * 64 + (lr & 63), n = (lr >> 5) * 64 + h * 32 + (lr & 31);
+      off[h == 0 ? 0 : 3][i] = (uint32_t)(m < ms ? m : ms - 1) * (uint32_t)(x_stride * 2) + c;
+      off[h == 0 ? 1 : 2][i] = (uint32_t)(n < ns ? n : ns - 1) * (uint32_t)(kp * 2) + c;
     }
+  }
+  const char* const xb = reinterpret_cast<const char*>(x + m0 * x_stride + first * kTileK);
+  const char* const rb = reinterpret_cast<const char*>(r + n0 * kp + first * kTileK);
+  const auto fill = [&](int h, int step) {
+    const char* const from = (h == 0 || h == 3 ? xb : rb) + (step < steps ? step : steps - 1) * (2 * kTileK);
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+      load_lds16(from, off[h][i], lds0 + ((step & 1) * kStage + h * kHalf + (wave * 16 + i * 8) * kTileK) * 2);
   };
-  f32x16 acc[TM][TN];
+  f32x4 acc[8][4];
 #pragma unroll
-  for (int i = 0; i < TM; i++)
+  for (int i = 0; i < 8; i++)
 #pragma unroll
-    for (int j = 0; j < TN; j++)
+    for (int j = 0; j < 4; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  bf16x8 fx[4][2], fr[2][2][2];
+  const auto read_x = [&](int h, int stage) {
+    const uint16_t* p = lds + stage * kStage + (h ? 3 : 0) * kHalf;
 #pragma unroll
-      for (int e = 0; e < 16; e++) acc[i][j][e] = 0.0f;
+    for (int t = 0; t < 4; t++)
+#pragma unroll
+      for (int k = 0; k < 2; k++)
+        fx[t][k] = as_bf16x8(*reinterpret_cast<const uint4*>(p + chunk_at(wm * 64 + 16 * t + (lane & 15), 4 * k + (lane >> 4))));
+  };
+  const auto read_r = [&](int h, int stage) {
+    const uint16_t* p = lds + stage * kStage + (h ? 2 : 1) * kHalf;
+#pragma unroll
+    for (int t = 0; t < 2; t++)
+#pragma unroll
+      for (int k = 0; k < 2; k++)
+        fr[h][t][k] = as_bf16x8(*reinterpret_cast<const uint4*>(p + chunk_at(wn * 32 + 16 * t + (lane & 15), 4 * k + (lane >> 4))));
+  };
+  // ends the phase's reading, multiplies, ends the phase
+  const auto multiply = [&](int hx, int hr) {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int k = 0; k < 2; k++)
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int j = 0; j < 2; j++)
+          acc[hx * 4 + i][hr * 2 + j] =
+              __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i][k], fr[hr][j][k], acc[hx * 4 + i][hr * 2 + j], 0, 0, 0);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  const auto landed8 = [] { asm volatile("s_waitcnt vmcnt(8)" ::: "memory"); };
 
-  fill(0);
-  const int steps = kp / kTileK;
+  fill(0, 0);
+  fill(1, 0);
+  fill(2, 0);
+  fill(3, 0);
+  fill(0, 1);
+  fill(1, 1);
+  asm volatile("s_waitcnt vmcnt(4)" ::: "memory");  // step 0
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  if (wm == 1) __builtin_amdgcn_s_barrier();
   for (int s = 0; s < steps; s++) {
-    // step s has landed, and every wavefront is done with step s - 1
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (s + 1 < steps) fill((s + 1) & 1);
-    const uint16_t* as = lds + (s & 1) * kStage;
-    const uint16_t* bs = as + BM * kTileK;
-#pragma unroll
-    for (int k = 0; k < kTileK / 16; k++) {
-      bf16x8 fa[TM], fb[TN];
-#pragma unroll
-      for (int i = 0; i < TM; i++) {
-        const int m = wm * (BM / WM) + i * 32 + (lane & 31);
-        fa[i] = as_bf16x8(*reinterpret_cast<const uint4*>(as + m * kTileK + 8 * ((2 * k + (lane >> 5)) ^ ((m >> 1) & 7))));
-      }
-#pragma unroll
-      for (int j = 0; j < TN; j++) {
-        const int n = wn * (BN / WN) + j * 32 + (lane & 31);
-        fb[j] = as_bf16x8(*reinterpret_cast<const uint4*>(bs + n * kTileK + 8 * ((2 * k + (lane >> 5)) ^ ((n >> 1) & 7))));
-      }
-#pragma unroll
-      for (int i = 0; i < TM; i++)
-#pragma unroll
-        for (int j = 0; j < TN; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-    }
+    const int stage = s & 1;
+    read_x(0, stage);
+    read_r(0, stage);
+    fill(2, s + 1);
+    landed8();
+    multiply(0, 0);
+    read_r(1, stage);
+    fill(3, s + 1);
+    landed8();
+    multiply(0, 1);
+    read_x(1, stage);
+    fill(0, s + 2);
+    multiply(1, 1);
+    fill(1, s + 2);
+    landed8();
+    multiply(1, 0);
   }
-  // The epilogue goes through LDS (each wavefront its own part of it), 32
-  // tokens at a time, so that y is written 16 bytes a lane.
+  if (wm == 0) __builtin_amdgcn_s_barrier();
+  // LDS is the epilogue's once every wavefront's loads have landed
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  constexpr int kCols = BN / WN, kPitch = kCols + 4;
-  static_assert(32 * kPitch * 4 * kWavesT <= 2 * kStage * 2, "the epilogue's stage fits the tiles'");
-  float* st = reinterpret_cast<float*>(lds) + wave * 32 * kPitch;
-  const bool yb = a.y_dtype == QUASAR_BF16;
-#pragma unroll
-  for (int i = 0; i < TM; i++) {
-#pragma unroll
-    for (int j = 0; j < TN; j++)
-#pragma unroll
-      for (int e = 0; e < 16; e++)
-        st[(8 * (e >> 2) + 4 * (lane >> 5) + (e & 3)) * kPitch + j * 32 + (lane & 31)] = acc[i][j][e];
-    wave_lds_fence();
-    constexpr int kLanes = kCols / 8;  // lanes a token's outputs take
-#pragma unroll 1
-    for (int p = 0; p < 32; p += 64 / kLanes) {
-      const int tr = p + lane / kLanes, c = (lane % kLanes) * 8;
-      const int64_t token = m0 + wm * (BM / WM) + i * 32 + tr, n = n0 + wn * kCols + c;
-      if (token >= a.tokens || n >= rows) continue;
-      const int left = (int)(rows - n < 8 ? rows - n : 8);
-      float v[8];
-#pragma unroll
-      for (int q = 0; q < 8; q++) v[q] = st[tr * kPitch + c + q];
-      if (a.x_scale) {
-        const float f = a.x_scale[token];
-#pragma unroll
-        for (int q = 0; q < 8; q++) v[q] *= f;
-      }
-      const auto add = [&](const void* p, int64_t e, bool bf16) {
-        if (bf16) {
-          Piece<kElemBF16> b;
-          b.load(p, e, left);
-#pragma unroll
-          for (int q = 0; q < 8; q++) v[q] += b.get(q);
-        } else {
-          Piece<kElemF32> b;
-          b.load(p, e, left);
-#pragma unroll
-          for (int q = 0; q < 8; q++) v[q] += b.get(q);
-        }
-      };
-      if (a.bias) add(a.bias, n, a.bias_dtype == QUASAR_BF16);
-      if (a.act != QUASAR_ACT_NONE) {
-#pragma unroll
-        for (int q = 0; q < 8; q++) v[q] = activate(v[q], a.act);
-      }
-      if (a.residual) add(a.residual, token * a.residual_stride + n, a.residual_dtype == QUASAR_BF16);
-      store_piece(a.y, token * a.y_stride + n, v, left, yb);
-    }
-    wave_lds_fence();
-  }
+  store_tile<8>(a, rows, acc, m0 + wm * 128, n0 + wn * 64, reinterpret_cast<float*>(lds) + wave * kSlab,
+                part ? part + (int64_t)split * a.tokens * rows : nullptr);
 }
 
-constexpr int64_t kStripTokens = 64;  // the strip kernel serves up to this many
+enum Form : int { kStrip, kFused, kTile };
+struct Choice {
+  Form form;
+  int splits, steps;  // fused: shares of the columns, and the steps of each
+  size_t bytes;       // workspace
+  int bm;             // fused: tokens a workgroup takes
+};
 
 int padded_cols(const quasar_desc& d) { return (int)((d.cols + kTileK - 1) / kTileK * kTileK); }
+
+// Splits the steps of `tiles` tiles into shares while that makes no more than
+// `most` workgroups, each of `least` steps or more.
+void split_steps(Choice& c, int64_t tiles, int steps, int64_t most, int least) {
+  while (c.splits < 16 && 2 * tiles * c.splits <= most && steps >= 2 * c.splits * least) c.splits *= 2;
+}
+
+// By the number of tokens (figures: us at rows x columns, INT4, this form against its neighbour):
+//  - up to 32 the strip kernel: 32 tokens 8.0 against 15 at 4096 x 4096, 20 against 26 at 4096 x 14336;
+//  - the tile kernel where its 256 x 256 tiles come near to filling the CUs and there are tokens enough to pay for
+//    writing r out (4096 tokens at 4096 x 4096: 115 against 173; 1024 at 14336 x 4096: 126 against 164, but 512
+//    there 114 against 86), or where the columns are many enough to be split (1500 at 4096 x 14336: 225 against 259);
+//  - the fused kernel between them.
+Choice choose(const quasar_desc& d, int64_t tokens) {
+  Choice c{kStrip, 1, 0, 0, 0};
+  int64_t tiles = ((tokens + 255) / 256) * ((d.rows + 255) / 256);
+  if (tokens <= 32) return c;
+  int steps;
+  if ((tokens >= 768 && tiles >= 160) || (tokens >= 1024 && d.cols >= 8192)) {
+    c.form = kTile;
+    steps = padded_cols(d) / kTileK;
+    split_steps(c, tiles, steps, kCUs, 16);
+    c.bytes = (size_t)(d.rows + tokens) * (size_t)padded_cols(d) * 2;
+  } else {
+    c.form = kFused;
+    c.bm = tokens <= 64 ? 64 : 128;
+    tiles = ((tokens + c.bm - 1) / c.bm) * ((d.rows + 127) / 128);
+    steps = (int)((d.cols + kFusedK - 1) / kFusedK);
+    // a workgroup for every CU, of two steps or more; a second one where both have 14
+    split_steps(c, tiles, steps, 2 * kCUs - 1, 2);
+    split_steps(c, tiles, steps, 2 * kCUs, 14);
+  }
+  c.steps = (steps + c.splits - 1) / c.splits;
+  c.splits = (steps + c.steps - 1) / c.steps;
+  if (c.splits > 1) c.bytes += (size_t)c.splits * (size_t)tokens * (size_t)d.rows * 4;
+  return c;
+}
 
 // x goes through the workspace unless the tile kernel can load its rows in
 // 16-byte pieces as they are.
 bool x_direct(int64_t cols, int x_dtype, const void* x, int64_t stride) {
-  return x_dtype == QUASAR_BF16 && cols % kTileK == 0 && stride % 8 == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+  return x_dtype == QUASAR_BF16 && cols % kTileK == 0 && stride % 8 == 0 && stride < (1 << 22) &&
+         (reinterpret_cast<uintptr_t>(x) & 15) == 0;
 }
 
 template <int FMT, int BITS, int XT>
 hipError_t launch(const quasar_desc& d, const quasar_linear& a, hipStream_t stream) {
-  Weights w{a.codes, a.scales, a.zeros, a.tensor_scale, d.rows, d.cols, FMT == QUASAR_NVFP4 ? 16 : d.group};
-  if (a.tokens <= kStripTokens) {
-    const dim3 block(64 * kStripWaves);
+  Weights w{a.codes, a.scales, a.zeros, a.tensor_scale, d.rows, d.cols, d.group == 64 ? 6 : 7};
+  const Choice c = choose(d, a.tokens);
+  if (c.form == kStrip) {
     const unsigned gx = (unsigned)((d.rows + 15) / 16);
-    if (a.tokens <= 16)
-      strip_kernel<FMT, BITS, XT, 1><<<dim3(gx), block, 0, stream>>>(w, a);
-    else if (a.tokens <= 32)
-      strip_kernel<FMT, BITS, XT, 2><<<dim3(gx), block, 0, stream>>>(w, a);
+    const auto strip = [&](auto nx) {
+      strip_kernel<FMT, BITS, XT, decltype(nx)::value><<<dim3(gx), dim3(64 * kStripWaves), 0, stream>>>(w, a);
+    };
+    if (a.tokens <= 4)
+      strip(std::integral_constant<int, 1>());
+    else if (a.tokens <= 8)
+      strip(std::integral_constant<int, 2>());
+    else if (a.tokens <= 16)
+      strip(std::integral_constant<int, 4>());
     else
-      strip_kernel<FMT, BITS, XT, 4><<<dim3(gx), block, 0, stream>>>(w, a);
+      strip(std::integral_constant<int, 8>());
     return hipGetLastError();
+  }
+  float* part = nullptr;  // the sums of the shares, [splits, tokens, rows]
+  const auto join = [&] {
+    const int64_t n = a.tokens * ((d.rows + 7) / 8);
+    join_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream>>>(a, d.rows, part, c.splits);
+    return hipGetLastError();
+  };
+  if (c.form == kFused) {
+    const int tm = (int)((a.tokens + c.bm - 1) / c.bm), tn = (int)((d.rows + 127) / 128);
+    if (c.splits > 1) part = reinterpret_cast<float*>(a.workspace);
+    const dim3 grid((unsigned)(tm * tn * c.splits));
+    if (c.bm == 64)
+      fused_kernel<FMT, BITS, XT, 64><<<grid, dim3(256), 0, stream>>>(w, a, tm, c.splits, c.steps, part);
+    else
+      fused_kernel<FMT, BITS, XT, 128><<<grid, dim3(256), 0, stream>>>(w, a, tm, c.splits, c.steps, part);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || !part ? e : join();
   }
   const int kp = padded_cols(d);
   uint16_t* r = reinterpret_cast<uint16_t*>(a.workspace);
   uint16_t* xo = r + d.rows * kp;
+  if (c.splits > 1) part = reinterpret_cast<float*>(xo + a.tokens * kp);
   const bool direct = x_direct(d.cols, a.x_dtype, a.x, a.x_stride);
   const int64_t wb = (d.rows * (kp / 32) + 255) / 256, xb = direct ? 0 : (a.tokens * (kp / 8) + 255) / 256;
   unpack_kernel<FMT, BITS, XT><<<dim3((unsigned)(wb + xb)), dim3(256), 0, stream>>>(w, a, kp, r, xo, (unsigned)wb);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  constexpr int BM = 128, BN = 128;
-  const int tm = (int)((a.tokens + BM - 1) / BM), tn = (int)((d.rows + BN - 1) / BN);
-  tile_kernel<BM, BN, 2, 2><<<dim3((unsigned)(tm * tn)), dim3(256), 2 * (BM + BN) * kTileK * 2, stream>>>(
-      a, direct ? reinterpret_cast<const uint16_t*>(a.x) : xo, direct ? a.x_stride : kp, r, d.rows, kp, tm, tn);
-  return hipGetLastError();
+  const int tm = (int)((a.tokens + 255) / 256), tn = (int)((d.rows + 255) / 256);
+  tile_kernel<<<dim3((unsigned)(tm * tn * c.splits)), dim3(512), 0, stream>>>(
+      a, direct ? reinterpret_cast<const uint16_t*>(a.x) : xo, direct ? a.x_stride : kp, r, d.rows, kp, tm, tn, c.steps,
+      part);
+  e = hipGetLastError();
+  return e != hipSuccess || !part ? e : join();
 }
 
 template <int FMT, int BITS>
@@ -435,12 +966,7 @@ hipError_t launch_x(const quasar_desc& d, const quasar_linear& a, hipStream_t st
 
 }  // namespace
 
-size_t linear_workspace(const quasar_desc& d, int64_t tokens, int x_dtype) {
-  (void)x_dtype;
-  if (tokens <= kStripTokens) return 0;
-  const size_t kp = (size_t)padded_cols(d);
-  return ((size_t)d.rows + (size_t)tokens) * kp * 2;
-}
+size_t linear_workspace(const quasar_desc& d, int64_t tokens) { return choose(d, tokens).bytes; }
 
 hipError_t launch_linear(const quasar_desc& d, const quasar_linear& a, hipStream_t stream) {
   switch (d.format) {

@@ -145,15 +145,17 @@ int quasar_distill_topk_backward(const quasar_distill* a, void* stream) { return
 int quasar_distill_topk_grad(const quasar_distill* a, void* stream) { return distill(a, 2, stream); }
 
 size_t quasar_linear_codes_workspace_bytes(const quasar_desc* d, int64_t tokens, int32_t x_dtype) {
+  (void)x_dtype;
   if (check_desc(d) != QUASAR_OK || tokens < 1 || tokens > kMaxRows) return 0;
-  return quasar::linear_workspace(*d, tokens, x_dtype);
+  return quasar::linear_workspace(*d, tokens);
 }
 
 int quasar_linear_codes_check(const quasar_desc* d, const quasar_linear* a) {
   if (a == nullptr) return QUASAR_ERR_ARG;
   QUASAR_TRY(check_desc(d));
-  // 32-bit columns and grids: 2^31 rows of either side are beyond the memory of the card
-  if (a->tokens < 0 || a->tokens > (int64_t)1 << 28 || d->rows > (int64_t)1 << 28 || d->cols > (int64_t)1 << 24)
+  // byte offsets inside 256 rows of r, and grids, stay inside 32 bits (y of 2^27 tiles is beyond the card's memory)
+  if (a->tokens < 0 || a->tokens > (int64_t)1 << 28 || d->rows > (int64_t)1 << 28 || d->cols > (int64_t)1 << 22 ||
+      ((a->tokens + 127) / 128) * ((d->rows + 127) / 128) > (int64_t)1 << 27)
     return QUASAR_ERR_SHAPE;
   if (a->x_dtype != QUASAR_BF16 && a->x_dtype != QUASAR_E4M3) return QUASAR_ERR_FORMAT;
   if (!f32_or_bf16(a->y_dtype) || (a->bias && !f32_or_bf16(a->bias_dtype)) ||
@@ -172,7 +174,7 @@ int quasar_linear_codes_check(const quasar_desc* d, const quasar_linear* a) {
   QUASAR_TRY(check_matrix(a->residual, a->tokens, d->rows, a->residual_stride, a->residual_dtype));
   QUASAR_TRY(check_matrix(a->y, a->tokens, d->rows, a->y_stride, a->y_dtype));
   if (misaligned(a->x_scale, 4) || (a->bias && misaligned(a->bias, size_of(a->bias_dtype)))) return QUASAR_ERR_ALIGN;
-  const size_t need = quasar::linear_workspace(*d, a->tokens, a->x_dtype);
+  const size_t need = quasar::linear_workspace(*d, a->tokens);
   if (need > 0 && (a->workspace == nullptr || a->workspace_bytes < need)) return QUASAR_ERR_WORKSPACE;
   return QUASAR_OK;
 }

@@ -20,7 +20,7 @@ size_t distill_workspace(int64_t rows, int64_t classes);
 hipError_t launch_distill(const quasar_distill& a, int what, hipStream_t stream);
 
 // linear_kernel.hip
-size_t linear_workspace(const quasar_desc& d, int64_t tokens, int x_dtype);
+size_t linear_workspace(const quasar_desc& d, int64_t tokens);
 hipError_t launch_linear(const quasar_desc& d, const quasar_linear& a, hipStream_t stream);
 
 }  // namespace quasar
