@@ -62,6 +62,9 @@ struct Piece<kElemBF16> {
   __device__ __forceinline__ float get(int i) const {
     return (i & 1) ? as_f32(d[i >> 1] & 0xffff0000u) : as_f32(d[i >> 1] << 16);
   }
+  // To the compiler the elements change here: what it formed from them before
+  // is not kept in registers for a use after.
+  __device__ __forceinline__ void refresh() { asm volatile("" : "+v"(d[0]), "+v"(d[1]), "+v"(d[2]), "+v"(d[3])); }
 };
 template <>
 struct Piece<kElemF32> {
@@ -78,6 +81,7 @@ struct Piece<kElemF32> {
     }
   }
   __device__ __forceinline__ float get(int i) const { return f[i]; }
+  __device__ __forceinline__ void refresh() {}
 };
 
 // Eight values to a tensor of fp32 or bf16 elements (nearest even), the first n of them.
