@@ -9,6 +9,10 @@
 #include "ops_internal.h"
 
 namespace quasar {
+
+// floats from one part of dweight to the next
+__host__ __device__ constexpr int parts_pitch(int cols) { return (cols + 3) & ~3; }
+
 namespace {
 
 constexpr int kNormThreads = 256;
@@ -241,24 +245,38 @@ __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_
 #pragma unroll
   for (int v = 0; v < NV; v++) {
     const int c = (v * TPR + t) * 8;
-    store_piece<false>(parts, (int64_t)blockIdx.x * cols + c, dw[v], cols - c);
+    store_piece<false>(parts, (int64_t)blockIdx.x * parts_pitch(cols) + c, dw[v], cols - c);
   }
 }
 
-// dweight[c] = sum of parts[0 .. n)[c]: 32 columns a workgroup, each by 8
-// threads whose sums meet in LDS.
+// dweight[c] = sum of parts[0 .. n)[c]: 16 columns a workgroup, four a thread,
+// the parts shared out over 64 rows of threads whose sums meet in LDS.
 __global__ __launch_bounds__(256) void parts_kernel(const float* parts, int n, int cols, float* out) {
-  __shared__ float s[8][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
-  float sum = 0.0f;
-  if (c < cols)
-    for (int i = y; i < n; i += 8) sum += parts[(int64_t)i * cols + c];
-  s[y][x] = sum;
-  __syncthreads();
-  if (y == 0 && c < cols) {
+  __shared__ float s[64][17];
+  const int x = (threadIdx.x & 3) * 4, y = threadIdx.x >> 2, c = blockIdx.x * 16 + x, pitch = parts_pitch(cols);
+  float sum[4] = {};
+  if (c < cols) {
+#pragma unroll 8
+    for (int i = y; i < n; i += 64) {
+      const float4 v = *reinterpret_cast<const float4*>(parts + (int64_t)i * pitch + c);
+      sum[0] += v.x;
+      sum[1] += v.y;
+      sum[2] += v.z;
+      sum[3] += v.w;
+    }
+  }
 #pragma unroll
-    for (int i = 1; i < 8; i++) sum += s[i][x];
-    out[c] = sum;
+  for (int i = 0; i < 4; i++) s[y][x + i] = sum[i];
+  __syncthreads();
+  // four threads a column sum 16 each, then meet (they are a quad)
+  if (threadIdx.x < 64) {
+    const int col = threadIdx.x >> 2, q = threadIdx.x & 3;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) t += s[q * 16 + i][col];
+    t += dpp_f32<kDppXor1>(t);
+    t += dpp_f32<kDppXor2>(t);
+    if (q == 0 && blockIdx.x * 16 + col < cols) out[blockIdx.x * 16 + col] = t;
   }
 }
 
@@ -272,7 +290,7 @@ hipError_t launch_backward_types(const quasar_norm_backward& a, hipStream_t stre
     norm_backward_kernel<GT, HT, TPR, NV><<<dim3(n), dim3(threads), 0, stream>>>(a, parts);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !a.dweight || n == 1) return e;
-    parts_kernel<<<dim3((unsigned)((a.cols + 31) / 32)), dim3(256), 0, stream>>>(parts, n, (int)a.cols, a.dweight);
+    parts_kernel<<<dim3((unsigned)((a.cols + 15) / 16)), dim3(256), 0, stream>>>(parts, n, (int)a.cols, a.dweight);
     return hipGetLastError();
   });
 }
@@ -285,6 +303,11 @@ hipError_t launch_norm(const quasar_norm& a, hipStream_t stream) {
     return xb ? launch_norm_types<kElemBF16, kElemNone>(a, stream) : launch_norm_types<kElemF32, kElemNone>(a, stream);
   if (rb) return xb ? launch_norm_types<kElemBF16, kElemBF16>(a, stream) : launch_norm_types<kElemF32, kElemBF16>(a, stream);
   return xb ? launch_norm_types<kElemBF16, kElemF32>(a, stream) : launch_norm_types<kElemF32, kElemF32>(a, stream);
+}
+
+size_t norm_backward_workspace(int64_t rows, int64_t cols) {
+  const int n = norm_backward_parts(rows, cols);
+  return n > 1 ? (size_t)n * parts_pitch((int)cols) * sizeof(float) : 0;
 }
 
 int norm_backward_parts(int64_t rows, int64_t cols) {

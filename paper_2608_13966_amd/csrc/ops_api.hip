@@ -72,8 +72,7 @@ int quasar_add_rms_norm(const quasar_norm* a, void* stream) {
 
 size_t quasar_add_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
   if (rows < 1 || rows > kMaxRows || cols < 1 || cols > QUASAR_NORM_MAX_COLS) return 0;
-  const int n = quasar::norm_backward_parts(rows, cols);
-  return n > 1 ? (size_t)n * (size_t)cols * sizeof(float) : 0;
+  return quasar::norm_backward_workspace(rows, cols);
 }
 
 int quasar_add_rms_norm_backward_check(const quasar_norm_backward* a) {

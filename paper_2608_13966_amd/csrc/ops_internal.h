@@ -12,7 +12,8 @@ constexpr int kCUs = 256;  // compute units of the card
 
 // norm_kernel.hip
 hipError_t launch_norm(const quasar_norm& a, hipStream_t stream);
-int norm_backward_parts(int64_t rows, int64_t cols);  // rows of cols floats in the workspace; 0: none
+int norm_backward_parts(int64_t rows, int64_t cols);  // workgroups, each with its share of dweight
+size_t norm_backward_workspace(int64_t rows, int64_t cols);
 hipError_t launch_norm_backward(const quasar_norm_backward& a, hipStream_t stream);
 
 // distill_kernel.hip; what: 0 loss, 1 gradient, 2 both
