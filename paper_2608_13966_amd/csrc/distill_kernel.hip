@@ -14,7 +14,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kListed = QUASAR_DISTILL_MAX_LISTED;
-constexpr int kMostPart = 16384;
+
 
 // max and sum of exp2((z - max) c) of a set of logits; an empty set is (-inf, 0)
 struct MaxSum {
@@ -101,25 +101,47 @@ __device__ __forceinline__ void take(MaxSum& r, const Piece<T>& p, float c) {
   r.s += ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
 }
 
-// max and sum over the elements [e0, e1) of a row (base: the row's first element)
-template <int T>
-__device__ MaxSum scan(const void* z, int64_t base, int e0, int e1, float c) {
-  MaxSum r{-INFINITY, 0.0f};
-  for (int e = e0 + (int)threadIdx.x * 8; e < e1; e += kThreads * 8) {
-    Piece<T> p;
-    p.load(z, base + e, e1 - e, 0xff80);  // -inf past the end
-    take(r, p, c);
+// NV pieces a thread of a part of a row: classes [e0, e0 + 2048 NV), whole
+// pieces only; the last part has the V % 8 classes past them, one a thread.  All
+// loads are in flight at once.
+template <int T, int NV>
+struct Part {
+  static constexpr int kClasses = kThreads * 8 * NV, kSize = elem_size<T>();
+  Piece<T> p[NV];
+  float last;
+  int at, bytes, rest;  // this thread's first byte, the part's bytes, the class past the pieces (or V)
+
+  __device__ __forceinline__ Part(int V, int e0) {
+    const int left = (V & ~7) - e0;
+    at = (int)threadIdx.x * 8 * kSize;
+    bytes = (left < kClasses ? left : kClasses) * kSize;
+    rest = e0 + kClasses >= V ? (V & ~7) + (int)threadIdx.x : V;
+    last = -INFINITY;
   }
-  return r;
+  __device__ __forceinline__ bool whole(int v) const { return v * kThreads * 8 * kSize + at < bytes; }
+  __device__ __forceinline__ void load(const void* row, int V, int e0) {
+    const __amdgpu_buffer_rsrc_t b = wave_buffer(const_cast<char*>(reinterpret_cast<const char*>(row)) + (int64_t)e0 * kSize, bytes);
+#pragma unroll
+    for (int v = 0; v < NV; v++) load_piece<T>(p[v], b, at, v * kThreads * 8 * kSize);
+    if (rest < V) last = elem(row, rest, T == kElemBF16);
+  }
+};
+// r joined with one more logit
+__device__ __forceinline__ MaxSum take_one(MaxSum r, float z, float c) {
+  return join(r, z == -INFINITY ? MaxSum{z, 0.0f} : MaxSum{z, z == z ? 1.0f : z}, c);
 }
 
-template <int WAVES = kWaves>
-__device__ __forceinline__ MaxSum group_join(MaxSum r, float c, MaxSum* s) {
+__device__ __forceinline__ MaxSum wave_join(MaxSum r, float c) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     const MaxSum b{__shfl_xor(r.m, o, 64), __shfl_xor(r.s, o, 64)};
     r = join(r, b, c);
   }
+  return r;
+}
+template <int WAVES = kWaves>
+__device__ __forceinline__ MaxSum group_join(MaxSum r, float c, MaxSum* s) {
+  r = wave_join(r, c);
   if ((threadIdx.x & 63) == 0) s[wave_index()] = r;
   __syncthreads();
   r = s[0];
@@ -132,48 +154,51 @@ __device__ __forceinline__ float lse_of(MaxSum r, float it) { return r.m * it + 
 
 // Workgroup b works on part b % parts of row b / parts.
 // Partial maximum and sum of one part of a row, into part[b].
-template <int T>
-__global__ __launch_bounds__(kThreads) void distill_scan_kernel(quasar_distill a, int per, int parts, MaxSum* part) {
+template <int T, int NV>
+__global__ __launch_bounds__(kThreads) void distill_scan_kernel(quasar_distill a, int parts, MaxSum* part) {
   __shared__ MaxSum s[kWaves];
-  const int row = blockIdx.x / (unsigned)parts, at = blockIdx.x % (unsigned)parts;
+  const int row = blockIdx.x / (unsigned)parts, e0 = blockIdx.x % (unsigned)parts * Part<T, NV>::kClasses;
   const float c = kLog2e / a.temperature;
-  const int e0 = at * per, V = (int)a.classes, e1 = e0 + per < V ? e0 + per : V;
-  const MaxSum r = group_join(scan<T>(a.logits, row * a.logits_stride, e0, e1, c), c, s);
+  const int V = (int)a.classes;
+  Part<T, NV> z(V, e0);
+  z.load(reinterpret_cast<const char*>(a.logits) + row * a.logits_stride * elem_size<T>(), V, e0);
+  MaxSum r{-INFINITY, 0.0f};
+#pragma unroll
+  for (int v = 0; v < NV; v++)
+    if (z.whole(v)) take(r, z.p[v], c);
+  if (z.rest < V) r = take_one(r, z.last, c);
+  r = group_join(r, c, s);
   if (threadIdx.x == 0) part[blockIdx.x] = r;
 }
 
-// One part of a row's gradient, and (part 0) its loss and lse.  lse is joined
-// from the row's `sums` partial ones, or (0) taken from a.lse.
-template <int T>
-__global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a, int what, int per, int parts,
-                                                               const MaxSum* part, int sums) {
+// One part of a row's gradient, and (part 0) its loss and lse.  what: 0 the loss
+// alone (one workgroup a row), 1 the gradient alone, 2 both.  lse is joined from
+// the row's `sums` partial ones, or (0) taken from a.lse.
+template <int T, int NV>
+__global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a, int what, int parts, const MaxSum* part,
+                                                               int sums) {
   __shared__ Listed l;
   __shared__ float red[4 * kWaves];
   const int64_t row = blockIdx.x / (unsigned)parts, base = row * a.logits_stride, gbase = row * a.grad_stride;
-  const int at = blockIdx.x % (unsigned)parts;
+  const int at = blockIdx.x % (unsigned)parts, e0 = at * Part<T, NV>::kClasses;
   const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
   const int V = (int)a.classes;
-  const int e0 = at * per, e1 = e0 + per < V ? e0 + per : V;
+  Part<T, NV> z(V, e0);
+  if (what != 0) z.load(reinterpret_cast<const char*>(a.logits) + base * elem_size<T>(), V, e0);
+  MaxSum r{-INFINITY, 0.0f};  // of the row's parts: each wavefront joins them
+  for (int i = threadIdx.x & 63; i < sums; i += 64) r = join(r, part[row * sums + i], c);
   float plogp = 0.0f;
   const bool live = load_listed(a, row, l, red, plogp);
+  const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
+  float lse = 0.0f;
   if (!live) {
     if (what != 1 && at == 0 && threadIdx.x == 0) a.loss[row] = a.lse[row] = 0.0f;
-    if (what == 0) return;
-    const float zero[8] = {};
-    for (int e = e0 + (int)threadIdx.x * 8; e < e1; e += kThreads * 8)
-      store_piece<T == kElemBF16>(a.grad, gbase + e, zero, e1 - e);
-    return;
-  }
-  const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
-  float lse;
-  if (sums > 0) {
-    MaxSum r = part[row * sums];
-    for (int i = 1; i < sums; i++) r = join(r, part[row * sums + i], c);
-    lse = lse_of(r, it);
+  } else if (sums > 0) {
+    lse = lse_of(wave_join(r, c), it);
   } else {
     lse = a.lse[row];
   }
-  if (what != 1 && at == 0) {
+  if (live && what != 1 && at == 0) {
     float s = 0.0f;
     for (int k = threadIdx.x; k < a.listed; k += kThreads)
       if (l.index[k] >= 0 && !(l.p[k] == 0.0f))
@@ -189,33 +214,35 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
   // the student's probability; z / tau and lse may be large, their difference is taken first
   const auto soft = [&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, it, -lse) * kLog2e); };
   // the listed classes' gradients, from their logits before `grad` may overwrite them
+  const int e1 = e0 + Part<T, NV>::kClasses < V ? e0 + Part<T, NV>::kClasses : V;
+  const auto ours = [&](int ix) { return ix >= e0 && ix < e1; };
   constexpr int kPer = kListed / kThreads;
   float mine[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; j++) {
     const int k = threadIdx.x + j * kThreads;
     mine[j] = 0.0f;
-    if (k >= a.listed) continue;
-    const int ix = l.index[k];
-    if (ix < e0 || ix >= e1) continue;
-    mine[j] = g * (soft(elem(a.logits, base + ix, T == kElemBF16)) - listed_p(l, a.listed, ix));
+    if (live && k < a.listed && ours(l.index[k]))
+      mine[j] = g * (soft(elem(a.logits, base + l.index[k], T == kElemBF16)) - listed_p(l, a.listed, l.index[k]));
   }
   __syncthreads();
-  for (int e = e0 + (int)threadIdx.x * 8; e < e1; e += kThreads * 8) {
-    Piece<T> p;
-    p.load(a.logits, base + e, e1 - e);
+  const __amdgpu_buffer_rsrc_t out =
+      wave_buffer(reinterpret_cast<char*>(a.grad) + (gbase + e0) * elem_size<T>(), z.bytes);
+#pragma unroll
+  for (int v = 0; v < NV; v++) {
     float d[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) d[i] = g * soft(p.get(i));
-    store_piece<T == kElemBF16>(a.grad, gbase + e, d, e1 - e);
+    for (int i = 0; i < 8; i++) d[i] = soft(z.p[v].get(i));
+#pragma unroll
+    for (int i = 0; i < 8; i++) d[i] = live ? g * d[i] : 0.0f;
+    store_piece<T == kElemBF16>(out, z.at, v * kThreads * 8 * elem_size<T>(), d);
   }
+  if (z.rest < V) put_elem(a.grad, gbase + z.rest, live ? g * soft(z.last) : 0.0f, T == kElemBF16);
   __syncthreads();
 #pragma unroll
   for (int j = 0; j < kPer; j++) {
     const int k = threadIdx.x + j * kThreads;
-    if (k >= a.listed) continue;
-    const int ix = l.index[k];
-    if (ix >= e0 && ix < e1) put_elem(a.grad, gbase + ix, mine[j], T == kElemBF16);
+    if (live && k < a.listed && ours(l.index[k])) put_elem(a.grad, gbase + l.index[k], mine[j], T == kElemBF16);
   }
 }
 
@@ -226,10 +253,9 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
 // as it is summed), so loads and stores overlap.  The lists are a row ahead too,
 // their entries' loads before the row's (loads return in order: an entry asked
 // for after them would come after them, and hold the first wavefront up).
-// WHAT: 0 the loss, 1 the gradient from a.lse, 2 both.
-template <int T, int NT, int NV, int WHAT>
+// GRAD: the gradient too.
+template <int T, int NT, int NV, bool GRAD>
 __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) {
-  constexpr bool GRAD = WHAT != 0, SUM = WHAT != 1;
   constexpr int kPer = kListed / NT;  // entries a thread fetches
   struct Row {  // of rows in turn
     Listed l;
@@ -242,41 +268,49 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
   const int tid = threadIdx.x, lane = tid & 63, V = (int)a.classes, K = a.listed;
   const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
   Piece<T> pc[NV];
-  // pieces are whole (all lanes' where the row goes that far); the row's last V % 8 classes are one a thread
-  const auto whole = [&](int v) { return (v + 1) * NT * 8 <= V || (v * NT + tid + 1) * 8 <= V; };
-  const auto load = [&](int v, int64_t row) {
-    pc[v].load(a.logits, row * a.logits_stride + (v * NT + tid) * 8, whole(v) ? 8 : 0, 0xff80);
+  // Pieces are whole: a row's buffer ends with its last one; the V % 8 classes past it are one a thread.  No load or
+  // store stands behind a branch: the compiler would make the first use of any load wait for all of them.  A
+  // workgroup without a next row loads its own again.
+  constexpr int kSize = elem_size<T>();
+  const int mine = tid * 8 * kSize, bytes = (V & ~7) * kSize;
+  const auto whole = [&](int v) { return v * NT * 8 * kSize + mine < bytes; };
+  const auto buffer = [&](const void* p, int64_t stride, int64_t row) {
+    return wave_buffer(const_cast<char*>(reinterpret_cast<const char*>(p)) + row * stride * kSize, bytes);
   };
+  const auto load = [&](int v, __amdgpu_buffer_rsrc_t b) { load_piece<T>(pc[v], b, mine, v * NT * 8 * kSize); };
   const int rest = (V & ~7) + tid;
   float last = -INFINITY;
   const auto load_last = [&](int64_t row) {
-    if (rest < V) last = elem(a.logits, row * a.logits_stride + rest, T == kElemBF16);
+    last = elem(a.logits, row * a.logits_stride + (rest < V ? rest : 0), T == kElemBF16);
   };
   // the list of a row: entries, then (in LDS, with the teacher's logits / tau) their logits
-  int64_t ix[kPer];
-  float te[kPer], ze[kPer];
+  int32_t ix[kPer], ih[kPer];
+  uint16_t te[kPer], tl[kPer];
+  float ze[kPer];
   const auto load_list = [&](int64_t row) {
 #pragma unroll
     for (int j = 0; j < kPer; j++) {
-      const int k = tid + j * NT;
-      const int64_t e = row * K + k;
-      if (k < K) {
-        ix[j] = a.index_bits == 64 ? reinterpret_cast<const int64_t*>(a.index)[e]
-                                   : (int64_t) reinterpret_cast<const int32_t*>(a.index)[e];
-        te[j] = elem(a.teacher, e, a.teacher_dtype == QUASAR_BF16);
-      }
+      const int64_t e = row * K + (tid + j * NT < K ? tid + j * NT : 0);
+      // 64-bit entries by their halves: the same two loads for either type
+      const int32_t* const lo = reinterpret_cast<const int32_t*>(a.index) + (a.index_bits == 64 ? 2 * e : e);
+      ix[j] = lo[0];
+      ih[j] = lo[a.index_bits == 64 ? 1 : 0];
+      const bool tb = a.teacher_dtype == QUASAR_BF16;
+      te[j] = reinterpret_cast<const uint16_t*>(a.teacher)[tb ? e : 2 * e + 1];
+      tl[j] = reinterpret_cast<const uint16_t*>(a.teacher)[tb ? e : 2 * e];
     }
   };
   const auto put_list = [&](Row& o, int64_t row) {
 #pragma unroll
     for (int j = 0; j < kPer; j++) {
       const int k = tid + j * NT;
+      const bool ok = ix[j] >= 0 && ix[j] < V && (a.index_bits == 32 || ih[j] == 0);
+      const float t = as_f32((uint32_t)te[j] << 16 | (a.teacher_dtype == QUASAR_BF16 ? 0u : tl[j]));
       if (k < K) {
-        const bool ok = ix[j] >= 0 && ix[j] < V;
-        o.l.index[k] = ok ? (int)ix[j] : -1;
-        o.l.p[k] = ok ? te[j] * it : -INFINITY;
-        ze[j] = elem(a.logits, row * a.logits_stride + (ok ? ix[j] : 0), T == kElemBF16);
+        o.l.index[k] = ok ? ix[j] : -1;
+        o.l.p[k] = ok ? t * it : -INFINITY;
       }
+      ze[j] = elem(a.logits, row * a.logits_stride + (ok ? ix[j] : 0), T == kElemBF16);
     }
   };
   const auto put_logits = [&](Row& o) {
@@ -287,7 +321,7 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
   if (blockIdx.x < a.rows) {
     load_list(blockIdx.x);
 #pragma unroll
-    for (int v = 0; v < NV; v++) load(v, blockIdx.x);
+    for (int v = 0; v < NV; v++) load(v, buffer(a.logits, a.logits_stride, blockIdx.x));
     load_last(blockIdx.x);
     put_list(rows[0], blockIdx.x);
     put_logits(rows[0]);
@@ -296,20 +330,18 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
     Row &o = rows[turn], &n = rows[turn ^ 1];
-    const int64_t next = row + gridDim.x;
+    const int64_t next = row + gridDim.x < a.rows ? row + gridDim.x : row;
     const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
-    if (next < a.rows) load_list(next);
-    float lse = SUM ? 0.0f : a.lse[row];
+    const __amdgpu_buffer_rsrc_t coming = buffer(a.logits, a.logits_stride, next);
+    load_list(next);
     MaxSum r{-INFINITY, 0.0f};
-    if constexpr (SUM) {
 #pragma unroll
-      for (int v = 0; v < NV; v++) {
-        take(r, pc[v], c);
-        if (!GRAD && next < a.rows) load(v, next);
-      }
+    for (int v = 0; v < NV; v++) {
+      if (whole(v)) take(r, pc[v], c);
+      if constexpr (!GRAD) load(v, coming);
     }
-    if (SUM && rest < V) r = join(r, last == -INFINITY ? MaxSum{last, 0.0f} : MaxSum{last, last == last ? 1.0f : last}, c);
-    if (!GRAD && next < a.rows) load_last(next);
+    if (rest < V) r = take_one(r, last, c);
+    if constexpr (!GRAD) load_last(next);
     if (tid < 64) {
       float m = -INFINITY, s = 0.0f, h = 0.0f;
       bool nan = false;
@@ -335,14 +367,10 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
         o.live = live;
       }
     }
-    if constexpr (SUM) {
-      r = group_join<NT / 64>(r, c, o.s);  // its barrier shows the list too
-      lse = lse_of(r, it);
-    } else {
-      __syncthreads();
-    }
+    r = group_join<NT / 64>(r, c, o.s);  // its barrier shows the list too
     const bool live = o.live;
-    if (SUM && tid < 64) {
+    const float lse = lse_of(r, it);
+    if (tid < 64) {
       float s = 0.0f;
       if (live)
         for (int k = lane; k < K; k += 64)
@@ -353,15 +381,12 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
         a.lse[row] = live ? lse : 0.0f;
       }
     }
-    if (next < a.rows) put_list(n, next);
+    put_list(n, next);
     if constexpr (GRAD) {
       const int64_t gbase = row * a.grad_stride;
-      const float g = (!SUM && a.grad_loss ? a.grad_loss[row] : a.grad_scale) * weight * it;
-      const float ls = SUM ? __builtin_amdgcn_logf(r.s) : 0.0f;
-      // the student's probability; the logits and lse may be large, their difference is taken first
-      const auto soft = [&](float z) {
-        return __builtin_amdgcn_exp2f(SUM ? __builtin_fmaf(z - r.m, c, -ls) : __builtin_fmaf(z, it, -lse) * kLog2e);
-      };
+      const __amdgpu_buffer_rsrc_t going = buffer(a.grad, a.grad_stride, row);
+      const float g = a.grad_scale * weight * it, ls = __builtin_amdgcn_logf(r.s);
+      const auto soft = [&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z - r.m, c, -ls)); };
 #pragma unroll
       for (int v = 0; v < NV; v++) {
         float d[8];
@@ -370,11 +395,11 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
         for (int i = 0; i < 8; i++) d[i] = soft(pc[v].get(i));
 #pragma unroll
         for (int i = 0; i < 8; i++) d[i] = live ? g * d[i] : 0.0f;
-        if (whole(v)) store_piece<T == kElemBF16>(a.grad, gbase + (v * NT + tid) * 8, d, 8);
-        if (next < a.rows) load(v, next);
+        store_piece<T == kElemBF16>(going, mine, v * NT * 8 * kSize, d);
+        load(v, coming);
       }
       if (rest < V) put_elem(a.grad, gbase + rest, live ? g * soft(last) : 0.0f, T == kElemBF16);
-      if (next < a.rows) load_last(next);
+      load_last(next);
       __syncthreads();  // the listed classes' gradients over the others'
       if (live) {
         for (int k = tid; k < K; k += NT) {
@@ -383,22 +408,23 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
             put_elem(a.grad, gbase + at, g * (soft(o.z[k]) - listed_p(o.l, K, at)), T == kElemBF16);
         }
       }
-      if (next < a.rows) put_logits(n);
+      put_logits(n);
     } else {
-      if (next < a.rows) put_logits(n);
+      put_logits(n);
       __syncthreads();
     }
   }
 }
 
-// The split form: classes a workgroup takes, so that about four run on a CU,
-// 2048 at least (a piece of eight a thread) and 16384 at most.
-int part_of(int64_t rows, int64_t classes) {
-  const int64_t want = rows >= 4096 ? kMostPart : rows * classes / (4 * kCUs);
-  return (int)(want <= 2048 ? 2048 : want >= kMostPart ? kMostPart : (want + 2047) / 2048 * 2048);
+// The split form: pieces a thread takes (1, 2, 4 or 8), so that two
+// workgroups or more run on a CU.
+int part_pieces(int64_t rows, int64_t classes) {
+  int nv = 8;
+  while (nv > 1 && rows * ((classes + 2048 * nv - 1) / (2048 * nv)) < 2 * kCUs) nv /= 2;
+  return nv;
 }
 int parts_of(int64_t rows, int64_t classes) {
-  const int per = part_of(rows, classes);
+  const int per = 2048 * part_pieces(rows, classes);
   return (int)((classes + per - 1) / per);
 }
 
@@ -408,15 +434,15 @@ constexpr int kMostPieces = T == kElemBF16 ? 16 : 8;
 
 bool resident(int64_t rows, int64_t classes, bool bf16) {
   const int64_t most = 1024 * 8 * (bf16 ? kMostPieces<kElemBF16> : kMostPieces<kElemF32>);
-  return classes <= most && (rows >= kCUs || classes <= kMostPart);
+  return classes <= most && (rows >= kCUs || classes <= 16384);
 }
 
-template <int T, int WHAT>
+template <int T, bool GRAD>
 hipError_t launch_resident(const quasar_distill& a, hipStream_t stream) {
 #define QUASAR_RESIDENT(NT, NV)                                                                     \
   if (a.classes <= (NT) * 8 * (NV)) {                                                               \
     const int64_t most = (int64_t)kCUs * (1024 / (NT));                                             \
-    distill_resident_kernel<T, NT, NV, WHAT>                                                        \
+    distill_resident_kernel<T, NT, NV, GRAD>                                                        \
         <<<dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(NT), 0, stream>>>(a);              \
     return hipGetLastError();                                                                       \
   }
@@ -431,6 +457,40 @@ hipError_t launch_resident(const quasar_distill& a, hipStream_t stream) {
   return hipErrorInvalidValue;
 }
 
+template <int T, int NV>
+hipError_t launch_split(const quasar_distill& a, int what, hipStream_t stream) {
+  const int parts = parts_of(a.rows, a.classes);
+  const dim3 grid((unsigned)(a.rows * parts)), block(kThreads);
+  MaxSum* ws = reinterpret_cast<MaxSum*>(a.workspace);
+  const auto row_kernel = [&](int w, int sums) {
+    distill_row_kernel<T, NV><<<w == 0 ? dim3((unsigned)a.rows) : grid, block, 0, stream>>>(a, w, w == 0 ? 1 : parts, ws,
+                                                                                          sums);
+    return hipGetLastError();
+  };
+  if (what == 1) return row_kernel(1, 0);
+  distill_scan_kernel<T, NV><<<grid, block, 0, stream>>>(a, parts, ws);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  // in place, the loss is taken before another part's gradient overwrites a listed logit
+  if (what == 2 && parts > 1 && a.grad == a.logits) {
+    e = row_kernel(0, parts);
+    return e != hipSuccess ? e : row_kernel(1, 0);
+  }
+  return row_kernel(what, parts);
+}
+
+template <int T>
+hipError_t launch_type(const quasar_distill& a, int what, hipStream_t stream) {
+  if (what != 1 && resident(a.rows, a.classes, T == kElemBF16))
+    return what == 0 ? launch_resident<T, false>(a, stream) : launch_resident<T, true>(a, stream);
+  switch (part_pieces(a.rows, a.classes)) {
+    case 1: return launch_split<T, 1>(a, what, stream);
+    case 2: return launch_split<T, 2>(a, what, stream);
+    case 4: return launch_split<T, 4>(a, what, stream);
+    default: return launch_split<T, 8>(a, what, stream);
+  }
+}
+
 }  // namespace
 
 size_t distill_workspace(int64_t rows, int64_t classes) {
@@ -438,42 +498,7 @@ size_t distill_workspace(int64_t rows, int64_t classes) {
 }
 
 hipError_t launch_distill(const quasar_distill& a, int what, hipStream_t stream) {
-  const bool bf16 = a.logits_dtype == QUASAR_BF16;
-  if (resident(a.rows, a.classes, bf16)) {
-    if (bf16)
-      return what == 0   ? launch_resident<kElemBF16, 0>(a, stream)
-             : what == 1 ? launch_resident<kElemBF16, 1>(a, stream)
-                         : launch_resident<kElemBF16, 2>(a, stream);
-    return what == 0   ? launch_resident<kElemF32, 0>(a, stream)
-           : what == 1 ? launch_resident<kElemF32, 1>(a, stream)
-                       : launch_resident<kElemF32, 2>(a, stream);
-  }
-  const int parts = parts_of(a.rows, a.classes), per = part_of(a.rows, a.classes);
-  MaxSum* ws = reinterpret_cast<MaxSum*>(a.workspace);
-  const auto row_kernel = [&](int w, int n, int sums) {
-    const dim3 grid((unsigned)(a.rows * n)), block(kThreads);
-    const int each = n == 1 ? (int)a.classes : per;
-    if (bf16)
-      distill_row_kernel<kElemBF16><<<grid, block, 0, stream>>>(a, w, each, n, ws, sums);
-    else
-      distill_row_kernel<kElemF32><<<grid, block, 0, stream>>>(a, w, each, n, ws, sums);
-    return hipGetLastError();
-  };
-  if (what != 1) {
-    const dim3 grid((unsigned)(a.rows * parts)), block(kThreads);
-    if (bf16)
-      distill_scan_kernel<kElemBF16><<<grid, block, 0, stream>>>(a, per, parts, ws);
-    else
-      distill_scan_kernel<kElemF32><<<grid, block, 0, stream>>>(a, per, parts, ws);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    // in place, the loss is taken before another part's gradient overwrites a listed logit
-    if (what == 2 && parts > 1 && a.grad == a.logits) {
-      e = row_kernel(0, 1, parts);
-      return e != hipSuccess ? e : row_kernel(1, parts, 0);
-    }
-  }
-  return what == 1 ? row_kernel(1, parts, 0) : row_kernel(what, what == 0 ? 1 : parts, parts);
+  return a.logits_dtype == QUASAR_BF16 ? launch_type<kElemBF16>(a, what, stream) : launch_type<kElemF32>(a, what, stream);
 }
 
 }  // namespace quasar

@@ -116,6 +116,34 @@ __device__ __forceinline__ void store_piece(void* base, int64_t e, const float (
     store_piece<false>(base, e, v, n);
 }
 
+// Eight elements at byte `at` (the lane's) + `from` (uniform) of a wavefront's
+// buffer (wave_buffer in device_common.h): past its end loads give 0 and
+// stores do nothing, without a branch.
+template <int T>
+__device__ __forceinline__ void load_piece(Piece<T>& p, __amdgpu_buffer_rsrc_t b, int at, int from) {
+  if constexpr (T == kElemBF16) {
+    const u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(b, at, from, 0);
+    p.d[0] = t.x; p.d[1] = t.y; p.d[2] = t.z; p.d[3] = t.w;
+  } else {
+    const u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(b, at, from, 0);
+    const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(b, at + 16, from, 0);
+    p.f[0] = as_f32(t.x); p.f[1] = as_f32(t.y); p.f[2] = as_f32(t.z); p.f[3] = as_f32(t.w);
+    p.f[4] = as_f32(u.x); p.f[5] = as_f32(u.y); p.f[6] = as_f32(u.z); p.f[7] = as_f32(u.w);
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ void store_piece(__amdgpu_buffer_rsrc_t b, int at, int from, const float (&v)[8]) {
+  if constexpr (BF16) {
+    const u32x4 t = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    __builtin_amdgcn_raw_buffer_store_b128(t, b, at, from, 0);
+  } else {
+    const u32x4 t = {as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])};
+    const u32x4 u = {as_u32(v[4]), as_u32(v[5]), as_u32(v[6]), as_u32(v[7])};
+    __builtin_amdgcn_raw_buffer_store_b128(t, b, at, from, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(u, b, at + 16, from, 0);
+  }
+}
+
 // Eight values as E4M3 bytes (nearest even; |v| <= 448 (1 + 2^-4) rounds
 // inside the format, NaN gives its NaN).
 __device__ __forceinline__ uint2 pack_e4m3x8(const float (&v)[8]) {
