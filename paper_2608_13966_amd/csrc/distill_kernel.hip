@@ -1,10 +1,12 @@
 // distill_kernel.hip -- the loss against a teacher's top logits and its
 // gradient (quasar_ops.h).
 //
-// The listed classes of a row are few: every workgroup that works on a row
-// takes them into LDS and normalises the teacher's side itself.  The student's
-// row is what costs: it is read for lse as a running maximum and a sum of
-// exponentials (rescaled when the maximum grows), and for the gradient again.
+// The listed classes of a row are few: one wavefront of every workgroup that
+// works on a row takes them into LDS and normalises the teacher's side.  The
+// student's row is what costs: it is read for lse as a running maximum and a sum
+// of exponentials (rescaled when the maximum grows), and needed for the gradient
+// again: a row that fits one workgroup's registers stays there (resident
+// kernel), others, and rows too few to fill the CUs, go in parts twice.
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -43,41 +45,49 @@ __device__ __forceinline__ float listed_p(const Listed& l, int K, int ix) {
   return p;
 }
 
-// Loads row `row`'s list; the teacher's probabilities are in l.p after the
-// call (a barrier ends it).  False: no entry has p > 0, or row_weight is 0.
-// plogp: sum of p log p.
-__device__ bool load_listed(const quasar_distill& a, int64_t row, Listed& l, float* red, float& plogp) {
-  const int K = a.listed;
-  const float it = 1.0f / a.temperature;
-  if (a.row_weight && a.row_weight[row] == 0.0f) return false;
-  float m = -INFINITY;
+// A row's list in LDS, the work of one wavefront; a barrier has to follow.
+struct RowList {
+  Listed l;
+  float z[kListed];  // the student's logits there
+  float plogp;       // sum of p log p
+  int live;          // 0: masked (row_weight 0, or no entry with p > 0)
+};
+// From the entries' teacher logits / tau in o.l.p to their probabilities.
+__device__ __forceinline__ void normalise(RowList& o, int K, float weight) {
+  const int lane = threadIdx.x & 63;
+  wave_lds_fence();
+  float m = -INFINITY, s = 0.0f, h = 0.0f;
   bool nan = false;
-  for (int k = threadIdx.x; k < K; k += kThreads) {
-    const int64_t e = row * K + k;
-    const int64_t ix = a.index_bits == 64 ? reinterpret_cast<const int64_t*>(a.index)[e]
-                                          : (int64_t) reinterpret_cast<const int32_t*>(a.index)[e];
-    const bool ok = ix >= 0 && ix < a.classes;
-    const float t = ok ? elem(a.teacher, e, a.teacher_dtype == QUASAR_BF16) * it : -INFINITY;
-    l.index[k] = ok ? (int)ix : -1;
-    l.p[k] = t;
-    m = fmaxf(m, t);
-    nan |= t != t;
+  for (int k = lane; k < K; k += 64) {
+    m = fmaxf(m, o.l.p[k]);
+    nan |= o.l.p[k] != o.l.p[k];
   }
-  m = group_reduce<kWaves>(m, red, MaxOp());
-  const bool any_nan = __syncthreads_or(nan);
-  if (m == -INFINITY && !any_nan) return false;
+  m = wave_reduce(m, MaxOp());
+  const bool live = weight != 0.0f && (m != -INFINITY || __ballot(nan) != 0);
+  if (live) {
+    for (int k = lane; k < K; k += 64) s += __builtin_amdgcn_exp2f((o.l.p[k] - m) * kLog2e);
+    s = wave_reduce(s, SumOp());
+    const float ls = __logf(s), is = 1.0f / s;
+    for (int k = lane; k < K; k += 64) {
+      const float t = o.l.p[k] - m, p = __builtin_amdgcn_exp2f(t * kLog2e) * is;
+      o.l.p[k] = p;
+      if (!(p == 0.0f)) h += p * (t - ls);
+    }
+    h = wave_reduce(h, SumOp());
+  }
+  if (lane == 0) {
+    o.plogp = h;
+    o.live = live;
+  }
+}
+// The row's loss; the first wavefront's lanes get it.
+__device__ __forceinline__ float loss_of(const RowList& o, int K, float weight, float lse, float it) {
   float s = 0.0f;
-  for (int k = threadIdx.x; k < K; k += kThreads) s += __builtin_amdgcn_exp2f((l.p[k] - m) * kLog2e);
-  s = group_reduce<kWaves>(s, red + kWaves, SumOp());
-  const float ls = __logf(s), is = 1.0f / s;
-  float h = 0.0f;
-  for (int k = threadIdx.x; k < K; k += kThreads) {
-    const float t = l.p[k] - m, p = __builtin_amdgcn_exp2f(t * kLog2e) * is;
-    l.p[k] = p;
-    if (!(p == 0.0f)) h += p * (t - ls);
-  }
-  plogp = group_reduce<kWaves>(h, red + 2 * kWaves, SumOp());
-  return true;
+  if (o.live)
+    for (int k = threadIdx.x & 63; k < K; k += 64)
+      if (o.l.index[k] >= 0 && !(o.l.p[k] == 0.0f)) s += o.l.p[k] * (lse - o.z[k] * it);
+  s = wave_reduce(s, SumOp());
+  return o.live ? weight * (o.plogp + s) : 0.0f;
 }
 
 // r joined with eight more logits
@@ -177,55 +187,43 @@ __global__ __launch_bounds__(kThreads) void distill_scan_kernel(quasar_distill a
 template <int T, int NV>
 __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a, int what, int parts, const MaxSum* part,
                                                                int sums) {
-  __shared__ Listed l;
-  __shared__ float red[4 * kWaves];
+  __shared__ RowList o;
   const int64_t row = blockIdx.x / (unsigned)parts, base = row * a.logits_stride, gbase = row * a.grad_stride;
   const int at = blockIdx.x % (unsigned)parts, e0 = at * Part<T, NV>::kClasses;
   const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
-  const int V = (int)a.classes;
+  const int V = (int)a.classes, K = a.listed;
+  const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
+  if (threadIdx.x < 64) {
+    for (int k = threadIdx.x; k < K; k += 64) {
+      const int64_t e = row * K + k;
+      const int64_t ix = a.index_bits == 64 ? reinterpret_cast<const int64_t*>(a.index)[e]
+                                            : (int64_t) reinterpret_cast<const int32_t*>(a.index)[e];
+      const bool ok = ix >= 0 && ix < V;
+      o.l.index[k] = ok ? (int)ix : -1;
+      o.l.p[k] = ok ? elem(a.teacher, e, a.teacher_dtype == QUASAR_BF16) * it : -INFINITY;
+      o.z[k] = elem(a.logits, base + (ok ? ix : 0), T == kElemBF16);
+    }
+  }
   Part<T, NV> z(V, e0);
   if (what != 0) z.load(reinterpret_cast<const char*>(a.logits) + base * elem_size<T>(), V, e0);
   MaxSum r{-INFINITY, 0.0f};  // of the row's parts: each wavefront joins them
   for (int i = threadIdx.x & 63; i < sums; i += 64) r = join(r, part[row * sums + i], c);
-  float plogp = 0.0f;
-  const bool live = load_listed(a, row, l, red, plogp);
-  const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
-  float lse = 0.0f;
-  if (!live) {
-    if (what != 1 && at == 0 && threadIdx.x == 0) a.loss[row] = a.lse[row] = 0.0f;
-  } else if (sums > 0) {
-    lse = lse_of(wave_join(r, c), it);
-  } else {
-    lse = a.lse[row];
-  }
-  if (live && what != 1 && at == 0) {
-    float s = 0.0f;
-    for (int k = threadIdx.x; k < a.listed; k += kThreads)
-      if (l.index[k] >= 0 && !(l.p[k] == 0.0f))
-        s += l.p[k] * (lse - elem(a.logits, base + l.index[k], T == kElemBF16) * it);
-    s = group_reduce<kWaves>(s, red + 3 * kWaves, SumOp());
+  if (threadIdx.x < 64) normalise(o, K, weight);
+  const float lse = sums > 0 ? lse_of(wave_join(r, c), it) : a.lse[row];
+  __syncthreads();
+  const bool live = o.live;
+  if (what != 1 && at == 0 && threadIdx.x < 64) {
+    const float loss = loss_of(o, K, weight, lse, it);
     if (threadIdx.x == 0) {
-      a.loss[row] = weight * (plogp + s);
-      a.lse[row] = lse;
+      a.loss[row] = loss;
+      a.lse[row] = live ? lse : 0.0f;
     }
   }
   if (what == 0) return;
   const float g = (a.grad_loss ? a.grad_loss[row] : a.grad_scale) * weight * it;
   // the student's probability; z / tau and lse may be large, their difference is taken first
   const auto soft = [&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, it, -lse) * kLog2e); };
-  // the listed classes' gradients, from their logits before `grad` may overwrite them
   const int e1 = e0 + Part<T, NV>::kClasses < V ? e0 + Part<T, NV>::kClasses : V;
-  const auto ours = [&](int ix) { return ix >= e0 && ix < e1; };
-  constexpr int kPer = kListed / kThreads;
-  float mine[kPer];
-#pragma unroll
-  for (int j = 0; j < kPer; j++) {
-    const int k = threadIdx.x + j * kThreads;
-    mine[j] = 0.0f;
-    if (live && k < a.listed && ours(l.index[k]))
-      mine[j] = g * (soft(elem(a.logits, base + l.index[k], T == kElemBF16)) - listed_p(l, a.listed, l.index[k]));
-  }
-  __syncthreads();
   const __amdgpu_buffer_rsrc_t out =
       wave_buffer(reinterpret_cast<char*>(a.grad) + (gbase + e0) * elem_size<T>(), z.bytes);
 #pragma unroll
@@ -235,14 +233,14 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
     for (int i = 0; i < 8; i++) d[i] = soft(z.p[v].get(i));
 #pragma unroll
     for (int i = 0; i < 8; i++) d[i] = live ? g * d[i] : 0.0f;
-    store_piece<T == kElemBF16>(out, z.at, v * kThreads * 8 * elem_size<T>(), d);
+    store_piece<T == kElemBF16>(out, z.at + v * kThreads * 8 * elem_size<T>(), d);
   }
   if (z.rest < V) put_elem(a.grad, gbase + z.rest, live ? g * soft(z.last) : 0.0f, T == kElemBF16);
-  __syncthreads();
-#pragma unroll
-  for (int j = 0; j < kPer; j++) {
-    const int k = threadIdx.x + j * kThreads;
-    if (live && k < a.listed && ours(l.index[k])) put_elem(a.grad, gbase + l.index[k], mine[j], T == kElemBF16);
+  __syncthreads();  // the listed classes' gradients over the others'
+  if (!live) return;
+  for (int k = threadIdx.x; k < K; k += kThreads) {
+    const int ix = o.l.index[k];
+    if (ix >= e0 && ix < e1) put_elem(a.grad, gbase + ix, g * (soft(o.z[k]) - listed_p(o.l, K, ix)), T == kElemBF16);
   }
 }
 
@@ -257,15 +255,11 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
 template <int T, int NT, int NV, bool GRAD>
 __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) {
   constexpr int kPer = kListed / NT;  // entries a thread fetches
-  struct Row {  // of rows in turn
-    Listed l;
-    float z[kListed];
+  struct Row : RowList {
     MaxSum s[NT / 64];
-    float plogp;
-    int live;
   };
-  __shared__ Row rows[2];
-  const int tid = threadIdx.x, lane = tid & 63, V = (int)a.classes, K = a.listed;
+  __shared__ Row rows[2];  // of rows in turn
+  const int tid = threadIdx.x, V = (int)a.classes, K = a.listed;
   const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
   Piece<T> pc[NV];
   // Pieces are whole: a row's buffer ends with its last one; the V % 8 classes past it are one a thread.  No load or
@@ -342,42 +336,14 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
     }
     if (rest < V) r = take_one(r, last, c);
     if constexpr (!GRAD) load_last(next);
-    if (tid < 64) {
-      float m = -INFINITY, s = 0.0f, h = 0.0f;
-      bool nan = false;
-      for (int k = lane; k < K; k += 64) {
-        m = fmaxf(m, o.l.p[k]);
-        nan |= o.l.p[k] != o.l.p[k];
-      }
-      m = wave_reduce(m, MaxOp());
-      const bool live = weight != 0.0f && (m != -INFINITY || __ballot(nan) != 0);
-      if (live) {
-        for (int k = lane; k < K; k += 64) s += __builtin_amdgcn_exp2f((o.l.p[k] - m) * kLog2e);
-        s = wave_reduce(s, SumOp());
-        const float ls = __logf(s), is = 1.0f / s;
-        for (int k = lane; k < K; k += 64) {
-          const float t = o.l.p[k] - m, p = __builtin_amdgcn_exp2f(t * kLog2e) * is;
-          o.l.p[k] = p;
-          if (!(p == 0.0f)) h += p * (t - ls);
-        }
-        h = wave_reduce(h, SumOp());
-      }
-      if (lane == 0) {
-        o.plogp = h;
-        o.live = live;
-      }
-    }
+    if (tid < 64) normalise(o, K, weight);
     r = group_join<NT / 64>(r, c, o.s);  // its barrier shows the list too
     const bool live = o.live;
     const float lse = lse_of(r, it);
     if (tid < 64) {
-      float s = 0.0f;
-      if (live)
-        for (int k = lane; k < K; k += 64)
-          if (o.l.index[k] >= 0 && !(o.l.p[k] == 0.0f)) s += o.l.p[k] * (lse - o.z[k] * it);
-      s = wave_reduce(s, SumOp());
-      if (lane == 0) {
-        a.loss[row] = live ? weight * (o.plogp + s) : 0.0f;
+      const float loss = loss_of(o, K, weight, lse, it);
+      if (tid == 0) {
+        a.loss[row] = loss;
         a.lse[row] = live ? lse : 0.0f;
       }
     }
@@ -395,7 +361,7 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
         for (int i = 0; i < 8; i++) d[i] = soft(pc[v].get(i));
 #pragma unroll
         for (int i = 0; i < 8; i++) d[i] = live ? g * d[i] : 0.0f;
-        store_piece<T == kElemBF16>(going, mine, v * NT * 8 * kSize, d);
+        store_piece<T == kElemBF16>(going, mine + v * NT * 8 * kSize, d);
         load(v, coming);
       }
       if (rest < V) put_elem(a.grad, gbase + rest, live ? g * soft(last) : 0.0f, T == kElemBF16);

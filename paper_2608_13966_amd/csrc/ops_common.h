@@ -131,16 +131,20 @@ __device__ __forceinline__ void load_piece(Piece<T>& p, __amdgpu_buffer_rsrc_t b
     p.f[4] = as_f32(u.x); p.f[5] = as_f32(u.y); p.f[6] = as_f32(u.z); p.f[7] = as_f32(u.w);
   }
 }
+// The stores' offset is the vector one alone: after a 128-bit buffer store with
+// a scalar offset register the compiler puts no wait state before an overwrite
+// of the data's first register, and such stores wrote the overwriting value's
+// dword here now and then.
 template <bool BF16>
-__device__ __forceinline__ void store_piece(__amdgpu_buffer_rsrc_t b, int at, int from, const float (&v)[8]) {
+__device__ __forceinline__ void store_piece(__amdgpu_buffer_rsrc_t b, int at, const float (&v)[8]) {
   if constexpr (BF16) {
     const u32x4 t = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-    __builtin_amdgcn_raw_buffer_store_b128(t, b, at, from, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(t, b, at, 0, 0);
   } else {
     const u32x4 t = {as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])};
     const u32x4 u = {as_u32(v[4]), as_u32(v[5]), as_u32(v[6]), as_u32(v[7])};
-    __builtin_amdgcn_raw_buffer_store_b128(t, b, at, from, 0);
-    __builtin_amdgcn_raw_buffer_store_b128(u, b, at + 16, from, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(t, b, at, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(u, b, at + 16, 0, 0);
   }
 }
 
