@@ -52,6 +52,39 @@ struct RowList {
   float plogp;       // sum of p log p
   int live;          // 0: masked (row_weight 0, or no entry with p > 0)
 };
+// Entry k of a row's list as it lies in memory: the same loads for either type
+// of index and of teacher, without a branch.
+struct Entry {
+  int32_t lo, hi;
+  uint16_t top, low;
+  __device__ __forceinline__ Entry() {}
+  __device__ __forceinline__ Entry(const quasar_distill& a, int64_t row, int k) {
+    const int64_t e = row * a.listed + k;
+    const bool wide = a.index_bits == 64, tb = a.teacher_dtype == QUASAR_BF16;
+    const int32_t* const i = reinterpret_cast<const int32_t*>(a.index) + (wide ? 2 * e : e);
+    lo = i[0];
+    hi = i[wide ? 1 : 0];
+    const uint16_t* const t = reinterpret_cast<const uint16_t*>(a.teacher) + (tb ? e : 2 * e);
+    top = t[tb ? 0 : 1];
+    low = t[0];
+  }
+  // the class, or -1
+  __device__ __forceinline__ int at(const quasar_distill& a) const {
+    return lo >= 0 && lo < (int)a.classes && (a.index_bits == 32 || hi == 0) ? lo : -1;
+  }
+  __device__ __forceinline__ float teacher(const quasar_distill& a) const {
+    return as_f32((uint32_t)top << 16 | (a.teacher_dtype == QUASAR_BF16 ? 0u : low));
+  }
+  // into the list; its logit as well
+  template <int T>
+  __device__ __forceinline__ void put(const quasar_distill& a, RowList& o, int k, int64_t base, float it) const {
+    const int ix = at(a);
+    o.l.index[k] = ix;
+    o.l.p[k] = ix >= 0 ? teacher(a) * it : -INFINITY;
+    o.z[k] = elem(a.logits, base + (ix >= 0 ? ix : 0), T == kElemBF16);
+  }
+};
+
 // From the entries' teacher logits / tau in o.l.p to their probabilities.
 __device__ __forceinline__ void normalise(RowList& o, int K, float weight) {
   const int lane = threadIdx.x & 63;
@@ -193,19 +226,15 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
   const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
   const int V = (int)a.classes, K = a.listed;
   const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
-  if (threadIdx.x < 64) {
-    for (int k = threadIdx.x; k < K; k += 64) {
-      const int64_t e = row * K + k;
-      const int64_t ix = a.index_bits == 64 ? reinterpret_cast<const int64_t*>(a.index)[e]
-                                            : (int64_t) reinterpret_cast<const int32_t*>(a.index)[e];
-      const bool ok = ix >= 0 && ix < V;
-      o.l.index[k] = ok ? (int)ix : -1;
-      o.l.p[k] = ok ? elem(a.teacher, e, a.teacher_dtype == QUASAR_BF16) * it : -INFINITY;
-      o.z[k] = elem(a.logits, base + (ok ? ix : 0), T == kElemBF16);
-    }
-  }
+  // the list's first 64 entries are asked for before the row, whose loads would hold them up
+  const int lane = threadIdx.x & 63;
+  const Entry first(a, row, lane < K ? lane : 0);
   Part<T, NV> z(V, e0);
   if (what != 0) z.load(reinterpret_cast<const char*>(a.logits) + base * elem_size<T>(), V, e0);
+  if (threadIdx.x < 64) {
+    if (lane < K) first.put<T>(a, o, lane, base, it);
+    for (int k = lane + 64; k < K; k += 64) Entry(a, row, k).put<T>(a, o, k, base, it);
+  }
   MaxSum r{-INFINITY, 0.0f};  // of the row's parts: each wavefront joins them
   for (int i = threadIdx.x & 63; i < sums; i += 64) r = join(r, part[row * sums + i], c);
   if (threadIdx.x < 64) normalise(o, K, weight);
@@ -278,33 +307,21 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
     last = elem(a.logits, row * a.logits_stride + (rest < V ? rest : 0), T == kElemBF16);
   };
   // the list of a row: entries, then (in LDS, with the teacher's logits / tau) their logits
-  int32_t ix[kPer], ih[kPer];
-  uint16_t te[kPer], tl[kPer];
+  Entry en[kPer];
   float ze[kPer];
   const auto load_list = [&](int64_t row) {
 #pragma unroll
-    for (int j = 0; j < kPer; j++) {
-      const int64_t e = row * K + (tid + j * NT < K ? tid + j * NT : 0);
-      // 64-bit entries by their halves: the same two loads for either type
-      const int32_t* const lo = reinterpret_cast<const int32_t*>(a.index) + (a.index_bits == 64 ? 2 * e : e);
-      ix[j] = lo[0];
-      ih[j] = lo[a.index_bits == 64 ? 1 : 0];
-      const bool tb = a.teacher_dtype == QUASAR_BF16;
-      te[j] = reinterpret_cast<const uint16_t*>(a.teacher)[tb ? e : 2 * e + 1];
-      tl[j] = reinterpret_cast<const uint16_t*>(a.teacher)[tb ? e : 2 * e];
-    }
+    for (int j = 0; j < kPer; j++) en[j] = Entry(a, row, tid + j * NT < K ? tid + j * NT : 0);
   };
   const auto put_list = [&](Row& o, int64_t row) {
 #pragma unroll
     for (int j = 0; j < kPer; j++) {
-      const int k = tid + j * NT;
-      const bool ok = ix[j] >= 0 && ix[j] < V && (a.index_bits == 32 || ih[j] == 0);
-      const float t = as_f32((uint32_t)te[j] << 16 | (a.teacher_dtype == QUASAR_BF16 ? 0u : tl[j]));
+      const int k = tid + j * NT, ix = en[j].at(a);
       if (k < K) {
-        o.l.index[k] = ok ? ix[j] : -1;
-        o.l.p[k] = ok ? t * it : -INFINITY;
+        o.l.index[k] = ix;
+        o.l.p[k] = ix >= 0 ? en[j].teacher(a) * it : -INFINITY;
       }
-      ze[j] = elem(a.logits, row * a.logits_stride + (ok ? ix[j] : 0), T == kElemBF16);
+      ze[j] = elem(a.logits, row * a.logits_stride + (ix >= 0 ? ix : 0), T == kElemBF16);
     }
   };
   const auto put_logits = [&](Row& o) {
