@@ -557,8 +557,8 @@ constexpr int kFusedK = 128;
 __device__ __forceinline__ int wide_at(int m, int c) { return m * kFusedK + 8 * (c ^ (m & 15)); }
 
 template <int FMT, int BITS, int XT, int BM>
-__global__ __launch_bounds__(256, BM == 64 ? 3 : 2) void fused_kernel(Weights w, quasar_linear a, int tiles_m, int splits,
-                                                                      int steps_per, float* part) {
+__global__ __launch_bounds__(256, 2) void fused_kernel(Weights w, quasar_linear a, int tiles_m, int splits, int steps_per,
+                                                       float* part) {
   constexpr int TM = BM / 32, NX = BM / 16;  // 16-token tiles of a wavefront; chunks of x a thread fetches
   __shared__ __align__(16) uint16_t lds[(BM + 128) * kFusedK];
   static_assert(4 * kSlab * 4 <= (int)sizeof(lds), "the epilogue's stage fits");
@@ -586,17 +586,10 @@ __global__ __launch_bounds__(256, BM == 64 ? 3 : 2) void fused_kernel(Weights w,
   } f[2];
   const auto fetch = [&](Fetched& o, int s) {
     const int k = s * kFusedK;
-    if (k + kFusedK <= K) {
-      o.w[0].load(row0, k + 32 * wq);
-      o.w[1].load(row1, k + 32 * wq);
+    o.w[0].load(row0, k + 32 * wq);
+    o.w[1].load(row1, k + 32 * wq);
 #pragma unroll
-      for (int i = 0; i < NX; i++) o.x[i].load(xp[i], k);
-    } else {
-      o.w[0].load(row0, k + 32 * wq, K - k - 32 * wq);
-      o.w[1].load(row1, k + 32 * wq, K - k - 32 * wq);
-#pragma unroll
-      for (int i = 0; i < NX; i++) o.x[i].load(xp[i], k, k + 8 * xc < K);
-    }
+    for (int i = 0; i < NX; i++) o.x[i].load(xp[i], k);
   };
   const auto stage = [&](Fetched& o) {
 #pragma unroll
@@ -619,11 +612,10 @@ __global__ __launch_bounds__(256, BM == 64 ? 3 : 2) void fused_kernel(Weights w,
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  const auto step = [&](Fetched& o, int s) {
-    meet();  // every wavefront is done with the step before
-    stage(o);
-    if (s + 2 < s1) fetch(o, s + 2);
+  // matrix instructions first, where the CU's other workgroup decodes meanwhile (5 to 8% at 512 tokens)
+  const auto multiply = [&] {
     meet();
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < 4; k++) {
       bf16x8 mx[TM], mr[4];
@@ -638,14 +630,47 @@ __global__ __launch_bounds__(256, BM == 64 ? 3 : 2) void fused_kernel(Weights w,
 #pragma unroll
         for (int j = 0; j < 4; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx[i], mr[j], acc[i][j], 0, 0, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
+    meet();  // every wavefront is done with the step
   };
-  fetch(f[0], s0);
-  if (s0 + 1 < s1) fetch(f[1], s0 + 1);
-  for (int s = s0; s < s1; s += 2) {
-    step(f[0], s);
-    if (s + 1 < s1) step(f[1], s + 1);
+  // Whole steps, two in flight.  The loop's fetches stand behind no branch (the compiler would make the first use
+  // of any wait for all of them); the last two or three steps come after it.
+  const int whole = K / kFusedK < s1 ? K / kFusedK : s1, n = whole - s0;
+  if (n >= 2) {
+    fetch(f[0], s0);
+    fetch(f[1], s0 + 1);
+    int s = s0;
+    for (; s + 3 < whole; s += 2) {
+      stage(f[0]);
+      fetch(f[0], s + 2);
+      multiply();
+      stage(f[1]);
+      fetch(f[1], s + 3);
+      multiply();
+    }
+    stage(f[0]);
+    if (s + 2 < whole) fetch(f[0], s + 2);
+    multiply();
+    stage(f[1]);
+    multiply();
+    if (s + 2 < whole) {
+      stage(f[0]);
+      multiply();
+    }
+  } else if (n == 1) {
+    fetch(f[0], s0);
+    stage(f[0]);
+    multiply();
   }
-  meet();
+  if (whole < s1) {  // the columns past the whole steps
+    const int k = whole * kFusedK;
+    f[0].w[0].load(row0, k + 32 * wq, K - k - 32 * wq);
+    f[0].w[1].load(row1, k + 32 * wq, K - k - 32 * wq);
+#pragma unroll
+    for (int i = 0; i < NX; i++) f[0].x[i].load(xp[i], k, k + 8 * xc < K);
+    stage(f[0]);
+    multiply();
+  }
   store_tile<TM>(a, w.rows, acc, m0 + wm * (BM / 2), n0 + wn * 64, reinterpret_cast<float*>(lds) + wave * kSlab,
                  part ? part + (int64_t)split * a.tokens * w.rows : nullptr);
 }
@@ -669,23 +694,34 @@ __global__ __launch_bounds__(256) void join_kernel(quasar_linear a, int64_t rows
 // ---- many tokens --------------------------------------------------------------
 // r in bf16 [rows, kp], columns past the last zero; then (workgroups from
 // weight_blocks on) x in bf16 [tokens, kp] likewise, where it is not used as
-// it is.  A thread makes 32 weights, or 8 activations.
+// it is.  A thread makes 32 weights, which go through LDS so that a wavefront
+// stores whole lines, or 8 activations.
 template <int FMT, int BITS, int XT>
 __global__ __launch_bounds__(256) void unpack_kernel(Weights w, quasar_linear a, int kp, uint16_t* r, uint16_t* xo,
                                                      unsigned weight_blocks) {
   if (blockIdx.x < weight_blocks) {
-    const int per = kp / 32;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t row = i / per;
-    if (row >= w.rows) return;
-    const int k = (int)(i - row * per) * 32;
+    __shared__ uint4 lds[256 * 4];
+    const int lane = threadIdx.x & 63, per = kp / 32;
+    uint4* const mine = lds + wave_index() * 256;
+    const int64_t first = (int64_t)blockIdx.x * 256 + wave_index() * 64, i = first + lane, total = w.rows * per;
+    const int64_t row = i < total ? i / per : 0;
+    const int k = i < total ? (int)(i - row * per) * 32 : 0;
     const WeightRow<FMT, BITS> at(w, row);
     Strip<FMT, BITS> strip;
     const int left = (int)w.cols - k;
     strip.load(at, k, left);
     strip.ready(at.tensor_scale);
+    // strip l's chunk c lies at 4 l + (c ^ l / 4 % 4): both sides without bank conflicts
 #pragma unroll
-    for (int c = 0; c < 4; c++) st128(r + row * kp + k + 8 * c, 8 * c < left ? strip.chunk(c) : make_uint4(0u, 0u, 0u, 0u));
+    for (int c = 0; c < 4; c++)
+      mine[4 * lane + (c ^ ((lane >> 2) & 3))] = 8 * c < left ? strip.chunk(c) : make_uint4(0u, 0u, 0u, 0u);
+    wave_lds_fence();
+    uint4* const out = reinterpret_cast<uint4*>(r) + first * 4;
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+      const int chunk = 64 * j + lane, l = chunk >> 2;
+      if (first + l < total) out[chunk] = mine[4 * l + ((chunk & 3) ^ ((l >> 2) & 3))];
+    }
   } else {
     const int per = kp / 8;
     const int64_t i = (int64_t)(blockIdx.x - weight_blocks) * 256 + threadIdx.x;
