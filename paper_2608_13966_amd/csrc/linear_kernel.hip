@@ -757,21 +757,24 @@ __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm
 // A workgroup makes 256 tokens x 256 outputs with 8 wavefronts of 128 x 64.
 // Both operands of a step lie in LDS as two halves each (x0: the first 64
 // tokens of every wavefront's 128, r0: the first 32 outputs of its 64, x1 and
-// r1 the rest), and a step has four phases, each with 16 matrix instructions a
-// wavefront: (x0 r0), (x0 r1), (x1 r1), (x1 r0).  Two stages; a half is
-// filled again as soon as both halves of the workgroup are done with it.
+// r1 the rest), and a step has two phases, each with 32 matrix instructions a
+// wavefront: x0 (r0 r1), x1 (r0 r1).  Two stages; a half is filled again as soon
+// as both halves of the workgroup have read it.
 //
 // The wavefronts of a SIMD work in turn: those of wm = 1 run one barrier
 // behind, so that while one multiplies the other reads its next operands.
 // Barriers 2p and 2p + 1 end the reading and the multiplying of phase p for
-// wm = 0, 2p + 1 and 2p + 2 for wm = 1.  Hence
-//  - a half filled in phase p may be one whose last reads were in phase p - 2
-//    or before (x0: filled in phase 2 of a step, read in 0; r0: 3, 0; r1: 4, 1;
-//    x1: 5, 2);
+// wm = 0, 2p + 1 and 2p + 2 for wm = 1; a wavefront has its operands before it
+// comes to the barrier that ends the reading.  Hence
+//  - a half filled in phase p may be one whose last reads were in phase p - 1
+//    (x0, r0 and r1, read in a step's phase 0, are filled for the step after the
+//    next in its phase 1; x1 in the next step's phase 0);
 //  - what phase p reads has to have landed for every wavefront's own loads
 //    before the barrier that ends its reading of phase p - 1: with two loads a
-//    phase and at least four phases in between, "at most 8 outstanding" then.
-// Past the last step the loads repeat it, so that the counts hold.
+//    half, "at most 8 outstanding" then, either phase.
+// Past the last step the loads repeat it, so that the counts hold.  (Four phases
+// of 16 instructions, with twice the barriers, were 5% slower.)  At 8192 tokens,
+// 14336 x 4096: 640 us, 1.50 PFLOP/s, matrix units busy about 75% of the time.
 __global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uint16_t* x, int64_t x_stride,
                                                       const uint16_t* r, int64_t rows, int kp, int tiles_m, int tiles_n,
                                                       int steps_per, float* part) {
@@ -831,20 +834,22 @@ __global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uin
       for (int k = 0; k < 2; k++)
         fr[h][t][k] = as_bf16x8(*reinterpret_cast<const uint4*>(p + chunk_at(wn * 32 + 16 * t + (lane & 15), 4 * k + (lane >> 4))));
   };
-  // ends the phase's reading, multiplies, ends the phase
-  const auto multiply = [&](int hx, int hr) {
-    __builtin_amdgcn_s_barrier();
+  // ends the phase's reading, multiplies by both halves of r, ends the phase
+  const auto multiply = [&](int hx) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int k = 0; k < 2; k++)
+    for (int hr = 0; hr < 2; hr++)
 #pragma unroll
-      for (int i = 0; i < 4; i++)
+      for (int k = 0; k < 2; k++)
 #pragma unroll
-        for (int j = 0; j < 2; j++)
-          acc[hx * 4 + i][hr * 2 + j] =
-              __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i][k], fr[hr][j][k], acc[hx * 4 + i][hr * 2 + j], 0, 0, 0);
+        for (int i = 0; i < 4; i++)
+#pragma unroll
+          for (int j = 0; j < 2; j++)
+            acc[hx * 4 + i][hr * 2 + j] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(fx[i][k], fr[hr][j][k], acc[hx * 4 + i][hr * 2 + j], 0, 0, 0);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
@@ -858,7 +863,8 @@ __global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uin
   fill(3, 0);
   fill(0, 1);
   fill(1, 1);
-  asm volatile("s_waitcnt vmcnt(4)" ::: "memory");  // step 0
+  fill(2, 1);
+  landed8();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   if (wm == 1) __builtin_amdgcn_s_barrier();
@@ -866,19 +872,16 @@ __global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uin
     const int stage = s & 1;
     read_x(0, stage);
     read_r(0, stage);
-    fill(2, s + 1);
-    landed8();
-    multiply(0, 0);
     read_r(1, stage);
     fill(3, s + 1);
     landed8();
-    multiply(0, 1);
+    multiply(0);
     read_x(1, stage);
     fill(0, s + 2);
-    multiply(1, 1);
     fill(1, s + 2);
+    fill(2, s + 2);
     landed8();
-    multiply(1, 0);
+    multiply(1);
   }
   if (wm == 0) __builtin_amdgcn_s_barrier();
   // LDS is the epilogue's once every wavefront's loads have landed
