@@ -42,7 +42,7 @@ const Tensor& matrix(const Tensor& t, const char* what, int64_t rows, int64_t co
   TORCH_CHECK_VALUE(t.dim() == 2 && t.size(0) == rows && t.size(1) == cols, what, " must be a tensor of shape (", rows,
                     ", ", cols, "), not ", shape_str(t.sizes()));
   TORCH_CHECK_VALUE(t.device() == dev, what, " is on ", t.device(), ", not on ", dev);
-  TORCH_CHECK_VALUE(t.stride(1) == 1 || cols == 1, what, ": the last dimension must have unit stride");
+  TORCH_CHECK_VALUE(t.stride(1) == 1 || cols == 1 || rows == 0, what, ": the last dimension must have unit stride");
   return t;
 }
 

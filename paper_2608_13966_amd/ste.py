@@ -6,6 +6,10 @@ whose optimiser step is the fused AdamW + reconstruction of libquasar.so.
 The forward/backward products are ordinary torch matmuls (the model around
 the path); the optimiser update and the reconstruction run in the HIP kernels
 behind ``quasar_adamw_reconstruct``.
+
+``add_rms_norm`` and ``distill_topk_loss`` are the autograd forms of the
+operators of ``ops`` that training uses; their tensors may have any number of
+leading dimensions.
 """
 from __future__ import annotations
 
@@ -13,6 +17,7 @@ import math
 
 import torch
 
+from . import ops
 from . import quasar as Q
 
 
@@ -95,3 +100,79 @@ class QuasarLinear(torch.nn.Module):
                 or own.get("zeros", own) is not out["zeros"]):
             self.codes, self.scales, self.zeros = out["codes"], out["scales"], out["zeros"]
         weight.grad = None
+
+    def packed(self):
+        """The layer's codes as ``ops.linear_codes`` takes them.  It holds the
+        layer's own tensors: ask again after a step."""
+        cfg = self.cfg
+        return ops.PackedWeight(*self.weight.shape, self.codes, self.scales, self.zeros, fmt=cfg["fmt"],
+                                bits=cfg["bits"], group=cfg["group"])
+
+
+# ---- autograd forms ----------------------------------------------------------------
+
+def _rows(t):
+    """t as the operators take it: 2-D, rows that do not overlap, unit stride in the last dimension."""
+    t = t.reshape(math.prod(t.shape[:-1]), t.shape[-1])
+    return t if t.stride(1) == 1 and t.stride(0) >= t.shape[1] else t.contiguous()
+
+
+class _AddRMSNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        ctx.set_materialize_grads(False)
+        o = ops.add_rms_norm(_rows(x), weight, None if residual is None else _rows(residual), eps=eps)
+        ctx.save_for_backward(o["h"], weight, o["rstd"])
+        ctx.types = x.dtype, None if residual is None else residual.dtype
+        y = o["y"].view(x.shape)
+        return y if residual is None else (y, o["h"].view(x.shape))
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dh=None):
+        h, weight, rstd = ctx.saved_tensors
+        x_type, r_type = ctx.types
+        need_x, need_w, need_r = ctx.needs_input_grad[:3]
+        if dy is None:  # only the stream went on
+            return (dh.to(x_type) if need_x and dh is not None else None, None,
+                    dh if need_r else None, None)
+        o = ops.add_rms_norm_backward(_rows(dy), h, weight, rstd, None if dh is None else _rows(dh),
+                                      dx_dtype=None if dh is not None else r_type or x_type, want_dweight=need_w)
+        dx = o["dx"].view(dy.shape)
+        return (dx.to(x_type) if need_x else None, o["dw"].to(weight.dtype) if need_w else None,
+                dx.to(r_type) if need_r else None, None)
+
+
+def add_rms_norm(x, weight, residual=None, *, eps=1e-6):
+    """``ops.add_rms_norm`` with gradients: y, or (y, h) with a residual, where
+    h = x + residual is the stream that goes on; y has x's type, h residual's."""
+    return _AddRMSNorm.apply(x, weight, residual, eps)
+
+
+class _DistillTopK(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, index, teacher, temperature, row_weight):
+        flat, index, teacher = _rows(logits), _rows(index), _rows(teacher)
+        row_weight = None if row_weight is None else row_weight.reshape(-1).contiguous()
+        o = ops.distill_topk(flat, index, teacher, temperature=temperature, row_weight=row_weight)
+        ctx.save_for_backward(flat, index, teacher, o["lse"], row_weight)
+        ctx.shape, ctx.temperature = logits.shape, temperature
+        return o["loss"].view(logits.shape[:-1])
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        flat, index, teacher, lse, row_weight = ctx.saved_tensors
+        if not ctx.needs_input_grad[0]:
+            return None, None, None, None, None
+        o = ops.distill_topk_backward(flat, index, teacher, lse, temperature=ctx.temperature, row_weight=row_weight,
+                                      grad_loss=grad_loss.reshape(-1).contiguous())
+        return o["grad"].view(ctx.shape), None, None, None, None
+
+
+def distill_topk_loss(logits, index, teacher, *, temperature=1.0, row_weight=None):
+    """``ops.distill_topk`` with the gradient of the logits: the loss of each
+    row, for any reduction.  Two passes over the logits; where the loss is a
+    plain mean or sum, ``ops.distill_topk_grad`` makes loss and gradient in one
+    (``logits.backward(grad)``)."""
+    return _DistillTopK.apply(logits, index, teacher, temperature, row_weight)
