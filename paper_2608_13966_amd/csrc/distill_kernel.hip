@@ -31,26 +31,65 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c) {
   return MaxSum{m, a.s * fa + b.s * fb};
 }
 
-struct Listed {
-  int index[kListed];   // -1: no entry
-  float p[kListed];     // the teacher's probability
-};
-
-// The probability of class ix: all entries of it.
-__device__ __forceinline__ float listed_p(const Listed& l, int K, int ix) {
-  float p = 0.0f;
-#pragma unroll 4
-  for (int i = 0; i < K; i++)
-    if (l.index[i] == ix) p += l.p[i];
-  return p;
-}
-
-// A row's list in LDS, the work of one wavefront; a barrier has to follow.
+// A row's list in LDS, K entries.
+//
+// The gradient of a class takes the probabilities of all its entries, but few
+// lists name a class twice.  `seen` tells: a hash table of the classes (open
+// addressing, at most half full), each with kTwice once a second entry has come
+// to it.  Only those classes look through the list (all of them doing so took
+// 10 us of a row of 197 entries); the sum is in the list's order either way.
 struct RowList {
-  Listed l;
-  float z[kListed];  // the student's logits there
-  float plogp;       // sum of p log p
-  int live;          // 0: masked (row_weight 0, or no entry with p > 0)
+  static constexpr uint32_t kNone = 0xffffffffu, kTwice = 0x80000000u;
+  int* index;      // -1: no entry
+  float* p;        // the teacher's probability
+  float* z;        // the student's logit
+  uint32_t* seen;  // 2^bits slots
+  float* stats;    // sum of p log p; then whether the row is not masked (row_weight 0, or no entry with p > 0)
+  int bits;
+
+  static __host__ __device__ __forceinline__ int bits_of(int K) {
+    int b = 5;
+    while ((1 << b) < 2 * K) b++;
+    return b;
+  }
+  // floats of LDS
+  static __host__ __device__ __forceinline__ int size(int K) { return 3 * K + (1 << bits_of(K)) + 2; }
+  __device__ __forceinline__ RowList(float* lds, int K)
+      : index(reinterpret_cast<int*>(lds)),
+        p(lds + K),
+        z(lds + 2 * K),
+        seen(reinterpret_cast<uint32_t*>(lds + 3 * K)),
+        stats(lds + size(K) - 2),
+        bits(bits_of(K)) {}
+
+  __device__ __forceinline__ bool live() const { return stats[1] != 0.0f; }
+  // a barrier between clear(), note() and probability()
+  template <int NT>
+  __device__ __forceinline__ void clear() const {
+    for (int i = threadIdx.x; i < 1 << bits; i += NT) seen[i] = kNone;
+  }
+  __device__ __forceinline__ int slot(int ix) const { return (int)((uint32_t)ix * 0x9e3779b1u >> (32 - bits)); }
+  __device__ __forceinline__ void note(int ix) const {
+    for (int i = slot(ix);; i = (i + 1) & ((1 << bits) - 1)) {
+      const uint32_t had = atomicCAS(&seen[i], kNone, (uint32_t)ix);
+      if (had == kNone) return;
+      if ((had & ~kTwice) == (uint32_t)ix) {
+        atomicOr(&seen[i], kTwice);
+        return;
+      }
+    }
+  }
+  // of the class of entry k, which has been noted
+  __device__ __forceinline__ float probability(int k, int K) const {
+    const int ix = index[k];
+    int i = slot(ix);
+    while ((seen[i] & ~kTwice) != (uint32_t)ix) i = (i + 1) & ((1 << bits) - 1);
+    if (!(seen[i] & kTwice)) return p[k];
+    float sum = 0.0f;
+    for (int j = 0; j < K; j++)
+      if (index[j] == ix) sum += p[j];
+    return sum;
+  }
 };
 // Entry k of a row's list as it lies in memory: the same loads for either type
 // of index and of teacher, without a branch.
@@ -77,50 +116,51 @@ struct Entry {
   }
   // into the list; its logit as well
   template <int T>
-  __device__ __forceinline__ void put(const quasar_distill& a, RowList& o, int k, int64_t base, float it) const {
+  __device__ __forceinline__ void put(const quasar_distill& a, const RowList& o, int k, int64_t base, float it) const {
     const int ix = at(a);
-    o.l.index[k] = ix;
-    o.l.p[k] = ix >= 0 ? teacher(a) * it : -INFINITY;
+    o.index[k] = ix;
+    o.p[k] = ix >= 0 ? teacher(a) * it : -INFINITY;
     o.z[k] = elem(a.logits, base + (ix >= 0 ? ix : 0), T == kElemBF16);
   }
 };
 
-// From the entries' teacher logits / tau in o.l.p to their probabilities.
-__device__ __forceinline__ void normalise(RowList& o, int K, float weight) {
+// From the entries' teacher logits / tau in o.p to their probabilities.
+__device__ __forceinline__ void normalise(const RowList& o, int K, float weight) {
   const int lane = threadIdx.x & 63;
   wave_lds_fence();
   float m = -INFINITY, s = 0.0f, h = 0.0f;
   bool nan = false;
   for (int k = lane; k < K; k += 64) {
-    m = fmaxf(m, o.l.p[k]);
-    nan |= o.l.p[k] != o.l.p[k];
+    m = fmaxf(m, o.p[k]);
+    nan |= o.p[k] != o.p[k];
   }
   m = wave_reduce(m, MaxOp());
   const bool live = weight != 0.0f && (m != -INFINITY || __ballot(nan) != 0);
   if (live) {
-    for (int k = lane; k < K; k += 64) s += __builtin_amdgcn_exp2f((o.l.p[k] - m) * kLog2e);
+    for (int k = lane; k < K; k += 64) s += __builtin_amdgcn_exp2f((o.p[k] - m) * kLog2e);
     s = wave_reduce(s, SumOp());
     const float ls = __logf(s), is = 1.0f / s;
     for (int k = lane; k < K; k += 64) {
-      const float t = o.l.p[k] - m, p = __builtin_amdgcn_exp2f(t * kLog2e) * is;
-      o.l.p[k] = p;
+      const float t = o.p[k] - m, p = __builtin_amdgcn_exp2f(t * kLog2e) * is;
+      o.p[k] = p;
       if (!(p == 0.0f)) h += p * (t - ls);
     }
     h = wave_reduce(h, SumOp());
   }
   if (lane == 0) {
-    o.plogp = h;
-    o.live = live;
+    o.stats[0] = h;
+    o.stats[1] = live ? 1.0f : 0.0f;
   }
 }
 // The row's loss; the first wavefront's lanes get it.
 __device__ __forceinline__ float loss_of(const RowList& o, int K, float weight, float lse, float it) {
   float s = 0.0f;
-  if (o.live)
+  const bool live = o.live();
+  if (live)
     for (int k = threadIdx.x & 63; k < K; k += 64)
-      if (o.l.index[k] >= 0 && !(o.l.p[k] == 0.0f)) s += o.l.p[k] * (lse - o.z[k] * it);
+      if (o.index[k] >= 0 && !(o.p[k] == 0.0f)) s += o.p[k] * (lse - o.z[k] * it);
   s = wave_reduce(s, SumOp());
-  return o.live ? weight * (o.plogp + s) : 0.0f;
+  return live ? weight * (o.stats[0] + s) : 0.0f;
 }
 
 // r joined with eight more logits
@@ -220,11 +260,12 @@ __global__ __launch_bounds__(kThreads) void distill_scan_kernel(quasar_distill a
 template <int T, int NV>
 __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a, int what, int parts, const MaxSum* part,
                                                                int sums) {
-  __shared__ RowList o;
+  extern __shared__ float lds[];
   const int64_t row = blockIdx.x / (unsigned)parts, base = row * a.logits_stride, gbase = row * a.grad_stride;
   const int at = blockIdx.x % (unsigned)parts, e0 = at * Part<T, NV>::kClasses;
   const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
   const int V = (int)a.classes, K = a.listed;
+  const RowList o(lds, K);
   const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
   // the list's first 64 entries are asked for before the row, whose loads would hold them up
   const int lane = threadIdx.x & 63;
@@ -235,12 +276,13 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
     if (lane < K) first.put<T>(a, o, lane, base, it);
     for (int k = lane + 64; k < K; k += 64) Entry(a, row, k).put<T>(a, o, k, base, it);
   }
+  if (what != 0) o.clear<kThreads>();
   MaxSum r{-INFINITY, 0.0f};  // of the row's parts: each wavefront joins them
   for (int i = threadIdx.x & 63; i < sums; i += 64) r = join(r, part[row * sums + i], c);
   if (threadIdx.x < 64) normalise(o, K, weight);
   const float lse = sums > 0 ? lse_of(wave_join(r, c), it) : a.lse[row];
   __syncthreads();
-  const bool live = o.live;
+  const bool live = o.live();
   if (what != 1 && at == 0 && threadIdx.x < 64) {
     const float loss = loss_of(o, K, weight, lse, it);
     if (threadIdx.x == 0) {
@@ -253,6 +295,8 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
   // the student's probability; z / tau and lse may be large, their difference is taken first
   const auto soft = [&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, it, -lse) * kLog2e); };
   const int e1 = e0 + Part<T, NV>::kClasses < V ? e0 + Part<T, NV>::kClasses : V;
+  for (int k = threadIdx.x; k < K; k += kThreads)
+    if (o.index[k] >= e0 && o.index[k] < e1) o.note(o.index[k]);
   const __amdgpu_buffer_rsrc_t out =
       wave_buffer(reinterpret_cast<char*>(a.grad) + (gbase + e0) * elem_size<T>(), z.bytes);
 #pragma unroll
@@ -268,8 +312,8 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
   __syncthreads();  // the listed classes' gradients over the others'
   if (!live) return;
   for (int k = threadIdx.x; k < K; k += kThreads) {
-    const int ix = o.l.index[k];
-    if (ix >= e0 && ix < e1) put_elem(a.grad, gbase + ix, g * (soft(o.z[k]) - listed_p(o.l, K, ix)), T == kElemBF16);
+    const int ix = o.index[k];
+    if (ix >= e0 && ix < e1) put_elem(a.grad, gbase + ix, g * (soft(o.z[k]) - o.probability(k, K)), T == kElemBF16);
   }
 }
 
@@ -284,11 +328,10 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
 template <int T, int NT, int NV, bool GRAD>
 __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) {
   constexpr int kPer = kListed / NT;  // entries a thread fetches
-  struct Row : RowList {
-    MaxSum s[NT / 64];
-  };
-  __shared__ Row rows[2];  // of rows in turn
+  extern __shared__ float lds[];
+  __shared__ MaxSum sums[2][NT / 64];
   const int tid = threadIdx.x, V = (int)a.classes, K = a.listed;
+  const auto list = [&](int turn) { return RowList(lds + turn * RowList::size(K), K); };  // of rows in turn
   const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
   Piece<T> pc[NV];
   // Pieces are whole: a row's buffer ends with its last one; the V % 8 classes past it are one a thread.  No load or
@@ -313,18 +356,18 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
 #pragma unroll
     for (int j = 0; j < kPer; j++) en[j] = Entry(a, row, tid + j * NT < K ? tid + j * NT : 0);
   };
-  const auto put_list = [&](Row& o, int64_t row) {
+  const auto put_list = [&](const RowList& o, int64_t row) {
 #pragma unroll
     for (int j = 0; j < kPer; j++) {
       const int k = tid + j * NT, ix = en[j].at(a);
       if (k < K) {
-        o.l.index[k] = ix;
-        o.l.p[k] = ix >= 0 ? en[j].teacher(a) * it : -INFINITY;
+        o.index[k] = ix;
+        o.p[k] = ix >= 0 ? en[j].teacher(a) * it : -INFINITY;
       }
       ze[j] = elem(a.logits, row * a.logits_stride + (ix >= 0 ? ix : 0), T == kElemBF16);
     }
   };
-  const auto put_logits = [&](Row& o) {
+  const auto put_logits = [&](const RowList& o) {
 #pragma unroll
     for (int j = 0; j < kPer; j++)
       if (tid + j * NT < K) o.z[tid + j * NT] = ze[j];
@@ -334,13 +377,14 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
 #pragma unroll
     for (int v = 0; v < NV; v++) load(v, buffer(a.logits, a.logits_stride, blockIdx.x));
     load_last(blockIdx.x);
-    put_list(rows[0], blockIdx.x);
-    put_logits(rows[0]);
+    put_list(list(0), blockIdx.x);
+    put_logits(list(0));
+    if constexpr (GRAD) list(0).template clear<NT>();
   }
   __syncthreads();
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, turn ^= 1) {
-    Row &o = rows[turn], &n = rows[turn ^ 1];
+    const RowList o = list(turn), n = list(turn ^ 1);
     const int64_t next = row + gridDim.x < a.rows ? row + gridDim.x : row;
     const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
     const __amdgpu_buffer_rsrc_t coming = buffer(a.logits, a.logits_stride, next);
@@ -354,8 +398,8 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
     if (rest < V) r = take_one(r, last, c);
     if constexpr (!GRAD) load_last(next);
     if (tid < 64) normalise(o, K, weight);
-    r = group_join<NT / 64>(r, c, o.s);  // its barrier shows the list too
-    const bool live = o.live;
+    r = group_join<NT / 64>(r, c, sums[turn]);  // its barrier shows the list too
+    const bool live = o.live();
     const float lse = lse_of(r, it);
     if (tid < 64) {
       const float loss = loss_of(o, K, weight, lse, it);
@@ -366,6 +410,10 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
     }
     put_list(n, next);
     if constexpr (GRAD) {
+      n.template clear<NT>();
+      // the last wavefronts: the first one has had the loss to make
+      for (int k = NT - 1 - tid; k < K; k += NT)
+        if (o.index[k] >= 0) o.note(o.index[k]);
       const int64_t gbase = row * a.grad_stride;
       const __amdgpu_buffer_rsrc_t going = buffer(a.grad, a.grad_stride, row);
       const float g = a.grad_scale * weight * it, ls = __builtin_amdgcn_logf(r.s);
@@ -385,12 +433,12 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
       load_last(next);
       __syncthreads();  // the listed classes' gradients over the others'
       if (live) {
-        for (int k = tid; k < K; k += NT) {
-          const int at = o.l.index[k];
-          if (at >= 0)
-            put_elem(a.grad, gbase + at, g * (soft(o.z[k]) - listed_p(o.l, K, at)), T == kElemBF16);
+        for (int k = NT - 1 - tid; k < K; k += NT) {
+          const int at = o.index[k];
+          if (at >= 0) put_elem(a.grad, gbase + at, g * (soft(o.z[k]) - o.probability(k, K)), T == kElemBF16);
         }
       }
+      if (next == row) break;
       put_logits(n);
     } else {
       put_logits(n);
@@ -422,11 +470,12 @@ bool resident(int64_t rows, int64_t classes, bool bf16) {
 
 template <int T, bool GRAD>
 hipError_t launch_resident(const quasar_distill& a, hipStream_t stream) {
+  const size_t lds = 2 * RowList::size(a.listed) * sizeof(float);
 #define QUASAR_RESIDENT(NT, NV)                                                                     \
   if (a.classes <= (NT) * 8 * (NV)) {                                                               \
     const int64_t most = (int64_t)kCUs * (1024 / (NT));                                             \
     distill_resident_kernel<T, NT, NV, GRAD>                                                        \
-        <<<dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(NT), 0, stream>>>(a);              \
+        <<<dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(NT), lds, stream>>>(a);            \
     return hipGetLastError();                                                                       \
   }
   constexpr int P = kMostPieces<T>;
@@ -444,10 +493,11 @@ template <int T, int NV>
 hipError_t launch_split(const quasar_distill& a, int what, hipStream_t stream) {
   const int parts = parts_of(a.rows, a.classes);
   const dim3 grid((unsigned)(a.rows * parts)), block(kThreads);
+  const size_t lds = RowList::size(a.listed) * sizeof(float);
   MaxSum* ws = reinterpret_cast<MaxSum*>(a.workspace);
   const auto row_kernel = [&](int w, int sums) {
-    distill_row_kernel<T, NV><<<w == 0 ? dim3((unsigned)a.rows) : grid, block, 0, stream>>>(a, w, w == 0 ? 1 : parts, ws,
-                                                                                          sums);
+    distill_row_kernel<T, NV><<<w == 0 ? dim3((unsigned)a.rows) : grid, block, lds, stream>>>(a, w, w == 0 ? 1 : parts, ws,
+                                                                                            sums);
     return hipGetLastError();
   };
   if (what == 1) return row_kernel(1, 0);

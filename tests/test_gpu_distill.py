@@ -183,6 +183,20 @@ def test_entries_out_of_range_and_listed_twice():
     assert torch.equal(O.distill_topk_grad(z, i32, val, temperature=0.5, grad_scale=0.25)["grad"], o["grad"])
 
 
+@pytest.mark.parametrize("t,v,k,distinct", [(4, 70, 64, 8), (3, 5000, 1024, 64), (300, 3000, 200, 40), (2, 140001, 1000, 100),
+                                            (2, 2 ** 20 + 7, 512, 500)])
+@pytest.mark.parametrize("dtype,index", [("bf16", torch.int64), ("fp32", torch.int32)])
+def test_lists_that_name_classes_often(t, v, k, distinct, dtype, index):
+    """A class's entries add up, a few tens of them at most (what the bound of a sum allows)."""
+    z, _, val = make(t, v, k, dtype, "fp32", index, seed=k)
+    g = torch.Generator(device=DEV).manual_seed(distinct)
+    classes = torch.stack([torch.randperm(v, generator=g, device=DEV)[:distinct] for _ in range(t)])
+    classes[:, 0], classes[:, -1] = 0, v - 1
+    idx = classes.gather(1, torch.randint(0, distinct, (t, k), generator=g, device=DEV)).to(index)
+    idx[:, ::7] = -1
+    all_three(z, idx, val, 1.5)
+
+
 @pytest.mark.parametrize("v", [700, 33000])
 def test_student_logits_at_minus_infinity(v):
     """Classes that the student cannot take: probability 0 and gradient 0 where the teacher does not list them; a
