@@ -40,9 +40,13 @@ __device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float c) {
 // 10 us of a row of 197 entries); the sum is in the list's order either way.
 struct RowList {
   static constexpr uint32_t kNone = 0xffffffffu, kTwice = 0x80000000u;
-  int* index;      // -1: no entry
-  float* p;        // the teacher's probability
-  float* z;        // the student's logit
+  struct One {
+    int index;  // -1: no entry
+    float p;    // the teacher's probability
+    float z;    // the student's logit
+    int slot;   // in seen
+  };
+  One* e;
   uint32_t* seen;  // 2^bits slots
   float* stats;    // sum of p log p; then whether the row is not masked (row_weight 0, or no entry with p > 0)
   int bits;
@@ -53,13 +57,11 @@ struct RowList {
     return b;
   }
   // floats of LDS
-  static __host__ __device__ __forceinline__ int size(int K) { return 3 * K + (1 << bits_of(K)) + 2; }
+  static __host__ __device__ __forceinline__ int size(int K) { return 4 * K + (1 << bits_of(K)) + 4; }
   __device__ __forceinline__ RowList(float* lds, int K)
-      : index(reinterpret_cast<int*>(lds)),
-        p(lds + K),
-        z(lds + 2 * K),
-        seen(reinterpret_cast<uint32_t*>(lds + 3 * K)),
-        stats(lds + size(K) - 2),
+      : e(reinterpret_cast<One*>(lds)),
+        seen(reinterpret_cast<uint32_t*>(lds + 4 * K)),
+        stats(lds + size(K) - 4),
         bits(bits_of(K)) {}
 
   __device__ __forceinline__ bool live() const { return stats[1] != 0.0f; }
@@ -68,26 +70,24 @@ struct RowList {
   __device__ __forceinline__ void clear() const {
     for (int i = threadIdx.x; i < 1 << bits; i += NT) seen[i] = kNone;
   }
-  __device__ __forceinline__ int slot(int ix) const { return (int)((uint32_t)ix * 0x9e3779b1u >> (32 - bits)); }
-  __device__ __forceinline__ void note(int ix) const {
-    for (int i = slot(ix);; i = (i + 1) & ((1 << bits) - 1)) {
-      const uint32_t had = atomicCAS(&seen[i], kNone, (uint32_t)ix);
-      if (had == kNone) return;
-      if ((had & ~kTwice) == (uint32_t)ix) {
-        atomicOr(&seen[i], kTwice);
+  __device__ __forceinline__ void note(int k) const {
+    const uint32_t ix = (uint32_t)e[k].index;
+    for (uint32_t i = ix * 0x9e3779b1u >> (32 - bits);; i = (i + 1) & ((1u << bits) - 1u)) {
+      const uint32_t had = atomicCAS(&seen[i], kNone, ix);
+      if (had == kNone || (had & ~kTwice) == ix) {
+        if (had != kNone) atomicOr(&seen[i], kTwice);
+        e[k].slot = (int)i;
         return;
       }
     }
   }
   // of the class of entry k, which has been noted
   __device__ __forceinline__ float probability(int k, int K) const {
-    const int ix = index[k];
-    int i = slot(ix);
-    while ((seen[i] & ~kTwice) != (uint32_t)ix) i = (i + 1) & ((1 << bits) - 1);
-    if (!(seen[i] & kTwice)) return p[k];
+    if (!(seen[e[k].slot] & kTwice)) return e[k].p;
+    const int ix = e[k].index;
     float sum = 0.0f;
     for (int j = 0; j < K; j++)
-      if (index[j] == ix) sum += p[j];
+      if (e[j].index == ix) sum += e[j].p;
     return sum;
   }
 };
@@ -118,9 +118,9 @@ struct Entry {
   template <int T>
   __device__ __forceinline__ void put(const quasar_distill& a, const RowList& o, int k, int64_t base, float it) const {
     const int ix = at(a);
-    o.index[k] = ix;
-    o.p[k] = ix >= 0 ? teacher(a) * it : -INFINITY;
-    o.z[k] = elem(a.logits, base + (ix >= 0 ? ix : 0), T == kElemBF16);
+    o.e[k].index = ix;
+    o.e[k].p = ix >= 0 ? teacher(a) * it : -INFINITY;
+    o.e[k].z = elem(a.logits, base + (ix >= 0 ? ix : 0), T == kElemBF16);
   }
 };
 
@@ -131,18 +131,18 @@ __device__ __forceinline__ void normalise(const RowList& o, int K, float weight)
   float m = -INFINITY, s = 0.0f, h = 0.0f;
   bool nan = false;
   for (int k = lane; k < K; k += 64) {
-    m = fmaxf(m, o.p[k]);
-    nan |= o.p[k] != o.p[k];
+    m = fmaxf(m, o.e[k].p);
+    nan |= o.e[k].p != o.e[k].p;
   }
   m = wave_reduce(m, MaxOp());
   const bool live = weight != 0.0f && (m != -INFINITY || __ballot(nan) != 0);
   if (live) {
-    for (int k = lane; k < K; k += 64) s += __builtin_amdgcn_exp2f((o.p[k] - m) * kLog2e);
+    for (int k = lane; k < K; k += 64) s += __builtin_amdgcn_exp2f((o.e[k].p - m) * kLog2e);
     s = wave_reduce(s, SumOp());
     const float ls = __logf(s), is = 1.0f / s;
     for (int k = lane; k < K; k += 64) {
-      const float t = o.p[k] - m, p = __builtin_amdgcn_exp2f(t * kLog2e) * is;
-      o.p[k] = p;
+      const float t = o.e[k].p - m, p = __builtin_amdgcn_exp2f(t * kLog2e) * is;
+      o.e[k].p = p;
       if (!(p == 0.0f)) h += p * (t - ls);
     }
     h = wave_reduce(h, SumOp());
@@ -158,7 +158,7 @@ __device__ __forceinline__ float loss_of(const RowList& o, int K, float weight, 
   const bool live = o.live();
   if (live)
     for (int k = threadIdx.x & 63; k < K; k += 64)
-      if (o.index[k] >= 0 && !(o.p[k] == 0.0f)) s += o.p[k] * (lse - o.z[k] * it);
+      if (o.e[k].index >= 0 && !(o.e[k].p == 0.0f)) s += o.e[k].p * (lse - o.e[k].z * it);
   s = wave_reduce(s, SumOp());
   return live ? weight * (o.stats[0] + s) : 0.0f;
 }
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
   const auto soft = [&](float z) { return __builtin_amdgcn_exp2f(__builtin_fmaf(z, it, -lse) * kLog2e); };
   const int e1 = e0 + Part<T, NV>::kClasses < V ? e0 + Part<T, NV>::kClasses : V;
   for (int k = threadIdx.x; k < K; k += kThreads)
-    if (o.index[k] >= e0 && o.index[k] < e1) o.note(o.index[k]);
+    if (o.e[k].index >= e0 && o.e[k].index < e1) o.note(k);
   const __amdgpu_buffer_rsrc_t out =
       wave_buffer(reinterpret_cast<char*>(a.grad) + (gbase + e0) * elem_size<T>(), z.bytes);
 #pragma unroll
@@ -312,8 +312,8 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
   __syncthreads();  // the listed classes' gradients over the others'
   if (!live) return;
   for (int k = threadIdx.x; k < K; k += kThreads) {
-    const int ix = o.index[k];
-    if (ix >= e0 && ix < e1) put_elem(a.grad, gbase + ix, g * (soft(o.z[k]) - o.probability(k, K)), T == kElemBF16);
+    const int ix = o.e[k].index;
+    if (ix >= e0 && ix < e1) put_elem(a.grad, gbase + ix, g * (soft(o.e[k].z) - o.probability(k, K)), T == kElemBF16);
   }
 }
 
@@ -361,8 +361,8 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
     for (int j = 0; j < kPer; j++) {
       const int k = tid + j * NT, ix = en[j].at(a);
       if (k < K) {
-        o.index[k] = ix;
-        o.p[k] = ix >= 0 ? en[j].teacher(a) * it : -INFINITY;
+        o.e[k].index = ix;
+        o.e[k].p = ix >= 0 ? en[j].teacher(a) * it : -INFINITY;
       }
       ze[j] = elem(a.logits, row * a.logits_stride + (ix >= 0 ? ix : 0), T == kElemBF16);
     }
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
   const auto put_logits = [&](const RowList& o) {
 #pragma unroll
     for (int j = 0; j < kPer; j++)
-      if (tid + j * NT < K) o.z[tid + j * NT] = ze[j];
+      if (tid + j * NT < K) o.e[tid + j * NT].z = ze[j];
   };
   if (blockIdx.x < a.rows) {
     load_list(blockIdx.x);
@@ -413,7 +413,7 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
       n.template clear<NT>();
       // the last wavefronts: the first one has had the loss to make
       for (int k = NT - 1 - tid; k < K; k += NT)
-        if (o.index[k] >= 0) o.note(o.index[k]);
+        if (o.e[k].index >= 0) o.note(k);
       const int64_t gbase = row * a.grad_stride;
       const __amdgpu_buffer_rsrc_t going = buffer(a.grad, a.grad_stride, row);
       const float g = a.grad_scale * weight * it, ls = __builtin_amdgcn_logf(r.s);
@@ -434,11 +434,10 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
       __syncthreads();  // the listed classes' gradients over the others'
       if (live) {
         for (int k = NT - 1 - tid; k < K; k += NT) {
-          const int at = o.index[k];
-          if (at >= 0) put_elem(a.grad, gbase + at, g * (soft(o.z[k]) - o.probability(k, K)), T == kElemBF16);
+          const int at = o.e[k].index;
+          if (at >= 0) put_elem(a.grad, gbase + at, g * (soft(o.e[k].z) - o.probability(k, K)), T == kElemBF16);
         }
       }
-      if (next == row) break;
       put_logits(n);
     } else {
       put_logits(n);
