@@ -17,6 +17,21 @@ namespace {
 
 constexpr int kNormThreads = 256;
 
+// Eight elements, the first n of which exist (the others 0).
+__device__ __forceinline__ void load_floats(const void* base, int64_t e, int n, bool bf16, float (&v)[8]) {
+  if (bf16) {
+    Piece<kElemBF16> p;
+    p.load(base, e, n);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = p.get(i);
+  } else {
+    Piece<kElemF32> p;
+    p.load(base, e, n);
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[i] = p.get(i);
+  }
+}
+
 // TPR threads work on one row (64: a wavefront, without a barrier; more: a
 // workgroup), NV pieces of eight elements each.
 template <int XT, int RT, int TPR, int NV>
@@ -62,22 +77,11 @@ __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_
     }
   }
   float top = 0.0f;
-  const bool w_bf16 = a.weight_dtype == QUASAR_BF16;
 #pragma unroll
   for (int v = 0; v < NV; v++) {
     const int c = (v * TPR + t) * 8;
     float w[8];
-    if (w_bf16) {
-      Piece<kElemBF16> p;
-      p.load(a.weight, c, cols - c);
-#pragma unroll
-      for (int i = 0; i < 8; i++) w[i] = p.get(i);
-    } else {
-      Piece<kElemF32> p;
-      p.load(a.weight, c, cols - c);
-#pragma unroll
-      for (int i = 0; i < 8; i++) w[i] = p.get(i);
-    }
+    load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w);
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       h[v][i] = h[v][i] * rstd * w[i];
@@ -162,15 +166,11 @@ __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_
   const int sub = kRows > 1 ? wave_index() : 0;
   const int cols = (int)a.cols;
   const float rcols = 1.0f / (float)cols;
-  float w[NV][8], dw[NV][8];
+  float w[NV][8], dw[NV][8] = {};
 #pragma unroll
   for (int v = 0; v < NV; v++) {
     const int c = (v * TPR + t) * 8;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      dw[v][i] = 0.0f;
-      w[v][i] = c + i < cols ? elem(a.weight, c + i, a.weight_dtype == QUASAR_BF16) : 0.0f;
-    }
+    load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w[v]);
   }
   int flip = 0;
   for (int64_t row = (int64_t)blockIdx.x * kRows + sub; row < a.rows; row += (int64_t)gridDim.x * kRows) {
@@ -182,6 +182,16 @@ __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_
       const int c = (v * TPR + t) * 8;
       pg[v].load(a.dy, eg + c, cols - c);
       ph[v].load(a.h, eh + c, cols - c);
+    }
+    // dh is asked for with the rest where there are registers for it
+    constexpr bool kEarly = TPR <= 256;
+    float dh[NV][8];
+    if (kEarly && a.dh) {
+#pragma unroll
+      for (int v = 0; v < NV; v++) {
+        const int c = (v * TPR + t) * 8;
+        load_floats(a.dh, ed + c, cols - c, a.dx_dtype == QUASAR_BF16, dh[v]);
+      }
     }
     const float rstd = a.rstd[row];
     float dot = 0.0f;
@@ -206,23 +216,12 @@ __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_
         const float n = ph[v].get(i) * rstd;
         dx[i] = rstd * __builtin_fmaf(-m, n, pg[v].get(i) * w[v][i]);
       }
-      if (a.dx_dtype == QUASAR_BF16) {
-        if (a.dh) {
-          Piece<kElemBF16> p;
-          p.load(a.dh, ed + c, n8);
+      if (a.dh) {
+        if constexpr (!kEarly) load_floats(a.dh, ed + c, n8, a.dx_dtype == QUASAR_BF16, dh[v]);
 #pragma unroll
-          for (int i = 0; i < 8; i++) dx[i] += p.get(i);
-        }
-        store_piece<true>(a.dx, ex + c, dx, n8);
-      } else {
-        if (a.dh) {
-          Piece<kElemF32> p;
-          p.load(a.dh, ed + c, n8);
-#pragma unroll
-          for (int i = 0; i < 8; i++) dx[i] += p.get(i);
-        }
-        store_piece<false>(a.dx, ex + c, dx, n8);
+        for (int i = 0; i < 8; i++) dx[i] += dh[v][i];
       }
+      store_piece(a.dx, ex + c, dx, n8, a.dx_dtype == QUASAR_BF16);
     }
   }
   if (!parts) return;
@@ -311,9 +310,10 @@ size_t norm_backward_workspace(int64_t rows, int64_t cols) {
 }
 
 int norm_backward_parts(int64_t rows, int64_t cols) {
-  const int64_t per = cols <= 2048 ? 4 : 1;  // rows a workgroup takes at once
-  const int64_t groups = (rows + per - 1) / per;
-  return (int)(groups < 4 * kCUs ? groups : 4 * kCUs);
+  const int64_t per = cols <= 2048 ? 4 : 1;           // rows a workgroup takes at once
+  const int64_t most = (cols <= 8192 ? 4 : 2) * kCUs;  // what runs at once (of 1024 threads: two a CU)
+  const int64_t groups = (rows + per - 1) / per, rounds = groups <= most ? 1 : (groups + most - 1) / most;
+  return (int)((groups + rounds - 1) / rounds);  // no more parts than that many rounds need
 }
 
 hipError_t launch_norm_backward(const quasar_norm_backward& a, hipStream_t stream) {
