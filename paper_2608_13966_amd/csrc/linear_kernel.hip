@@ -359,8 +359,9 @@ struct Block16 {
   }
 };
 
-// A workgroup makes 16 outputs for up to 4 NX tokens (NX 1, 2, 4, or 8 for 32);
-// its wavefronts split the columns in steps of 128 and meet in LDS.  The lane
+// A workgroup makes 16 outputs for up to 4 NX tokens (NX 1, 2, 4, or 8 for 32)
+// over its share of the columns (split of 2^log_splits; the shares meet in
+// part); its wavefronts split them in steps of 128 and meet in LDS.  The lane
 // of row l % 16 and quarter l / 16 decodes the 32 weights of its quarter of a
 // step; matrix instruction i takes the eighths i of all four quarters, x
 // likewise (the order of the columns inside a sum is free).  Both operands go
@@ -370,7 +371,7 @@ struct Block16 {
 // LDS then hold fewer wavefronts.)
 constexpr int kStripWaves = 8;
 template <int FMT, int BITS, int XT, int NX>
-__global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quasar_linear a) {
+__global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quasar_linear a, int log_splits, float* part) {
   constexpr int kTokens = 4 * NX, TT = kTokens > 16 ? 2 : 1;
   constexpr int kPart = Block16<FMT, BITS>::kBytes + kTokens * 256;
   __shared__ __align__(16) char lds[kStripWaves * kPart];
@@ -379,10 +380,13 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
   const int r16 = lane & 15, quarter = lane >> 4;
   char* const mine = lds + wave * kPart;
   char* const xs = mine + Block16<FMT, BITS>::kBytes;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
-  // whole steps, in shares that differ by one at the most; the columns past them are the last wavefront's
-  const int K = (int)w.cols, steps = K / 128;
-  const int s0 = steps * wave / kStripWaves, s1 = steps * (wave + 1) / kStripWaves;
+  const int split = blockIdx.x & ((1u << log_splits) - 1u);
+  const int64_t n0 = (int64_t)(blockIdx.x >> log_splits) * 16;
+  // whole steps, in shares that differ by one at the most; the columns past them are the last share's
+  const int K = (int)w.cols, steps = K / 128, log_shares = 3 + log_splits;
+  static_assert(kStripWaves == 1 << 3, "shares of a workgroup");
+  const int share = split * kStripWaves + wave;
+  const int s0 = (int)((uint32_t)steps * share >> log_shares), s1 = (int)((uint32_t)steps * (share + 1) >> log_shares);
   const typename Block16<FMT, BITS>::Place place(w, n0, lane);
   struct Fetched {
     Block16<FMT, BITS> w;
@@ -431,7 +435,7 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
     Block16<FMT, BITS>::get(place, mine, r16, quarter, strip);
     multiply(strip);
   }
-  if (wave == kStripWaves - 1 && steps * 128 < K) {
+  if (share == (1 << log_shares) - 1 && steps * 128 < K) {
     const int k = steps * 128 + quarter * 32;
     const WeightRow<FMT, BITS> row(w, n0 + r16 < w.rows ? n0 + r16 : w.rows - 1);
     Strip<FMT, BITS> strip;
@@ -462,6 +466,10 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
 #pragma unroll
     for (int q = 0; q < kStripWaves; q++)
       v += reinterpret_cast<const float*>(lds + q * kPart)[(4 * (t >> 4) + (n & 3)) * 64 + (n >> 2) * 16 + (t & 15)];
+    if (part) {
+      part[((int64_t)split * tokens + t) * w.rows + n0 + n] = v;
+      continue;
+    }
     if (a.x_scale) v *= a.x_scale[t];
     if (a.bias) v += elem(a.bias, n0 + n, a.bias_dtype == QUASAR_BF16);
     v = activate(v, a.act);
@@ -682,11 +690,17 @@ __global__ __launch_bounds__(256) void join_kernel(quasar_linear a, int64_t rows
   if (token >= a.tokens) return;
   const int left = (int)(rows - n < 8 ? rows - n : 8);
   float v[8] = {};
-  for (int s = 0; s < splits; s++) {
-    Piece<kElemF32> p;
-    p.load(part, ((int64_t)s * a.tokens + token) * rows + n, left);
+  for (int s = 0; s < splits; s += 8) {  // eight shares in flight at once
+    Piece<kElemF32> p[8];
 #pragma unroll
-    for (int q = 0; q < 8; q++) v[q] += p.get(q);
+    for (int j = 0; j < 8; j++)
+      if (s + j < splits) p[j].load(part, ((int64_t)(s + j) * a.tokens + token) * rows + n, left);
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+      if (s + j < splits) {
+#pragma unroll
+        for (int q = 0; q < 8; q++) v[q] += p[j].get(q);
+      }
   }
   finish8(a, token, n, left, v);
 }
@@ -894,7 +908,7 @@ __global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uin
 enum Form : int { kStrip, kFused, kTile };
 struct Choice {
   Form form;
-  int splits, steps;  // fused: shares of the columns, and the steps of each
+  int splits, steps;  // shares of the columns, and (fused, tile) the steps of each
   size_t bytes;       // workspace
   int bm;             // fused: tokens a workgroup takes
 };
@@ -902,22 +916,30 @@ struct Choice {
 int padded_cols(const quasar_desc& d) { return (int)((d.cols + kTileK - 1) / kTileK * kTileK); }
 
 // Splits the steps of `tiles` tiles into shares while that makes no more than
-// `most` workgroups, each of `least` steps or more.
+// `most` workgroups, each of `least` steps or more.  (With 16 shares at most, 84 tokens at 192 x 14336 took 19.5 us, not
+// 17; with 64 they take 17 as well.)
 void split_steps(Choice& c, int64_t tiles, int steps, int64_t most, int least) {
-  while (c.splits < 16 && 2 * tiles * c.splits <= most && steps >= 2 * c.splits * least) c.splits *= 2;
+  while (c.splits < 32 && 2 * tiles * c.splits <= most && steps >= 2 * c.splits * least) c.splits *= 2;
 }
 
 // By the number of tokens (figures: us at rows x columns, INT4, this form against its neighbour):
-//  - up to 32 the strip kernel: 32 tokens 8.0 against 15 at 4096 x 4096, 20 against 26 at 4096 x 14336;
+//  - up to 32 the strip kernel: 32 tokens 7.6 against 13 at 4096 x 4096, 20 against 25 at 4096 x 14336.  A wavefront
+//    of it with eight steps or more shares them with other workgroups, down to two, while the CUs are not full (192 x
+//    14336: 1 token 6.8 against 8.8, 32 tokens 9.7 against 16; with four steps the join costs more: 6.0 against 4.6);
 //  - the tile kernel where its 256 x 256 tiles come near to filling the CUs and there are tokens enough to pay for
 //    writing r out (4096 tokens at 4096 x 4096: 115 against 173; 1024 at 14336 x 4096: 126 against 164, but 512
 //    there 114 against 86), or where the columns are many enough to be split (1500 at 4096 x 14336: 225 against 259);
 //  - the fused kernel between them.
 Choice choose(const quasar_desc& d, int64_t tokens) {
   Choice c{kStrip, 1, 0, 0, 0};
-  int64_t tiles = ((tokens + 255) / 256) * ((d.rows + 255) / 256);
-  if (tokens <= 32) return c;
-  int steps;
+  int64_t tiles = (d.rows + 15) / 16;
+  int steps = (int)(d.cols / 128 / kStripWaves);
+  if (tokens <= 32) {
+    if (steps >= 8) split_steps(c, tiles, steps, kCUs, 2);
+    if (c.splits > 1) c.bytes = (size_t)c.splits * (size_t)tokens * (size_t)d.rows * 4;
+    return c;
+  }
+  tiles = ((tokens + 255) / 256) * ((d.rows + 255) / 256);
   if ((tokens >= 768 && tiles >= 160) || (tokens >= 1024 && d.cols >= 8192)) {
     c.form = kTile;
     steps = padded_cols(d) / kTileK;
@@ -949,10 +971,18 @@ template <int FMT, int BITS, int XT>
 hipError_t launch(const quasar_desc& d, const quasar_linear& a, hipStream_t stream) {
   Weights w{a.codes, a.scales, a.zeros, a.tensor_scale, d.rows, d.cols, d.group == 64 ? 6 : 7};
   const Choice c = choose(d, a.tokens);
+  float* part = nullptr;  // the sums of the shares, [splits, tokens, rows]
+  const auto join = [&] {
+    const int64_t n = a.tokens * ((d.rows + 7) / 8);
+    join_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream>>>(a, d.rows, part, c.splits);
+    return hipGetLastError();
+  };
   if (c.form == kStrip) {
-    const unsigned gx = (unsigned)((d.rows + 15) / 16);
+    const unsigned gx = (unsigned)((d.rows + 15) / 16 * c.splits);
+    if (c.splits > 1) part = reinterpret_cast<float*>(a.workspace);
     const auto strip = [&](auto nx) {
-      strip_kernel<FMT, BITS, XT, decltype(nx)::value><<<dim3(gx), dim3(64 * kStripWaves), 0, stream>>>(w, a);
+      strip_kernel<FMT, BITS, XT, decltype(nx)::value>
+          <<<dim3(gx), dim3(64 * kStripWaves), 0, stream>>>(w, a, __builtin_ctz(c.splits), part);
     };
     if (a.tokens <= 4)
       strip(std::integral_constant<int, 1>());
@@ -962,14 +992,9 @@ hipError_t launch(const quasar_desc& d, const quasar_linear& a, hipStream_t stre
       strip(std::integral_constant<int, 4>());
     else
       strip(std::integral_constant<int, 8>());
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || !part ? e : join();
   }
-  float* part = nullptr;  // the sums of the shares, [splits, tokens, rows]
-  const auto join = [&] {
-    const int64_t n = a.tokens * ((d.rows + 7) / 8);
-    join_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream>>>(a, d.rows, part, c.splits);
-    return hipGetLastError();
-  };
   if (c.form == kFused) {
     const int tm = (int)((a.tokens + c.bm - 1) / c.bm), tn = (int)((d.rows + 127) / 128);
     if (c.splits > 1) part = reinterpret_cast<float*>(a.workspace);

@@ -135,6 +135,25 @@ def test_nvfp4_columns_that_are_no_multiple_of_a_tile(k, m):
         check(O.linear_codes(x, w, x_scale=s, y_dtype="fp32")["y"], x, r, s)
 
 
+@pytest.mark.parametrize("fmt,bits,group", FORMATS)
+@pytest.mark.parametrize("m,k", [(1, 8192), (6, 8256), (13, 12224), (32, 33024), (84, 14400)])
+def test_few_outputs_of_many_columns(fmt, bits, group, m, k):
+    """The columns are shared out over workgroups."""
+    k = k // 128 * 128 if group > 64 and fmt != "rubin" else k
+    n = 40 if fmt == "rubin" else 35
+    w, r = layer(n, k, fmt, bits, group, seed=m)
+    x, s = acts(m, k, k, "fp8")
+    g = torch.Generator(device=DEV).manual_seed(7)
+    bias = torch.randn(n, generator=g, device=DEV)
+    res = torch.randn(m, n, generator=g, device=DEV)
+    y = O.linear_codes(x, w, x_scale=s, bias=bias, residual=res, act="silu", y_dtype="fp32")["y"]
+    check(y, x, r, s, bias, res, "silu")
+    x, _ = acts(m, k, k + 1)
+    y = O.linear_codes(x, w)["y"]
+    check(y, x, r)
+    assert torch.equal(y, O.linear_codes(x, w)["y"])
+
+
 @pytest.mark.parametrize("m", [4, 30, 140])
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
 @pytest.mark.parametrize("bt,rt,yt", [("fp32", "bf16", "bf16"), ("bf16", "fp32", "fp32"), (None, "bf16", "fp32"),
