@@ -51,6 +51,9 @@ struct Weights {  // what r is made from
   int shift;  // a group is 2^shift columns (INT)
 };
 
+// floats from one token's partial sums to the next one's: whole pieces, aligned
+__host__ __device__ constexpr int64_t part_pitch(int64_t rows) { return (rows + 7) & ~(int64_t)7; }
+
 // Where one row's codes and parameters lie.
 template <int FMT, int BITS>
 struct WeightRow {
@@ -467,7 +470,7 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
     for (int q = 0; q < kStripWaves; q++)
       v += reinterpret_cast<const float*>(lds + q * kPart)[(4 * (t >> 4) + (n & 3)) * 64 + (n >> 2) * 16 + (t & 15)];
     if (part) {
-      part[((int64_t)split * tokens + t) * w.rows + n0 + n] = v;
+      part[((int64_t)split * tokens + t) * part_pitch(w.rows) + n0 + n] = v;
       continue;
     }
     if (a.x_scale) v *= a.x_scale[t];
@@ -519,7 +522,7 @@ __device__ __forceinline__ void finish8(const quasar_linear& a, int64_t token, i
 // A wavefront's tile of 16 TM tokens x 64 outputs from its accumulators
 // (acc[i][j][e]: token 16 i + 4 (lane / 16) + e, output 16 j + lane % 16), 32
 // tokens at a time through its part `st` of LDS (kSlab floats), so that y is
-// written 16 bytes a lane.  part: the sums go there [tokens, rows] instead.
+// written 16 bytes a lane.  part: the sums go there [tokens, part_pitch] instead.
 constexpr int kSlabPitch = 64 + 4, kSlab = 32 * kSlabPitch;
 template <int TM>
 __device__ __forceinline__ void store_tile(const quasar_linear& a, int64_t rows, const f32x4 (&acc)[TM][4], int64_t m0,
@@ -545,7 +548,7 @@ __device__ __forceinline__ void store_tile(const quasar_linear& a, int64_t rows,
 #pragma unroll
         for (int q = 0; q < 8; q++) v[q] = st[tr * kSlabPitch + c + q];
         if (part)
-          store_piece<false>(part, token * rows + n, v, left);
+          store_piece<false>(part, token * part_pitch(rows) + n, v, 8);
         else
           finish8(a, token, n, left, v);
       }
@@ -680,7 +683,7 @@ __global__ __launch_bounds__(256, 2) void fused_kernel(Weights w, quasar_linear 
     multiply();
   }
   store_tile<TM>(a, w.rows, acc, m0 + wm * (BM / 2), n0 + wn * 64, reinterpret_cast<float*>(lds) + wave * kSlab,
-                 part ? part + (int64_t)split * a.tokens * w.rows : nullptr);
+                 part ? part + (int64_t)split * a.tokens * part_pitch(w.rows) : nullptr);
 }
 
 // y from the sums of `splits` shares of the columns, eight outputs a thread.
@@ -694,7 +697,7 @@ __global__ __launch_bounds__(256) void join_kernel(quasar_linear a, int64_t rows
     Piece<kElemF32> p[8];
 #pragma unroll
     for (int j = 0; j < 8; j++)
-      if (s + j < splits) p[j].load(part, ((int64_t)(s + j) * a.tokens + token) * rows + n, left);
+      if (s + j < splits) p[j].load(part, ((int64_t)(s + j) * a.tokens + token) * part_pitch(rows) + n, 8);
 #pragma unroll
     for (int j = 0; j < 8; j++)
       if (s + j < splits) {
@@ -902,7 +905,7 @@ __global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uin
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
   store_tile<8>(a, rows, acc, m0 + wm * 128, n0 + wn * 64, reinterpret_cast<float*>(lds) + wave * kSlab,
-                part ? part + (int64_t)split * a.tokens * rows : nullptr);
+                part ? part + (int64_t)split * a.tokens * part_pitch(rows) : nullptr);
 }
 
 enum Form : int { kStrip, kFused, kTile };
@@ -936,7 +939,7 @@ Choice choose(const quasar_desc& d, int64_t tokens) {
   int steps = (int)(d.cols / 128 / kStripWaves);
   if (tokens <= 32) {
     if (steps >= 8) split_steps(c, tiles, steps, kCUs, 2);
-    if (c.splits > 1) c.bytes = (size_t)c.splits * (size_t)tokens * (size_t)d.rows * 4;
+    if (c.splits > 1) c.bytes = (size_t)c.splits * (size_t)tokens * (size_t)part_pitch(d.rows) * 4;
     return c;
   }
   tiles = ((tokens + 255) / 256) * ((d.rows + 255) / 256);
@@ -956,7 +959,7 @@ Choice choose(const quasar_desc& d, int64_t tokens) {
   }
   c.steps = (steps + c.splits - 1) / c.splits;
   c.splits = (steps + c.steps - 1) / c.steps;
-  if (c.splits > 1) c.bytes += (size_t)c.splits * (size_t)tokens * (size_t)d.rows * 4;
+  if (c.splits > 1) c.bytes += (size_t)c.splits * (size_t)tokens * (size_t)part_pitch(d.rows) * 4;
   return c;
 }
 
@@ -971,7 +974,7 @@ template <int FMT, int BITS, int XT>
 hipError_t launch(const quasar_desc& d, const quasar_linear& a, hipStream_t stream) {
   Weights w{a.codes, a.scales, a.zeros, a.tensor_scale, d.rows, d.cols, d.group == 64 ? 6 : 7};
   const Choice c = choose(d, a.tokens);
-  float* part = nullptr;  // the sums of the shares, [splits, tokens, rows]
+  float* part = nullptr;  // the sums of the shares, [splits, tokens, part_pitch(rows)]
   const auto join = [&] {
     const int64_t n = a.tokens * ((d.rows + 7) / 8);
     join_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream>>>(a, d.rows, part, c.splits);
