@@ -17,21 +17,6 @@ namespace {
 
 constexpr int kNormThreads = 256;
 
-// Eight elements, the first n of which exist (the others 0).
-__device__ __forceinline__ void load_floats(const void* base, int64_t e, int n, bool bf16, float (&v)[8]) {
-  if (bf16) {
-    Piece<kElemBF16> p;
-    p.load(base, e, n);
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = p.get(i);
-  } else {
-    Piece<kElemF32> p;
-    p.load(base, e, n);
-#pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = p.get(i);
-  }
-}
-
 // TPR threads work on one row (64: a wavefront, without a barrier; more: a
 // workgroup), NV pieces of eight elements each.
 template <int XT, int RT, int TPR, int NV>

@@ -40,13 +40,13 @@ __device__ __forceinline__ void put_elem(void* p, int64_t i, float v, bool bf16)
 }
 
 // Eight consecutive elements in their storage form; n of them exist (n >= 8:
-// all), the rest read as `fill` bits.
+// all), the rest read as 0.
 template <int T>
 struct Piece;
 template <>
 struct Piece<kElemBF16> {
   uint32_t d[4];
-  __device__ __forceinline__ void load(const void* base, int64_t e, int n, uint16_t fill = 0) {
+  __device__ __forceinline__ void load(const void* base, int64_t e, int n) {
     const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + e;
     if (n >= 8) {
       const uint4 t = ld16_any(p);
@@ -54,7 +54,7 @@ struct Piece<kElemBF16> {
     } else {
 #pragma unroll
       for (int i = 0; i < 4; i++) {
-        const uint32_t lo = 2 * i < n ? p[2 * i] : fill, hi = 2 * i + 1 < n ? p[2 * i + 1] : fill;
+        const uint32_t lo = 2 * i < n ? p[2 * i] : 0, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0;
         d[i] = lo | (hi << 16);
       }
     }
@@ -69,7 +69,7 @@ struct Piece<kElemBF16> {
 template <>
 struct Piece<kElemF32> {
   float f[8];
-  __device__ __forceinline__ void load(const void* base, int64_t e, int n, uint16_t fill = 0) {
+  __device__ __forceinline__ void load(const void* base, int64_t e, int n) {
     const float* p = reinterpret_cast<const float*>(base) + e;
     if (n >= 8) {
       const uint4 a = ld16_any(p), b = ld16_any(p + 4);
@@ -77,12 +77,40 @@ struct Piece<kElemF32> {
       f[4] = as_f32(b.x); f[5] = as_f32(b.y); f[6] = as_f32(b.z); f[7] = as_f32(b.w);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; i++) f[i] = i < n ? p[i] : as_f32((uint32_t)fill << 16);
+      for (int i = 0; i < 8; i++) f[i] = i < n ? p[i] : 0.0f;
     }
   }
   __device__ __forceinline__ float get(int i) const { return f[i]; }
   __device__ __forceinline__ void refresh() {}
 };
+
+// Eight elements from each of N places on, the first n[i] of which exist (the
+// others 0).  All loads are issued before the first is waited for.
+template <int N>
+__device__ __forceinline__ void load_floats(const void* base, const int64_t (&e)[N], const int (&n)[N], bool bf16,
+                                            float (&v)[N][8]) {
+  const auto load = [&](auto piece) {
+    decltype(piece) p[N];
+#pragma unroll
+    for (int j = 0; j < N; j++) p[j].load(base, e[j], n[j]);
+#pragma unroll
+    for (int j = 0; j < N; j++)
+#pragma unroll
+      for (int i = 0; i < 8; i++) v[j][i] = p[j].get(i);
+  };
+  if (bf16)
+    load(Piece<kElemBF16>());
+  else
+    load(Piece<kElemF32>());
+}
+__device__ __forceinline__ void load_floats(const void* base, int64_t e, int n, bool bf16, float (&v)[8]) {
+  const int64_t es[1] = {e};
+  const int ns[1] = {n};
+  float vs[1][8];
+  load_floats(base, es, ns, bf16, vs);
+#pragma unroll
+  for (int i = 0; i < 8; i++) v[i] = vs[0][i];
+}
 
 // Eight values to a tensor of fp32 or bf16 elements (nearest even), the first n of them.
 template <bool BF16>
