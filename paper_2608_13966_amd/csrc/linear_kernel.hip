@@ -1007,7 +1007,9 @@ Choice choose(const quasar_desc& d, int64_t tokens) {
     c.bytes = (size_t)(d.rows + tokens) * (size_t)padded_cols(d) * 2;
   } else {
     c.form = kFused;
-    c.bm = tokens <= 64 ? 64 : 128;
+    // tiles of 64 tokens where few fill the matrix (128 tokens: 1024 x 384 7.5 against 10.3, 1024 x 14336 20.5 against
+    // 23.7, 4096 x 4096 21.6 against 24.7; with 128 tiles of 64 tokens, 203 at 4096 x 14336, 59 against 49)
+    c.bm = tokens <= 64 || (tokens + 63) / 64 * ((d.rows + 127) / 128) <= kCUs / 4 ? 64 : 128;
     tiles = ((tokens + c.bm - 1) / c.bm) * ((d.rows + 127) / 128);
     steps = (int)((d.cols + kFusedK - 1) / kFusedK);
     // a workgroup for every CU, of two steps or more; a second one where both have 14
