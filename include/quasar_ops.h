@@ -147,7 +147,8 @@ size_t quasar_distill_topk_workspace_bytes(int64_t rows, int64_t classes);
  * tensor_scale stand for, in bf16 -- bit for bit the r that quasar_reconstruct
  * gives for a bf16 W and that a layer is trained with -- formed in the kernel
  * from the codes.  desc gives its shape, format, bits and group; its clip and
- * dtype fields are validated but unused.  Products are accumulated in fp32.
+ * dtype fields are validated but unused.  INT scales are below 2^100 in size (the
+ * kernels multiply them by up to 2^24).  Products are accumulated in fp32.
  */
 typedef enum {
   QUASAR_ACT_NONE = 0,

@@ -9,8 +9,9 @@
 //  - few tokens (strip kernel): the codes are what has to be read.  They go
 //    from memory to registers, become bf16 there and feed 16x16x32 matrix
 //    instructions directly; nothing is written but y.
-//  - many tokens (tile kernel): r is written out once in bf16 (unpack kernel),
-//    then multiplied in LDS-staged tiles.
+//  - more (fused kernel): r is formed in LDS, a tile's step at a time.
+//  - many (tile kernel): r is written out once in bf16 (unpack kernel), then
+//    multiplied in LDS-staged tiles.
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -400,7 +401,10 @@ struct Block16 {
 // through the wavefront's own part of LDS; the next step's loads are in flight
 // meanwhile.  (Two or four steps in flight, or 4 or 16 wavefronts, were up to
 // 25% slower at 4096 x 4096 to 14336 x 4096 and 1 to 32 tokens: registers and
-// LDS then hold fewer wavefronts.)
+// LDS then hold fewer wavefronts.)  4096 x 4096, 4 bits, 1 token: 4.8 us, a
+// launch (2.9) and the codes at 4.4 TB/s; 14336 x 4096, 2 bits, 8 tokens of 8 bits: 11.9
+// us, of which the copy of the codes and parameters would be 4.3: bound by the
+// decoding (VALU and LDS) between loads.
 constexpr int kStripWaves = 8;
 template <int FMT, int BITS, int XT, int NX>
 __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quasar_linear a, int log_splits, float* part) {
@@ -615,7 +619,12 @@ __device__ __forceinline__ void store_tile(const quasar_linear& a, int64_t rows,
 // (split of splits), in steps of 128.  Each thread fetches its weights and
 // activations of the next two steps into registers while this one is
 // multiplied, and turns them into bf16 in LDS after it, so r is never written to memory.
-// LDS holds one step: another workgroup of the CU multiplies meanwhile.
+// LDS holds one step: another workgroup of the CU multiplies meanwhile.  203
+// tokens, 4096 x 14336, 3 bits: 47 us, 510 TFLOP/s (and 7 to join the shares);
+// matrix units busy 33%, VALU and LDS as much, one after the other: the two
+// workgroups overlap little.  (Groups of four wavefronts that decode and multiply
+// in turn, 128 or 256 tokens a workgroup, took as long, as did each wavefront
+// decoding right into its operands, at 1.4 times the LDS reads.)
 // Chunk c of row m of a step lies at chunk c ^ m % 16 of the row's 256 bytes.
 constexpr int kFusedK = 128;
 __device__ __forceinline__ int wide_at(int m, int c) { return m * kFusedK + 8 * (c ^ (m & 15)); }
@@ -848,7 +857,8 @@ __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm
 //    half, "at most 8 outstanding" then, either phase.
 // Past the last step the loads repeat it, so that the counts hold.  (Four phases
 // of 16 instructions, with twice the barriers, were 5% slower.)  At 8192 tokens,
-// 14336 x 4096: 640 us, 1.50 PFLOP/s, matrix units busy about 75% of the time.
+// 14336 x 4096: 640 to 700 us as the clock goes, 1.4 to 1.5 PFLOP/s, matrix units
+// busy 81% of the time.
 __global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uint16_t* x, int64_t x_stride,
                                                       const uint16_t* r, int64_t rows, int kp, int tiles_m, int tiles_n,
                                                       int steps_per, float* part) {
