@@ -411,7 +411,8 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
   constexpr int kTokens = 4 * NX, TT = kTokens > 16 ? 2 : 1;
   constexpr int kPart = Block16<FMT, BITS>::kBytes + kTokens * 256;
   __shared__ __align__(16) char lds[kStripWaves * kPart];
-  static_assert(kPart >= TT * 1024, "the partial sums fit");
+  constexpr int kSums = 64 + 4;  // from one register's sums to the next one's: their readers use all banks
+  static_assert(kPart >= TT * 16 * kSums, "the partial sums fit");
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int r16 = lane & 15, quarter = lane >> 4;
   char* const mine = lds + wave * kPart;
@@ -493,7 +494,7 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
 #pragma unroll
   for (int t = 0; t < TT; t++)
 #pragma unroll
-    for (int i = 0; i < 4; i++) sums[(4 * t + i) * 64 + lane] = acc[t][i];
+    for (int i = 0; i < 4; i++) sums[(4 * t + i) * kSums + lane] = acc[t][i];
   __syncthreads();
   for (int o = threadIdx.x; o < 256 * TT; o += 64 * kStripWaves) {
     const int n = o & 15, t = o >> 4;
@@ -501,7 +502,7 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
     float sum[1] = {0.0f}, &v = sum[0];
 #pragma unroll
     for (int q = 0; q < kStripWaves; q++)
-      v += reinterpret_cast<const float*>(lds + q * kPart)[(4 * (t >> 4) + (n & 3)) * 64 + (n >> 2) * 16 + (t & 15)];
+      v += reinterpret_cast<const float*>(lds + q * kPart)[(4 * (t >> 4) + (n & 3)) * kSums + (n >> 2) * 16 + (t & 15)];
     if (part) {
       part[((int64_t)split * tokens + t) * part_pitch(w.rows) + n0 + n] = v;
       continue;
@@ -625,9 +626,10 @@ __device__ __forceinline__ void store_tile(const quasar_linear& a, int64_t rows,
 // workgroups overlap little.  (Groups of four wavefronts that decode and multiply
 // in turn, 128 or 256 tokens a workgroup, took as long, as did each wavefront
 // decoding right into its operands, at 1.4 times the LDS reads.)
-// Chunk c of row m of a step lies at chunk c ^ m % 16 of the row's 256 bytes.
+// Chunk c of row m of a step lies at chunk c ^ 2 (c / 8) ^ m % 16 of the row's 256
+// bytes: neither 8 rows' chunk c nor two rows' chunks i, 4 + i, 8 + i and 12 + i share banks.
 constexpr int kFusedK = 128;
-__device__ __forceinline__ int wide_at(int m, int c) { return m * kFusedK + 8 * (c ^ (m & 15)); }
+__device__ __forceinline__ int wide_at(int m, int c) { return m * kFusedK + 8 * (c ^ (c >> 3 << 1) ^ (m & 15)); }
 
 template <int FMT, int BITS, int XT, int BM>
 __global__ __launch_bounds__(256, 2) void fused_kernel(Weights w, quasar_linear a, int tiles_m, int splits, int steps_per,
