@@ -392,7 +392,7 @@ struct Block16 {
   }
 };
 
-// A workgroup makes 16 outputs for up to 4 NX tokens (NX 1, 2, 4, or 8 for 32)
+// A workgroup makes 16 NB outputs for up to 4 NX tokens (NX 1, 2, 4, or 8 for 32)
 // over its share of the columns (split of 2^log_splits; the shares meet in
 // part); its wavefronts split them in steps of 128 and meet in LDS.  The lane
 // of row l % 16 and quarter l / 16 decodes the 32 weights of its quarter of a
@@ -406,27 +406,29 @@ struct Block16 {
 // us, of which the copy of the codes and parameters would be 4.3: bound by the
 // decoding (VALU and LDS) between loads.
 constexpr int kStripWaves = 8;
-template <int FMT, int BITS, int XT, int NX>
+template <int FMT, int BITS, int XT, int NX, int NB>
 __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quasar_linear a, int log_splits, float* part) {
   constexpr int kTokens = 4 * NX, TT = kTokens > 16 ? 2 : 1;
-  constexpr int kPart = Block16<FMT, BITS>::kBytes + kTokens * 256;
+  constexpr int kBlock = Block16<FMT, BITS>::kBytes, kPart = NB * kBlock + kTokens * 256;
   __shared__ __align__(16) char lds[kStripWaves * kPart];
   constexpr int kSums = 64 + 4;  // from one register's sums to the next one's: their readers use all banks
-  static_assert(kPart >= TT * 16 * kSums, "the partial sums fit");
+  static_assert(kPart >= NB * TT * 16 * kSums, "the partial sums fit");
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int r16 = lane & 15, quarter = lane >> 4;
   char* const mine = lds + wave * kPart;
-  char* const xs = mine + Block16<FMT, BITS>::kBytes;
+  char* const xs = mine + NB * kBlock;
   const int split = blockIdx.x & ((1u << log_splits) - 1u);
-  const int64_t n0 = (int64_t)(blockIdx.x >> log_splits) * 16;
+  const int64_t n0 = (int64_t)(blockIdx.x >> log_splits) * (16 * NB);
+  const auto first = [&](int b) { return n0 + 16 * b < w.rows ? n0 + 16 * b : n0; };  // a block past the matrix: the one before again
   // whole steps, in shares that differ by one at the most; the columns past them are the last share's
   const int K = (int)w.cols, steps = K / 128, log_shares = 3 + log_splits;
   static_assert(kStripWaves == 1 << 3, "shares of a workgroup");
   const int share = split * kStripWaves + wave;
   const int s0 = (int)((uint32_t)steps * share >> log_shares), s1 = (int)((uint32_t)steps * (share + 1) >> log_shares);
-  const typename Block16<FMT, BITS>::Place place(w, n0, lane);
+  const typename Block16<FMT, BITS>::Place place0(w, n0, lane), place1(w, first(NB - 1), lane);
+  const auto place = [&](int b) -> const auto& { return b == 0 ? place0 : place1; };
   struct Fetched {
-    Block16<FMT, BITS> w;
+    Block16<FMT, BITS> w[NB];
     XChunk<XT> x[NX];
   } f = {};
   // x: 8 columns a lane, 16 lanes a token; NX times 4 tokens
@@ -435,24 +437,31 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
 #pragma unroll
   for (int i = 0; i < NX; i++) xe[i] = (4 * i + (lane >> 4)) * a.x_stride + 8 * kk;
   const auto fetch = [&](Fetched& o, int s) {
-    o.w.load(place, s * 128, lane);
+#pragma unroll
+    for (int b = 0; b < NB; b++) o.w[b].load(place(b), s * 128, lane);
 #pragma unroll
     for (int i = 0; i < NX; i++)
       if (4 * i + (lane >> 4) < tokens) o.x[i].load(a.x, xe[i] + s * 128);
   };
-  f32x4 acc[TT];
+  f32x4 acc[NB][TT];
 #pragma unroll
-  for (int t = 0; t < TT; t++) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  for (int b = 0; b < NB; b++)
+#pragma unroll
+    for (int t = 0; t < TT; t++) acc[b][t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   // token t's eighth e of a step lies at chunk e * kTokens + (t ^ e % kTokens): both sides without bank conflicts
-  const auto multiply = [&](Strip<FMT, BITS>& strip) {
+  const auto multiply = [&](const Strip<FMT, BITS> (&strip)[NB]) {
 #pragma unroll
     for (int i = 0; i < 4; i++) {
-      const bf16x8 r = as_bf16x8(strip.chunk(i));
+      bf16x8 r[NB];
+#pragma unroll
+      for (int b = 0; b < NB; b++) r[b] = as_bf16x8(strip[b].chunk(i));
 #pragma unroll
       for (int t = 0; t < TT; t++) {
         const int e = 4 * quarter + i, col = (16 * t + r16) & (kTokens - 1);
         const uint4 x = *reinterpret_cast<const uint4*>(xs + 16 * (e * kTokens + (col ^ (e & (kTokens - 1)))));
-        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r, as_bf16x8(x), acc[t], 0, 0, 0);
+#pragma unroll
+        for (int b = 0; b < NB; b++)
+          acc[b][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(r[b], as_bf16x8(x), acc[b][t], 0, 0, 0);
       }
     }
   };
@@ -463,21 +472,27 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
   if (s0 < s1) fetch(f, s0);
   for (int s = s0; s < s1; s++) {
     wave_lds_fence();
-    f.w.put(place, mine, lane);
+#pragma unroll
+    for (int b = 0; b < NB; b++) f.w[b].put(place(b), mine + b * kBlock, lane);
 #pragma unroll
     for (int i = 0; i < NX; i++) put_x(i, f.x[i]);
     if (s + 1 < s1) fetch(f, s + 1);
     wave_lds_fence();
-    Strip<FMT, BITS> strip;
-    Block16<FMT, BITS>::get(place, mine, r16, quarter, strip);
+    Strip<FMT, BITS> strip[NB];
+#pragma unroll
+    for (int b = 0; b < NB; b++) Block16<FMT, BITS>::get(place(b), mine + b * kBlock, r16, quarter, strip[b]);
     multiply(strip);
   }
   if (share == (1 << log_shares) - 1 && steps * 128 < K) {
     const int k = steps * 128 + quarter * 32;
-    const WeightRow<FMT, BITS> row(w, n0 + r16 < w.rows ? n0 + r16 : w.rows - 1);
-    Strip<FMT, BITS> strip;
-    strip.load(row, k, K - k);
-    strip.ready(row.tensor_scale);
+    Strip<FMT, BITS> strip[NB];
+#pragma unroll
+    for (int b = 0; b < NB; b++) {
+      const int64_t n = n0 + 16 * b + r16;
+      const WeightRow<FMT, BITS> row(w, n < w.rows ? n : w.rows - 1);
+      strip[b].load(row, k, K - k);
+      strip[b].ready(row.tensor_scale);
+    }
     wave_lds_fence();
 #pragma unroll
     for (int i = 0; i < NX; i++) {
@@ -492,17 +507,19 @@ __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quas
   wave_lds_fence();
   float* const sums = reinterpret_cast<float*>(mine);
 #pragma unroll
-  for (int t = 0; t < TT; t++)
+  for (int b = 0; b < NB; b++)
 #pragma unroll
-    for (int i = 0; i < 4; i++) sums[(4 * t + i) * kSums + lane] = acc[t][i];
+    for (int t = 0; t < TT; t++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) sums[(4 * (b * TT + t) + i) * kSums + lane] = acc[b][t][i];
   __syncthreads();
-  for (int o = threadIdx.x; o < 256 * TT; o += 64 * kStripWaves) {
-    const int n = o & 15, t = o >> 4;
+  for (int o = threadIdx.x; o < 256 * TT * NB; o += 64 * kStripWaves) {
+    const int n = o & (16 * NB - 1), t = o / (16 * NB);
     if (n0 + n >= w.rows || t >= tokens) continue;
     float sum[1] = {0.0f}, &v = sum[0];
 #pragma unroll
     for (int q = 0; q < kStripWaves; q++)
-      v += reinterpret_cast<const float*>(lds + q * kPart)[(4 * (t >> 4) + (n & 3)) * kSums + (n >> 2) * 16 + (t & 15)];
+      v += reinterpret_cast<const float*>(lds + q * kPart)[(4 * ((n >> 4) * TT + (t >> 4)) + (n & 3)) * kSums + (n >> 2 & 3) * 16 + (t & 15)];
     if (part) {
       part[((int64_t)split * tokens + t) * part_pitch(w.rows) + n0 + n] = v;
       continue;
@@ -1052,11 +1069,19 @@ hipError_t launch(const quasar_desc& d, const quasar_linear& a, hipStream_t stre
     return hipGetLastError();
   };
   if (c.form == kStrip) {
-    const unsigned gx = (unsigned)((d.rows + 15) / 16 * c.splits);
+    // 32 outputs a workgroup where there are many and x is what takes time: 24 and 32 tokens in bf16 at 14336 x 4096
+    // 18.4 and 19.7 against 23.3 and 24.5, at 8192 x 4096 10.5 and 11.4 against 12.1 and 12.5, at 4096 x 4096 9.7 and 9.9
+    // against 7.3 and 7.5; 8 tokens at 14336 x 4096 12.2 against 11.6, 32 of 8 bits there 19.3 against 19.1
+    const bool two = XT == kElemBF16 && a.tokens > 16 && d.rows >= 8192;
+    const unsigned gx = (unsigned)((d.rows + (two ? 31 : 15)) / (two ? 32 : 16) * c.splits);
     if (c.splits > 1) part = reinterpret_cast<float*>(a.workspace);
     const auto strip = [&](auto nx) {
-      strip_kernel<FMT, BITS, XT, decltype(nx)::value>
-          <<<dim3(gx), dim3(64 * kStripWaves), 0, stream>>>(w, a, __builtin_ctz(c.splits), part);
+      constexpr int NX = decltype(nx)::value, NB = NX == 8 && XT == kElemBF16 ? 2 : 1;
+      const dim3 block(64 * kStripWaves);
+      if (two)
+        strip_kernel<FMT, BITS, XT, NX, NB><<<dim3(gx), block, 0, stream>>>(w, a, __builtin_ctz(c.splits), part);
+      else
+        strip_kernel<FMT, BITS, XT, NX, 1><<<dim3(gx), block, 0, stream>>>(w, a, __builtin_ctz(c.splits), part);
     };
     if (a.tokens <= 4)
       strip(std::integral_constant<int, 1>());

@@ -154,6 +154,21 @@ def test_few_outputs_of_many_columns(fmt, bits, group, m, k):
     assert torch.equal(y, O.linear_codes(x, w)["y"])
 
 
+@pytest.mark.parametrize("fmt,bits,group", FORMATS)
+@pytest.mark.parametrize("m", [17, 32])
+@pytest.mark.parametrize("n", [8200, 8224])
+def test_many_outputs_of_few_tokens(fmt, bits, group, m, n):
+    """Two blocks of 16 outputs a workgroup, the last of them past the matrix or not."""
+    k = 384 if fmt != "nvfp4" else 400
+    w, r = layer(n, k, fmt, bits, group, seed=m)
+    x, _ = acts(m, k, n)
+    g = torch.Generator(device=DEV).manual_seed(8)
+    bias, res = torch.randn(n, generator=g, device=DEV), torch.randn(m, n, generator=g, device=DEV)
+    y = O.linear_codes(x, w, bias=bias, residual=res, act="gelu", y_dtype="fp32")["y"]
+    check(y, x, r, None, bias, res, "gelu")
+    check(O.linear_codes(x, w)["y"], x, r)
+
+
 @pytest.mark.parametrize("m", [4, 30, 140])
 @pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
 @pytest.mark.parametrize("bt,rt,yt", [("fp32", "bf16", "bf16"), ("bf16", "fp32", "fp32"), (None, "bf16", "fp32"),
