@@ -226,6 +226,7 @@ py::object distill(int what, const Tensor& logits, const Tensor& index, const Te
   if (row_weight) vector_f32(*row_weight, "row_weight", rows, dev);
   Maybe loss, lse, grad, ws;
   if (what == 1) {
+    TORCH_CHECK_TYPE(saved, where, ": lse must be a tensor, not None");
     lse = vector_f32(*saved, "lse", rows, dev);
     if (grad_loss) vector_f32(*grad_loss, "grad_loss", rows, dev);
   } else {

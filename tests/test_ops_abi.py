@@ -243,6 +243,12 @@ def test_wrappers_refuse_before_launch():
         O.linear_codes(xb, pw, residual=torch.zeros(4, 9))
 
 
+def test_backward_without_the_saved_log_sum_is_refused():
+    x, ix, t = torch.zeros(4, 64), torch.zeros(4, 3, dtype=torch.int64), torch.zeros(4, 3)
+    with pytest.raises(TypeError, match="lse"):
+        O.distill_topk_backward(x, ix, t, None)
+
+
 def test_tensors_off_the_gpu_are_refused_as_torch_does():
     x = torch.zeros(4, 64)
     with pytest.raises(Exception) as want:
