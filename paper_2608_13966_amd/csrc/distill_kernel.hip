@@ -20,7 +20,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 constexpr int kListed = QUASAR_DISTILL_MAX_LISTED;
-
+constexpr int kListedWave = 256;  // where one wavefront takes a row
 
 // max and sum of exp2((z - max) c) of a set of logits; an empty set is (-inf, 0)
 struct MaxSum {
@@ -322,7 +322,7 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
 }
 
 // ---- a row in registers ---------------------------------------------------------
-// One workgroup takes whole rows, NV pieces of eight classes a thread, which stay
+// One workgroup (or wavefront) takes whole rows, NV pieces of eight classes a thread, which stay
 // in registers from their only read to the gradient; each piece's registers take
 // the next row's as soon as its gradient is stored (without a gradient: as soon
 // as it is summed), so loads and stores overlap.  The lists are a row ahead too,
@@ -331,7 +331,7 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
 // GRAD: the gradient too.
 template <int T, int NT, int NV, bool GRAD>
 __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) {
-  constexpr int kPer = kListed / NT;  // entries a thread fetches
+  constexpr int kPer = (NT == 64 ? kListedWave : kListed) / NT;  // entries a thread fetches
   extern __shared__ float lds[];
   __shared__ MaxSum sums[2][NT / 64];
   const int tid = threadIdx.x, V = (int)a.classes, K = a.listed;
@@ -455,6 +455,7 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
 int part_pieces(int64_t rows, int64_t classes) {
   int nv = 8;
   while (nv > 1 && rows * ((classes + 2048 * nv - 1) / (2048 * nv)) < 2 * kCUs) nv /= 2;
+  while (nv > 1 && 1024 * nv >= classes) nv /= 2;  // pieces past the row cost as many instructions
   return nv;
 }
 int parts_of(int64_t rows, int64_t classes) {
@@ -471,18 +472,33 @@ bool resident(int64_t rows, int64_t classes, bool bf16) {
   return classes <= most && (rows >= kCUs || classes <= 16384);
 }
 
+// A row that one wavefront holds takes one where there are rows enough for them
+// (four a CU): no wavefront waits for another then.  Loss and gradient, us, against
+// 256 threads a row: 8192 x 4000 with 64 listed 34.3, 40.9; 8192 x 1200 20.5, 34.7;
+// but 300 x 4000 with 256 listed 13.0, 9.4.
+//
+// Wavefronts a CU, by what a thread holds (more than fit only queue): 8192 x 4000, 256
+// threads a row, 45.2 with 16, 42.1 with 20, 40.2 with 24, 43.3 with 32; one wavefront a
+// row 34.3 with 12, 34.8 with 16, 38.4 with 24.
 template <int T, bool GRAD>
 hipError_t launch_resident(const quasar_distill& a, hipStream_t stream) {
   const size_t lds = 2 * RowList::size(a.listed) * sizeof(float);
 #define QUASAR_RESIDENT(NT, NV)                                                                     \
   if (a.classes <= (NT) * 8 * (NV)) {                                                               \
-    const int64_t most = (int64_t)kCUs * (1024 / (NT));                                             \
+    constexpr int held = (NV) * 8 * elem_size<T>();                                                 \
+    constexpr int waves = (NT) == 64 ? 12 : (NT) > 256 || held > 64 ? 16 : held > 32 ? 20 : 24;     \
+    const int64_t most = (int64_t)kCUs * (waves * 64 / (NT));                                       \
     distill_resident_kernel<T, NT, NV, GRAD>                                                        \
         <<<dim3((unsigned)(a.rows < most ? a.rows : most)), dim3(NT), lds, stream>>>(a);            \
     return hipGetLastError();                                                                       \
   }
   constexpr int P = kMostPieces<T>;
+  if (a.rows >= 4 * kCUs && a.listed <= kListedWave) {
+    QUASAR_RESIDENT(64, P / 4)
+    QUASAR_RESIDENT(64, P / 2)
+  }
   QUASAR_RESIDENT(256, 2)
+  if constexpr (P / 4 > 2) QUASAR_RESIDENT(256, P / 4)
   QUASAR_RESIDENT(256, P / 2)
   QUASAR_RESIDENT(256, P)
   QUASAR_RESIDENT(512, P)

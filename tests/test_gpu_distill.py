@@ -197,6 +197,28 @@ def test_lists_that_name_classes_often(t, v, k, distinct, dtype, index):
     all_three(z, idx, val, 1.5)
 
 
+@pytest.mark.parametrize("t,v,k", [(1024, 1, 1), (1025, 9, 5), (3080, 1023, 64), (1024, 2048, 256), (1100, 2049, 7),
+                                   (1031, 4096, 64), (1024, 4097, 64), (1024, 2000, 257), (6200, 300, 20), (1023, 4096, 40),
+                                   (1500, 8192, 30), (1040, 8193, 8), (1040, 6001, 300)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_many_short_rows(t, v, k, dtype):
+    """A wavefront or a few a row, several rows in turn; masked rows among them; the gradient in the logits' place."""
+    z, idx, val = make(t, v, k, dtype, index=torch.int32, seed=t + k)
+    wt = torch.rand(t, device=DEV) + 0.5
+    wt[5::17] = 0.0
+    idx[3::19] = -1
+    dead = (wt == 0) | (idx < 0).all(1)
+    o = all_three(z, idx, val, 1.5, wt)
+    for x in o["loss"], o["lse"], o["grad"]:
+        assert (x[dead] == 0).all()
+    zz = z.clone()
+    a = O.distill_topk_grad(zz, idx, val, temperature=1.5, row_weight=wt, grad_scale=0.25,
+                            out={"grad": zz, "loss": torch.empty(t, device=DEV), "lse": torch.empty(t, device=DEV)})
+    assert all(torch.equal(a[x], o[x]) for x in ("loss", "lse", "grad"))
+    few = O.distill_topk_grad(z[:40], idx[:40], val[:40], temperature=1.5, row_weight=wt[:40], grad_scale=0.25)
+    check(z[:40], idx[:40], val[:40], few, 1.5, wt[:40], 0.25)
+
+
 @pytest.mark.parametrize("v", [700, 33000])
 def test_student_logits_at_minus_infinity(v):
     """Classes that the student cannot take: probability 0 and gradient 0 where the teacher does not list them; a
