@@ -1011,6 +1011,32 @@ void split_steps(Choice& c, int64_t tiles, int steps, int64_t most, int least) {
   while (c.splits < 32 && 2 * tiles * c.splits <= most && steps >= 2 * c.splits * least) c.splits *= 2;
 }
 
+// Shares of the columns for the fused kernel: those of the least time, from what was
+// measured of its parts.  A step of 128 tokens takes 1.8 us where a CU has one
+// workgroup, 2.35 where it has two (64 tokens: 1.1 and 1.8); a round of workgroups
+// costs 2 more, the join of the shares 3 and what it and they move at 5.2 TB/s.
+// (With powers of two that fill the CUs once or twice: 179 tokens at 4113 x 11904
+// 67 us, so 48; 250 at 9000 x 9088 95, so 74; 60 at 16000 x 1024 19, so 13; 900 at
+// 1500 x 12288 69, so 61.)
+int fused_splits(int64_t tiles, int steps, int bm, int64_t sums) {
+  const double one = bm == 64 ? 1.1 : 1.8, two = bm == 64 ? 1.8 : 2.35;
+  int best = 1, last = 0;
+  double least = 0.0;
+  for (int s = 1; s <= 32 && s <= steps; s++) {
+    const int per = (steps + s - 1) / s;
+    if (per == last) continue;  // more shares of as many steps
+    last = per;
+    const int64_t groups = tiles * ((steps + per - 1) / per), full = groups / (2 * kCUs), rest = groups % (2 * kCUs);
+    const double us = full * (2.0 + per * two) + (rest == 0 ? 0.0 : 2.0 + per * (rest <= kCUs ? one : two)) +
+                      (per == steps ? 0.0 : 3.0 + (double)sums * ((steps + per - 1) / per) * 8 / 5.2e6);
+    if (s == 1 || us < least) {
+      best = s;
+      least = us;
+    }
+  }
+  return best;
+}
+
 // By the number of tokens (figures: us at rows x columns, INT4, this form against its neighbour):
 //  - up to 32 the strip kernel: 32 tokens 7.6 against 13 at 4096 x 4096, 20 against 25 at 4096 x 14336.  A wavefront
 //    of it with eight steps or more shares them with other workgroups, down to two, while the CUs are not full (192 x
@@ -1041,9 +1067,7 @@ Choice choose(const quasar_desc& d, int64_t tokens) {
     c.bm = tokens <= 64 || (tokens + 63) / 64 * ((d.rows + 127) / 128) <= kCUs / 4 ? 64 : 128;
     tiles = ((tokens + c.bm - 1) / c.bm) * ((d.rows + 127) / 128);
     steps = (int)((d.cols + kFusedK - 1) / kFusedK);
-    // a workgroup for every CU, of two steps or more; a second one where both have 14
-    split_steps(c, tiles, steps, 2 * kCUs - 1, 2);
-    split_steps(c, tiles, steps, 2 * kCUs, 14);
+    c.splits = fused_splits(tiles, steps, c.bm, tokens * part_pitch(d.rows));
   }
   c.steps = (steps + c.splits - 1) / c.splits;
   c.splits = (steps + c.steps - 1) / c.steps;

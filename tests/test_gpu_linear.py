@@ -154,6 +154,23 @@ def test_few_outputs_of_many_columns(fmt, bits, group, m, k):
     assert torch.equal(y, O.linear_codes(x, w)["y"])
 
 
+@pytest.mark.parametrize("m,n,k,fmt,bits,group", [
+    (179, 1040, 11904, "int", 3, 128), (250, 2250, 9088, "int_sym", 3, 64), (60, 4000, 1040, "nvfp4", 4, 16),
+    (301, 1500, 4160, "rubin", 3, 512), (300, 5000, 1024, "int", 4, 64), (700, 500, 2944, "int", 2, 64),
+    (47, 1581, 560, "nvfp4", 4, 16), (96, 8200, 640, "int", 4, 64)])
+@pytest.mark.parametrize("xt", ["bf16", "fp8"])
+def test_columns_shared_out_unevenly(m, n, k, fmt, bits, group, xt):
+    """Shares of any number, the last of fewer steps than the others."""
+    n = n // 8 * 8 if fmt == "rubin" else n
+    w, r = layer(n, k, fmt, bits, group, seed=m)
+    x, s = acts(m, k, n, xt)
+    g = torch.Generator(device=DEV).manual_seed(9)
+    bias, res = torch.randn(n, generator=g, device=DEV), torch.randn(m, n, generator=g, device=DEV)
+    y = O.linear_codes(x, w, x_scale=s, bias=bias, residual=res, act="gelu", y_dtype="fp32")["y"]
+    check(y, x, r, s, bias, res, "gelu")
+    check(O.linear_codes(x, w, x_scale=s)["y"], x, r, s)
+
+
 @pytest.mark.parametrize("fmt,bits,group", FORMATS)
 @pytest.mark.parametrize("m", [17, 32])
 @pytest.mark.parametrize("n", [8200, 8224])
