@@ -1011,30 +1011,34 @@ void split_steps(Choice& c, int64_t tiles, int steps, int64_t most, int least) {
   while (c.splits < 32 && 2 * tiles * c.splits <= most && steps >= 2 * c.splits * least) c.splits *= 2;
 }
 
-// Shares of the columns for the fused kernel: those of the least time, from what was
-// measured of its parts.  A step of 128 tokens takes 1.8 us where a CU has one
-// workgroup, 2.35 where it has two (64 tokens: 1.1 and 1.8); a round of workgroups
-// costs 2 more, the join of the shares 3 and what it and they move at 5.2 TB/s.
-// (With powers of two that fill the CUs once or twice: 179 tokens at 4113 x 11904
-// 67 us, so 48; 250 at 9000 x 9088 95, so 74; 60 at 16000 x 1024 19, so 13; 900 at
-// 1500 x 12288 69, so 61.)
-int fused_splits(int64_t tiles, int steps, int bm, int64_t sums) {
-  const double one = bm == 64 ? 1.1 : 1.8, two = bm == 64 ? 1.8 : 2.35;
-  int best = 1, last = 0;
+// Tiles of 64 or 128 tokens and shares of the columns for the fused kernel: those of
+// the least time, from what was measured of its parts.  A step of 128 tokens takes 1.8
+// us where a CU has one workgroup, 2.35 where it has two (64 tokens: 1.15 and 1.8); a
+// round of workgroups costs 2 more, the join of the shares 3 and what it and they move
+// at 5.2 TB/s.  (With shares in powers of two that fill the CUs once or twice: 179
+// tokens at 4113 x 11904 67 us, so 48; 250 at 9000 x 9088 95, so 74; 60 at 16000 x 1024
+// 19, so 13; 900 at 1500 x 12288 69, so 61.  203 at 4096 x 14336: 59 in tiles of 64, 48
+// in tiles of 128; 320 at 6000 x 2048: 23.7 in tiles of 64, 28 in tiles of 128.)
+void choose_fused(Choice& c, int64_t tokens, int64_t rows, int steps) {
   double least = 0.0;
-  for (int s = 1; s <= 32 && s <= steps; s++) {
-    const int per = (steps + s - 1) / s;
-    if (per == last) continue;  // more shares of as many steps
-    last = per;
-    const int64_t groups = tiles * ((steps + per - 1) / per), full = groups / (2 * kCUs), rest = groups % (2 * kCUs);
-    const double us = full * (2.0 + per * two) + (rest == 0 ? 0.0 : 2.0 + per * (rest <= kCUs ? one : two)) +
-                      (per == steps ? 0.0 : 3.0 + (double)sums * ((steps + per - 1) / per) * 8 / 5.2e6);
-    if (s == 1 || us < least) {
-      best = s;
-      least = us;
+  for (int bm = 64; bm <= 128; bm += 64) {
+    const double one = bm == 64 ? 1.15 : 1.8, two = bm == 64 ? 1.8 : 2.35;
+    const int64_t tiles = ((tokens + bm - 1) / bm) * ((rows + 127) / 128);
+    for (int s = 1, last = 0; s <= 32 && s <= steps && (s == 1 || tiles * s <= 4 * kCUs); s++) {
+      const int per = (steps + s - 1) / s;
+      if (per == last) continue;  // as many steps a share
+      last = per;
+      const int64_t groups = tiles * s, full = groups / (2 * kCUs), rest = groups % (2 * kCUs);
+      const double us = full * (2.0 + per * two) + (rest == 0 ? 0.0 : 2.0 + per * (rest <= kCUs ? one : two)) +
+                        (s == 1 ? 0.0 : 3.0 + (double)(tokens * part_pitch(rows)) * s * (8 / 5.2e6));
+      if (c.bm == 0 || us < least) {
+        c.bm = bm;
+        c.splits = s;
+        c.steps = per;
+        least = us;
+      }
     }
   }
-  return best;
 }
 
 // By the number of tokens (figures: us at rows x columns, INT4, this form against its neighbour):
@@ -1059,18 +1063,13 @@ Choice choose(const quasar_desc& d, int64_t tokens) {
     c.form = kTile;
     steps = padded_cols(d) / kTileK;
     split_steps(c, tiles, steps, kCUs, 16);
+    c.steps = (steps + c.splits - 1) / c.splits;
+    c.splits = (steps + c.steps - 1) / c.steps;
     c.bytes = (size_t)(d.rows + tokens) * (size_t)padded_cols(d) * 2;
   } else {
     c.form = kFused;
-    // tiles of 64 tokens where few fill the matrix (128 tokens: 1024 x 384 7.5 against 10.3, 1024 x 14336 20.5 against
-    // 23.7, 4096 x 4096 21.6 against 24.7; with 128 tiles of 64 tokens, 203 at 4096 x 14336, 59 against 49)
-    c.bm = tokens <= 64 || (tokens + 63) / 64 * ((d.rows + 127) / 128) <= kCUs / 4 ? 64 : 128;
-    tiles = ((tokens + c.bm - 1) / c.bm) * ((d.rows + 127) / 128);
-    steps = (int)((d.cols + kFusedK - 1) / kFusedK);
-    c.splits = fused_splits(tiles, steps, c.bm, tokens * part_pitch(d.rows));
+    choose_fused(c, tokens, d.rows, (int)((d.cols + kFusedK - 1) / kFusedK));
   }
-  c.steps = (steps + c.splits - 1) / c.splits;
-  c.splits = (steps + c.steps - 1) / c.steps;
   if (c.splits > 1) c.bytes += (size_t)c.splits * (size_t)tokens * (size_t)part_pitch(d.rows) * 4;
   return c;
 }
