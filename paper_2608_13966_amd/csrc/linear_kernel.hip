@@ -402,7 +402,7 @@ struct Block16 {
 // meanwhile.  (Two or four steps in flight, or 4 or 16 wavefronts, were up to
 // 25% slower at 4096 x 4096 to 14336 x 4096 and 1 to 32 tokens: registers and
 // LDS then hold fewer wavefronts.)  4096 x 4096, 4 bits, 1 token: 4.8 us, a
-// launch (2.9) and the codes at 4.4 TB/s; 14336 x 4096, 2 bits, 8 tokens of 8 bits: 11.9
+// launch (2.9) and the codes at 4.4 TB/s; 14336 x 4096, 2 bits, 8 tokens of 8 bits: 11.6
 // us, of which the copy of the codes and parameters would be 4.3: bound by the
 // decoding (VALU and LDS) between loads.
 constexpr int kStripWaves = 8;
@@ -639,7 +639,7 @@ __device__ __forceinline__ void store_tile(const quasar_linear& a, int64_t rows,
 // multiplied, and turns them into bf16 in LDS after it, so r is never written to memory.
 // LDS holds one step: another workgroup of the CU multiplies meanwhile.  203
 // tokens, 4096 x 14336, 3 bits: 47 us, 510 TFLOP/s (and 7 to join the shares);
-// matrix units busy 33%, VALU and LDS as much, one after the other: the two
+// matrix units busy 34%, VALU and LDS as much, one after the other: the two
 // workgroups overlap little.  (Groups of four wavefronts that decode and multiply
 // in turn, 128 or 256 tokens a workgroup, took as long, as did each wavefront
 // decoding right into its operands, at 1.4 times the LDS reads.)
@@ -1005,8 +1005,7 @@ struct Choice {
 int padded_cols(const quasar_desc& d) { return (int)((d.cols + kTileK - 1) / kTileK * kTileK); }
 
 // Splits the steps of `tiles` tiles into shares while that makes no more than
-// `most` workgroups, each of `least` steps or more.  (With 16 shares at most, 84 tokens at 192 x 14336 took 19.5 us, not
-// 17; with 64 they take 17 as well.)
+// `most` workgroups, each of `least` steps or more.
 void split_steps(Choice& c, int64_t tiles, int steps, int64_t most, int least) {
   while (c.splits < 32 && 2 * tiles * c.splits <= most && steps >= 2 * c.splits * least) c.splits *= 2;
 }
@@ -1015,7 +1014,8 @@ void split_steps(Choice& c, int64_t tiles, int steps, int64_t most, int least) {
 // the least time, from what was measured of its parts.  A step of 128 tokens takes 1.8
 // us where a CU has one workgroup, 2.35 where it has two (64 tokens: 1.15 and 1.8); a
 // round of workgroups costs 2 more, the join of the shares 3 and what it and they move
-// at 5.2 TB/s.  (With shares in powers of two that fill the CUs once or twice: 179
+// at 5.2 TB/s.  (With 16 shares at most, 84 tokens at 192 x 14336 took 19.5 us, not 17;
+// with 64 they took 17 as well.  With shares in powers of two that fill the CUs once or twice: 179
 // tokens at 4113 x 11904 67 us, so 48; 250 at 9000 x 9088 95, so 74; 60 at 16000 x 1024
 // 19, so 13; 900 at 1500 x 12288 69, so 61.  203 at 4096 x 14336: 59 in tiles of 64, 48
 // in tiles of 128; 320 at 6000 x 2048: 23.7 in tiles of 64, 28 in tiles of 128.)
