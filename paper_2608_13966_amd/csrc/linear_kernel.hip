@@ -1015,9 +1015,9 @@ void split_steps(Choice& c, int64_t tiles, int steps, int64_t most, int least) {
 // us where a CU has one workgroup, 2.35 where it has two (64 tokens: 1.15 and 1.8); a
 // round of workgroups costs 2 more, the join of the shares 3 and what it and they move
 // at 5.2 TB/s.  (With 16 shares at most, 84 tokens at 192 x 14336 took 19.5 us, not 17;
-// with 64 they took 17 as well.  With shares in powers of two that fill the CUs once or twice: 179
-// tokens at 4113 x 11904 67 us, so 48; 250 at 9000 x 9088 95, so 74; 60 at 16000 x 1024
-// 19, so 13; 900 at 1500 x 12288 69, so 61.  203 at 4096 x 14336: 59 in tiles of 64, 48
+// with 64 they took 17 as well.  With shares in powers of two that fill the CUs once or
+// twice: 179 tokens at 4113 x 11904 67 us, so 48; 250 at 9000 x 9088 95, so 74; 60 at
+// 16000 x 1024 19, so 13; 900 at 1500 x 12288 69, so 61.  203 at 4096 x 14336: 59 in tiles of 64, 48
 // in tiles of 128; 320 at 6000 x 2048: 23.7 in tiles of 64, 28 in tiles of 128.)
 void choose_fused(Choice& c, int64_t tokens, int64_t rows, int steps) {
   double least = 0.0;
@@ -1046,8 +1046,10 @@ void choose_fused(Choice& c, int64_t tokens, int64_t rows, int steps) {
 //    of it with eight steps or more shares them with other workgroups, down to two, while the CUs are not full (192 x
 //    14336: 1 token 6.8 against 8.8, 32 tokens 9.7 against 16; with four steps the join costs more: 6.0 against 4.6);
 //  - the tile kernel where its 256 x 256 tiles come near to filling the CUs and there are tokens enough to pay for
-//    writing r out (4096 tokens at 4096 x 4096: 115 against 173; 1024 at 14336 x 4096: 126 against 164, but 512
-//    there 114 against 86), or where the columns are many enough to be split (1500 at 4096 x 14336: 225 against 259);
+//    writing r out (6000 tokens at 2000 x 4096, 192 tiles: 87 against 146; 768 at 14336 x 4096: 98 against 135; 2500 at
+//    4096 x 2048, 160 tiles: 50 against 68, but 4000 at 2048 x 2048, 128 tiles, 58 against 44), or where the columns are
+//    many enough to be split (1500 at 4096 x 14336, 96 tiles: 186 against 235, but 1024 at 2048 x 16384, 32 tiles, 105
+//    against 91);
 //  - the fused kernel between them.
 Choice choose(const quasar_desc& d, int64_t tokens) {
   Choice c{kStrip, 1, 0, 0, 0};
@@ -1059,7 +1061,7 @@ Choice choose(const quasar_desc& d, int64_t tokens) {
     return c;
   }
   tiles = ((tokens + 255) / 256) * ((d.rows + 255) / 256);
-  if ((tokens >= 768 && tiles >= 160) || (tokens >= 1024 && d.cols >= 8192)) {
+  if ((tokens >= 768 && tiles >= 160) || (tokens >= 1024 && d.cols >= 8192 && tiles >= 48)) {
     c.form = kTile;
     steps = padded_cols(d) / kTileK;
     split_steps(c, tiles, steps, kCUs, 16);

@@ -171,6 +171,31 @@ def test_columns_shared_out_unevenly(m, n, k, fmt, bits, group, xt):
     check(O.linear_codes(x, w, x_scale=s)["y"], x, r, s)
 
 
+@pytest.mark.parametrize("m,n,k", [(768, 13600, 192), (1025, 8200, 320), (1030, 3336, 8256)])
+@pytest.mark.parametrize("fmt,bits,group", FORMATS)
+def test_many_tokens(m, n, k, fmt, bits, group):
+    """r is written out first; whole tiles and ragged ones, the columns of the last case shared out."""
+    k = (k + 127) // 128 * 128 if group == 128 else k + 16 if fmt == "nvfp4" else k
+    w, r = layer(n, k, fmt, bits, group, seed=m)
+    g = torch.Generator(device=DEV).manual_seed(10)
+    bias, res = torch.randn(n, generator=g, device=DEV), torch.randn(m, n, generator=g, device=DEV)
+    x, s = acts(m, k, n, "fp8")
+    check(O.linear_codes(x, w, x_scale=s, bias=bias, residual=res, act="silu", y_dtype="fp32")["y"], x, r, s, bias, res,
+          "silu")
+    x, _ = acts(m, k, n + 1)
+    y = O.linear_codes(x, w)["y"]
+    check(y, x, r)
+    # rows that the kernel cannot load as they are, the residual's buffer as y's
+    far, _ = acts(m, k, n + 1, pad=3, off=5)
+    far.copy_(x)
+    out = {"y": res.clone()}
+    check(O.linear_codes(far, w, residual=out["y"], y_dtype="fp32", out=out)["y"], x, r, res=res)
+    x[7], x[m - 1, 3] = float("nan"), float("inf")
+    z = O.linear_codes(x, w)["y"]
+    keep = [t for t in range(m) if t not in (7, m - 1)]
+    assert z[7].isnan().all() and torch.equal(z[keep], y[keep])
+
+
 @pytest.mark.parametrize("fmt,bits,group", FORMATS)
 @pytest.mark.parametrize("m", [17, 32])
 @pytest.mark.parametrize("n", [8200, 8224])
