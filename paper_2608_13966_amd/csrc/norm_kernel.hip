@@ -85,10 +85,9 @@ __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_
   }
   if (!a.q) return;
   top = group_reduce<kWaves>(top, red[1], MaxOp());
-  // at least 2^-120, whose reciprocal is finite; NaN for a row that is not finite
+  // NaN for a row that is not finite
   float scale = fmaxf(top / 448.0f, 0x1p-120f);
   if (!(ss < INFINITY)) scale = __builtin_nanf("");
-  const float inv = 1.0f / scale;
   if (t == 0) a.scale[row] = scale;
   const int64_t eq = row * a.q_stride;
 #pragma unroll
@@ -96,7 +95,7 @@ __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_
     const int c = (v * TPR + t) * 8, n = cols - c;
     float s[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) s[i] = h[v][i] * inv;
+    for (int i = 0; i < 8; i++) s[i] = h[v][i] / scale;  // not y (1 / scale): that takes the neighbouring byte at an edge
     const uint2 b = pack_e4m3x8(s);
     uint8_t* p = a.q + eq + c;
     if (n >= 8) {

@@ -277,3 +277,23 @@ def test_strided_by_zero_is_refused():
         O.add_rms_norm(x, torch.ones(64, device=DEV))
     assert e.value.status == Q.ERR_SHAPE
     assert np.isfinite(float(x.sum()))
+
+
+@pytest.mark.parametrize("shape", [(64, 4096), (300, 1537), (40, 9000), (1000, 70)], ids=str)
+@pytest.mark.parametrize("residual", [False, True])
+def test_eight_bit_rows_are_the_rounded_quotients(shape, residual):
+    """scale = max |y| / 448 and q = E4M3(y / scale) of the y of the same call, each one fp32 division: bit for bit what
+    those give on the CPU.  (y times the reciprocal falls on the neighbouring byte for one value in millions: half of
+    each row lies at the edges between bytes, where a rounding of the reciprocal decides.)"""
+    x = gen(shape, torch.float32, 30)
+    w = torch.ones(shape[1], device=DEV)
+    n = shape[1] // 2
+    edge = (2.0 + torch.arange(n, device=DEV) % 14 + 0.5) / 16  # halves of the last bit of E4M3
+    x[:, :n] = edge * torch.exp2(-(torch.arange(n, device=DEV) % 5).float())
+    x[:, n] = 448.0 / 64  # the largest: x at an edge is y / scale at an edge but for rounding
+    o = O.add_rms_norm(x, w, torch.zeros_like(x) if residual else None, eps=EPS, quantize=True)
+    y = o["y"].cpu()
+    scale = y.abs().amax(1) / 448
+    assert torch.equal(o["scale"].cpu(), scale)
+    want = (y / scale[:, None]).to(torch.float8_e4m3fn)
+    assert torch.equal(o["q"].cpu().view(torch.uint8), want.view(torch.uint8))
