@@ -209,7 +209,7 @@ struct Part {
   __device__ __forceinline__ void load(const void* row, int V, int e0) {
     const __amdgpu_buffer_rsrc_t b = wave_buffer(const_cast<char*>(reinterpret_cast<const char*>(row)) + (int64_t)e0 * kSize, bytes);
 #pragma unroll
-    for (int v = 0; v < NV; v++) load_piece<T>(p[v], b, at, v * kThreads * 8 * kSize);
+    for (int v = 0; v < NV; v++) load_piece<T>(p[v], b, at + v * kThreads * 8 * kSize);
     if (rest < V) last = elem(row, rest, T == kElemBF16);
   }
 };
@@ -347,7 +347,7 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
   const auto buffer = [&](const void* p, int64_t stride, int64_t row) {
     return wave_buffer(const_cast<char*>(reinterpret_cast<const char*>(p)) + row * stride * kSize, bytes);
   };
-  const auto load = [&](int v, __amdgpu_buffer_rsrc_t b) { load_piece<T>(pc[v], b, mine, v * NT * 8 * kSize); };
+  const auto load = [&](int v, __amdgpu_buffer_rsrc_t b) { load_piece<T>(pc[v], b, mine + v * NT * 8 * kSize); };
   const int rest = (V & ~7) + tid;
   float last = -INFINITY;
   const auto load_last = [&](int64_t row) {

@@ -144,22 +144,23 @@ __device__ __forceinline__ void store_piece(void* base, int64_t e, const float (
     store_piece<false>(base, e, v, n);
 }
 
-// Eight elements at byte `at` (the lane's) + `from` (uniform) of a wavefront's
-// buffer (wave_buffer in device_common.h): past its end loads give 0 and
-// stores do nothing, without a branch.
+// Eight elements at byte `at` of a wavefront's buffer (wave_buffer in
+// device_common.h): past its end loads give 0 and stores do nothing, without a
+// branch.  The whole offset is the vector one: the check against the buffer's
+// end is specified for that, not for a scalar offset beside it.
 template <int T>
-__device__ __forceinline__ void load_piece(Piece<T>& p, __amdgpu_buffer_rsrc_t b, int at, int from) {
+__device__ __forceinline__ void load_piece(Piece<T>& p, __amdgpu_buffer_rsrc_t b, int at) {
   if constexpr (T == kElemBF16) {
-    const u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(b, at, from, 0);
+    const u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0);
     p.d[0] = t.x; p.d[1] = t.y; p.d[2] = t.z; p.d[3] = t.w;
   } else {
-    const u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(b, at, from, 0);
-    const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(b, at + 16, from, 0);
+    const u32x4 t = __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0);
+    const u32x4 u = __builtin_amdgcn_raw_buffer_load_b128(b, at + 16, 0, 0);
     p.f[0] = as_f32(t.x); p.f[1] = as_f32(t.y); p.f[2] = as_f32(t.z); p.f[3] = as_f32(t.w);
     p.f[4] = as_f32(u.x); p.f[5] = as_f32(u.y); p.f[6] = as_f32(u.z); p.f[7] = as_f32(u.w);
   }
 }
-// The stores' offset is the vector one alone: after a 128-bit buffer store with
+// For stores there is one more reason: after a 128-bit buffer store with
 // a scalar offset register the compiler puts no wait state before an overwrite
 // of the data's first register, and such stores wrote the overwriting value's
 // dword here now and then.
