@@ -13,6 +13,7 @@
 #include <ATen/ATen.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
+#include <c10/core/StreamGuard.h>
 
 #include "quasar_ops.h"
 
@@ -23,7 +24,8 @@ namespace {
 using at::Tensor;
 using Maybe = std::optional<Tensor>;
 
-py::object g_stream;  // stream handle of a tensor's device (refuses tensors that are on no GPU)
+py::object g_stream;        // handle of torch's current stream on a tensor's device (refuses tensors that are on no GPU)
+py::object g_torch_stream;  // torch's stream of a handle and a device
 
 std::string shape_str(at::IntArrayRef s) {
   std::string r = "(";
@@ -94,9 +96,25 @@ void* ptr(const Maybe& t) { return t ? t->data_ptr() : nullptr; }
 int64_t stride(const Maybe& t) { return t ? t->stride(0) : 0; }
 py::object obj(const Maybe& t) { return t ? py::cast(*t) : py::none(); }
 
-void* stream_of(const py::object& stream, const Tensor& t) {
-  return reinterpret_cast<void*>((stream.is_none() ? g_stream(t) : stream).cast<uintptr_t>());
-}
+// The stream of a call.  One that the caller names is torch's current one
+// meanwhile: what is allocated or filled on the way belongs to it, so memory
+// that is freed again (a workspace, or an output that is dropped) goes to no
+// other stream's work while this one's kernels use it, nor comes from there.
+class Stream {
+ public:
+  Stream(const py::object& given, const at::Device& dev) : given_(given) {
+    if (given.is_none()) return;
+    const py::object s = g_torch_stream(given, (int)dev.index());
+    guard_.emplace(c10::Stream(c10::Stream::UNSAFE, dev, s.attr("stream_id").cast<c10::StreamId>()));
+  }
+  void* handle(const Tensor& t) const {
+    return reinterpret_cast<void*>((given_.is_none() ? g_stream(t) : given_).cast<uintptr_t>());
+  }
+
+ private:
+  const py::object& given_;
+  std::optional<c10::StreamGuard> guard_;
+};
 
 at::ScalarType type_of(int c) { return c == QUASAR_BF16 ? at::kBFloat16 : at::kFloat; }
 
@@ -106,6 +124,7 @@ py::object add_rms_norm(const Tensor& x, const Tensor& weight, const Maybe& resi
   TORCH_CHECK_VALUE(x.dim() == 2, "add_rms_norm: x must be 2-D");
   const int64_t rows = x.size(0), cols = x.size(1);
   const at::Device dev = x.device();
+  const Stream on(stream, dev);
   matrix(x, "x", rows, cols, dev);
   vector(weight, "weight", cols, dev);
   quasar_norm a{};
@@ -137,7 +156,7 @@ py::object add_rms_norm(const Tensor& x, const Tensor& weight, const Maybe& resi
   a.y_stride = stride(y);
   a.q_stride = stride(q);
   a.eps = (float)eps;
-  const int s = quasar_add_rms_norm(&a, stream_of(stream, x));
+  const int s = quasar_add_rms_norm(&a, on.handle(x));
   if (s != QUASAR_OK) return py::int_(s);
   py::dict o;
   o["h"] = h ? *h : x;
@@ -153,6 +172,7 @@ py::object add_rms_norm_backward(const Tensor& dy, const Tensor& h, const Tensor
   TORCH_CHECK_VALUE(dy.dim() == 2, "add_rms_norm_backward: dy must be 2-D");
   const int64_t rows = dy.size(0), cols = dy.size(1);
   const at::Device dev = dy.device();
+  const Stream on(stream, dev);
   matrix(dy, "dy", rows, cols, dev);
   matrix(h, "h", rows, cols, dev);
   vector(weight, "weight", cols, dev);
@@ -189,7 +209,7 @@ py::object add_rms_norm_backward(const Tensor& dy, const Tensor& h, const Tensor
   a.h_stride = h.stride(0);
   a.dh_stride = stride(dh);
   a.dx_stride = dx.stride(0);
-  const int s = quasar_add_rms_norm_backward(&a, stream_of(stream, dy));
+  const int s = quasar_add_rms_norm_backward(&a, on.handle(dy));
   if (s != QUASAR_OK) return py::int_(s);
   py::dict o;
   o["dx"] = dx;
@@ -207,6 +227,7 @@ py::object distill(int what, const Tensor& logits, const Tensor& index, const Te
   TORCH_CHECK_VALUE(logits.dim() == 2, where, ": logits must be 2-D");
   const int64_t rows = logits.size(0), classes = logits.size(1);
   const at::Device dev = logits.device();
+  const Stream on(stream, dev);
   matrix(logits, "logits", rows, classes, dev);
   quasar_distill a{};
   a.rows = rows;
@@ -249,7 +270,7 @@ py::object distill(int what, const Tensor& logits, const Tensor& index, const Te
   a.grad_stride = stride(grad);
   a.temperature = (float)temperature;
   a.grad_scale = (float)grad_scale;
-  void* const st = stream_of(stream, logits);
+  void* const st = on.handle(logits);
   const int s = what == 0   ? quasar_distill_topk(&a, st)
                 : what == 1 ? quasar_distill_topk_backward(&a, st)
                             : quasar_distill_topk_grad(&a, st);
@@ -292,6 +313,7 @@ py::object linear_codes(const Tensor& x, const Packed& w, const Maybe& x_scale, 
   TORCH_CHECK_VALUE(x.dim() == 2, "linear_codes: x must be 2-D");
   const int64_t tokens = x.size(0), rows = w.desc.rows;
   const at::Device dev = w.codes.device();
+  const Stream on(stream, dev);
   matrix(x, "x", tokens, w.desc.cols, dev);
   quasar_linear a{};
   a.tokens = tokens;
@@ -320,7 +342,7 @@ py::object linear_codes(const Tensor& x, const Packed& w, const Maybe& x_scale, 
   a.y_stride = y.stride(0);
   a.y_dtype = y_dtype;
   a.act = act;
-  const int s = quasar_linear_codes(&w.desc, &a, stream_of(stream, x));
+  const int s = quasar_linear_codes(&w.desc, &a, on.handle(x));
   if (s != QUASAR_OK) return py::int_(s);
   py::dict o;
   o["y"] = y;
@@ -331,7 +353,10 @@ py::object linear_codes(const Tensor& x, const Packed& w, const Maybe& x_scale, 
 }  // namespace
 
 PYBIND11_MODULE(_ops_binding, m) {
-  m.def("set_stream_function", [](py::object f) { g_stream = std::move(f); });
+  m.def("set_stream_functions", [](py::object current, py::object of_handle) {
+    g_stream = std::move(current);
+    g_torch_stream = std::move(of_handle);
+  });
   m.def("add_rms_norm", &add_rms_norm);
   m.def("add_rms_norm_backward", &add_rms_norm_backward);
   m.def("distill", &distill);
@@ -339,5 +364,5 @@ PYBIND11_MODULE(_ops_binding, m) {
   py::class_<Packed>(m, "Packed")
       .def(py::init<int64_t, int64_t, int, int, int, Tensor, Tensor, Maybe, Maybe>());
   // released before the interpreter is
-  py::module_::import("atexit").attr("register")(py::cpp_function([] { g_stream = py::object(); }));
+  py::module_::import("atexit").attr("register")(py::cpp_function([] { g_stream = g_torch_stream = py::object(); }));
 }

@@ -4,10 +4,11 @@ a teacher's top logits, and the product from packed codes.
 
 Argument checks and marshalling only, as in ``quasar`` (in C++, ``_ops_binding``):
 the work runs in the HIP kernels behind the C entry points, there is no CPU path,
-and every call is
-asynchronous on ``stream`` (default: torch's current stream on the tensors'
-device).  Tensors are 2-D with unit stride in the last dimension; rows may have
-any stride.  Each function returns a dict of tensors; a dict it returned may be
+and every call is asynchronous on ``stream`` (a ``hipStream_t`` as an int, as a
+torch stream's ``cuda_stream``; default: torch's current stream on the tensors'
+device).  What a call allocates belongs to that stream, as if it were torch's
+current one.  Tensors are 2-D with unit stride in the last dimension; rows may
+have any stride.  Each function returns a dict of tensors; a dict it returned may be
 passed as ``out`` to a later call of the same sizes and arguments, whose results
 then overwrite it and which allocates nothing.
 
@@ -162,7 +163,7 @@ def _load():
                                "(there is no fallback path)")
         import torch  # noqa: F401  the module's own libraries
         from . import _ops_binding as m
-        m.set_stream_function(Q._stream)
+        m.set_stream_functions(Q._stream, Q._torch_stream)
         _binding = m
     return _binding
 

@@ -183,6 +183,13 @@ def _stream(t):
     return torch.cuda.current_stream(t.device).cuda_stream
 
 
+def _torch_stream(handle, device):
+    """torch's stream with this hipStream_t on ``device`` (0: the device's default stream)."""
+    import torch
+    h = int(handle)
+    return torch.cuda.ExternalStream(h, device=device) if h else torch.cuda.default_stream(device)
+
+
 def quasar_reconstruct(d: Descriptor, W, v, g, codes, scales, zeros, r, best_clip, err, tensor_scale,
                        tensor_amax, workspace, workspace_bytes: int, stream) -> int:
     return lib().quasar_reconstruct(d.ref, _p(W), _p(v), _p(g), _p(codes), _p(scales), _p(zeros), _p(r),
