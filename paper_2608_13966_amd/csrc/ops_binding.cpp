@@ -104,6 +104,7 @@ class Stream {
  public:
   Stream(const py::object& given, const at::Device& dev) : given_(given) {
     if (given.is_none()) return;
+    TORCH_CHECK_VALUE(dev.is_cuda(), "tensors on ", dev, " with a stream: they have to be on its GPU");
     const py::object s = g_torch_stream(given, (int)dev.index());
     guard_.emplace(c10::Stream(c10::Stream::UNSAFE, dev, s.attr("stream_id").cast<c10::StreamId>()));
   }

@@ -256,3 +256,17 @@ def test_tensors_off_the_gpu_are_refused_as_torch_does():
     with pytest.raises(want.type) as got:
         O.add_rms_norm(x, torch.ones(64))
     assert str(got.value) == str(want.value)
+
+
+def test_tensors_off_the_gpu_are_refused_with_a_stream_too():
+    """Their pointers would go to a kernel.  No rows: where it is not refused nothing is launched either."""
+    x, w, one = torch.zeros(0, 64), torch.ones(64), torch.zeros(0)
+    i, t = torch.zeros(0, 3, dtype=torch.int64), torch.zeros(0, 3)
+    c, s = torch.zeros(8 * 64, dtype=torch.uint8), torch.zeros(8)
+    pw = O.PackedWeight(8, 128, c, s, s, fmt="int", bits=4)
+    for call in (lambda: O.add_rms_norm(x, w, stream=1), lambda: O.add_rms_norm_backward(x, x, w, one, stream=1),
+                 lambda: O.distill_topk(x, i, t, stream=1), lambda: O.distill_topk_grad(x, i, t, stream=1),
+                 lambda: O.distill_topk_backward(x, i, t, one, stream=0),
+                 lambda: O.linear_codes(torch.zeros(0, 128, dtype=torch.bfloat16), pw, stream=0)):
+        with pytest.raises(ValueError, match="cpu"):
+            call()
