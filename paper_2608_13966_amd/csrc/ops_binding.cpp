@@ -13,6 +13,7 @@
 #include <ATen/ATen.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/StreamGuard.h>
 
 #include "quasar_ops.h"
@@ -96,17 +97,21 @@ void* ptr(const Maybe& t) { return t ? t->data_ptr() : nullptr; }
 int64_t stride(const Maybe& t) { return t ? t->stride(0) : 0; }
 py::object obj(const Maybe& t) { return t ? py::cast(*t) : py::none(); }
 
-// The stream of a call.  One that the caller names is torch's current one
-// meanwhile: what is allocated or filled on the way belongs to it, so memory
-// that is freed again (a workspace, or an output that is dropped) goes to no
-// other stream's work while this one's kernels use it, nor comes from there.
+// The device and stream of a call, current while it lasts.  The device because
+// the handle of a default stream is 0 on every one: the launch would go to the
+// device that is current, whatever the tensors' is.  The stream, where the
+// caller names one, because what is allocated or filled on the way then belongs
+// to it: memory that is freed again (a workspace, or an output that is dropped)
+// goes to no other stream's work while this one's kernels use it, nor comes from
+// there.
 class Stream {
  public:
   Stream(const py::object& given, const at::Device& dev) : given_(given) {
+    if (!dev.is_cpu()) device_.reset_device(dev);
     if (given.is_none()) return;
     TORCH_CHECK_VALUE(dev.is_cuda(), "tensors on ", dev, " with a stream: they have to be on its GPU");
     const py::object s = g_torch_stream(given, (int)dev.index());
-    guard_.emplace(c10::Stream(c10::Stream::UNSAFE, dev, s.attr("stream_id").cast<c10::StreamId>()));
+    stream_.emplace(c10::Stream(c10::Stream::UNSAFE, dev, s.attr("stream_id").cast<c10::StreamId>()));
   }
   void* handle(const Tensor& t) const {
     return reinterpret_cast<void*>((given_.is_none() ? g_stream(t) : given_).cast<uintptr_t>());
@@ -114,7 +119,8 @@ class Stream {
 
  private:
   const py::object& given_;
-  std::optional<c10::StreamGuard> guard_;
+  c10::OptionalDeviceGuard device_;
+  std::optional<c10::StreamGuard> stream_;
 };
 
 at::ScalarType type_of(int c) { return c == QUASAR_BF16 ? at::kBFloat16 : at::kFloat; }
