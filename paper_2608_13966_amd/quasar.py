@@ -12,6 +12,7 @@ allocate the outputs and call them.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import threading
@@ -188,6 +189,17 @@ def _torch_stream(handle, device):
     import torch
     h = int(handle)
     return torch.cuda.ExternalStream(h, device=device) if h else torch.cuda.default_stream(device)
+
+
+def _allocating(stream, t):
+    """The context of what a call allocates: a stream that the caller names is
+    torch's current one in it, so the memory belongs to that stream (freed, it
+    goes to no other stream's work while the call's kernels use it) and what
+    fills it comes before the kernels."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    return torch.cuda.stream(_torch_stream(stream, t.device))
 
 
 def quasar_reconstruct(d: Descriptor, W, v, g, codes, scales, zeros, r, best_clip, err, tensor_scale,
@@ -395,7 +407,8 @@ def reconstruct(W, v, g=None, *, fmt="int", bits=4, group=128, clips=(1.0,), bet
                    g_dtype=_dtype_code(g) if g is not None else BF16, beta2=beta2, weighting=weighting,
                    param_dtype=param_dtype)
     if out is None:
-        out = alloc_outputs(d, W, want_r=want_r, want_diag=want_diag, has_amax=tensor_amax is not None)
+        with _allocating(stream, W):
+            out = alloc_outputs(d, W, want_r=want_r, want_diag=want_diag, has_amax=tensor_amax is not None)
     if stream is None:
         stream = _stream(W)
     s = quasar_reconstruct(d, W, v, g, out["codes"], out["scales"], out["zeros"], out["r"], out["best_clip"],
@@ -427,11 +440,12 @@ def adamw_reconstruct(W, m, v, g, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, weigh
                    g_dtype=_dtype_code(g), beta2=beta2, weighting=weighting, param_dtype=param_dtype)
     rd = BF16 if r_dtype in (None, "bf16") else F32
     if out is None:
-        out = alloc_outputs(d, W, want_r=False, want_diag=want_diag, has_amax=True)
-        if want_r:
-            out["r"] = torch.empty(W.shape, dtype=torch.bfloat16 if rd == BF16 else torch.float32, device=W.device)
-        out["amax_out"] = (torch.empty(4, dtype=torch.float32, device=W.device)
-                           if (want_amax_out and fmt == "nvfp4") else None)
+        with _allocating(stream, W):
+            out = alloc_outputs(d, W, want_r=False, want_diag=want_diag, has_amax=True)
+            if want_r:
+                out["r"] = torch.empty(W.shape, dtype=torch.bfloat16 if rd == BF16 else torch.float32, device=W.device)
+            out["amax_out"] = (torch.empty(4, dtype=torch.float32, device=W.device)
+                               if (want_amax_out and fmt == "nvfp4") else None)
     if stream is None:
         stream = _stream(W)
     opt = AdamW(lr, beta1, beta2, eps, weight_decay, int(step))
@@ -468,11 +482,12 @@ def adamw_reconstruct_batch(items, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, weig
         dd = Descriptor(W.shape[0], W.shape[1], fmt=fmt, bits=bits, group=group, clips=clips,
                         w_dtype=_dtype_code(W), g_dtype=_dtype_code(g), beta2=beta2, weighting=weighting,
                         param_dtype=param_dtype)
-        o = alloc_outputs(dd, W, want_r=False, want_diag=want_diag, has_amax=True)
-        if want_r:
-            o["r"] = torch.empty(W.shape, dtype=torch.bfloat16 if rd == BF16 else torch.float32, device=W.device)
-        o["amax_out"] = (torch.empty(4, dtype=torch.float32, device=W.device)
-                         if (want_amax_out and fmt == "nvfp4") else None)
+        with _allocating(stream, W):
+            o = alloc_outputs(dd, W, want_r=False, want_diag=want_diag, has_amax=True)
+            if want_r:
+                o["r"] = torch.empty(W.shape, dtype=torch.bfloat16 if rd == BF16 else torch.float32, device=W.device)
+            o["amax_out"] = (torch.empty(4, dtype=torch.float32, device=W.device)
+                             if (want_amax_out and fmt == "nvfp4") else None)
         o["desc"] = dd
         outs.append(o)
         mats.append(AdamWMatrix(W.shape[0], W.shape[1], _p(W), _p(m), _p(v), _p(g), _p(o["codes"]),
@@ -495,7 +510,8 @@ def absmax_batch(Ws, *, stream=None):
     _check_same([(W,) for W in Ws], slots=("W",), what="absmax_batch")
     W0 = Ws[0]
     d = Descriptor(W0.shape[0], W0.shape[1], fmt="nvfp4", w_dtype=_dtype_code(W0))
-    outs = [torch.zeros(4, dtype=torch.float32, device=W0.device) for _ in Ws]
+    with _allocating(stream, W0):
+        outs = [torch.zeros(4, dtype=torch.float32, device=W0.device) for _ in Ws]
     mats = [Matrix(W.shape[0], W.shape[1], _p(W)) for W in Ws]
     if stream is None:
         stream = _stream(W0)
@@ -535,7 +551,8 @@ def reconstruct_batch(items, *, fmt="int", bits=4, group=128, clips=(1.0,), beta
         dd = Descriptor(W.shape[0], W.shape[1], fmt=fmt, bits=bits, group=group, clips=clips,
                         w_dtype=_dtype_code(W), g_dtype=_dtype_code(g) if g is not None else BF16, beta2=beta2,
                         weighting=weighting, param_dtype=param_dtype)
-        o = alloc_outputs(dd, W, want_r=want_r, want_diag=want_diag, has_amax=True)
+        with _allocating(stream, W):
+            o = alloc_outputs(dd, W, want_r=want_r, want_diag=want_diag, has_amax=True)
         o["desc"] = dd
         outs.append(o)
         mats.append(matrix(W, v, g, o, amax))
