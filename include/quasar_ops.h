@@ -46,7 +46,7 @@ extern "C" {
  */
 #define QUASAR_NORM_MAX_COLS 32768
 typedef struct {
-  int64_t rows, cols;        /* 0 <= rows, 1 <= cols <= QUASAR_NORM_MAX_COLS */
+  int64_t rows, cols;        /* 0 <= rows < 2^31, 1 <= cols <= QUASAR_NORM_MAX_COLS */
   const void* x;             /* [rows, cols] */
   const void* residual;      /* [rows, cols], or NULL: h = x */
   const void* weight;        /* [cols] */

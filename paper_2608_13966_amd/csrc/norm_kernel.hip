@@ -126,13 +126,32 @@ hipError_t with_shape(int64_t cols, F f) {
   return hipErrorInvalidValue;
 }
 
+// n rows from row r on
+quasar_norm rows_of(quasar_norm a, int64_t r, int64_t n) {
+  a.rows = n;
+  a.x = rows_on(a.x, r, a.x_stride, size_of(a.x_dtype));
+  a.residual = rows_on(a.residual, r, a.residual_stride, size_of(a.residual_dtype));
+  a.h = rows_on(a.h, r, a.h_stride, size_of(a.residual_dtype));
+  a.y = rows_on(a.y, r, a.y_stride, size_of(a.y_dtype));
+  a.q = rows_on(a.q, r, a.q_stride, 1);
+  a.scale = rows_on(a.scale, r, 1, 4);
+  a.rstd = rows_on(a.rstd, r, 1, 4);
+  return a;
+}
+
 template <int XT, int RT>
 hipError_t launch_norm_types(const quasar_norm& a, hipStream_t stream) {
   return with_shape(a.cols, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
     constexpr int threads = TPR < kNormThreads ? kNormThreads : TPR, rows = threads / TPR;
-    norm_kernel<XT, RT, TPR, NV><<<dim3((unsigned)((a.rows + rows - 1) / rows)), dim3(threads), 0, stream>>>(a);
-    return hipGetLastError();
+    constexpr int64_t most = most_groups(threads) * rows;
+    for (int64_t r = 0; r < a.rows; r += most) {
+      const quasar_norm s = rows_of(a, r, a.rows - r < most ? a.rows - r : most);
+      norm_kernel<XT, RT, TPR, NV><<<dim3((unsigned)((s.rows + rows - 1) / rows)), dim3(threads), 0, stream>>>(s);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   });
 }
 

@@ -6,12 +6,13 @@
 
 namespace {
 
-constexpr int64_t kMaxRows = 0x7fffffff;         // of a grid
+using quasar::size_of;
+
+constexpr int64_t kMaxRows = 0x7fffffff;
 constexpr int64_t kMaxStride = (int64_t)1 << 40;  // rows * stride stays far inside int64
 
 bool f32_or_bf16(int32_t t) { return t == QUASAR_F32 || t == QUASAR_BF16; }
 bool misaligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) != 0; }
-uintptr_t size_of(int32_t t) { return t == QUASAR_F32 ? 4 : t == QUASAR_E4M3 ? 1 : 2; }
 
 // one matrix operand (p may be NULL: absent)
 int check_matrix(const void* p, int64_t rows, int64_t cols, int64_t stride, int32_t dtype) {

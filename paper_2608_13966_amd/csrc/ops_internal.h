@@ -4,11 +4,25 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "quasar_ops.h"
 
 namespace quasar {
 
 constexpr int kCUs = 256;  // compute units of the card
+
+// Workgroups of a launch: HIP takes fewer than 2^32 threads in a grid.  A call
+// with more rows than that many take is launched in pieces of its rows.
+constexpr int64_t most_groups(int threads) { return 0xffffffffll / threads; }
+
+inline int64_t size_of(int32_t dtype) { return dtype == QUASAR_F32 ? 4 : dtype == QUASAR_E4M3 ? 1 : 2; }
+// p (may be NULL) `rows` rows on
+template <typename T>
+T* rows_on(T* p, int64_t rows, int64_t stride, int64_t size) {
+  using byte = std::conditional_t<std::is_const_v<T>, const char, char>;
+  return p ? reinterpret_cast<T*>(reinterpret_cast<byte*>(p) + rows * stride * size) : nullptr;
+}
 
 // norm_kernel.hip
 hipError_t launch_norm(const quasar_norm& a, hipStream_t stream);

@@ -297,3 +297,18 @@ def test_eight_bit_rows_are_the_rounded_quotients(shape, residual):
     assert torch.equal(o["scale"].cpu(), scale)
     want = (y / scale[:, None]).to(torch.float8_e4m3fn)
     assert torch.equal(o["q"].cpu().view(torch.uint8), want.view(torch.uint8))
+
+
+def test_more_rows_than_a_grid_takes():
+    """2^26 rows, four a workgroup of 256 threads, would be 2^32 threads: rows on either side of that."""
+    rows, cols = (1 << 26) + 6, 8
+    g = torch.Generator(device=DEV).manual_seed(31)
+    x, res = (torch.randn(rows, cols, device=DEV, generator=g, dtype=torch.bfloat16) for _ in range(2))
+    w = gen((1, cols), torch.float32, 32)[0]
+    o = O.add_rms_norm(x, w, res, eps=EPS, quantize=True)
+    cut = (1 << 26) - 4
+    for a, b in ((0, cut), (cut, rows)):
+        part = O.add_rms_norm(x[a:b], w, res[a:b], eps=EPS, quantize=True)
+        for k in ("h", "y", "q", "scale", "rstd"):
+            assert torch.equal(o[k][a:b].view(torch.uint8), part[k].view(torch.uint8)), k
+    check_forward(x[-40:], w, res[-40:], {k: o[k][-40:] for k in ("h", "y", "q", "scale", "rstd")})
