@@ -109,7 +109,7 @@ size_t quasar_add_rms_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
  */
 #define QUASAR_DISTILL_MAX_LISTED 1024
 typedef struct {
-  int64_t rows, classes;     /* 0 <= rows, 1 <= classes < 2^31 - 2^16 */
+  int64_t rows, classes;     /* 0 <= rows, 1 <= classes < 2^31 - 2^16, rows * ceil(classes / 1024) < 2^31 */
   int32_t listed;            /* K, 1 .. QUASAR_DISTILL_MAX_LISTED */
   int32_t logits_dtype;      /* of logits and grad: QUASAR_F32 or QUASAR_BF16 */
   int32_t teacher_dtype;     /* QUASAR_F32 or QUASAR_BF16 */

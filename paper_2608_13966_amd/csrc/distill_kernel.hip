@@ -508,9 +508,24 @@ hipError_t launch_resident(const quasar_distill& a, hipStream_t stream) {
   return hipErrorInvalidValue;
 }
 
+// n rows from row r on
+quasar_distill rows_of(quasar_distill a, int64_t r, int64_t n, int parts) {
+  const int64_t size = size_of(a.logits_dtype);
+  a.rows = n;
+  a.logits = rows_on(a.logits, r, a.logits_stride, size);
+  a.grad = rows_on(a.grad, r, a.grad_stride, size);
+  a.index = rows_on(a.index, r, a.listed, a.index_bits / 8);
+  a.teacher = rows_on(a.teacher, r, a.listed, size_of(a.teacher_dtype));
+  a.row_weight = rows_on(a.row_weight, r, 1, 4);
+  a.grad_loss = rows_on(a.grad_loss, r, 1, 4);
+  a.loss = rows_on(a.loss, r, 1, 4);
+  a.lse = rows_on(a.lse, r, 1, 4);
+  a.workspace = rows_on(a.workspace, r, parts, sizeof(MaxSum));
+  return a;
+}
+
 template <int T, int NV>
-hipError_t launch_split(const quasar_distill& a, int what, hipStream_t stream) {
-  const int parts = parts_of(a.rows, a.classes);
+hipError_t launch_split_rows(const quasar_distill& a, int what, int parts, hipStream_t stream) {
   const dim3 grid((unsigned)(a.rows * parts)), block(kThreads);
   const size_t lds = RowList::size(a.listed) * sizeof(float);
   MaxSum* ws = reinterpret_cast<MaxSum*>(a.workspace);
@@ -529,6 +544,17 @@ hipError_t launch_split(const quasar_distill& a, int what, hipStream_t stream) {
     return e != hipSuccess ? e : row_kernel(1, 0);
   }
   return row_kernel(what, parts);
+}
+
+template <int T, int NV>
+hipError_t launch_split(const quasar_distill& a, int what, hipStream_t stream) {
+  const int parts = parts_of(a.rows, a.classes);
+  const int64_t most = most_groups(kThreads) / parts;
+  for (int64_t r = 0; r < a.rows; r += most) {
+    const hipError_t e = launch_split_rows<T, NV>(rows_of(a, r, a.rows - r < most ? a.rows - r : most, parts), what, parts, stream);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <int T>

@@ -110,7 +110,7 @@ size_t quasar_distill_topk_workspace_bytes(int64_t rows, int64_t classes) {
 int quasar_distill_topk_check(const quasar_distill* a, int what) {
   if (a == nullptr || what < 0 || what > 2) return QUASAR_ERR_ARG;
   if (a->rows < 0 || a->classes < 1 || a->classes >= kMaxRows - 65535) return QUASAR_ERR_SHAPE;
-  // a workgroup per 2^10 classes at the most, in one grid
+  // parts of rows, of 2^11 classes or more, are counted in 32 bits
   if (a->rows > kMaxRows / ((a->classes + 1023) / 1024)) return QUASAR_ERR_SHAPE;
   if (a->listed < 1 || a->listed > QUASAR_DISTILL_MAX_LISTED) return QUASAR_ERR_SHAPE;
   if (!f32_or_bf16(a->logits_dtype) || !f32_or_bf16(a->teacher_dtype)) return QUASAR_ERR_FORMAT;

@@ -341,3 +341,19 @@ def test_refusals():
         with pytest.raises(Q.QuasarError) as e:
             O.distill_topk_grad(z, idx, val, **kw)
         assert e.value.status == Q.ERR_ARG
+
+
+def test_more_rows_than_a_grid_takes():
+    """The gradient alone takes a workgroup of 256 threads a row: from 2^24 rows on more than 2^32 threads."""
+    t, v = (1 << 24) + 7, 8
+    z, idx, val = make(t, v, 2, "bf16", "bf16", torch.int32, seed=16)
+    wt, gl = torch.rand(t, device=DEV), torch.randn(t, device=DEV)
+    wt[5::31] = 0.0
+    lse = O.distill_topk(z, idx, val, row_weight=wt, temperature=1.5)["lse"]
+    o = O.distill_topk_backward(z, idx, val, lse, row_weight=wt, grad_loss=gl, temperature=1.5)
+    cut = (1 << 24) - 3
+    for s in (slice(0, cut), slice(cut, t)):
+        part = O.distill_topk_backward(z[s], idx[s], val[s], lse[s], row_weight=wt[s], grad_loss=gl[s], temperature=1.5)
+        assert torch.equal(o["grad"][s], part["grad"])
+    s = slice(t - 50, t)
+    check(z[s], idx[s], val[s], {"grad": o["grad"][s], "lse": lse[s]}, 1.5, wt[s], gl[s], what=("grad", "lse"))
