@@ -158,7 +158,8 @@ typedef enum {
 } quasar_activation;
 
 typedef struct {
-  int64_t tokens;            /* >= 0 */
+  int64_t tokens;            /* 0 <= tokens <= 2^28, with rows <= 2^28 and cols <= 2^22, as far as a grid takes the
+                                workgroups: up to 16 tokens (8 bits: 32) rows <= 2^27 - 16; else past 2^37 outputs */
   const void* x;             /* [tokens, cols] */
   const float* x_scale;      /* [tokens], or NULL: 1 */
   const uint8_t* codes;      /* as quasar_reconstruct writes them */

@@ -826,13 +826,15 @@ __global__ __launch_bounds__(256) void unpack_kernel(Weights w, quasar_linear a,
     }
   } else {
     const int per = kp / 8;
-    const int64_t i = (int64_t)(blockIdx.x - weight_blocks) * 256 + threadIdx.x;
-    const int64_t t = i / per;
-    if (t >= a.tokens) return;
-    const int k = (int)(i - t * per) * 8;
-    XChunk<XT> c;
-    c.load(a.x, t * a.x_stride + k, k < w.cols);
-    st128(xo + t * kp + k, c.bf16());
+    const int64_t total = a.tokens * per, step = (int64_t)(gridDim.x - weight_blocks) * 256;
+    // more than once only past the threads that a grid takes
+    for (int64_t i = (int64_t)(blockIdx.x - weight_blocks) * 256 + threadIdx.x; i < total; i += step) {
+      const int64_t t = i / per;
+      const int k = (int)(i - t * per) * 8;
+      XChunk<XT> c;
+      c.load(a.x, t * a.x_stride + k, k < w.cols);
+      st128(xo + t * kp + k, c.bf16());
+    }
   }
 }
 
@@ -1076,6 +1078,20 @@ Choice choose(const quasar_desc& d, int64_t tokens) {
   return c;
 }
 
+// 32 outputs a workgroup of the strip kernel where there are many and x is what takes time: 24 and 32 tokens in bf16 at
+// 14336 x 4096 18.4 and 19.7 against 23.3 and 24.5, at 8192 x 4096 10.5 and 11.4 against 12.1 and 12.5, at 4096 x 4096
+// 9.7 and 9.9 against 7.3 and 7.5; 8 tokens at 14336 x 4096 12.2 against 11.6, 32 of 8 bits there 19.3 against 19.1.
+bool strip_two(const quasar_desc& d, int64_t tokens, int x_dtype) {
+  return x_dtype == QUASAR_BF16 && tokens > 16 && d.rows >= 8192;
+}
+int64_t strip_groups(const quasar_desc& d, const Choice& c, bool two) {
+  return (d.rows + (two ? 31 : 15)) / (two ? 32 : 16) * c.splits;
+}
+int64_t tiles_of(const quasar_desc& d, int64_t tokens, int bm, int bn) {
+  return ((tokens + bm - 1) / bm) * ((d.rows + bn - 1) / bn);
+}
+int64_t unpack_weight_groups(const quasar_desc& d) { return (d.rows * (padded_cols(d) / 32) + 255) / 256; }
+
 // x goes through the workspace unless the tile kernel can load its rows in
 // 16-byte pieces as they are.
 bool x_direct(int64_t cols, int x_dtype, const void* x, int64_t stride) {
@@ -1094,11 +1110,8 @@ hipError_t launch(const quasar_desc& d, const quasar_linear& a, hipStream_t stre
     return hipGetLastError();
   };
   if (c.form == kStrip) {
-    // 32 outputs a workgroup where there are many and x is what takes time: 24 and 32 tokens in bf16 at 14336 x 4096
-    // 18.4 and 19.7 against 23.3 and 24.5, at 8192 x 4096 10.5 and 11.4 against 12.1 and 12.5, at 4096 x 4096 9.7 and 9.9
-    // against 7.3 and 7.5; 8 tokens at 14336 x 4096 12.2 against 11.6, 32 of 8 bits there 19.3 against 19.1
-    const bool two = XT == kElemBF16 && a.tokens > 16 && d.rows >= 8192;
-    const unsigned gx = (unsigned)((d.rows + (two ? 31 : 15)) / (two ? 32 : 16) * c.splits);
+    const bool two = strip_two(d, a.tokens, a.x_dtype);
+    const unsigned gx = (unsigned)strip_groups(d, c, two);
     if (c.splits > 1) part = reinterpret_cast<float*>(a.workspace);
     const auto strip = [&](auto nx) {
       constexpr int NX = decltype(nx)::value, NB = NX == 8 && XT == kElemBF16 ? 2 : 1;
@@ -1120,9 +1133,9 @@ hipError_t launch(const quasar_desc& d, const quasar_linear& a, hipStream_t stre
     return e != hipSuccess || !part ? e : join();
   }
   if (c.form == kFused) {
-    const int tm = (int)((a.tokens + c.bm - 1) / c.bm), tn = (int)((d.rows + 127) / 128);
+    const int tm = (int)((a.tokens + c.bm - 1) / c.bm);
     if (c.splits > 1) part = reinterpret_cast<float*>(a.workspace);
-    const dim3 grid((unsigned)(tm * tn * c.splits));
+    const dim3 grid((unsigned)(tiles_of(d, a.tokens, c.bm, 128) * c.splits));
     if (c.bm == 64)
       fused_kernel<FMT, BITS, XT, 64><<<grid, dim3(256), 0, stream>>>(w, a, tm, c.splits, c.steps, part);
     else
@@ -1135,7 +1148,9 @@ hipError_t launch(const quasar_desc& d, const quasar_linear& a, hipStream_t stre
   uint16_t* xo = r + d.rows * kp;
   if (c.splits > 1) part = reinterpret_cast<float*>(xo + a.tokens * kp);
   const bool direct = x_direct(d.cols, a.x_dtype, a.x, a.x_stride);
-  const int64_t wb = (d.rows * (kp / 32) + 255) / 256, xb = direct ? 0 : (a.tokens * (kp / 8) + 255) / 256;
+  const int64_t wb = unpack_weight_groups(d), most = most_groups(256) - wb;
+  int64_t xb = direct ? 0 : (a.tokens * (kp / 8) + 255) / 256;
+  if (xb > most) xb = most;
   unpack_kernel<FMT, BITS, XT><<<dim3((unsigned)(wb + xb)), dim3(256), 0, stream>>>(w, a, kp, r, xo, (unsigned)wb);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
@@ -1155,6 +1170,14 @@ hipError_t launch_x(const quasar_desc& d, const quasar_linear& a, hipStream_t st
 }  // namespace
 
 size_t linear_workspace(const quasar_desc& d, int64_t tokens) { return choose(d, tokens).bytes; }
+
+bool linear_fits(const quasar_desc& d, int64_t tokens, int x_dtype, size_t& workspace) {
+  const Choice c = choose(d, tokens);
+  workspace = c.bytes;
+  if (c.form == kStrip) return strip_groups(d, c, strip_two(d, tokens, x_dtype)) <= most_groups(64 * kStripWaves);
+  if (c.form == kFused) return tiles_of(d, tokens, c.bm, 128) * c.splits <= most_groups(256);
+  return tiles_of(d, tokens, 256, 256) * c.splits <= most_groups(512) && unpack_weight_groups(d) < most_groups(256);
+}
 
 hipError_t launch_linear(const quasar_desc& d, const quasar_linear& a, hipStream_t stream) {
   switch (d.format) {

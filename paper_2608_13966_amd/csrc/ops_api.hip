@@ -169,12 +169,13 @@ int quasar_linear_codes_check(const quasar_desc* d, const quasar_linear* a) {
       misaligned(a->tensor_scale, 4) || misaligned(a->workspace, 16))
     return QUASAR_ERR_ALIGN;
   if (a->tokens == 0) return QUASAR_OK;
+  size_t need;
+  if (!quasar::linear_fits(*d, a->tokens, a->x_dtype, need)) return QUASAR_ERR_SHAPE;
   if (!a->x || !a->y) return QUASAR_ERR_ARG;
   QUASAR_TRY(check_matrix(a->x, a->tokens, d->cols, a->x_stride, a->x_dtype));
   QUASAR_TRY(check_matrix(a->residual, a->tokens, d->rows, a->residual_stride, a->residual_dtype));
   QUASAR_TRY(check_matrix(a->y, a->tokens, d->rows, a->y_stride, a->y_dtype));
   if (misaligned(a->x_scale, 4) || (a->bias && misaligned(a->bias, size_of(a->bias_dtype)))) return QUASAR_ERR_ALIGN;
-  const size_t need = quasar::linear_workspace(*d, a->tokens);
   if (need > 0 && (a->workspace == nullptr || a->workspace_bytes < need)) return QUASAR_ERR_WORKSPACE;
   return QUASAR_OK;
 }

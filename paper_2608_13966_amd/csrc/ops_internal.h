@@ -36,6 +36,8 @@ hipError_t launch_distill(const quasar_distill& a, int what, hipStream_t stream)
 
 // linear_kernel.hip
 size_t linear_workspace(const quasar_desc& d, int64_t tokens);
+// whether the kernels' workgroups fit a grid; and linear_workspace()
+bool linear_fits(const quasar_desc& d, int64_t tokens, int x_dtype, size_t& workspace);
 hipError_t launch_linear(const quasar_desc& d, const quasar_linear& a, hipStream_t stream);
 
 }  // namespace quasar

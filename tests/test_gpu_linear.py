@@ -334,3 +334,24 @@ def test_norm_into_product():
     f = O.add_rms_norm(x, torch.ones(k, device=DEV), want_y=False, quantize=True)
     y = O.linear_codes(f["q"], w, x_scale=f["scale"], y_dtype="fp32")["y"]
     check(y, f["q"].float(), r, f["scale"])
+
+
+def test_more_activations_than_a_grid_has_threads():
+    """2^28 tokens of 128 columns in 8 bits (34 GB): eight a thread they are 2^32 threads' work."""
+    n, k, m = 8, 128, 1 << 28
+    w, r = layer(n, k, "int", 4, 128, seed=18)
+    torch.cuda.empty_cache()
+    g = torch.Generator(device=DEV).manual_seed(19)
+    x = torch.randint(0, 0x58, (m, k), device=DEV, generator=g, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    y = O.linear_codes(x, w)["y"]
+    rt = r.float().t().contiguous()
+    for a in range(0, m, 1 << 24):
+        part = x[a:a + (1 << 24)].float()
+        want = part @ rt
+        size = part.abs_() @ rt.abs()
+        # both sums in fp32, k u of their terms' sizes each at worst; y's own rounding
+        assert ((y[a:a + (1 << 24)].float() - want).abs() <= 2 * (k + 4) * U * size + 2.0 ** -8 * 1.01 * want.abs()).all(), a
+        del part, want, size
+    check(y[-500:], x[-500:].float(), r)
+    del x, y
+    torch.cuda.empty_cache()

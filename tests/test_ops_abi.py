@@ -270,3 +270,20 @@ def test_tensors_off_the_gpu_are_refused_with_a_stream_too():
                  lambda: O.linear_codes(torch.zeros(0, 128, dtype=torch.bfloat16), pw, stream=0)):
         with pytest.raises(ValueError, match="cpu"):
             call()
+
+
+def test_linear_sizes_that_no_grid_takes():
+    """HIP takes fewer than 2^32 threads in a grid: what has more is refused by the check, not by the launch."""
+    def status(rows, cols, tokens, xd=Q.BF16):
+        d = Q.Descriptor(rows, cols, fmt="int", bits=2, group=64)
+        return _linear(d, tokens=tokens, x_dtype=xd, x_stride=cols, y_stride=rows, residual_stride=rows)
+
+    # 16 outputs a workgroup of 512 threads, or 32 (17 to 32 tokens in bf16)
+    assert status((1 << 27) - 16, 64, 1) == Q.OK and status((1 << 27) - 15, 64, 1) == Q.ERR_SHAPE
+    assert status(1 << 27, 64, 32, O.E4M3) == Q.ERR_SHAPE and status(1 << 27, 64, 32) == Q.OK
+    assert status((1 << 28) - 32, 64, 20) == Q.OK and status(1 << 28, 64, 20) == Q.ERR_SHAPE
+    # 256 x 256 outputs a workgroup of 512 threads
+    assert status(2048, 64, (1 << 28) - 256) == Q.OK and status(2049, 64, (1 << 28) - 256) == Q.ERR_SHAPE
+    assert status(256, 128, 1 << 28, O.E4M3) == Q.OK  # many more activations than threads
+    # every size that was accepted before, and that a card holds
+    assert status(1 << 20, 1 << 14, 1000) == Q.OK and status(1 << 22, 4096, 8192) == Q.OK
