@@ -357,3 +357,32 @@ def test_more_rows_than_a_grid_takes():
         assert torch.equal(o["grad"][s], part["grad"])
     s = slice(t - 50, t)
     check(z[s], idx[s], val[s], {"grad": o["grad"][s], "lse": lse[s]}, 1.5, wt[s], gl[s], what=("grad", "lse"))
+
+
+@pytest.mark.parametrize("t,v,k", [(1100, 1200, 200), (300, 17000, 64), (5, 9000, 1000), (3, 140001, 64), (2, 200, 200)])
+@pytest.mark.parametrize("tau", [1.0, 0.7])
+def test_loss_has_no_error_of_the_logits_size(t, v, k, tau):
+    """The loss depends on differences of logits alone.  On a grid of 1/64 these are exact in fp32 whatever is added to
+    all, so adding 512 to the student's row, or to the teacher's, changes no bit of it; and it is off from the formula
+    in 64 bits by no more than its parts' errors, which know no 512: with y = (z - max) / tau, d = (t - max) / tau,
+      log q: 3 u |y| + log of the sum, whose terms are off by (3 |y| + 4) u and their sum by 64 u more;
+      log p: likewise from d; and the products' and the sum's own, p's error included: (3 |d| + 72) u of their size."""
+    z, idx, val = make(t, v, k, "fp32", "fp32", torch.int32, seed=17)
+    z, val = (64 * z).round() / 64, (64 * val).round() / 64
+    idx[0, k // 2:] = -1
+    runs = [O.distill_topk(a, idx, b, temperature=tau)["loss"] for a, b in ((z, val), (z + 512, val), (z, val - 512))]
+    runs += [O.distill_topk_grad(z + 512, idx, val + 512, temperature=tau)["loss"]]
+    assert all(torch.equal(r, runs[0]) for r in runs)
+    loss, _, _, _, _, at = reference(z, idx, val, tau)
+    y = (z.double() - z.double().amax(1, keepdim=True)) / tau
+    d = torch.where(idx >= 0, val.double(), -math.inf)
+    d = (d - d.amax(1, keepdim=True)) / tau
+    p, q = torch.softmax(d, 1), torch.softmax(y, 1)
+    d = torch.where(idx >= 0, d, 0.0)
+    yk, lq = y.gather(1, at).abs(), torch.log_softmax(y, 1).gather(1, at)
+    lp = torch.where(idx >= 0, p.clamp_min(1e-300).log(), 0.0)
+    sum_q = ((q * (3 * y.abs() + 4)).sum(1) + 64 + 2 * torch.logsumexp(y, 1).abs())[:, None]
+    sum_p = ((p * (3 * d.abs() + 4)).sum(1) + 64 + 2 * torch.where(idx >= 0, lp - d, 0.0).abs().amax(1))[:, None]
+    tol = (p * (3 * yk + sum_q + 3 * d.abs() + sum_p + (lp - lq).abs() * (3 * d.abs() + 72 + sum_p))).sum(1) * U
+    off = (runs[0].double() - loss).abs()
+    assert (off <= tol).all(), float((off / tol).max())
