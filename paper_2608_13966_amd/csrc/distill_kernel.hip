@@ -178,9 +178,12 @@ __device__ __forceinline__ void take(MaxSum& r, const Piece<T>& p, float c) {
   float m = r.m;
 #pragma unroll
   for (int i = 0; i < 8; i++) m = fmaxf(m, p.get(i));
-  if (m == -INFINITY) {  // nothing but -inf so far: no exponent to take, but a NaN among them stays
+  // no exponent to take: of nothing but -inf nothing counts, beside +inf it alone does, and a NaN stays
+  if (fabsf(m) == INFINITY) {
+    if (m != r.m && r.s == r.s) r.s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; i++) r.s += p.get(i) != p.get(i) ? p.get(i) : 0.0f;
+    for (int i = 0; i < 8; i++) r.s += p.get(i) != p.get(i) ? p.get(i) : p.get(i) == INFINITY ? 1.0f : 0.0f;
+    r.m = m;
     return;
   }
   if (m != r.m) {

@@ -386,3 +386,34 @@ def test_loss_has_no_error_of_the_logits_size(t, v, k, tau):
     tol = (p * (3 * yk + sum_q + 3 * d.abs() + sum_p + (lp - lq).abs() * (3 * d.abs() + 72 + sum_p))).sum(1) * U
     off = (runs[0].double() - loss).abs()
     assert (off <= tol).all(), float((off / tol).max())
+
+
+@pytest.mark.parametrize("t,v", [(1100, 1203), (1100, 4097), (300, 17003), (6, 9000), (6, 140003)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_student_logits_at_plus_infinity(t, v, dtype):
+    """As the formula has it: the log-sum is +inf, the loss +inf (NaN where the infinite class is listed: inf - inf), the
+    gradient -p of the finite classes and NaN of the infinite one.  A NaN beside it makes all of them NaN."""
+    z, idx, val = make(t, v, 8, dtype, seed=18)
+    inf = float("inf")
+    free = [c for c in range(v - 1, -1, -1)]
+    at = [next(c for c in free[a:] if c not in idx[r].tolist()) for r, a in ((0, 0), (1, v - 3), (2, 0), (3, v // 2))]
+    z[0, at[0]] = inf                      # past the whole pieces
+    z[1, at[1]] = inf                      # in the first piece
+    z[2, int(idx[2, 3])] = inf             # listed, and one that is not
+    z[2, at[2]] = inf
+    z[3, at[3]], z[3, at[3] - 1] = inf, float("nan")
+    f = O.distill_topk(z, idx, val, temperature=1.5)
+    o = O.distill_topk_grad(z, idx, val, temperature=1.5, grad_scale=0.25)
+    b = O.distill_topk_backward(z, idx, val, f["lse"], temperature=1.5, grad_scale=0.25)
+    loss, lse, grad, _, p, listed = reference(z, idx, val, 1.5, None, 0.25)
+    for x in (f, o):
+        assert (x["lse"][:3] == inf).all() and x["lse"][3].isnan()
+        assert (x["loss"][:2] == inf).all() and x["loss"][2:4].isnan().all()
+    for x in (o["grad"], b["grad"]):
+        g = x[:3].double()
+        assert torch.equal(g.isnan(), grad[:3].isnan())
+        where = ~g.isnan()
+        assert ((g - grad[:3]).abs()[where] <= (VB if dtype == "bf16" else 1e-5) * grad[:3].abs()[where]).all()
+        assert x[3].isnan().all()
+    rest = slice(4, t)
+    check(z[rest], idx[rest], val[rest], {k: o[k][rest] for k in ("loss", "lse", "grad")}, 1.5, None, 0.25)
