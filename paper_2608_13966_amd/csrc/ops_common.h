@@ -223,6 +223,7 @@ __device__ __forceinline__ float group_reduce(float x, float* s, Op op) {
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2eRest = (float)(1.44269504088896340736 - (double)kLog2e);
 constexpr float kLn2 = 0.69314718055994530942f;
 
 }  // namespace quasar

@@ -355,3 +355,23 @@ def test_more_activations_than_a_grid_has_threads():
     check(y[-500:], x[-500:].float(), r)
     del x, y
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("m", [1, 20, 60, 1100])
+def test_silu_to_the_last_bits(m):
+    """Of values that are exact (bias, x being 0), in fp32: an exponential's 2 u, four roundings more, 8 u at most."""
+    n, k = 40000 if m > 1000 else 4096, 64
+    g = torch.Generator(device=DEV).manual_seed(20)
+    codes = torch.randint(0, 256, (n * k // 2,), device=DEV, generator=g, dtype=torch.uint8)
+    scales, zeros = torch.rand(n, device=DEV, generator=g), torch.randn(n, device=DEV, generator=g)
+    w = O.PackedWeight(n, k, codes, scales, zeros, bits=4, group=64)
+    bias = torch.linspace(-60, 60, n, device=DEV)
+    bias[::3] = 2 * torch.randn(bias[::3].shape, device=DEV, generator=g)
+    inf = float("inf")
+    bias[:6] = torch.tensor([-1000.0, 1000.0, 0.0, inf, -inf, float("nan")], device=DEV)
+    y = O.linear_codes(torch.zeros(m, k, device=DEV, dtype=torch.bfloat16), w, bias=bias, act="silu", y_dtype="fp32")["y"]
+    assert (y[:, 0].abs() < 1e-37).all() and (y[:, 1] == 1000).all() and (y[:, 2] == 0).all() and (y[:, 3] == inf).all()
+    assert y[:, 4:6].isnan().all()  # -inf / (1 + inf), and NaN
+    v = bias[6:].double()
+    want = v / (1 + (-v).exp())
+    assert ((y[:, 6:].double() - want).abs() <= 8 * U * want.abs()).all(), float(((y[:, 6:].double() / want - 1).abs() / U).max())
