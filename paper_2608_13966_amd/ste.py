@@ -136,8 +136,11 @@ class _AddRMSNorm(torch.autograd.Function):
         if dy is None:  # only the stream went on
             return (dh.to(x_type) if need_x and dh is not None else None, None,
                     dh if need_r else None, None)
-        o = ops.add_rms_norm_backward(_rows(dy), h, weight, rstd, None if dh is None else _rows(dh),
-                                      dx_dtype=None if dh is not None else r_type or x_type, want_dweight=need_w)
+        # in the widest type that an input takes it in
+        wide = torch.float32 in (need_x and x_type, need_r and r_type)
+        dx_type = torch.float32 if wide else r_type or x_type
+        o = ops.add_rms_norm_backward(_rows(dy), h, weight, rstd, None if dh is None else _rows(dh.to(dx_type)),
+                                      dx_dtype=dx_type, want_dweight=need_w)
         dx = o["dx"].view(dy.shape)
         return (dx.to(x_type) if need_x else None, o["dw"].to(weight.dtype) if need_w else None,
                 dx.to(r_type) if need_r else None, None)

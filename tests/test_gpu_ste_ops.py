@@ -161,3 +161,33 @@ def test_packed_codes_of_a_layer_are_its_r():
         assert torch.equal(y.t(), layer.r)
         layer(rand(4, 128, seed=1)).square().sum().backward()
         layer.step()
+
+
+@pytest.mark.parametrize("x_type,r_type", [(torch.float32, torch.bfloat16), (torch.bfloat16, torch.float32),
+                                           (torch.bfloat16, torch.bfloat16)])
+@pytest.mark.parametrize("stream_too", [False, True])
+def test_norm_gradients_have_their_inputs_precision(x_type, r_type, stream_too):
+    """Each input's gradient is rounded to its own type once: an fp32 input's not to the other's bf16 first.  The formula
+    with the h that the forward pass kept, in 64 bits; its bound as above."""
+    x, res = rand(30, 200, seed=1, dtype=x_type).requires_grad_(), rand(30, 200, seed=2, dtype=r_type).requires_grad_()
+    w = (1 + 0.1 * rand(200, seed=3)).requires_grad_()
+    y, h = ste.add_rms_norm(x, w, res, eps=EPS)
+    dy, dh = rand(30, 200, seed=4, dtype=y.dtype), rand(30, 200, seed=5, dtype=h.dtype) if stream_too else None
+    torch.autograd.backward([y, h] if stream_too else [y], [dy, dh] if stream_too else [dy])
+    rstd = ((x.detach().double() + res.detach().double()).square().mean(-1, keepdim=True) + EPS).rsqrt()
+    n, u = h.detach().double() * rstd, dy.double() * w.detach().double()
+    dx, size = rstd * (u - n * (u * n).mean(-1, keepdim=True)), rstd * (u.abs() + n.abs() * (u * n).abs().mean(-1, keepdim=True))
+    if stream_too:
+        dx, size = dx + dh.double(), size + dh.double().abs()
+    # rstd's own error beside the others': another (200 + 16) u of each term, three times a term at most
+    tol = 4 * size * (200 + 16) * U
+    for t in (x, res):
+        assert t.grad.dtype is t.dtype
+        assert bool(((t.grad.double() - dx).abs() <= tol + (V * dx.abs() * 1.01 if t.dtype is torch.bfloat16 else 0)).all())
+
+
+def test_a_frozen_input_does_not_widen_the_gradient():
+    x, res, w = rand(4, 64, seed=1), rand(4, 64, seed=2, dtype=torch.bfloat16).requires_grad_(), rand(64, seed=3)
+    y, h = ste.add_rms_norm(x, w, res)
+    torch.autograd.backward([y, h], [rand(4, 64, seed=4), rand(4, 64, seed=5, dtype=torch.bfloat16)])
+    assert res.grad.dtype is torch.bfloat16 and x.grad is None
