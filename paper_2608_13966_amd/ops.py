@@ -7,10 +7,11 @@ the work runs in the HIP kernels behind the C entry points, there is no CPU path
 and every call is asynchronous on ``stream`` (a ``hipStream_t`` as an int, as a
 torch stream's ``cuda_stream``; default: torch's current stream on the tensors'
 device).  What a call allocates belongs to that stream, as if it were torch's
-current one.  Tensors are 2-D with unit stride in the last dimension; rows may
-have any stride.  Each function returns a dict of tensors; a dict it returned may be
-passed as ``out`` to a later call of the same sizes and arguments, whose results
-then overwrite it and which allocates nothing.
+current one.  Matrices have unit stride in the last dimension and rows of any
+stride that keeps them apart; the teacher's lists are contiguous.  Each function
+returns a dict of tensors; a dict it returned may be passed as ``out`` to a later
+call of the same sizes and arguments, whose results then overwrite it and which
+allocates nothing.
 
 The functions named ``quasar_*`` (``EXPORTS``) mirror the C entry points.
 ``ste`` has the autograd forms (``add_rms_norm``, ``distill_topk_loss``).

@@ -155,7 +155,7 @@ def add_rms_norm(x, weight, residual=None, *, eps=1e-6):
 class _DistillTopK(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, index, teacher, temperature, row_weight):
-        flat, index, teacher = _rows(logits), _rows(index), _rows(teacher)
+        flat, index, teacher = _rows(logits), _rows(index).contiguous(), _rows(teacher).contiguous()
         row_weight = None if row_weight is None else row_weight.reshape(-1).contiguous()
         o = ops.distill_topk(flat, index, teacher, temperature=temperature, row_weight=row_weight)
         ctx.save_for_backward(flat, index, teacher, o["lse"], row_weight)

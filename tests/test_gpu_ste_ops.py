@@ -191,3 +191,17 @@ def test_a_frozen_input_does_not_widen_the_gradient():
     y, h = ste.add_rms_norm(x, w, res)
     torch.autograd.backward([y, h], [rand(4, 64, seed=4), rand(4, 64, seed=5, dtype=torch.bfloat16)])
     assert res.grad.dtype is torch.bfloat16 and x.grad is None
+
+
+def test_distill_takes_lists_cut_from_longer_ones():
+    z = rand(2, 6, 500, seed=1)
+    values, index = torch.topk(rand(2, 6, 500, seed=2), 40, dim=-1)
+    runs = []
+    for i, t in ((index[..., :16], values[..., :16]), (index[..., :16].contiguous(), values[..., :16].contiguous()),
+                 (index.transpose(0, 1)[..., :16].contiguous().transpose(0, 1), values[..., :16])):
+        a = z.clone().requires_grad_()
+        loss = ste.distill_topk_loss(a, i, t, row_weight=torch.ones(12, 2, device="cuda")[:, 0].reshape(2, 6))
+        loss.sum().backward()
+        runs.append((loss.detach(), a.grad))
+    for loss, grad in runs[1:]:
+        assert torch.equal(loss, runs[0][0]) and torch.equal(grad, runs[0][1])
