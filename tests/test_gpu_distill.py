@@ -417,3 +417,16 @@ def test_student_logits_at_plus_infinity(t, v, dtype):
         assert x[3].isnan().all()
     rest = slice(4, t)
     check(z[rest], idx[rest], val[rest], {k: o[k][rest] for k in ("loss", "lse", "grad")}, 1.5, None, 0.25)
+
+
+@pytest.mark.parametrize("t,v", [(3, 140001), (40, 60000)])
+def test_loss_workspace_is_reused(t, v):
+    g = torch.Generator(device=DEV).manual_seed(24)
+    z = torch.randn(t, v, device=DEV, generator=g)
+    values, idx = torch.topk(z + torch.randn(t, v, device=DEV, generator=g), 16, dim=1)
+    want = {k: a.clone() for k, a in O.distill_topk_grad(z, idx, values).items()}
+    o = O.distill_topk_grad(z, idx, values)
+    space = o["workspace"].fill_(255)
+    a = O.distill_topk_grad(z, idx, values, out=o)
+    assert a["workspace"].data_ptr() == space.data_ptr()
+    assert all(torch.equal(a[k], want[k]) for k in ("loss", "lse", "grad"))

@@ -375,3 +375,28 @@ def test_silu_to_the_last_bits(m):
     v = bias[6:].double()
     want = v / (1 + (-v).exp())
     assert ((y[:, 6:].double() - want).abs() <= 8 * U * want.abs()).all(), float(((y[:, 6:].double() / want - 1).abs() / U).max())
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 40, 8192), (20, 200, 16384), (140, 200, 4096), (500, 130, 9088), (1500, 3000, 8192)])
+@pytest.mark.parametrize("rt,yt", [("bf16", "bf16"), ("fp32", "fp32"), ("fp32", "bf16")])
+def test_residual_in_place_through_shared_columns(m, n, k, rt, yt):
+    """Where workgroups share the columns their sums meet in the workspace, and the residual is read when they are
+    joined: in y's place where it has its type.  What the workspace held before does not matter."""
+    dt = {"bf16": torch.bfloat16, "fp32": torch.float32}
+    w, r = layer(n, k, "int", 4, 64, seed=21)
+    x, _ = acts(m, k, 22)
+    g = torch.Generator(device=DEV).manual_seed(23)
+    res, bias = torch.randn(m, n, device=DEV, generator=g).to(dt[rt]), torch.randn(n, device=DEV, generator=g)
+    want = O.linear_codes(x, w, residual=res, bias=bias, act="gelu", y_dtype=yt)
+    check(want["y"], x, r, bias=bias, res=res, act="gelu")
+    space = want["workspace"]
+    assert space is not None
+    space.fill_(255)  # NaN
+    y = res.clone() if rt == yt else torch.full_like(want["y"], float("nan"))
+    o = O.linear_codes(x, w, residual=y if rt == yt else res, bias=bias, act="gelu", y_dtype=yt,
+                       out={"y": y, "workspace": space})
+    assert o["y"] is y and o["workspace"].data_ptr() == space.data_ptr()
+    assert torch.equal(y, want["y"])
+    small = torch.empty(space.numel() - 1, device=DEV, dtype=torch.uint8)  # too small: a new one is taken
+    o = O.linear_codes(x, w, residual=res, bias=bias, act="gelu", y_dtype=yt, out={"y": y, "workspace": small})
+    assert o["workspace"].numel() >= space.numel() and torch.equal(y, want["y"])
