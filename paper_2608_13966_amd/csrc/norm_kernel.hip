@@ -19,6 +19,18 @@ namespace {
 
 constexpr int kNormThreads = 256;
 
+// x / d rounded to nearest, inv = 1 / d rounded to nearest: the product's error is
+// taken off twice (the remainders are exact), the first time to within one place,
+// from where the second gives the rounded quotient (Markstein).  x inv alone puts
+// a value at the edge between two bytes on the wrong one.  16384 x 4096 bf16, q alone
+// and all in the last-level cache: 36 us, with the compiler's division for any divisor
+// 42, with x inv 35; 524288 x 128: 174, 212, 151; with y and from memory no difference.
+__device__ __forceinline__ float quotient(float x, float d, float inv) {
+  float q = x * inv;
+  q = __builtin_fmaf(__builtin_fmaf(-q, d, x), inv, q);
+  return __builtin_fmaf(__builtin_fmaf(-q, d, x), inv, q);
+}
+
 // TPR threads work on one row (64: a wavefront, without a barrier; more: a
 // workgroup), NV pieces of eight elements each.
 template <int XT, int RT, int TPR, int NV>
@@ -90,12 +102,18 @@ __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_
   if (!(ss < INFINITY)) scale = __builtin_nanf("");
   if (t == 0) a.scale[row] = scale;
   const int64_t eq = row * a.q_stride;
+  const float inv = 1.0f / scale;
+  const bool plain = !(scale >= 0x1p-80f && scale <= 0x1p100f);  // the remainders may not be exact, or nothing finite
 #pragma unroll
   for (int v = 0; v < NV; v++) {
     const int c = (v * TPR + t) * 8, n = cols - c;
     float s[8];
 #pragma unroll
-    for (int i = 0; i < 8; i++) s[i] = h[v][i] / scale;  // not y (1 / scale): that takes the neighbouring byte at an edge
+    for (int i = 0; i < 8; i++) s[i] = quotient(h[v][i], scale, inv);
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) s[i] = h[v][i] / scale;
+    }
     const uint2 b = pack_e4m3x8(s);
     uint8_t* p = a.q + eq + c;
     if (n >= 8) {

@@ -312,3 +312,25 @@ def test_more_rows_than_a_grid_takes():
         for k in ("h", "y", "q", "scale", "rstd"):
             assert torch.equal(o[k][a:b].view(torch.uint8), part[k].view(torch.uint8)), k
     check_forward(x[-40:], w, res[-40:], {k: o[k][-40:] for k in ("h", "y", "q", "scale", "rstd")})
+
+
+@pytest.mark.parametrize("size", [2.0 ** -100, 2.0 ** -85, 2.0 ** -40, 1.0, 2.0 ** 60, 2.0 ** 110])
+def test_eight_bit_rows_of_any_size(size):
+    """The quotients of the last test with y as large or small as fp32 has it (a weight of that size)."""
+    n = 300
+    x = gen((50, n), torch.float32, 33)
+    x[:, ::2] = ((2.0 + torch.arange(n // 2, device=DEV) % 14 + 0.5) / 16)
+    x[:, 1] = 7.0
+    w = torch.full((n,), size, device=DEV)
+    o = O.add_rms_norm(x, w, eps=EPS, quantize=True)
+    y = o["y"].cpu()
+    scale = y.abs().amax(1) / 448
+    assert torch.equal(o["scale"].cpu(), scale)
+    want = (y / scale[:, None]).to(torch.float8_e4m3fn)
+    assert torch.equal(o["q"].cpu().view(torch.uint8), want.view(torch.uint8))
+    # a weight that makes one column overflow: its scale is infinite, finite values are 0 of it
+    w[5] = float("inf")
+    o = O.add_rms_norm(x, w, eps=EPS, quantize=True)
+    assert (o["scale"] == float("inf")).all()
+    q = o["q"].float()
+    assert q[:, 5].isnan().all() and (q[:, :5] == 0).all() and (q[:, 6:] == 0).all()
