@@ -143,13 +143,17 @@ __device__ __forceinline__ void normalise(const RowList& o, int K, float weight,
   m = wave_reduce(m, MaxOp());
   const bool live = weight != 0.0f && (m != -INFINITY || __ballot(nan) != 0);
   if (live) {
-    for (int k = lane; k < K; k += 64) s += expf((o.e[k].p - m) / tau);
-    s = wave_reduce(s, SumOp());
-    const float ls = logf(s);
     for (int k = lane; k < K; k += 64) {
-      const float t = (o.e[k].p - m) / tau;
-      o.e[k].p = expf(t) / s;
-      o.logp[k] = t - ls;
+      const float t = (o.e[k].p - m) / tau, e = expf(t);
+      o.logp[k] = t;
+      o.e[k].p = e;
+      s += e;
+    }
+    s = wave_reduce(s, SumOp());
+    const float ls = logf(s), is = 1.0f / s;
+    for (int k = lane; k < K; k += 64) {
+      o.e[k].p *= is;
+      o.logp[k] -= ls;
     }
   }
   if (lane == 0) *o.some = live ? 1.0f : 0.0f;
