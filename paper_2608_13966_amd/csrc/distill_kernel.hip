@@ -131,7 +131,7 @@ struct Entry {
 };
 
 // From the entries' teacher logits in o.p to their probabilities and the logarithms of them.
-__device__ __forceinline__ void normalise(const RowList& o, int K, float weight, float tau) {
+__device__ __forceinline__ void normalise(const RowList& o, int K, float weight, Divisor tau) {
   const int lane = threadIdx.x & 63;
   wave_lds_fence();
   float m = -INFINITY, s = 0.0f;
@@ -144,13 +144,13 @@ __device__ __forceinline__ void normalise(const RowList& o, int K, float weight,
   const bool live = weight != 0.0f && (m != -INFINITY || __ballot(nan) != 0);
   if (live) {
     for (int k = lane; k < K; k += 64) {
-      const float t = (o.e[k].p - m) / tau, e = expf(t);
+      const float t = tau.of(o.e[k].p - m), e = exp_of(t);
       o.logp[k] = t;
       o.e[k].p = e;
       s += e;
     }
     s = wave_reduce(s, SumOp());
-    const float ls = logf(s), is = 1.0f / s;
+    const float ls = log_of(s), is = 1.0f / s;
     for (int k = lane; k < K; k += 64) {
       o.e[k].p *= is;
       o.logp[k] -= ls;
@@ -163,14 +163,13 @@ __device__ __forceinline__ void normalise(const RowList& o, int K, float weight,
 // summed: sum p log p and sum p log q are large against a small loss (300
 // rows of 1200 classes, 200 listed, tau 0.7, against the formula in 64 bits: off by
 // 3.3e-7, the difference of the two sums by 1.0e-6).
-__device__ __forceinline__ float loss_of(const RowList& o, int K, float weight, MaxSum r, float tau) {
+__device__ __forceinline__ float loss_of(const RowList& o, int K, float weight, float m, float log_sum, Divisor tau) {
   float s = 0.0f;
   const bool live = o.live();
-  const float log_sum = logf(r.s);
   if (live)
     for (int k = threadIdx.x & 63; k < K; k += 64) {
       const float p = o.e[k].p;
-      if (o.e[k].index >= 0 && !(p == 0.0f)) s += p * (o.logp[k] - ((o.e[k].z - r.m) / tau - log_sum));
+      if (o.e[k].index >= 0 && !(p == 0.0f)) s += p * (o.logp[k] - (tau.of(o.e[k].z - m) - log_sum));
     }
   s = wave_reduce(s, SumOp());
   return live ? weight * s : 0.0f;
@@ -249,7 +248,7 @@ __device__ __forceinline__ MaxSum group_join(MaxSum r, float c, MaxSum* s) {
   return r;
 }
 
-__device__ __forceinline__ float lse_of(MaxSum r, float tau) { return r.m / tau + logf(r.s); }
+__device__ __forceinline__ float lse_of(float m, float log_sum, Divisor tau) { return tau.of(m) + log_sum; }
 
 // Workgroup b works on part b % parts of row b / parts.
 // Partial maximum and sum of one part of a row, into part[b].
@@ -279,7 +278,8 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
   extern __shared__ float lds[];
   const int64_t row = blockIdx.x / (unsigned)parts, base = row * a.logits_stride, gbase = row * a.grad_stride;
   const int at = blockIdx.x % (unsigned)parts, e0 = at * Part<T, NV>::kClasses;
-  const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
+  const Divisor tau(a.temperature);
+  const float it = tau.hi, c = uniform_f32(kLog2e / a.temperature);
   const int V = (int)a.classes, K = a.listed;
   const RowList o(lds, K);
   const float weight = a.row_weight ? a.row_weight[row] : 1.0f;
@@ -295,13 +295,13 @@ __global__ __launch_bounds__(kThreads) void distill_row_kernel(quasar_distill a,
   if (what != 0) o.clear<kThreads>();
   MaxSum r{-INFINITY, 0.0f};  // of the row's parts: each wavefront joins them
   for (int i = threadIdx.x & 63; i < sums; i += 64) r = join(r, part[row * sums + i], c);
-  if (threadIdx.x < 64) normalise(o, K, weight, a.temperature);
+  if (threadIdx.x < 64) normalise(o, K, weight, tau);
   if (sums > 0) r = wave_join(r, c);
-  const float lse = sums > 0 ? lse_of(r, a.temperature) : a.lse[row];
+  const float lse = sums > 0 ? lse_of(r.m, log_of(r.s), tau) : a.lse[row];
   __syncthreads();
   const bool live = o.live();
   if (what != 1 && at == 0 && threadIdx.x < 64) {
-    const float loss = loss_of(o, K, weight, r, a.temperature);
+    const float loss = loss_of(o, K, weight, r.m, log_of(r.s), tau);
     if (threadIdx.x == 0) {
       a.loss[row] = loss;
       a.lse[row] = live ? lse : 0.0f;
@@ -349,7 +349,8 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
   __shared__ MaxSum sums[2][NT / 64];
   const int tid = threadIdx.x, V = (int)a.classes, K = a.listed;
   const auto list = [&](int turn) { return RowList(lds + turn * RowList::size(K), K); };  // of rows in turn
-  const float it = 1.0f / a.temperature, c = kLog2e / a.temperature;
+  const Divisor tau(a.temperature);
+  const float it = tau.hi, c = uniform_f32(kLog2e / a.temperature);
   Piece<T> pc[NV];
   // Pieces are whole: a row's buffer ends with its last one; the V % 8 classes past it are one a thread.  No load or
   // store stands behind a branch: the compiler would make the first use of any load wait for all of them.  A
@@ -414,14 +415,19 @@ __global__ __launch_bounds__(NT) void distill_resident_kernel(quasar_distill a) 
     }
     if (rest < V) r = take_one(r, last, c);
     if constexpr (!GRAD) load_last(next);
-    if (tid < 64) normalise(o, K, weight, a.temperature);
+    if (tid < 64) normalise(o, K, weight, tau);
     r = group_join<NT / 64>(r, c, sums[turn]);  // its barrier shows the list too
     const bool live = o.live();
     if (tid < 64) {
-      const float loss = loss_of(o, K, weight, r, a.temperature);
+      // of their own to the compiler: it began what follows ahead of the branch, in every wavefront, and spilled pieces
+      // for it (the loss of 4096 x 131072 took 227 us, so 195)
+      float rm = r.m, rs = r.s;
+      asm volatile("" : "+v"(rm), "+v"(rs));
+      const float log_sum = log_of(rs);
+      const float loss = loss_of(o, K, weight, rm, log_sum, tau);
       if (tid == 0) {
         a.loss[row] = loss;
-        a.lse[row] = live ? lse_of(r, a.temperature) : 0.0f;
+        a.lse[row] = live ? lse_of(rm, log_sum, tau) : 0.0f;
       }
     }
     put_list(n, next);

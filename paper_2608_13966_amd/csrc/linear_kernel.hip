@@ -254,14 +254,10 @@ __device__ __forceinline__ float normal_tail(float u) {
   return p * t * __builtin_amdgcn_exp2f(u * u * (-0.5f * kLog2e));
 }
 
-// exp(-|v|) does not overflow; its argument in units of log 2 has its rounding
-// and the constant's made good: within 8 x 2^-24 of the result (v times the hardware's
-// reciprocal and exponential alone: 62 x 2^-24 at v = -85).
+// exp(-|v|) does not overflow.  Within 8 x 2^-24 of the result (v times the
+// hardware's reciprocal and exponential alone: 62 x 2^-24 at v = -85).
 __device__ __forceinline__ float silu(float v) {
-  const float a = fminf(fabsf(v), 128.0f), t = -a * kLog2e;
-  const float rest = __builtin_fmaf(-a, kLog2e, -t) - a * kLog2eRest;
-  float e = __builtin_amdgcn_exp2f(t);
-  e = __builtin_fmaf(e, rest * kLn2, e);
+  const float e = exp_of(-fabsf(v));
   return (v >= 0.0f ? v : v * e) / (1.0f + e);
 }
 

@@ -225,5 +225,31 @@ __device__ __forceinline__ float group_reduce(float x, float* s, Op op) {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLog2eRest = (float)(1.44269504088896340736 - (double)kLog2e);
 constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLn2Rest = (float)(0.69314718055994530942 - (double)kLn2);
+
+// exp(x) and log(x) from the hardware's exponential and logarithm to base 2, the
+// rounding of the argument (the result) and of the constant made good: 2 to 4 x
+// 2^-24 relative.  x <= 0 or NaN; x >= 1, 0 or NaN.  (expf and logf hold registers
+// for arguments that do not occur here: with them a kernel full of pieces spilled.)
+__device__ __forceinline__ float exp_of(float x) {
+  const float t = x * kLog2e, rest = __builtin_fmaf(x, kLog2e, -t) + x * kLog2eRest;
+  const float e = __builtin_amdgcn_exp2f(t);
+  return t < -150.0f ? 0.0f : __builtin_fmaf(e, rest * kLn2, e);
+}
+__device__ __forceinline__ float log_of(float x) {
+  const float y = __builtin_amdgcn_logf(x), t = y * kLn2, rest = __builtin_fmaf(y, kLn2, -t) + y * kLn2Rest;
+  return x == 0.0f ? t : t + rest;
+}
+// Quotients by the same number in every lane: its reciprocal in two parts.
+struct Divisor {
+  float hi, lo;
+  __device__ __forceinline__ explicit Divisor(float d) {
+    hi = uniform_f32(1.0f / d);
+    lo = uniform_f32(__builtin_fmaf(-d, hi, 1.0f) * hi);
+  }
+  __device__ __forceinline__ float of(float x) const {
+    return fabsf(x) == INFINITY ? x : __builtin_fmaf(x, hi, x * lo);
+  }
+};
 
 }  // namespace quasar
