@@ -179,7 +179,7 @@ typedef struct {
 
 int quasar_linear_codes(const quasar_desc* desc, const quasar_linear* a, void* stream);
 int quasar_linear_codes_check(const quasar_desc* desc, const quasar_linear* a);
-/* Device scratch the call needs for this many tokens; 0 where it needs none, or for an invalid desc. */
+/* Device scratch the call needs for this many tokens, of either x_dtype; 0 where it needs none, or for an invalid desc. */
 size_t quasar_linear_codes_workspace_bytes(const quasar_desc* desc, int64_t tokens, int32_t x_dtype);
 
 #ifdef __cplusplus

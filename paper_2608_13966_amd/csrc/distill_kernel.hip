@@ -8,9 +8,10 @@
 // again: a row that fits one workgroup's registers stays there (resident
 // kernel), others, and rows too few to fill the CUs, go in parts twice.
 //
-// Bound by memory: bf16, 64 listed, loss and gradient of 4096 x 131072 466 us, 4.6
-// TB/s (a copy of 4 GiB: 4.8); the gradient alone of 4096 x 32000 99 us, 5.3 TB/s.
-// Few rows are latency: 48 x 50021 in fp32 4.2 + 7.2 us.
+// Bound by memory: bf16, 64 listed, loss and gradient of 4096 x 131072 469 us, 4.6
+// TB/s (a copy of 4 GiB: 4.8); the gradient alone of 4096 x 32000 100 us, 5.3 TB/s.
+// In parts the row is read twice: loss and gradient of 4096 x 151936 677 us (481 at
+// the copy's rate).  Few rows are latency: 48 x 50021 in fp32 4.1 + 7.4 us.
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -485,6 +486,15 @@ int parts_of(int64_t rows, int64_t classes) {
 template <int T>
 constexpr int kMostPieces = T == kElemBF16 ? 16 : 8;
 
+// Rows in registers (one launch, one read) where they fill the CUs or are short;
+// in parts where a few long ones would leave CUs idle.  Loss and gradient (the loss
+// alone), us, bf16 with 64 listed, this form against the parts: 48 x 4000 6.8 against
+// 7.4 (4.9, 6.5); 48 x 16384 8.2, 7.7 (6.3, 6.7); 16 x 32000 10.6, 7.1 (8.0, 6.4); 48 x
+// 50021 in fp32 15.1, 10.4 (8.2, 7.4); 4096 x 32000 121, 159 (59, 56); 4096 x 131072
+// 469, 590 (194, 189).  Between them the rule is not always the faster one: 180 x 50000
+// 12.9, 15.9 (7.8, 9.5) but in parts, and a row of more than 65536 classes (fp32: 32768)
+// has a CU to itself, so 257 of them take nearly as long as 512: 257 x 131072 51, 37
+// (29, 18), 512 x 131072 68, 68 (37, 27).
 bool resident(int64_t rows, int64_t classes, bool bf16) {
   const int64_t most = 1024 * 8 * (bf16 ? kMostPieces<kElemBF16> : kMostPieces<kElemF32>);
   return classes <= most && (rows >= kCUs || classes <= 16384);
@@ -492,12 +502,12 @@ bool resident(int64_t rows, int64_t classes, bool bf16) {
 
 // A row that one wavefront holds takes one where there are rows enough for them
 // (four a CU): no wavefront waits for another then.  Loss and gradient, us, against
-// 256 threads a row: 8192 x 4000 with 64 listed 34.3, 40.9; 8192 x 1200 20.5, 34.7;
+// 256 threads a row: 8192 x 4000 with 64 listed 32.9, 42.4; 8192 x 1200 20.8, 35.4;
 // but 300 x 4000 with 256 listed 13.0, 9.4.
 //
 // Wavefronts a CU, by what a thread holds (more than fit only queue): 8192 x 4000, 256
-// threads a row, 45.2 with 16, 42.1 with 20, 40.2 with 24, 43.3 with 32; one wavefront a
-// row 34.3 with 12, 34.8 with 16, 38.4 with 24.
+// threads a row, 46.6 with 16, 43.6 with 20, 42.4 with 24, 44.3 with 32; one wavefront a
+// row 37.0 with 8, 32.9 with 12, 36.1 with 16, 40.3 with 24.
 template <int T, bool GRAD>
 hipError_t launch_resident(const quasar_distill& a, hipStream_t stream) {
   const size_t lds = 2 * RowList::size(a.listed) * sizeof(float);

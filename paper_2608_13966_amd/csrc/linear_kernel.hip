@@ -408,10 +408,10 @@ struct Block16 {
 // through the wavefront's own part of LDS; the next step's loads are in flight
 // meanwhile.  (Two or four steps in flight, or 4 or 16 wavefronts, were up to
 // 25% slower at 4096 x 4096 to 14336 x 4096 and 1 to 32 tokens: registers and
-// LDS then hold fewer wavefronts.)  4096 x 4096, 4 bits, 1 token: 4.8 us, a
-// launch (2.9) and the codes at 4.4 TB/s; 14336 x 4096, 2 bits, 8 tokens of 8 bits: 11.6
-// us, of which the copy of the codes and parameters would be 4.3: bound by the
-// decoding (VALU and LDS) between loads.
+// LDS then hold fewer wavefronts.)  4096 x 4096, 4 bits, 1 token: 5.1 us, a
+// launch (2.9) and the codes at 4.3 TB/s; 14336 x 4096, 2 bits, 8 tokens of 8 bits: 11.7
+// us among others (one by one under a trace 11.6 to 13.4), of which the copy of the codes
+// and parameters would be 4.3: bound by the decoding (VALU and LDS) between loads.
 constexpr int kStripWaves = 8;
 template <int FMT, int BITS, int XT, int NX, int NB>
 __global__ __launch_bounds__(64 * kStripWaves) void strip_kernel(Weights w, quasar_linear a, int log_splits, float* part) {
@@ -885,7 +885,7 @@ __device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm
 //    half, "at most 8 outstanding" then, either phase.
 // Past the last step the loads repeat it, so that the counts hold.  (Four phases
 // of 16 instructions, with twice the barriers, were 5% slower.)  At 8192 tokens,
-// 14336 x 4096: 640 to 700 us as the clock goes, 1.4 to 1.5 PFLOP/s, matrix units
+// 14336 x 4096: 665 to 740 us as the clock goes, 1.3 to 1.45 PFLOP/s, matrix units
 // busy 81% of the time.
 __global__ __launch_bounds__(512, 2) void tile_kernel(quasar_linear a, const uint16_t* x, int64_t x_stride,
                                                       const uint16_t* r, int64_t rows, int kp, int tiles_m, int tiles_n,
@@ -1056,7 +1056,8 @@ void choose_fused(Choice& c, int64_t tokens, int64_t rows, int steps) {
 //    14336: 1 token 6.8 against 8.8, 32 tokens 9.7 against 16; with four steps the join costs more: 6.0 against 4.6);
 //  - the tile kernel where its 256 x 256 tiles come near to filling the CUs and there are tokens enough to pay for
 //    writing r out (6000 tokens at 2000 x 4096, 192 tiles: 87 against 146; 768 at 14336 x 4096: 98 against 135; 2500 at
-//    4096 x 2048, 160 tiles: 50 against 68, but 4000 at 2048 x 2048, 128 tiles, 58 against 44), or where the columns are
+//    4096 x 2048, 160 tiles: 57 against 68, but 4000 at 2048 x 2048, 128 tiles, 58 against 46; at 128 tiles of 4096 columns
+//    even: 2000 at 4096 x 4096 81 against 84, 2048 at 5000 x 4096 88 against 84), or where the columns are
 //    many enough to be split (1500 at 4096 x 14336, 96 tiles: 186 against 235, but 1024 at 2048 x 16384, 32 tiles, 105
 //    against 91);
 //  - the fused kernel between them.

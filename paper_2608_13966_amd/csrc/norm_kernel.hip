@@ -5,8 +5,10 @@
 // registers as its storage form widened to fp32, eight consecutive elements
 // (one 16-byte load in bf16) per lane and step, so the mean of squares, the
 // row's largest |y| and the outputs all come from one read.  At 16384 x 4096 in
-// bf16: forward (residual, y and q) 110 us, 5.5 TB/s; backward 102 + 6.6 us, 4.9
-// TB/s (a copy of 1 GiB: 5.2).  One row takes 3.1 us, little more than a launch.
+// bf16: forward (residual, y and q) 110 us, 5.5 TB/s; backward 101 + 6.7 us, 4.9
+// TB/s (a copy of 1 GiB: 5.2).  One row takes 3.2 us, little more than a launch.
+// Narrow rows leave lanes of their wavefront idle, 48 of 64 at 128 columns: 524288 x
+// 128, y alone 159 us (the bytes at the copy's rate: 52), backward 227 (78).
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -178,7 +180,7 @@ hipError_t launch_norm_types(const quasar_norm& a, hipStream_t stream) {
 // in every row, so its share of dweight stays in registers.  The shares of a
 // workgroup's row groups meet in LDS, those of the workgroups in `parts`
 // (parts_kernel sums them), in a fixed order.  That sum is what a launch more
-// costs: 777 x 1537 in fp32 takes 7.0 + 3.3 us.
+// costs: 777 x 1537 in fp32 takes 6.9 + 3.4 us.
 template <int GT, int HT, int TPR, int NV>
 __global__ __launch_bounds__(TPR < kNormThreads ? kNormThreads : TPR) void norm_backward_kernel(quasar_norm_backward a,
                                                                                                float* parts) {
