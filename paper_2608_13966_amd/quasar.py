@@ -191,6 +191,10 @@ def _torch_stream(handle, device):
     return torch.cuda.ExternalStream(h, device=device) if h else torch.cuda.default_stream(device)
 
 
+def _off_gpu(t):
+    return ValueError(f"tensors on {t.device} with a stream: they have to be on its GPU")
+
+
 def _allocating(stream, t):
     """The context of what a call allocates: a stream that the caller names is
     torch's current one in it, so the memory belongs to that stream (freed, it
@@ -198,6 +202,8 @@ def _allocating(stream, t):
     fills it comes before the kernels."""
     if stream is None:
         return contextlib.nullcontext()
+    if not t.is_cuda:
+        raise _off_gpu(t)
     import torch
     return torch.cuda.stream(_torch_stream(stream, t.device))
 
@@ -411,6 +417,8 @@ def reconstruct(W, v, g=None, *, fmt="int", bits=4, group=128, clips=(1.0,), bet
             out = alloc_outputs(d, W, want_r=want_r, want_diag=want_diag, has_amax=tensor_amax is not None)
     if stream is None:
         stream = _stream(W)
+    elif not W.is_cuda:
+        raise _off_gpu(W)
     s = quasar_reconstruct(d, W, v, g, out["codes"], out["scales"], out["zeros"], out["r"], out["best_clip"],
                            out["err"], out["tensor_scale"], tensor_amax, out["workspace"], out["workspace_bytes"],
                            stream)
@@ -448,6 +456,8 @@ def adamw_reconstruct(W, m, v, g, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, weigh
                                if (want_amax_out and fmt == "nvfp4") else None)
     if stream is None:
         stream = _stream(W)
+    elif not W.is_cuda:
+        raise _off_gpu(W)
     opt = AdamW(lr, beta1, beta2, eps, weight_decay, int(step))
     s = quasar_adamw_reconstruct(d, opt, W, m, v, g, out["codes"], out["scales"], out["zeros"], out.get("r"), rd,
                                  out["best_clip"], out["err"], out["tensor_scale"], tensor_amax,
@@ -495,6 +505,8 @@ def adamw_reconstruct_batch(items, *, lr, beta1=0.9, beta2=0.999, eps=1e-8, weig
                                 _p(o["tensor_scale"]), _p(amax), _p(o["amax_out"])))
     if stream is None:
         stream = _stream(W0)
+    elif not W0.is_cuda:
+        raise _off_gpu(W0)
     opt = AdamW(lr, beta1, beta2, eps, weight_decay, int(step))
     s = quasar_adamw_reconstruct_batch(d, opt, mats, rd, stream)
     if s != OK:
@@ -515,6 +527,8 @@ def absmax_batch(Ws, *, stream=None):
     mats = [Matrix(W.shape[0], W.shape[1], _p(W)) for W in Ws]
     if stream is None:
         stream = _stream(W0)
+    elif not W0.is_cuda:
+        raise _off_gpu(W0)
     s = quasar_absmax_batch(d, mats, outs, stream)
     if s != OK:
         raise QuasarError(s, "quasar_absmax_batch")
@@ -558,6 +572,8 @@ def reconstruct_batch(items, *, fmt="int", bits=4, group=128, clips=(1.0,), beta
         mats.append(matrix(W, v, g, o, amax))
     if stream is None:
         stream = _stream(W0)
+    elif not W0.is_cuda:
+        raise _off_gpu(W0)
     s = quasar_reconstruct_batch(d, mats, stream)
     if s != OK:
         raise QuasarError(s, "quasar_reconstruct_batch")

@@ -461,3 +461,22 @@ def test_tensors_off_the_gpu_are_refused_as_torch_does():
     with pytest.raises(want.type) as got:
         Q.reconstruct(W, torch.zeros_like(W))
     assert str(got.value) == str(want.value)
+
+
+def test_wrappers_refuse_tensors_off_the_gpu_with_a_stream():
+    """Host pointers never go to a kernel, also where the caller names the stream (without a GPU nothing would run)."""
+    torch = pytest.importorskip("torch")
+    if torch.cuda.is_available():
+        pytest.skip("the check of the refusal runs where no kernel can")
+    W = torch.zeros(4, 128, dtype=torch.bfloat16)
+    v, g = torch.zeros(4, 128), torch.zeros(4, 128)
+    f = W.float()
+    d = Q.Descriptor(4, 128)
+    out = Q.alloc_outputs(d, W)
+    for call in (lambda: Q.reconstruct(W, v, stream=1), lambda: Q.reconstruct(W, v, out=out, stream=1),
+                 lambda: Q.adamw_reconstruct(f, v, v, g, lr=1e-3, stream=1),
+                 lambda: Q.adamw_reconstruct(f, v, v, g, lr=1e-3, out=out, stream=1),
+                 lambda: Q.adamw_reconstruct_batch([(f, v, v, g)], lr=1e-3, stream=1),
+                 lambda: Q.reconstruct_batch([(W, v, None)], stream=1), lambda: Q.absmax_batch([W], stream=1)):
+        with pytest.raises(ValueError, match="cpu"):
+            call()
