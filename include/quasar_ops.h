@@ -4,7 +4,9 @@
  * trains the quantised model (the paper's distillation loss is the forward KL
  * divergence to the teacher, Sec. 6.1), the RMS norm with the residual's
  * addition (and an 8-bit output) between its layers, and the layers' product
- * from the packed codes that quasar_reconstruct emits.
+ * from the packed codes that quasar_reconstruct emits; and of what a training
+ * step takes next to them: the embedding, the layer norm, and activations kept
+ * in 8 bits for the backward pass.
  *
  * Conventions: those of quasar.h (device memory of the caller's, nothing
  * allocated or kept, asynchronous on `stream`, reentrant, argument errors
@@ -181,6 +183,173 @@ int quasar_linear_codes(const quasar_desc* desc, const quasar_linear* a, void* s
 int quasar_linear_codes_check(const quasar_desc* desc, const quasar_linear* a);
 /* Device scratch the call needs for this many tokens, of either x_dtype; 0 where it needs none, or for an invalid desc. */
 size_t quasar_linear_codes_workspace_bytes(const quasar_desc* desc, int64_t tokens, int32_t x_dtype);
+
+/* ---- layer norm with the residual's addition ----------------------------------
+ *
+ *   h = x + residual                       (fp32)
+ *   mean = sum(h) / cols, rstd = 1 / sqrt(sum((h - mean)^2) / cols + eps)
+ *   y = (h - mean) * rstd * weight + bias
+ *
+ * and, as asked for, h, y and y in 8 bits (q and scale) as quasar_add_rms_norm
+ * gives them; a row whose sum of squares is not finite has scale = NaN and
+ * every q NaN.  The deviations' squares are summed after the mean is known.
+ * cols is at most QUASAR_NORM_MAX_COLS.
+ */
+typedef struct {
+  int64_t rows, cols;        /* 0 <= rows < 2^31, 1 <= cols <= QUASAR_NORM_MAX_COLS */
+  const void* x;             /* [rows, cols] */
+  const void* residual;      /* [rows, cols], or NULL: h = x */
+  const void* weight;        /* [cols] */
+  const void* bias;          /* [cols], or NULL: 0 */
+  void* h;                   /* as quasar_norm's: may be `residual` itself, or x where the types agree */
+  void* y;                   /* [rows, cols], or NULL */
+  uint8_t* q;                /* [rows, cols] E4M3, or NULL */
+  float* scale;              /* [rows]; required with q, NULL without */
+  float* mean;               /* [rows], or NULL */
+  float* rstd;               /* [rows], or NULL */
+  int64_t x_stride, residual_stride, h_stride, y_stride, q_stride;
+  int32_t x_dtype, residual_dtype, weight_dtype, bias_dtype, y_dtype;  /* QUASAR_F32 or QUASAR_BF16 each */
+  float eps;                 /* finite, >= 0 */
+} quasar_layer_norm;
+
+int quasar_add_layer_norm(const quasar_layer_norm* a, void* stream);
+int quasar_add_layer_norm_check(const quasar_layer_norm* a);
+
+/*
+ * Its gradients, with n = (h - mean) * rstd and u = dy * weight:
+ *   dx = rstd (u - mean(u) - n mean(u n)) + dh   (the gradient of x and of residual)
+ *   dweight = sum over rows of dy n, dbias = sum over rows of dy   (fp32)
+ * q is taken straight through.  h, mean and rstd are what the forward pass gave
+ * (without a residual h is x).  The sums over rows have a fixed order.
+ */
+typedef struct {
+  int64_t rows, cols;
+  const void* dy;            /* [rows, cols] */
+  const void* h;             /* [rows, cols] */
+  const void* weight;        /* [cols] */
+  const float* mean;         /* [rows] */
+  const float* rstd;         /* [rows] */
+  const void* dh;            /* [rows, cols] in dx_dtype, the stream's own gradient, or NULL */
+  void* dx;                  /* [rows, cols]; may be dh itself with the same stride, or dy or h likewise where the
+                                types agree */
+  float* dweight;            /* [cols] (with no rows: not written), or NULL */
+  float* dbias;              /* likewise */
+  void* workspace;           /* quasar_add_layer_norm_backward_workspace_bytes(), where dweight or dbias is asked for */
+  size_t workspace_bytes;
+  int64_t dy_stride, h_stride, dh_stride, dx_stride;
+  int32_t dy_dtype, h_dtype, weight_dtype, dx_dtype;
+} quasar_layer_norm_backward;
+
+int quasar_add_layer_norm_backward(const quasar_layer_norm_backward* a, void* stream);
+int quasar_add_layer_norm_backward_check(const quasar_layer_norm_backward* a);
+size_t quasar_add_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols);
+
+/* ---- embedding ------------------------------------------------------------------
+ *
+ *   y[t] = scale * weight[index[t]]
+ *   dweight[v] = scale * sum over t with index[t] = v of dy[t]
+ *
+ * A token whose index is outside [0, rows) is none (-1 for padding): its y is 0
+ * and its dy, whatever it holds, reaches nothing.  The gradient writes every row
+ * of dweight, 0 where no token has it; a row's sum is in fp32, in an order that
+ * the tokens alone determine, rounded once.
+ */
+typedef struct {
+  int64_t rows, cols;        /* the table's: 1 <= rows < 2^31, 1 <= cols <= 2^20 */
+  int64_t tokens;            /* 0 <= tokens <= 2^28 */
+  const void* index;         /* [tokens], contiguous */
+  const void* weight;        /* [rows, cols] */
+  void* y;                   /* [tokens, cols] */
+  int64_t weight_stride, y_stride;
+  int32_t index_bits;        /* 32 or 64 */
+  int32_t weight_dtype, y_dtype;  /* QUASAR_F32 or QUASAR_BF16 each */
+  float scale;               /* finite */
+} quasar_embedding;
+
+int quasar_embed(const quasar_embedding* a, void* stream);
+int quasar_embed_check(const quasar_embedding* a);
+
+typedef struct {
+  int64_t rows, cols, tokens;
+  const void* index;         /* [tokens], contiguous */
+  const void* dy;            /* [tokens, cols] */
+  void* dweight;             /* [rows, cols] */
+  void* workspace;           /* quasar_embed_backward_workspace_bytes() */
+  size_t workspace_bytes;
+  int64_t dy_stride, dweight_stride;
+  int32_t index_bits;
+  int32_t dy_dtype, dweight_dtype;
+  float scale;
+} quasar_embedding_backward;
+
+int quasar_embed_backward(const quasar_embedding_backward* a, void* stream);
+int quasar_embed_backward_check(const quasar_embedding_backward* a);
+size_t quasar_embed_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t tokens);
+
+/* ---- activations kept in 8 bits ---------------------------------------------------
+ *
+ * A row is kept in stretches of 128 columns (the last one shorter), each with
+ * the smallest exponent e in [-120, 120] for which its largest finite |x| is at
+ * most 448 * 2^e:
+ *   q = E4M3(x * 2^-e), exponent = e + 127 in a byte
+ * so that q * 2^e is x to four significant bits, within 2^-10 * 2^e where x is
+ * smaller than 2^-6 * 2^e.  A stretch of zeros has e = -120; with e = 120 |q| is
+ * at most 240, so that q * 2^e is finite.  NaN and infinity are kept as NaN and
+ * leave their neighbours' exponent alone.
+ *
+ * The same pass makes y = act(x), from x itself.
+ */
+typedef struct {
+  int64_t rows, cols;        /* 0 <= rows < 2^31, 1 <= cols <= 2^24 */
+  const void* x;             /* [rows, cols] */
+  void* y;                   /* [rows, cols] = act(x), or NULL; may be x itself with the same type and stride */
+  uint8_t* q;                /* [rows, cols] E4M3 */
+  uint8_t* exponent;         /* [rows, ceil(cols / 128)] */
+  int64_t x_stride, y_stride, q_stride, exponent_stride;
+  int32_t x_dtype, y_dtype;  /* QUASAR_F32 or QUASAR_BF16 each */
+  int32_t act;               /* quasar_activation */
+} quasar_checkpoint;
+
+int quasar_checkpoint_rows(const quasar_checkpoint* a, void* stream);
+int quasar_checkpoint_rows_check(const quasar_checkpoint* a);
+
+/* dx = dy * act'(k), k = q * 2^e the activations that were kept; relu'(0) = 0 */
+typedef struct {
+  int64_t rows, cols;
+  const void* dy;            /* [rows, cols] */
+  const uint8_t* q;          /* [rows, cols] E4M3 */
+  const uint8_t* exponent;   /* [rows, ceil(cols / 128)] */
+  void* dx;                  /* [rows, cols]; may be dy itself with the same type and stride */
+  int64_t dy_stride, q_stride, exponent_stride, dx_stride;
+  int32_t dy_dtype, dx_dtype;
+  int32_t act;               /* quasar_activation, not QUASAR_ACT_NONE */
+} quasar_checkpoint_grad;
+
+int quasar_checkpoint_backward(const quasar_checkpoint_grad* a, void* stream);
+int quasar_checkpoint_backward_check(const quasar_checkpoint_grad* a);
+
+/*
+ * The weight gradient of a linear layer whose input was kept:
+ *   dweight[n, k] = sum over t of dy[t, n] * q[t, k] * 2^e
+ * Products are exact in fp32 (dy in fp32 is taken in three parts of bf16, of
+ * which values under 2^-126 in size are lost), sums are in fp32 in a fixed order.
+ */
+typedef struct {
+  int64_t tokens;            /* 0 <= tokens <= 2^28: none gives 0 */
+  int64_t rows, cols;        /* of the weight (out, in): 1 <= rows, cols <= 2^22 */
+  const void* dy;            /* [tokens, rows] */
+  const uint8_t* q;          /* [tokens, cols] E4M3 */
+  const uint8_t* exponent;   /* [tokens, ceil(cols / 128)] */
+  void* dweight;             /* [rows, cols] */
+  void* workspace;           /* quasar_linear_weight_grad_workspace_bytes() */
+  size_t workspace_bytes;
+  int64_t dy_stride, q_stride, exponent_stride, dweight_stride;
+  int32_t dy_dtype, dweight_dtype;  /* QUASAR_F32 or QUASAR_BF16 each */
+} quasar_weight_grad;
+
+int quasar_linear_weight_grad(const quasar_weight_grad* a, void* stream);
+int quasar_linear_weight_grad_check(const quasar_weight_grad* a);
+size_t quasar_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols, int32_t dy_dtype);
 
 #ifdef __cplusplus
 }

@@ -20,7 +20,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libquasar.so")
 SOURCES = ["api.hip", "int_kernel.hip", "int_cells_kernel.hip", "nvfp4_kernel.hip", "rubin_kernel.hip",
-           "ops_api.hip", "norm_kernel.hip", "distill_kernel.hip", "linear_kernel.hip"]
+           "ops_api.hip", "norm_kernel.hip", "distill_kernel.hip", "linear_kernel.hip", "layer_norm_kernel.hip",
+           "embed_kernel.hip", "checkpoint_kernel.hip", "weight_grad_kernel.hip"]
 ARCH = "gfx950"
 BINDING = os.path.join(HERE, "_ops_binding.so")  # the Python calls of ops.py, in C++
 

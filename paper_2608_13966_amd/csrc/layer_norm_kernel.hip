@@ -1,0 +1,401 @@
+// layer_norm_kernel.hip -- the layer norm with the residual's addition and its
+// gradients (quasar_ops.h).
+//
+// Both directions are bound by memory.  A row is read once and kept in registers
+// widened to fp32, eight consecutive elements (one 16-byte load in bf16) per lane
+// and step: the mean, then the squares of the deviations from it (two sums, since
+// sum(h^2) - cols mean^2 cancels where the mean is large), the row's largest |y| and
+// the outputs all come from one read.
+#include "ops_common.h"
+#include "ops_internal.h"
+
+namespace quasar {
+
+// floats from one part of dweight or dbias to the next
+__host__ __device__ constexpr int ln_pitch(int cols) { return (cols + 3) & ~3; }
+
+namespace {
+
+// Threads of a workgroup, and the rows that it works on at once, where TPR
+// threads (16 lanes, a wavefront, or a workgroup) work on one row.
+template <int TPR>
+struct Shape {
+  static constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR;
+  static __device__ __forceinline__ int lane() { return threadIdx.x & (TPR - 1); }
+  static __device__ __forceinline__ int row() { return TPR == 64 ? wave_index() : TPR > 64 ? 0 : threadIdx.x / TPR; }
+};
+
+// Over the TPR threads of a row; s: LDS of its own for each call where they are
+// several wavefronts.
+template <int TPR, typename Op>
+__device__ __forceinline__ float row_reduce(float x, float* s, Op op) {
+  if constexpr (TPR == 16) {
+    x = op(x, dpp_f32<kDppXor1>(x));
+    x = op(x, dpp_f32<kDppXor2>(x));
+    x = op(x, dpp_f32<kDppHalfMirror>(x));
+    return op(x, dpp_f32<kDppMirror>(x));
+  } else {
+    return group_reduce<TPR / 64>(x, s, op);
+  }
+}
+
+template <int XT, int RT, int TPR, int NV>
+__global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_kernel(quasar_layer_norm a) {
+  constexpr int kWaves = TPR < 64 ? 1 : TPR / 64;
+  __shared__ float red[3][kWaves];
+  const int t = Shape<TPR>::lane(), cols = (int)a.cols;
+  const int64_t row = (int64_t)blockIdx.x * Shape<TPR>::kRows + Shape<TPR>::row();
+  if (row >= a.rows) return;  // whole rows of 16 lanes; no barrier follows where there are several rows
+  float h[NV][8];
+  Piece<XT> px[NV];
+  Piece<RT == kElemNone ? XT : RT> pr[NV];
+  const int64_t ex = row * a.x_stride, er = row * a.residual_stride;
+#pragma unroll
+  for (int v = 0; v < NV; v++) {
+    const int c = (v * TPR + t) * 8;
+    px[v].load(a.x, ex + c, cols - c);
+    if constexpr (RT != kElemNone) pr[v].load(a.residual, er + c, cols - c);
+  }
+  float sum = 0.0f;
+#pragma unroll
+  for (int v = 0; v < NV; v++)
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      h[v][i] = px[v].get(i);
+      if constexpr (RT != kElemNone) h[v][i] += pr[v].get(i);
+      sum += h[v][i];
+    }
+  const float mean = row_reduce<TPR>(sum, red[0], SumOp()) / (float)cols;
+  if constexpr (RT != kElemNone) {
+    if (a.h) {
+      const int64_t eh = row * a.h_stride;
+#pragma unroll
+      for (int v = 0; v < NV; v++) {
+        const int c = (v * TPR + t) * 8;
+        store_piece<RT == kElemBF16>(a.h, eh + c, h[v], cols - c);
+      }
+    }
+  }
+  float ss = 0.0f;
+#pragma unroll
+  for (int v = 0; v < NV; v++) {
+    const int left = cols - (v * TPR + t) * 8;
+#pragma unroll
+    for (int i = 0; i < 8; i++) h[v][i] -= mean;
+    if (left < 8) {
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (i >= left) h[v][i] = 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; i++) ss = __builtin_fmaf(h[v][i], h[v][i], ss);
+  }
+  ss = row_reduce<TPR>(ss, red[1], SumOp());
+  const float rstd = 1.0f / __builtin_sqrtf(ss / (float)cols + a.eps);
+  if (t == 0) {
+    if (a.mean) a.mean[row] = mean;
+    if (a.rstd) a.rstd[row] = rstd;
+  }
+  float top = 0.0f;
+#pragma unroll
+  for (int v = 0; v < NV; v++) {
+    const int c = (v * TPR + t) * 8;
+    float w[8], b[8] = {};
+    load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w);
+    if (a.bias) load_floats(a.bias, c, cols - c, a.bias_dtype == QUASAR_BF16, b);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      h[v][i] = __builtin_fmaf(h[v][i] * rstd, w[i], b[i]);
+      top = fmaxf(top, fabsf(h[v][i]));
+    }
+  }
+  if (a.y) {
+    const int64_t ey = row * a.y_stride;
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      const int c = (v * TPR + t) * 8;
+      store_piece(a.y, ey + c, h[v], cols - c, a.y_dtype == QUASAR_BF16);
+    }
+  }
+  if (!a.q) return;
+  top = row_reduce<TPR>(top, red[2], MaxOp());
+  // NaN for a row that is not finite
+  float scale = fmaxf(top / 448.0f, 0x1p-120f);
+  if (!(ss < INFINITY)) scale = __builtin_nanf("");
+  if (t == 0) a.scale[row] = scale;
+  const int64_t eq = row * a.q_stride;
+  const float inv = 1.0f / scale;
+  const bool plain = !(scale >= 0x1p-80f && scale <= 0x1p100f);  // the remainders may not be exact, or nothing finite
+#pragma unroll
+  for (int v = 0; v < NV; v++) {
+    const int c = (v * TPR + t) * 8;
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; i++) s[i] = quotient(h[v][i], scale, inv);
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) s[i] = h[v][i] / scale;
+    }
+    store_bytes(a.q + eq + c, pack_e4m3x8(s), cols - c);
+  }
+}
+
+// f(TPR, NV) for the widest-fitting shape.
+template <typename F>
+hipError_t with_shape(int64_t cols, F f) {
+  using std::integral_constant;
+#define QUASAR_SHAPE(T, N) \
+  if (cols <= 8 * T * N) return f(integral_constant<int, T>(), integral_constant<int, N>())
+  QUASAR_SHAPE(16, 1);
+  QUASAR_SHAPE(16, 2);
+  QUASAR_SHAPE(64, 1);
+  QUASAR_SHAPE(64, 2);
+  QUASAR_SHAPE(64, 4);
+  QUASAR_SHAPE(256, 2);
+  QUASAR_SHAPE(256, 4);
+  QUASAR_SHAPE(1024, 2);
+  QUASAR_SHAPE(1024, 4);
+#undef QUASAR_SHAPE
+  return hipErrorInvalidValue;
+}
+
+// n rows from row r on
+quasar_layer_norm rows_of(quasar_layer_norm a, int64_t r, int64_t n) {
+  a.rows = n;
+  a.x = rows_on(a.x, r, a.x_stride, size_of(a.x_dtype));
+  a.residual = rows_on(a.residual, r, a.residual_stride, size_of(a.residual_dtype));
+  a.h = rows_on(a.h, r, a.h_stride, size_of(a.residual_dtype));
+  a.y = rows_on(a.y, r, a.y_stride, size_of(a.y_dtype));
+  a.q = rows_on(a.q, r, a.q_stride, 1);
+  a.scale = rows_on(a.scale, r, 1, 4);
+  a.mean = rows_on(a.mean, r, 1, 4);
+  a.rstd = rows_on(a.rstd, r, 1, 4);
+  return a;
+}
+
+template <int XT, int RT>
+hipError_t launch_types(const quasar_layer_norm& a, hipStream_t stream) {
+  return with_shape(a.cols, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+    constexpr int threads = Shape<TPR>::kThreads, rows = Shape<TPR>::kRows;
+    constexpr int64_t most = most_groups(threads) * rows;
+    for (int64_t r = 0; r < a.rows; r += most) {
+      const quasar_layer_norm s = rows_of(a, r, a.rows - r < most ? a.rows - r : most);
+      layer_norm_kernel<XT, RT, TPR, NV><<<dim3((unsigned)((s.rows + rows - 1) / rows)), dim3(threads), 0, stream>>>(s);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  });
+}
+
+// ---- backward ---------------------------------------------------------------
+// Groups of TPR threads take rows in turn; a thread meets the same columns in
+// every row, so its shares of dweight and dbias stay in registers.  The shares of
+// a workgroup's groups meet in its wavefronts and in LDS, those of the workgroups
+// in `parts` (ln_parts_kernel sums them), in a fixed order.
+template <int GT, int HT, int TPR, int NV>
+__global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_backward_kernel(quasar_layer_norm_backward a, float* dw_out,
+                                                                                   float* db_out, int64_t part_step) {
+  constexpr int kWaves = TPR < 64 ? 1 : TPR / 64, kRows = Shape<TPR>::kRows;
+  constexpr int kShares = TPR < 256 ? 4 : 1, kWide = TPR < 64 ? TPR : TPR < 256 ? 64 : 1;  // wavefronts with shares of their own
+  __shared__ float red[2][2][kWaves];
+  __shared__ float shares[kShares > 1 ? (kShares - 1) * kWide * NV * 8 : 1];
+  const int t = Shape<TPR>::lane(), cols = (int)a.cols;
+  const float rcols = 1.0f / (float)cols;
+  float w[NV][8], dw[NV][8] = {}, db[NV][8] = {};
+#pragma unroll
+  for (int v = 0; v < NV; v++) {
+    const int c = (v * TPR + t) * 8;
+    load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w[v]);
+  }
+  int flip = 0;
+  for (int64_t row = (int64_t)blockIdx.x * kRows + Shape<TPR>::row(); row < a.rows; row += (int64_t)gridDim.x * kRows) {
+    Piece<GT> pg[NV];
+    Piece<HT> ph[NV];
+    const int64_t eg = row * a.dy_stride, eh = row * a.h_stride, ed = row * a.dh_stride, ex = row * a.dx_stride;
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      const int c = (v * TPR + t) * 8;
+      pg[v].load(a.dy, eg + c, cols - c);
+      ph[v].load(a.h, eh + c, cols - c);
+    }
+    // dh is asked for with the rest where there are registers for it
+    constexpr bool kEarly = TPR <= 256;
+    float dh[NV][8];
+    if (kEarly && a.dh) {
+#pragma unroll
+      for (int v = 0; v < NV; v++) {
+        const int c = (v * TPR + t) * 8;
+        load_floats(a.dh, ed + c, cols - c, a.dx_dtype == QUASAR_BF16, dh[v]);
+      }
+    }
+    const float rstd = a.rstd[row], mean = a.mean[row];
+    float dot = 0.0f, sum = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NV; v++)
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        // past the row's end g and w are 0
+        const float n = (ph[v].get(i) - mean) * rstd, g = pg[v].get(i), u = g * w[v][i];
+        sum += u;
+        dot = __builtin_fmaf(u, n, dot);
+        dw[v][i] = __builtin_fmaf(g, n, dw[v][i]);
+        db[v][i] += g;
+      }
+    // two LDS rows in turn: a wavefront may be a row ahead of another's read
+    if constexpr (TPR <= 64) {
+      sum = row_reduce<TPR>(sum, nullptr, SumOp());
+      dot = row_reduce<TPR>(dot, nullptr, SumOp());
+    } else {
+      sum = wave_reduce(sum, SumOp());
+      dot = wave_reduce(dot, SumOp());
+      if ((threadIdx.x & 63) == 0) {
+        red[flip][0][wave_index()] = sum;
+        red[flip][1][wave_index()] = dot;
+      }
+      __syncthreads();
+      sum = red[flip][0][0];
+      dot = red[flip][1][0];
+#pragma unroll
+      for (int i = 1; i < kWaves; i++) {
+        sum += red[flip][0][i];
+        dot += red[flip][1][i];
+      }
+      flip ^= 1;
+    }
+    const float m = dot * rcols, mu = sum * rcols;
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      const int c = (v * TPR + t) * 8, n8 = cols - c;
+      float dx[8];
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const float n = (ph[v].get(i) - mean) * rstd;
+        dx[i] = rstd * __builtin_fmaf(-m, n, __builtin_fmaf(pg[v].get(i), w[v][i], -mu));
+      }
+      if (a.dh) {
+        if constexpr (!kEarly) load_floats(a.dh, ed + c, n8, a.dx_dtype == QUASAR_BF16, dh[v]);
+#pragma unroll
+        for (int i = 0; i < 8; i++) dx[i] += dh[v][i];
+      }
+      store_piece(a.dx, ex + c, dx, n8, a.dx_dtype == QUASAR_BF16);
+    }
+  }
+  // the groups of a wavefront, then the wavefronts
+  const auto meet = [&](float (&s)[NV][8], float* out) {
+    if constexpr (TPR == 16) {
+#pragma unroll
+      for (int v = 0; v < NV; v++)
+#pragma unroll
+        for (int i = 0; i < 8; i++) s[v][i] = pair_rows<32>(pair_rows<16>(s[v][i], SumOp()), SumOp());
+    }
+    if constexpr (kShares > 1) {
+      const int wave = wave_index();
+      __syncthreads();  // the other sum's reads are done
+      if (wave > 0 && (threadIdx.x & 63) < kWide) {
+#pragma unroll
+        for (int v = 0; v < NV; v++)
+#pragma unroll
+          for (int i = 0; i < 8; i++) shares[(((wave - 1) * NV + v) * 8 + i) * kWide + t] = s[v][i];
+      }
+      __syncthreads();
+      if (threadIdx.x >= kWide) return;
+#pragma unroll
+      for (int j = 0; j < kShares - 1; j++)
+#pragma unroll
+        for (int v = 0; v < NV; v++)
+#pragma unroll
+          for (int i = 0; i < 8; i++) s[v][i] += shares[((j * NV + v) * 8 + i) * kWide + t];
+    }
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      const int c = (v * TPR + t) * 8;
+      store_piece<false>(out, blockIdx.x * part_step + c, s[v], cols - c);
+    }
+  };
+  if (dw_out) meet(dw, dw_out);
+  if (db_out) meet(db, db_out);
+}
+
+// dweight[c] (blockIdx.y = 0) or dbias[c] = sum of its parts: 16 columns a
+// workgroup, four a thread, the parts shared out over 64 rows of threads whose
+// sums meet in LDS.
+__global__ __launch_bounds__(256) void ln_parts_kernel(const float* parts, int n, int cols, float* dw, float* db) {
+  __shared__ float s[64][17];
+  float* const out = blockIdx.y == 0 ? dw : db;
+  if (!out) return;
+  const int x = (threadIdx.x & 3) * 4, y = threadIdx.x >> 2, c = blockIdx.x * 16 + x, pitch = ln_pitch(cols);
+  parts += blockIdx.y * pitch;
+  float sum[4] = {};
+  if (c < cols) {
+#pragma unroll 8
+    for (int i = y; i < n; i += 64) {
+      const float4 v = *reinterpret_cast<const float4*>(parts + (int64_t)i * 2 * pitch + c);
+      sum[0] += v.x;
+      sum[1] += v.y;
+      sum[2] += v.z;
+      sum[3] += v.w;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; i++) s[y][x + i] = sum[i];
+  __syncthreads();
+  // four threads a column sum 16 each, then meet (they are a quad)
+  if (threadIdx.x < 64) {
+    const int col = threadIdx.x >> 2, q = threadIdx.x & 3;
+    float t = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; i++) t += s[q * 16 + i][col];
+    t += dpp_f32<kDppXor1>(t);
+    t += dpp_f32<kDppXor2>(t);
+    if (q == 0 && blockIdx.x * 16 + col < cols) out[blockIdx.x * 16 + col] = t;
+  }
+}
+
+// workgroups of the backward pass, each with its shares of dweight and dbias
+int backward_groups(int64_t rows, int64_t cols) {
+  const int64_t per = cols <= 256 ? 16 : cols <= 2048 ? 4 : 1;  // rows a workgroup takes at once
+  const int64_t most = (cols <= 8192 ? 4 : 2) * kCUs;          // what runs at once (of 1024 threads: two a CU)
+  const int64_t groups = (rows + per - 1) / per, rounds = groups <= most ? 1 : (groups + most - 1) / most;
+  return (int)((groups + rounds - 1) / rounds);  // no more parts than that many rounds need
+}
+
+template <int GT, int HT>
+hipError_t launch_backward_types(const quasar_layer_norm_backward& a, hipStream_t stream) {
+  return with_shape(a.cols, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+    const int n = backward_groups(a.rows, a.cols), pitch = ln_pitch((int)a.cols);
+    float* const parts = n == 1 ? nullptr : reinterpret_cast<float*>(a.workspace);
+    float* const dw = !a.dweight || n == 1 ? a.dweight : parts;
+    float* const db = !a.dbias || n == 1 ? a.dbias : parts + pitch;
+    layer_norm_backward_kernel<GT, HT, TPR, NV><<<dim3(n), dim3(Shape<TPR>::kThreads), 0, stream>>>(a, dw, db, 2 * pitch);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || n == 1 || (!a.dweight && !a.dbias)) return e;
+    ln_parts_kernel<<<dim3((unsigned)((a.cols + 15) / 16), 2), dim3(256), 0, stream>>>(parts, n, (int)a.cols, a.dweight,
+                                                                                       a.dbias);
+    return hipGetLastError();
+  });
+}
+
+}  // namespace
+
+hipError_t launch_layer_norm(const quasar_layer_norm& a, hipStream_t stream) {
+  const bool xb = a.x_dtype == QUASAR_BF16, rb = a.residual_dtype == QUASAR_BF16;
+  if (!a.residual) return xb ? launch_types<kElemBF16, kElemNone>(a, stream) : launch_types<kElemF32, kElemNone>(a, stream);
+  if (rb) return xb ? launch_types<kElemBF16, kElemBF16>(a, stream) : launch_types<kElemF32, kElemBF16>(a, stream);
+  return xb ? launch_types<kElemBF16, kElemF32>(a, stream) : launch_types<kElemF32, kElemF32>(a, stream);
+}
+
+size_t layer_norm_backward_workspace(int64_t rows, int64_t cols) {
+  const int n = backward_groups(rows, cols);
+  return n > 1 ? (size_t)n * 2 * ln_pitch((int)cols) * sizeof(float) : 0;
+}
+
+hipError_t launch_layer_norm_backward(const quasar_layer_norm_backward& a, hipStream_t stream) {
+  const bool gb = a.dy_dtype == QUASAR_BF16, hb = a.h_dtype == QUASAR_BF16;
+  if (gb) return hb ? launch_backward_types<kElemBF16, kElemBF16>(a, stream) : launch_backward_types<kElemBF16, kElemF32>(a, stream);
+  return hb ? launch_backward_types<kElemF32, kElemBF16>(a, stream) : launch_backward_types<kElemF32, kElemF32>(a, stream);
+}
+
+}  // namespace quasar

@@ -240,49 +240,6 @@ struct XChunk {
   }
 };
 
-// The upper tail of the normal distribution at u >= 0, erfc(u / sqrt 2) / 2 =
-// exp(-u^2 / 2) t Q(t) with t = 1 / (1 + 0.32 u): Q is of degree 9, fitted over
-// 0 < t <= 1 to the least relative error, 3.2e-8.  20 instructions without a
-// branch, erff some 100.
-__device__ __forceinline__ float normal_tail(float u) {
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.32f, u, 1.0f));
-  constexpr float q[10] = {0.12766153f,  0.12766095f, 0.11462236f,  0.0878291f,  0.05865397f,
-                           -0.00937758f, 0.06532805f, -0.14670749f, 0.09540728f, -0.02107818f};
-  float p = q[9];
-#pragma unroll
-  for (int i = 8; i >= 0; i--) p = __builtin_fmaf(p, t, q[i]);
-  return p * t * __builtin_amdgcn_exp2f(u * u * (-0.5f * kLog2e));
-}
-
-// exp(-|v|) does not overflow.  Within 8 x 2^-24 of the result (v times the
-// hardware's reciprocal and exponential alone: 62 x 2^-24 at v = -85).
-__device__ __forceinline__ float silu(float v) {
-  const float e = exp_of(-fabsf(v));
-  return (v >= 0.0f ? v : v * e) / (1.0f + e);
-}
-
-// N values at once: one branch for all, and their chains run side by side
-// (value by value, GELU took 7 of the 16 us of 80 x 843 x 256).
-template <int N>
-__device__ __forceinline__ void activate(float (&v)[N], int act) {
-  if (act == QUASAR_ACT_RELU) {
-#pragma unroll
-    for (int i = 0; i < N; i++) v[i] = v[i] < 0.0f ? 0.0f : v[i];  // NaN stays
-  } else if (act == QUASAR_ACT_SILU) {
-#pragma unroll
-    for (int i = 0; i < N; i++) v[i] = silu(v[i]);
-  } else if (act == QUASAR_ACT_GELU) {  // no cancellation for v < 0; at infinity as v (1 + erf) / 2 is
-    float tail[N];
-#pragma unroll
-    for (int i = 0; i < N; i++) tail[i] = normal_tail(fabsf(v[i]));
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-      const float p = fabsf(v[i]) * tail[i];
-      v[i] = v[i] > 0.0f ? v[i] - (tail[i] > 0.0f ? p : 0.0f) : -p;
-    }
-  }
-}
-
 // ---- few tokens ---------------------------------------------------------------
 // The codes and parameters of 16 rows x 128 columns in LDS, and how a
 // wavefront brings them there: a lane's load is a 16-byte piece whose

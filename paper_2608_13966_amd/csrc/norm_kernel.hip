@@ -21,18 +21,6 @@ namespace {
 
 constexpr int kNormThreads = 256;
 
-// x / d rounded to nearest, inv = 1 / d rounded to nearest: the product's error is
-// taken off twice (the remainders are exact), the first time to within one place,
-// from where the second gives the rounded quotient (Markstein).  x inv alone puts
-// a value at the edge between two bytes on the wrong one.  16384 x 4096 bf16, q alone
-// and all in the last-level cache: 36 us, with the compiler's division for any divisor
-// 42, with x inv 35; 524288 x 128: 174, 212, 151; with y and from memory no difference.
-__device__ __forceinline__ float quotient(float x, float d, float inv) {
-  float q = x * inv;
-  q = __builtin_fmaf(__builtin_fmaf(-q, d, x), inv, q);
-  return __builtin_fmaf(__builtin_fmaf(-q, d, x), inv, q);
-}
-
 // TPR threads work on one row (64: a wavefront, without a barrier; more: a
 // workgroup), NV pieces of eight elements each.
 template <int XT, int RT, int TPR, int NV>

@@ -9,6 +9,8 @@ namespace {
 using quasar::size_of;
 
 constexpr int64_t kMaxRows = 0x7fffffff;
+constexpr int64_t kMaxEmbedCols = 1 << 20, kMaxTokens = 1 << 28;  // embedding, weight gradient
+constexpr int64_t kMaxKeptCols = 1 << 24, kMaxWeight = 1 << 22;   // kept rows, weight gradient
 constexpr int64_t kMaxStride = (int64_t)1 << 40;  // rows * stride stays far inside int64
 
 bool f32_or_bf16(int32_t t) { return t == QUASAR_F32 || t == QUASAR_BF16; }
@@ -184,6 +186,181 @@ int quasar_linear_codes(const quasar_desc* d, const quasar_linear* a, void* stre
   QUASAR_TRY(quasar_linear_codes_check(d, a));
   if (a->tokens == 0) return QUASAR_OK;
   return status_of(quasar::launch_linear(*d, *a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int quasar_add_layer_norm_check(const quasar_layer_norm* a) {
+  if (a == nullptr) return QUASAR_ERR_ARG;
+  if (a->rows < 0 || a->rows > kMaxRows || a->cols < 1 || a->cols > QUASAR_NORM_MAX_COLS) return QUASAR_ERR_SHAPE;
+  if (!f32_or_bf16(a->x_dtype) || !f32_or_bf16(a->weight_dtype)) return QUASAR_ERR_FORMAT;
+  if (a->residual && !f32_or_bf16(a->residual_dtype)) return QUASAR_ERR_FORMAT;
+  if (a->bias && !f32_or_bf16(a->bias_dtype)) return QUASAR_ERR_FORMAT;
+  if (a->y && !f32_or_bf16(a->y_dtype)) return QUASAR_ERR_FORMAT;
+  if (!(a->eps >= 0.0f && a->eps < INFINITY)) return QUASAR_ERR_ARG;
+  if (a->rows == 0) return QUASAR_OK;
+  if (a->x == nullptr || a->weight == nullptr) return QUASAR_ERR_ARG;
+  if ((a->q == nullptr) != (a->scale == nullptr)) return QUASAR_ERR_ARG;
+  if (a->h && !a->residual) return QUASAR_ERR_ARG;
+  QUASAR_TRY(check_matrix(a->x, a->rows, a->cols, a->x_stride, a->x_dtype));
+  QUASAR_TRY(check_matrix(a->residual, a->rows, a->cols, a->residual_stride, a->residual_dtype));
+  QUASAR_TRY(check_matrix(a->h, a->rows, a->cols, a->h_stride, a->residual_dtype));
+  QUASAR_TRY(check_matrix(a->y, a->rows, a->cols, a->y_stride, a->y_dtype));
+  QUASAR_TRY(check_matrix(a->q, a->rows, a->cols, a->q_stride, QUASAR_E4M3));
+  if (misaligned(a->weight, size_of(a->weight_dtype)) || (a->bias && misaligned(a->bias, size_of(a->bias_dtype))) ||
+      misaligned(a->scale, 4) || misaligned(a->mean, 4) || misaligned(a->rstd, 4))
+    return QUASAR_ERR_ALIGN;
+  return QUASAR_OK;
+}
+
+int quasar_add_layer_norm(const quasar_layer_norm* a, void* stream) {
+  QUASAR_TRY(quasar_add_layer_norm_check(a));
+  if (a->rows == 0) return QUASAR_OK;
+  return status_of(quasar::launch_layer_norm(*a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+size_t quasar_add_layer_norm_backward_workspace_bytes(int64_t rows, int64_t cols) {
+  if (rows < 1 || rows > kMaxRows || cols < 1 || cols > QUASAR_NORM_MAX_COLS) return 0;
+  return quasar::layer_norm_backward_workspace(rows, cols);
+}
+
+int quasar_add_layer_norm_backward_check(const quasar_layer_norm_backward* a) {
+  if (a == nullptr) return QUASAR_ERR_ARG;
+  if (a->rows < 0 || a->rows > kMaxRows || a->cols < 1 || a->cols > QUASAR_NORM_MAX_COLS) return QUASAR_ERR_SHAPE;
+  if (!f32_or_bf16(a->dy_dtype) || !f32_or_bf16(a->h_dtype) || !f32_or_bf16(a->weight_dtype) ||
+      !f32_or_bf16(a->dx_dtype))
+    return QUASAR_ERR_FORMAT;
+  if (a->rows == 0) return QUASAR_OK;
+  if (!a->dy || !a->h || !a->weight || !a->mean || !a->rstd || !a->dx) return QUASAR_ERR_ARG;
+  QUASAR_TRY(check_matrix(a->dy, a->rows, a->cols, a->dy_stride, a->dy_dtype));
+  QUASAR_TRY(check_matrix(a->h, a->rows, a->cols, a->h_stride, a->h_dtype));
+  QUASAR_TRY(check_matrix(a->dh, a->rows, a->cols, a->dh_stride, a->dx_dtype));
+  QUASAR_TRY(check_matrix(a->dx, a->rows, a->cols, a->dx_stride, a->dx_dtype));
+  if (misaligned(a->weight, size_of(a->weight_dtype)) || misaligned(a->mean, 4) || misaligned(a->rstd, 4) ||
+      misaligned(a->dweight, 4) || misaligned(a->dbias, 4) || misaligned(a->workspace, 16))
+    return QUASAR_ERR_ALIGN;
+  const size_t need = a->dweight || a->dbias ? quasar::layer_norm_backward_workspace(a->rows, a->cols) : 0;
+  if (need > 0 && (a->workspace == nullptr || a->workspace_bytes < need)) return QUASAR_ERR_WORKSPACE;
+  return QUASAR_OK;
+}
+
+int quasar_add_layer_norm_backward(const quasar_layer_norm_backward* a, void* stream) {
+  QUASAR_TRY(quasar_add_layer_norm_backward_check(a));
+  if (a->rows == 0) return QUASAR_OK;
+  return status_of(quasar::launch_layer_norm_backward(*a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int quasar_embed_check(const quasar_embedding* a) {
+  if (a == nullptr) return QUASAR_ERR_ARG;
+  if (a->rows < 1 || a->rows > kMaxRows || a->cols < 1 || a->cols > kMaxEmbedCols || a->tokens < 0 || a->tokens > kMaxTokens)
+    return QUASAR_ERR_SHAPE;
+  if (!f32_or_bf16(a->weight_dtype) || !f32_or_bf16(a->y_dtype)) return QUASAR_ERR_FORMAT;
+  if (a->index_bits != 32 && a->index_bits != 64) return QUASAR_ERR_FORMAT;
+  if (!(fabsf(a->scale) < INFINITY)) return QUASAR_ERR_ARG;
+  if (a->tokens == 0) return QUASAR_OK;
+  if (!a->index || !a->weight || !a->y) return QUASAR_ERR_ARG;
+  QUASAR_TRY(check_matrix(a->weight, a->rows, a->cols, a->weight_stride, a->weight_dtype));
+  QUASAR_TRY(check_matrix(a->y, a->tokens, a->cols, a->y_stride, a->y_dtype));
+  return misaligned(a->index, (uintptr_t)a->index_bits / 8) ? QUASAR_ERR_ALIGN : QUASAR_OK;
+}
+
+int quasar_embed(const quasar_embedding* a, void* stream) {
+  QUASAR_TRY(quasar_embed_check(a));
+  if (a->tokens == 0) return QUASAR_OK;
+  return status_of(quasar::launch_embed(*a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+size_t quasar_embed_backward_workspace_bytes(int64_t rows, int64_t cols, int64_t tokens) {
+  if (rows < 1 || rows > kMaxRows || cols < 1 || cols > kMaxEmbedCols || tokens < 0 || tokens > kMaxTokens) return 0;
+  size_t bytes;
+  return quasar::embed_backward_fits(rows, cols, tokens, bytes) ? bytes : 0;
+}
+
+int quasar_embed_backward_check(const quasar_embedding_backward* a) {
+  if (a == nullptr) return QUASAR_ERR_ARG;
+  if (a->rows < 1 || a->rows > kMaxRows || a->cols < 1 || a->cols > kMaxEmbedCols || a->tokens < 0 || a->tokens > kMaxTokens)
+    return QUASAR_ERR_SHAPE;
+  if (!f32_or_bf16(a->dy_dtype) || !f32_or_bf16(a->dweight_dtype)) return QUASAR_ERR_FORMAT;
+  if (a->index_bits != 32 && a->index_bits != 64) return QUASAR_ERR_FORMAT;
+  if (!(fabsf(a->scale) < INFINITY)) return QUASAR_ERR_ARG;
+  size_t need;
+  if (!quasar::embed_backward_fits(a->rows, a->cols, a->tokens, need)) return QUASAR_ERR_SHAPE;
+  if (!a->dweight || (a->tokens > 0 && (!a->index || !a->dy))) return QUASAR_ERR_ARG;
+  QUASAR_TRY(check_matrix(a->dy, a->tokens, a->cols, a->dy_stride, a->dy_dtype));
+  QUASAR_TRY(check_matrix(a->dweight, a->rows, a->cols, a->dweight_stride, a->dweight_dtype));
+  if (misaligned(a->index, (uintptr_t)a->index_bits / 8) || misaligned(a->workspace, 16)) return QUASAR_ERR_ALIGN;
+  return a->workspace == nullptr || a->workspace_bytes < need ? QUASAR_ERR_WORKSPACE : QUASAR_OK;
+}
+
+int quasar_embed_backward(const quasar_embedding_backward* a, void* stream) {
+  QUASAR_TRY(quasar_embed_backward_check(a));
+  return status_of(quasar::launch_embed_backward(*a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int quasar_checkpoint_rows_check(const quasar_checkpoint* a) {
+  if (a == nullptr) return QUASAR_ERR_ARG;
+  if (a->rows < 0 || a->rows > kMaxRows || a->cols < 1 || a->cols > kMaxKeptCols) return QUASAR_ERR_SHAPE;
+  if (!f32_or_bf16(a->x_dtype) || (a->y && !f32_or_bf16(a->y_dtype))) return QUASAR_ERR_FORMAT;
+  if (a->act < QUASAR_ACT_NONE || a->act > QUASAR_ACT_GELU) return QUASAR_ERR_ARG;
+  if (a->rows == 0) return QUASAR_OK;
+  if (!a->x || !a->q || !a->exponent) return QUASAR_ERR_ARG;
+  QUASAR_TRY(check_matrix(a->x, a->rows, a->cols, a->x_stride, a->x_dtype));
+  QUASAR_TRY(check_matrix(a->y, a->rows, a->cols, a->y_stride, a->y_dtype));
+  QUASAR_TRY(check_matrix(a->q, a->rows, a->cols, a->q_stride, QUASAR_E4M3));
+  return check_matrix(a->exponent, a->rows, (a->cols + 127) / 128, a->exponent_stride, QUASAR_E4M3);
+}
+
+int quasar_checkpoint_rows(const quasar_checkpoint* a, void* stream) {
+  QUASAR_TRY(quasar_checkpoint_rows_check(a));
+  if (a->rows == 0) return QUASAR_OK;
+  return status_of(quasar::launch_checkpoint(*a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+int quasar_checkpoint_backward_check(const quasar_checkpoint_grad* a) {
+  if (a == nullptr) return QUASAR_ERR_ARG;
+  if (a->rows < 0 || a->rows > kMaxRows || a->cols < 1 || a->cols > kMaxKeptCols) return QUASAR_ERR_SHAPE;
+  if (!f32_or_bf16(a->dy_dtype) || !f32_or_bf16(a->dx_dtype)) return QUASAR_ERR_FORMAT;
+  if (a->act <= QUASAR_ACT_NONE || a->act > QUASAR_ACT_GELU) return QUASAR_ERR_ARG;
+  if (a->rows == 0) return QUASAR_OK;
+  if (!a->dy || !a->q || !a->exponent || !a->dx) return QUASAR_ERR_ARG;
+  QUASAR_TRY(check_matrix(a->dy, a->rows, a->cols, a->dy_stride, a->dy_dtype));
+  QUASAR_TRY(check_matrix(a->q, a->rows, a->cols, a->q_stride, QUASAR_E4M3));
+  QUASAR_TRY(check_matrix(a->exponent, a->rows, (a->cols + 127) / 128, a->exponent_stride, QUASAR_E4M3));
+  return check_matrix(a->dx, a->rows, a->cols, a->dx_stride, a->dx_dtype);
+}
+
+int quasar_checkpoint_backward(const quasar_checkpoint_grad* a, void* stream) {
+  QUASAR_TRY(quasar_checkpoint_backward_check(a));
+  if (a->rows == 0) return QUASAR_OK;
+  return status_of(quasar::launch_checkpoint_backward(*a, reinterpret_cast<hipStream_t>(stream)));
+}
+
+static bool weight_grad_sizes(int64_t tokens, int64_t rows, int64_t cols) {
+  return tokens >= 0 && tokens <= kMaxTokens && rows >= 1 && rows <= kMaxWeight && cols >= 1 && cols <= kMaxWeight;
+}
+
+size_t quasar_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols, int32_t dy_dtype) {
+  size_t bytes;
+  return weight_grad_sizes(tokens, rows, cols) && f32_or_bf16(dy_dtype) &&
+                 quasar::weight_grad_fits(tokens, rows, cols, dy_dtype, bytes) ? bytes : 0;
+}
+
+int quasar_linear_weight_grad_check(const quasar_weight_grad* a) {
+  if (a == nullptr) return QUASAR_ERR_ARG;
+  if (!weight_grad_sizes(a->tokens, a->rows, a->cols)) return QUASAR_ERR_SHAPE;
+  if (!f32_or_bf16(a->dy_dtype) || !f32_or_bf16(a->dweight_dtype)) return QUASAR_ERR_FORMAT;
+  size_t need;
+  if (!quasar::weight_grad_fits(a->tokens, a->rows, a->cols, a->dy_dtype, need)) return QUASAR_ERR_SHAPE;
+  if (!a->dweight || (a->tokens > 0 && (!a->dy || !a->q || !a->exponent))) return QUASAR_ERR_ARG;
+  QUASAR_TRY(check_matrix(a->dy, a->tokens, a->rows, a->dy_stride, a->dy_dtype));
+  QUASAR_TRY(check_matrix(a->q, a->tokens, a->cols, a->q_stride, QUASAR_E4M3));
+  QUASAR_TRY(check_matrix(a->exponent, a->tokens, (a->cols + 127) / 128, a->exponent_stride, QUASAR_E4M3));
+  QUASAR_TRY(check_matrix(a->dweight, a->rows, a->cols, a->dweight_stride, a->dweight_dtype));
+  if (misaligned(a->workspace, 16)) return QUASAR_ERR_ALIGN;
+  return need > 0 && (a->workspace == nullptr || a->workspace_bytes < need) ? QUASAR_ERR_WORKSPACE : QUASAR_OK;
+}
+
+int quasar_linear_weight_grad(const quasar_weight_grad* a, void* stream) {
+  QUASAR_TRY(quasar_linear_weight_grad_check(a));
+  return status_of(quasar::launch_weight_grad(*a, reinterpret_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

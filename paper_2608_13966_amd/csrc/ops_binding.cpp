@@ -357,6 +357,289 @@ py::object linear_codes(const Tensor& x, const Packed& w, const Maybe& x_scale, 
   return std::move(o);
 }
 
+// y_dtype, dx_dtype: a dtype code, or -1 for the default
+py::object add_layer_norm(const Tensor& x, const Tensor& weight, const Maybe& bias, const Maybe& residual, double eps,
+                          int y_dtype, bool want_y, bool quantize, const py::object& out, const py::object& stream) {
+  TORCH_CHECK_VALUE(x.dim() == 2, "add_layer_norm: x must be 2-D");
+  const int64_t rows = x.size(0), cols = x.size(1);
+  const at::Device dev = x.device();
+  const Stream on(stream, dev);
+  matrix(x, "x", rows, cols, dev);
+  vector(weight, "weight", cols, dev);
+  quasar_layer_norm a{};
+  a.rows = rows;
+  a.cols = cols;
+  a.x_dtype = code(x, "x");
+  a.weight_dtype = code(weight, "weight");
+  if (bias) a.bias_dtype = code(vector(*bias, "bias", cols, dev), "bias");
+  if (residual) a.residual_dtype = code(matrix(*residual, "residual", rows, cols, dev), "residual");
+  Maybe h, y, q, scale;
+  if (residual) h = result(out, "h", {rows, cols}, residual->scalar_type(), dev);
+  const Tensor mean = result(out, "mean", {rows}, at::kFloat, dev);
+  const Tensor rstd = result(out, "rstd", {rows}, at::kFloat, dev);
+  a.y_dtype = y_dtype < 0 ? a.x_dtype : y_dtype;
+  if (want_y) y = result(out, "y", {rows, cols}, type_of(a.y_dtype), dev);
+  if (quantize) {
+    q = result(out, "q", {rows, cols}, at::kFloat8_e4m3fn, dev);
+    scale = result(out, "scale", {rows}, at::kFloat, dev);
+  }
+  a.x = ptr(x);
+  a.residual = ptr(residual);
+  a.weight = ptr(weight);
+  a.bias = ptr(bias);
+  a.h = ptr(h);
+  a.y = ptr(y);
+  a.q = static_cast<uint8_t*>(ptr(q));
+  a.scale = static_cast<float*>(ptr(scale));
+  a.mean = static_cast<float*>(ptr(mean));
+  a.rstd = static_cast<float*>(ptr(rstd));
+  a.x_stride = x.stride(0);
+  a.residual_stride = stride(residual);
+  a.h_stride = stride(h);
+  a.y_stride = stride(y);
+  a.q_stride = stride(q);
+  a.eps = (float)eps;
+  const int s = quasar_add_layer_norm(&a, on.handle(x));
+  if (s != QUASAR_OK) return py::int_(s);
+  py::dict o;
+  o["h"] = h ? *h : x;
+  o["mean"] = mean;
+  o["rstd"] = rstd;
+  o["y"] = obj(y);
+  o["q"] = obj(q);
+  o["scale"] = obj(scale);
+  return std::move(o);
+}
+
+py::object add_layer_norm_backward(const Tensor& dy, const Tensor& h, const Tensor& weight, const Tensor& mean,
+                                   const Tensor& rstd, const Maybe& dh, int dx_dtype, bool want_dweight, bool want_dbias,
+                                   const py::object& out, const py::object& stream) {
+  TORCH_CHECK_VALUE(dy.dim() == 2, "add_layer_norm_backward: dy must be 2-D");
+  const int64_t rows = dy.size(0), cols = dy.size(1);
+  const at::Device dev = dy.device();
+  const Stream on(stream, dev);
+  matrix(dy, "dy", rows, cols, dev);
+  matrix(h, "h", rows, cols, dev);
+  vector(weight, "weight", cols, dev);
+  vector_f32(mean, "mean", rows, dev);
+  vector_f32(rstd, "rstd", rows, dev);
+  quasar_layer_norm_backward a{};
+  a.rows = rows;
+  a.cols = cols;
+  a.dy_dtype = code(dy, "dy");
+  a.h_dtype = code(h, "h");
+  a.weight_dtype = code(weight, "weight");
+  a.dx_dtype = dx_dtype < 0 ? a.h_dtype : dx_dtype;
+  if (dh) {
+    const int c = code(matrix(*dh, "dh", rows, cols, dev), "dh");
+    TORCH_CHECK_VALUE(dx_dtype < 0 || dx_dtype == c, "add_layer_norm_backward: dx has dh's type");
+    a.dx_dtype = c;
+  }
+  const Tensor dx = result(out, "dx", {rows, cols}, type_of(a.dx_dtype), dev);
+  Maybe dw, db, ws;
+  if (want_dweight) dw = result(out, "dw", {cols}, at::kFloat, dev);
+  if (want_dbias) db = result(out, "db", {cols}, at::kFloat, dev);
+  if (want_dweight || want_dbias) {
+    a.workspace_bytes = quasar_add_layer_norm_backward_workspace_bytes(rows, cols);
+    ws = workspace(out, a.workspace_bytes, dev);
+    if (rows == 0 && dw) dw->zero_();
+    if (rows == 0 && db) db->zero_();
+  }
+  a.dy = ptr(dy);
+  a.h = ptr(h);
+  a.weight = ptr(weight);
+  a.mean = static_cast<float*>(ptr(mean));
+  a.rstd = static_cast<float*>(ptr(rstd));
+  a.dh = ptr(dh);
+  a.dx = ptr(dx);
+  a.dweight = static_cast<float*>(ptr(dw));
+  a.dbias = static_cast<float*>(ptr(db));
+  a.workspace = ptr(ws);
+  a.dy_stride = dy.stride(0);
+  a.h_stride = h.stride(0);
+  a.dh_stride = stride(dh);
+  a.dx_stride = dx.stride(0);
+  const int s = quasar_add_layer_norm_backward(&a, on.handle(dy));
+  if (s != QUASAR_OK) return py::int_(s);
+  py::dict o;
+  o["dx"] = dx;
+  o["dw"] = obj(dw);
+  o["db"] = obj(db);
+  o["workspace"] = obj(ws);
+  return std::move(o);
+}
+
+// A list of tokens; the number of bits of each.
+int tokens_of(const Tensor& t, const at::Device& dev) {
+  TORCH_CHECK_TYPE(t.scalar_type() == at::kLong || t.scalar_type() == at::kInt, "tokens: unsupported dtype ", t.dtype());
+  TORCH_CHECK_VALUE(t.dim() == 1, "tokens must be 1-D, not ", shape_str(t.sizes()));
+  vector(t, "tokens", t.size(0), dev);
+  return t.scalar_type() == at::kLong ? 64 : 32;
+}
+
+py::object embed(const Tensor& tokens, const Tensor& weight, double scale, int y_dtype, const py::object& out,
+                 const py::object& stream) {
+  TORCH_CHECK_VALUE(weight.dim() == 2, "embed: weight must be 2-D");
+  const at::Device dev = weight.device();
+  const Stream on(stream, dev);
+  quasar_embedding a{};
+  a.rows = weight.size(0);
+  a.cols = weight.size(1);
+  matrix(weight, "weight", a.rows, a.cols, dev);
+  a.weight_dtype = code(weight, "weight");
+  a.index_bits = tokens_of(tokens, dev);
+  a.tokens = tokens.size(0);
+  a.y_dtype = y_dtype < 0 ? a.weight_dtype : y_dtype;
+  const Tensor y = result(out, "y", {a.tokens, a.cols}, type_of(a.y_dtype), dev);
+  a.index = ptr(tokens);
+  a.weight = ptr(weight);
+  a.y = ptr(y);
+  a.weight_stride = weight.stride(0);
+  a.y_stride = y.stride(0);
+  a.scale = (float)scale;
+  const int s = quasar_embed(&a, on.handle(weight));
+  if (s != QUASAR_OK) return py::int_(s);
+  py::dict o;
+  o["y"] = y;
+  return std::move(o);
+}
+
+py::object embed_backward(const Tensor& dy, const Tensor& tokens, int64_t rows, double scale, int dw_dtype,
+                          const py::object& out, const py::object& stream) {
+  TORCH_CHECK_VALUE(dy.dim() == 2, "embed_backward: dy must be 2-D");
+  const at::Device dev = dy.device();
+  const Stream on(stream, dev);
+  quasar_embedding_backward a{};
+  a.rows = rows;
+  a.cols = dy.size(1);
+  a.index_bits = tokens_of(tokens, dev);
+  a.tokens = tokens.size(0);
+  matrix(dy, "dy", a.tokens, a.cols, dev);
+  TORCH_CHECK_VALUE(rows >= 1, "embed_backward: rows must be 1 or more, not ", rows);
+  a.dy_dtype = code(dy, "dy");
+  a.dweight_dtype = dw_dtype < 0 ? a.dy_dtype : dw_dtype;
+  const Tensor dw = result(out, "dw", {rows, a.cols}, type_of(a.dweight_dtype), dev);
+  a.workspace_bytes = quasar_embed_backward_workspace_bytes(rows, a.cols, a.tokens);
+  const Maybe ws = workspace(out, a.workspace_bytes, dev);
+  a.index = ptr(tokens);
+  a.dy = ptr(dy);
+  a.dweight = ptr(dw);
+  a.workspace = ptr(ws);
+  a.dy_stride = dy.stride(0);
+  a.dweight_stride = dw.stride(0);
+  a.scale = (float)scale;
+  const int s = quasar_embed_backward(&a, on.handle(dy));
+  if (s != QUASAR_OK) return py::int_(s);
+  py::dict o;
+  o["dw"] = dw;
+  o["workspace"] = obj(ws);
+  return std::move(o);
+}
+
+py::object checkpoint_rows(const Tensor& x, int act, int y_dtype, bool want_y, const py::object& out, const py::object& stream) {
+  TORCH_CHECK_VALUE(x.dim() == 2, "checkpoint_rows: x must be 2-D");
+  const int64_t rows = x.size(0), cols = x.size(1), blocks = (cols + 127) / 128;
+  const at::Device dev = x.device();
+  const Stream on(stream, dev);
+  matrix(x, "x", rows, cols, dev);
+  quasar_checkpoint a{};
+  a.rows = rows;
+  a.cols = cols;
+  a.act = act;
+  a.x_dtype = code(x, "x");
+  a.y_dtype = y_dtype < 0 ? a.x_dtype : y_dtype;
+  const Tensor q = result(out, "q", {rows, cols}, at::kFloat8_e4m3fn, dev);
+  const Tensor e = result(out, "exponent", {rows, blocks}, at::kByte, dev);
+  Maybe y;
+  if (want_y) y = result(out, "y", {rows, cols}, type_of(a.y_dtype), dev);
+  a.x = ptr(x);
+  a.y = ptr(y);
+  a.q = static_cast<uint8_t*>(ptr(q));
+  a.exponent = static_cast<uint8_t*>(ptr(e));
+  a.x_stride = x.stride(0);
+  a.y_stride = stride(y);
+  a.q_stride = q.stride(0);
+  a.exponent_stride = e.stride(0);
+  const int s = quasar_checkpoint_rows(&a, on.handle(x));
+  if (s != QUASAR_OK) return py::int_(s);
+  py::dict o;
+  o["q"] = q;
+  o["exponent"] = e;
+  o["y"] = obj(y);
+  return std::move(o);
+}
+
+// What checkpoint_rows kept of [rows, cols].
+void kept(const Tensor& q, const Tensor& e, int64_t rows, int64_t cols, const at::Device& dev) {
+  TORCH_CHECK_TYPE(q.scalar_type() == at::kFloat8_e4m3fn, "q: unsupported dtype ", q.dtype());
+  TORCH_CHECK_TYPE(e.scalar_type() == at::kByte, "exponent: unsupported dtype ", e.dtype());
+  matrix(q, "q", rows, cols, dev);
+  matrix(e, "exponent", rows, (cols + 127) / 128, dev);
+}
+
+py::object checkpoint_backward(const Tensor& dy, const Tensor& q, const Tensor& e, int act, int dx_dtype, const py::object& out,
+                               const py::object& stream) {
+  TORCH_CHECK_VALUE(dy.dim() == 2, "checkpoint_backward: dy must be 2-D");
+  const int64_t rows = dy.size(0), cols = dy.size(1);
+  const at::Device dev = dy.device();
+  const Stream on(stream, dev);
+  matrix(dy, "dy", rows, cols, dev);
+  kept(q, e, rows, cols, dev);
+  quasar_checkpoint_grad a{};
+  a.rows = rows;
+  a.cols = cols;
+  a.act = act;
+  a.dy_dtype = code(dy, "dy");
+  a.dx_dtype = dx_dtype < 0 ? a.dy_dtype : dx_dtype;
+  const Tensor dx = result(out, "dx", {rows, cols}, type_of(a.dx_dtype), dev);
+  a.dy = ptr(dy);
+  a.q = static_cast<uint8_t*>(ptr(q));
+  a.exponent = static_cast<uint8_t*>(ptr(e));
+  a.dx = ptr(dx);
+  a.dy_stride = dy.stride(0);
+  a.q_stride = q.stride(0);
+  a.exponent_stride = e.stride(0);
+  a.dx_stride = dx.stride(0);
+  const int s = quasar_checkpoint_backward(&a, on.handle(dy));
+  if (s != QUASAR_OK) return py::int_(s);
+  py::dict o;
+  o["dx"] = dx;
+  return std::move(o);
+}
+
+py::object linear_weight_grad(const Tensor& dy, const Tensor& q, const Tensor& e, int dw_dtype, const py::object& out,
+                              const py::object& stream) {
+  TORCH_CHECK_VALUE(dy.dim() == 2 && q.dim() == 2, "linear_weight_grad: dy and q must be 2-D");
+  const at::Device dev = dy.device();
+  const Stream on(stream, dev);
+  quasar_weight_grad a{};
+  a.tokens = dy.size(0);
+  a.rows = dy.size(1);
+  a.cols = q.size(1);
+  matrix(dy, "dy", a.tokens, a.rows, dev);
+  kept(q, e, a.tokens, a.cols, dev);
+  a.dy_dtype = code(dy, "dy");
+  a.dweight_dtype = dw_dtype < 0 ? QUASAR_F32 : dw_dtype;
+  const Tensor dw = result(out, "dw", {a.rows, a.cols}, type_of(a.dweight_dtype), dev);
+  a.workspace_bytes = quasar_linear_weight_grad_workspace_bytes(a.tokens, a.rows, a.cols, a.dy_dtype);
+  const Maybe ws = workspace(out, a.workspace_bytes, dev);
+  a.dy = ptr(dy);
+  a.q = static_cast<uint8_t*>(ptr(q));
+  a.exponent = static_cast<uint8_t*>(ptr(e));
+  a.dweight = ptr(dw);
+  a.workspace = ptr(ws);
+  a.dy_stride = dy.stride(0);
+  a.q_stride = q.stride(0);
+  a.exponent_stride = e.stride(0);
+  a.dweight_stride = dw.stride(0);
+  const int s = quasar_linear_weight_grad(&a, on.handle(dy));
+  if (s != QUASAR_OK) return py::int_(s);
+  py::dict o;
+  o["dw"] = dw;
+  o["workspace"] = obj(ws);
+  return std::move(o);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_ops_binding, m) {
@@ -368,6 +651,13 @@ PYBIND11_MODULE(_ops_binding, m) {
   m.def("add_rms_norm_backward", &add_rms_norm_backward);
   m.def("distill", &distill);
   m.def("linear_codes", &linear_codes);
+  m.def("add_layer_norm", &add_layer_norm);
+  m.def("add_layer_norm_backward", &add_layer_norm_backward);
+  m.def("embed", &embed);
+  m.def("embed_backward", &embed_backward);
+  m.def("checkpoint_rows", &checkpoint_rows);
+  m.def("checkpoint_backward", &checkpoint_backward);
+  m.def("linear_weight_grad", &linear_weight_grad);
   py::class_<Packed>(m, "Packed")
       .def(py::init<int64_t, int64_t, int, int, int, Tensor, Tensor, Maybe, Maybe>());
   // released before the interpreter is

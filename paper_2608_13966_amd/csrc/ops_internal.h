@@ -40,4 +40,23 @@ size_t linear_workspace(const quasar_desc& d, int64_t tokens);
 bool linear_fits(const quasar_desc& d, int64_t tokens, int x_dtype, size_t& workspace);
 hipError_t launch_linear(const quasar_desc& d, const quasar_linear& a, hipStream_t stream);
 
+// layer_norm_kernel.hip
+hipError_t launch_layer_norm(const quasar_layer_norm& a, hipStream_t stream);
+size_t layer_norm_backward_workspace(int64_t rows, int64_t cols);
+hipError_t launch_layer_norm_backward(const quasar_layer_norm_backward& a, hipStream_t stream);
+
+// embed_kernel.hip
+hipError_t launch_embed(const quasar_embedding& a, hipStream_t stream);
+// whether the kernels' workgroups fit a grid; and the scratch memory that they need
+bool embed_backward_fits(int64_t rows, int64_t cols, int64_t tokens, size_t& workspace);
+hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t stream);
+
+// checkpoint_kernel.hip
+hipError_t launch_checkpoint(const quasar_checkpoint& a, hipStream_t stream);
+hipError_t launch_checkpoint_backward(const quasar_checkpoint_grad& a, hipStream_t stream);
+
+// weight_grad_kernel.hip
+bool weight_grad_fits(int64_t tokens, int64_t rows, int64_t cols, int dy_dtype, size_t& workspace);
+hipError_t launch_weight_grad(const quasar_weight_grad& a, hipStream_t stream);
+
 }  // namespace quasar

@@ -10,6 +10,11 @@ reconstruction, one fused AdamW + reconstruction a layer.  Serving: the norm
 writes 8-bit rows with their scales, which ``ops.linear_codes`` multiplies by
 the packed codes; nothing of the latent weights is read.  The teacher is a
 seeded random network of the same shape, the tokens are random.
+
+A second network has layer norms with biases (``ste.add_layer_norm``), its
+embedding scaled and its gradient summed by ``ste.embed``, and keeps what the
+backward pass needs of the linears' and GELUs' inputs in 8 bits
+(``QuasarLinear(checkpoint=True)``, ``ste.activation``).
 """
 from __future__ import annotations
 
@@ -19,14 +24,21 @@ from . import ops, ste
 
 
 class Student(torch.nn.Module):
+    """``norm``: "rms" or "layer"; ``embed_scale``: what the embedding's rows are
+    multiplied by (None: torch's own lookup and gradient); ``checkpoint``: the
+    linears and GELUs keep their inputs in 8 bits."""
+
     def __init__(self, vocab=2048, width=256, hidden=512, blocks=2, bits=4, group=64, lr=1e-3, device="cuda",
-                 seed=0):
+                 seed=0, norm="rms", embed_scale=None, checkpoint=False):
         super().__init__()
         gen = torch.Generator(device=device).manual_seed(seed)
-        make = dict(bits=bits, group=group, lr=lr, device=device, generator=gen)
+        make = dict(bits=bits, group=group, lr=lr, device=device, generator=gen, checkpoint=checkpoint)
+        self.layer, self.embed_scale, self.checkpoint = norm == "layer", embed_scale, checkpoint
         self.embed = torch.nn.Parameter(
             torch.randn(vocab, width, device=device, generator=gen).to(torch.bfloat16))
         self.norms = torch.nn.ParameterList(torch.ones(width, device=device) for _ in range(blocks + 1))
+        self.biases = torch.nn.ParameterList(
+            torch.zeros(width, device=device) for _ in range(blocks + 1 if self.layer else 0))
         self.up = torch.nn.ModuleList(ste.QuasarLinear(width, hidden, **make) for _ in range(blocks))
         self.down = torch.nn.ModuleList(ste.QuasarLinear(hidden, width, **make) for _ in range(blocks))
         self.head = ste.QuasarLinear(width, vocab, **make)
@@ -34,15 +46,21 @@ class Student(torch.nn.Module):
     def linears(self):
         return [*self.up, *self.down, self.head]
 
+    def _norm(self, i, x, residual=None):
+        if self.layer:
+            return ste.add_layer_norm(x, self.norms[i], self.biases[i], residual)
+        return ste.add_rms_norm(x, self.norms[i], residual)
+
     def forward(self, tokens):
-        stream, branch = self.embed[tokens], None
-        for norm, up, down in zip(self.norms, self.up, self.down):
+        stream = self.embed[tokens] if self.embed_scale is None else ste.embed(tokens, self.embed, scale=self.embed_scale)
+        gelu, branch = ste.activation if self.checkpoint else torch.nn.functional.gelu, None
+        for i, (up, down) in enumerate(zip(self.up, self.down)):
             if branch is None:
-                y = ste.add_rms_norm(stream, norm)
+                y = self._norm(i, stream)
             else:
-                y, stream = ste.add_rms_norm(branch, norm, stream)
-            branch = down(torch.nn.functional.gelu(up(y)))
-        y, _ = ste.add_rms_norm(branch, self.norms[-1], stream)
+                y, stream = self._norm(i, branch, stream)
+            branch = down(gelu(up(y)))
+        y, _ = self._norm(-1, branch, stream)
         return self.head(y)
 
 
@@ -52,7 +70,7 @@ class Trainer:
 
     def __init__(self, student, temperature=1.0, lr=1e-3):
         self.student, self.temperature = student, temperature
-        self.rest = torch.optim.AdamW([student.embed, *student.norms], lr=lr)
+        self.rest = torch.optim.AdamW([student.embed, *student.norms, *student.biases], lr=lr)
 
     def step(self, tokens, index, teacher, row_weight=None):
         logits = self.student(tokens)
@@ -73,6 +91,7 @@ class Server:
     def __init__(self, student, eight=True):
         self.embed = student.embed.detach()
         self.norms = [w.detach() for w in student.norms]
+        self.biases, self.embed_scale = [b.detach() for b in student.biases], student.embed_scale
         self.up, self.down = ([layer.packed() for layer in part] for part in (student.up, student.down))
         self.head, self.eight = student.head.packed(), eight
 
@@ -81,16 +100,23 @@ class Server:
             return ops.linear_codes(n["q"], weight, x_scale=n["scale"], **kw)["y"]
         return ops.linear_codes(n["y"], weight, **kw)["y"]
 
-    def _norm(self, x, weight, residual=None):
-        return ops.add_rms_norm(x, weight, residual, want_y=not self.eight, quantize=self.eight)
+    def _norm(self, i, x, residual=None):
+        how = dict(want_y=not self.eight, quantize=self.eight)
+        if self.biases:
+            return ops.add_layer_norm(x, self.norms[i], self.biases[i], residual, **how)
+        return ops.add_rms_norm(x, self.norms[i], residual, **how)
 
     def __call__(self, tokens):
-        x, stream = self.embed[tokens], None
-        for norm, up, down in zip(self.norms, self.up, self.down):
-            n = self._norm(x, norm, stream)
+        if self.embed_scale is None:
+            x = self.embed[tokens]
+        else:
+            x = ops.embed(tokens, self.embed, scale=self.embed_scale)["y"]
+        stream = None
+        for i, (up, down) in enumerate(zip(self.up, self.down)):
+            n = self._norm(i, x, stream)
             stream = n["h"]
             x = ops.linear_codes(self._linear(n, up, act="gelu"), down)["y"]
-        return self._linear(self._norm(x, self.norms[-1], stream), self.head, y_dtype="fp32")
+        return self._linear(self._norm(-1, x, stream), self.head, y_dtype="fp32")
 
 
 def top_logits(tokens, vocab, listed, seed=1, width=64, device="cuda"):
@@ -119,7 +145,13 @@ def run(steps=40, tokens=512, vocab=2048, listed=32, device="cuda", log=print, *
 
 
 def main():
-    s, _, t = run()
+    show(*run()[::2])
+    print("layer norms, a scaled embedding, activations kept in 8 bits:")
+    show(*run(norm="layer", embed_scale=1.0, checkpoint=True)[::2])
+
+
+def show(s, t):
+    """How the network served from its codes differs from the trained one."""
     with torch.no_grad():
         want = s(t).float()
         for eight in (False, True):

@@ -1,6 +1,7 @@
 """The operators around the reconstruction (the C ABI in include/quasar_ops.h):
 the RMS norm with the residual's addition and an 8-bit output, the loss against
-a teacher's top logits, and the product from packed codes.
+a teacher's top logits, and the product from packed codes; the embedding, the
+layer norm and activations kept in 8 bits for the backward pass.
 
 Argument checks and marshalling only, as in ``quasar`` (in C++, ``_ops_binding``):
 the work runs in the HIP kernels behind the C entry points, there is no CPU path,
@@ -14,7 +15,8 @@ call of the same sizes and arguments, whose results then overwrite it and which
 allocates nothing.
 
 The functions named ``quasar_*`` (``EXPORTS``) mirror the C entry points.
-``ste`` has the autograd forms (``add_rms_norm``, ``distill_topk_loss``).
+``ste`` has the autograd forms (``add_rms_norm``, ``add_layer_norm``, ``embed``,
+``activation``, ``distill_topk_loss``).
 """
 from __future__ import annotations
 
@@ -32,7 +34,13 @@ EXPORTS = ("quasar_add_rms_norm", "quasar_add_rms_norm_check", "quasar_add_rms_n
            "quasar_add_rms_norm_backward_check", "quasar_add_rms_norm_backward_workspace_bytes",
            "quasar_distill_topk", "quasar_distill_topk_backward", "quasar_distill_topk_grad",
            "quasar_distill_topk_check", "quasar_distill_topk_workspace_bytes",
-           "quasar_linear_codes", "quasar_linear_codes_check", "quasar_linear_codes_workspace_bytes")
+           "quasar_linear_codes", "quasar_linear_codes_check", "quasar_linear_codes_workspace_bytes",
+           "quasar_add_layer_norm", "quasar_add_layer_norm_check", "quasar_add_layer_norm_backward",
+           "quasar_add_layer_norm_backward_check", "quasar_add_layer_norm_backward_workspace_bytes",
+           "quasar_embed", "quasar_embed_check", "quasar_embed_backward", "quasar_embed_backward_check",
+           "quasar_embed_backward_workspace_bytes", "quasar_checkpoint_rows", "quasar_checkpoint_rows_check",
+           "quasar_checkpoint_backward", "quasar_checkpoint_backward_check", "quasar_linear_weight_grad",
+           "quasar_linear_weight_grad_check", "quasar_linear_weight_grad_workspace_bytes")
 
 _vp, _i64, _i32, _f32, _sz = C.c_void_p, C.c_int64, C.c_int32, C.c_float, C.c_size_t
 
@@ -70,6 +78,58 @@ class Linear(C.Structure):
                 ("x_dtype", _i32), ("bias_dtype", _i32), ("residual_dtype", _i32), ("y_dtype", _i32), ("act", _i32)]
 
 
+class LayerNorm(C.Structure):
+    """quasar_layer_norm"""
+    _fields_ = [("rows", _i64), ("cols", _i64), ("x", _vp), ("residual", _vp), ("weight", _vp), ("bias", _vp),
+                ("h", _vp), ("y", _vp), ("q", _vp), ("scale", _vp), ("mean", _vp), ("rstd", _vp), ("x_stride", _i64),
+                ("residual_stride", _i64), ("h_stride", _i64), ("y_stride", _i64), ("q_stride", _i64),
+                ("x_dtype", _i32), ("residual_dtype", _i32), ("weight_dtype", _i32), ("bias_dtype", _i32),
+                ("y_dtype", _i32), ("eps", _f32)]
+
+
+class LayerNormBackward(C.Structure):
+    """quasar_layer_norm_backward"""
+    _fields_ = [("rows", _i64), ("cols", _i64), ("dy", _vp), ("h", _vp), ("weight", _vp), ("mean", _vp), ("rstd", _vp),
+                ("dh", _vp), ("dx", _vp), ("dweight", _vp), ("dbias", _vp), ("workspace", _vp),
+                ("workspace_bytes", _sz), ("dy_stride", _i64), ("h_stride", _i64), ("dh_stride", _i64),
+                ("dx_stride", _i64), ("dy_dtype", _i32), ("h_dtype", _i32), ("weight_dtype", _i32), ("dx_dtype", _i32)]
+
+
+class Embedding(C.Structure):
+    """quasar_embedding"""
+    _fields_ = [("rows", _i64), ("cols", _i64), ("tokens", _i64), ("index", _vp), ("weight", _vp), ("y", _vp),
+                ("weight_stride", _i64), ("y_stride", _i64), ("index_bits", _i32), ("weight_dtype", _i32),
+                ("y_dtype", _i32), ("scale", _f32)]
+
+
+class EmbeddingBackward(C.Structure):
+    """quasar_embedding_backward"""
+    _fields_ = [("rows", _i64), ("cols", _i64), ("tokens", _i64), ("index", _vp), ("dy", _vp), ("dweight", _vp),
+                ("workspace", _vp), ("workspace_bytes", _sz), ("dy_stride", _i64), ("dweight_stride", _i64),
+                ("index_bits", _i32), ("dy_dtype", _i32), ("dweight_dtype", _i32), ("scale", _f32)]
+
+
+class Checkpoint(C.Structure):
+    """quasar_checkpoint"""
+    _fields_ = [("rows", _i64), ("cols", _i64), ("x", _vp), ("y", _vp), ("q", _vp), ("exponent", _vp),
+                ("x_stride", _i64), ("y_stride", _i64), ("q_stride", _i64), ("exponent_stride", _i64),
+                ("x_dtype", _i32), ("y_dtype", _i32), ("act", _i32)]
+
+
+class CheckpointGrad(C.Structure):
+    """quasar_checkpoint_grad"""
+    _fields_ = [("rows", _i64), ("cols", _i64), ("dy", _vp), ("q", _vp), ("exponent", _vp), ("dx", _vp),
+                ("dy_stride", _i64), ("q_stride", _i64), ("exponent_stride", _i64), ("dx_stride", _i64),
+                ("dy_dtype", _i32), ("dx_dtype", _i32), ("act", _i32)]
+
+
+class WeightGrad(C.Structure):
+    """quasar_weight_grad"""
+    _fields_ = [("tokens", _i64), ("rows", _i64), ("cols", _i64), ("dy", _vp), ("q", _vp), ("exponent", _vp),
+                ("dweight", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("dy_stride", _i64), ("q_stride", _i64),
+                ("exponent_stride", _i64), ("dweight_stride", _i64), ("dy_dtype", _i32), ("dweight_dtype", _i32)]
+
+
 _lib = None
 
 
@@ -79,6 +139,8 @@ def lib():
     if _lib is None:
         L = Q.lib()
         np_, bp, dp, lp, desc = (C.POINTER(t) for t in (Norm, NormBackward, Distill, Linear, Q.Desc))
+        ln, lb, eb, eg, kp, kg, wg = (C.POINTER(t) for t in (LayerNorm, LayerNormBackward, Embedding, EmbeddingBackward,
+                                                             Checkpoint, CheckpointGrad, WeightGrad))
         for name, args, res in (
                 ("quasar_add_rms_norm", [np_, _vp], C.c_int), ("quasar_add_rms_norm_check", [np_], C.c_int),
                 ("quasar_add_rms_norm_backward", [bp, _vp], C.c_int),
@@ -89,7 +151,18 @@ def lib():
                 ("quasar_distill_topk_check", [dp, C.c_int], C.c_int),
                 ("quasar_distill_topk_workspace_bytes", [_i64, _i64], _sz),
                 ("quasar_linear_codes", [desc, lp, _vp], C.c_int), ("quasar_linear_codes_check", [desc, lp], C.c_int),
-                ("quasar_linear_codes_workspace_bytes", [desc, _i64, _i32], _sz)):
+                ("quasar_linear_codes_workspace_bytes", [desc, _i64, _i32], _sz),
+                ("quasar_add_layer_norm", [ln, _vp], C.c_int), ("quasar_add_layer_norm_check", [ln], C.c_int),
+                ("quasar_add_layer_norm_backward", [lb, _vp], C.c_int),
+                ("quasar_add_layer_norm_backward_check", [lb], C.c_int),
+                ("quasar_add_layer_norm_backward_workspace_bytes", [_i64, _i64], _sz),
+                ("quasar_embed", [eb, _vp], C.c_int), ("quasar_embed_check", [eb], C.c_int),
+                ("quasar_embed_backward", [eg, _vp], C.c_int), ("quasar_embed_backward_check", [eg], C.c_int),
+                ("quasar_embed_backward_workspace_bytes", [_i64, _i64, _i64], _sz),
+                ("quasar_checkpoint_rows", [kp, _vp], C.c_int), ("quasar_checkpoint_rows_check", [kp], C.c_int),
+                ("quasar_checkpoint_backward", [kg, _vp], C.c_int), ("quasar_checkpoint_backward_check", [kg], C.c_int),
+                ("quasar_linear_weight_grad", [wg, _vp], C.c_int), ("quasar_linear_weight_grad_check", [wg], C.c_int),
+                ("quasar_linear_weight_grad_workspace_bytes", [_i64, _i64, _i64, _i32], _sz)):
             f = getattr(L, name)
             f.argtypes, f.restype = args, res
         _lib = L
@@ -146,6 +219,74 @@ def quasar_linear_codes_check(d: Q.Descriptor, a: Linear) -> int:
 
 def quasar_linear_codes_workspace_bytes(d: Q.Descriptor, tokens: int, x_dtype: int) -> int:
     return int(lib().quasar_linear_codes_workspace_bytes(d.ref, int(tokens), int(x_dtype)))
+
+
+def quasar_add_layer_norm(a: LayerNorm, stream) -> int:
+    return lib().quasar_add_layer_norm(C.byref(a), stream)
+
+
+def quasar_add_layer_norm_check(a: LayerNorm) -> int:
+    return lib().quasar_add_layer_norm_check(C.byref(a))
+
+
+def quasar_add_layer_norm_backward(a: LayerNormBackward, stream) -> int:
+    return lib().quasar_add_layer_norm_backward(C.byref(a), stream)
+
+
+def quasar_add_layer_norm_backward_check(a: LayerNormBackward) -> int:
+    return lib().quasar_add_layer_norm_backward_check(C.byref(a))
+
+
+def quasar_add_layer_norm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().quasar_add_layer_norm_backward_workspace_bytes(int(rows), int(cols)))
+
+
+def quasar_embed(a: Embedding, stream) -> int:
+    return lib().quasar_embed(C.byref(a), stream)
+
+
+def quasar_embed_check(a: Embedding) -> int:
+    return lib().quasar_embed_check(C.byref(a))
+
+
+def quasar_embed_backward(a: EmbeddingBackward, stream) -> int:
+    return lib().quasar_embed_backward(C.byref(a), stream)
+
+
+def quasar_embed_backward_check(a: EmbeddingBackward) -> int:
+    return lib().quasar_embed_backward_check(C.byref(a))
+
+
+def quasar_embed_backward_workspace_bytes(rows: int, cols: int, tokens: int) -> int:
+    return int(lib().quasar_embed_backward_workspace_bytes(int(rows), int(cols), int(tokens)))
+
+
+def quasar_checkpoint_rows(a: Checkpoint, stream) -> int:
+    return lib().quasar_checkpoint_rows(C.byref(a), stream)
+
+
+def quasar_checkpoint_rows_check(a: Checkpoint) -> int:
+    return lib().quasar_checkpoint_rows_check(C.byref(a))
+
+
+def quasar_checkpoint_backward(a: CheckpointGrad, stream) -> int:
+    return lib().quasar_checkpoint_backward(C.byref(a), stream)
+
+
+def quasar_checkpoint_backward_check(a: CheckpointGrad) -> int:
+    return lib().quasar_checkpoint_backward_check(C.byref(a))
+
+
+def quasar_linear_weight_grad(a: WeightGrad, stream) -> int:
+    return lib().quasar_linear_weight_grad(C.byref(a), stream)
+
+
+def quasar_linear_weight_grad_check(a: WeightGrad) -> int:
+    return lib().quasar_linear_weight_grad_check(C.byref(a))
+
+
+def quasar_linear_weight_grad_workspace_bytes(tokens: int, rows: int, cols: int, dy_dtype: int) -> int:
+    return int(lib().quasar_linear_weight_grad_workspace_bytes(int(tokens), int(rows), int(cols), int(dy_dtype)))
 
 
 # ---- the calls --------------------------------------------------------------------
@@ -310,3 +451,93 @@ def linear_codes(x, weight: PackedWeight, *, x_scale=None, bias=None, residual=N
         raise ValueError(f"linear_codes: act must be one of {', '.join(ACTS)}")
     return _done((_binding or _load()).linear_codes(x, weight._packed, x_scale, bias, residual, code,
                                                    _dtype(y_dtype, "y_dtype"), out, stream), "quasar_linear_codes")
+
+
+# ---- layer norm with the residual's addition ------------------------------------
+
+def add_layer_norm(x, weight, bias=None, residual=None, *, eps=1e-5, y_dtype=None, want_y=True, quantize=False, out=None,
+                   stream=None):
+    """h = x + residual; y = (h - mean(h)) / sqrt(var(h) + eps) * weight + bias, row by row.
+
+    Returns ``h`` (in residual's type; x itself without a residual), ``mean`` and
+    ``rstd`` (fp32, one per row), ``y`` and, with ``quantize``, ``q`` and
+    ``scale``, all as ``add_rms_norm``.  x, residual, weight and bias are fp32 or
+    bf16, each its own.  A given ``out`` may hold ``residual`` itself as
+    ``out["h"]``.
+    """
+    return _done((_binding or _load()).add_layer_norm(x, weight, bias, residual, eps, _dtype(y_dtype, "y_dtype"), want_y,
+                                                     quantize, out, stream), "quasar_add_layer_norm")
+
+
+def add_layer_norm_backward(dy, h, weight, mean, rstd, dh=None, *, dx_dtype=None, want_dweight=True, want_dbias=True,
+                            out=None, stream=None):
+    """The gradients of ``add_layer_norm``: ``dx`` (of x and of residual alike; in
+    dh's type, else ``dx_dtype``, default h's), ``dw`` and ``db`` (fp32).
+
+    dy is y's gradient; h, mean and rstd what the forward call returned; dh the
+    gradient of h itself (the rest of the stream's), or None.
+    """
+    return _done((_binding or _load()).add_layer_norm_backward(dy, h, weight, mean, rstd, dh, _dtype(dx_dtype, "dx_dtype"),
+                                                              want_dweight, want_dbias, out, stream),
+                 "quasar_add_layer_norm_backward")
+
+
+# ---- embedding --------------------------------------------------------------------
+
+def embed(tokens, weight, *, scale=1.0, y_dtype=None, out=None, stream=None):
+    """``y`` [tokens, cols] = scale * weight[tokens], in ``y_dtype`` (default weight's).
+
+    tokens: a contiguous list, int32 or int64; one outside the table (-1 for
+    padding) gives a row of zeros.  weight [rows, cols]: fp32 or bf16.
+    """
+    return _done((_binding or _load()).embed(tokens, weight, scale, _dtype(y_dtype, "y_dtype"), out, stream), "quasar_embed")
+
+
+def embed_backward(dy, tokens, rows, *, scale=1.0, dw_dtype=None, out=None, stream=None):
+    """The gradient of ``embed``'s table [rows, cols], whole: ``dw`` in
+    ``dw_dtype`` (default dy's), row v the scaled sum of the rows of dy whose
+    token is v, 0 where there are none.  Sums are in fp32, in an order that the
+    tokens alone determine; rows of dy whose token is outside the table are not
+    read."""
+    return _done((_binding or _load()).embed_backward(dy, tokens, rows, scale, _dtype(dw_dtype, "dw_dtype"), out, stream),
+                 "quasar_embed_backward")
+
+
+# ---- activations kept in 8 bits -----------------------------------------------------
+
+def _act(name, where, first=0):
+    code = ACTS.get(name)
+    if code is None or code < first:
+        raise ValueError(f"{where}: act must be one of {', '.join(list(ACTS)[first:])}")
+    return code
+
+
+def checkpoint_rows(x, *, act="none", y_dtype=None, want_y=None, out=None, stream=None):
+    """Keeps x [rows, cols] (fp32 or bf16) for the backward pass in 8 bits: ``q``
+    (torch.float8_e4m3fn) and ``exponent`` (uint8 [rows, ceil(cols / 128)]), of
+    which q * 2^(exponent - 127) is x to four significant bits, stretch of 128
+    columns by stretch.  NaN and infinity are kept as NaN.
+
+    The same pass makes ``y`` = act(x) from x itself (act: "none", "relu", "silu"
+    or "gelu"; ``want_y``: default with an act), in ``y_dtype`` (default x's);
+    ``out["y"]`` may be x itself.
+    """
+    code = _act(act, "checkpoint_rows")
+    return _done((_binding or _load()).checkpoint_rows(x, code, _dtype(y_dtype, "y_dtype"), code > 0 if want_y is None else want_y,
+                                                      out, stream), "quasar_checkpoint_rows")
+
+
+def checkpoint_backward(dy, q, exponent, *, act, dx_dtype=None, out=None, stream=None):
+    """``dx`` = dy * act'(k) with k the activations that ``checkpoint_rows`` kept, in
+    ``dx_dtype`` (default dy's); ``out["dx"]`` may be dy itself."""
+    return _done((_binding or _load()).checkpoint_backward(dy, q, exponent, _act(act, "checkpoint_backward", 1),
+                                                          _dtype(dx_dtype, "dx_dtype"), out, stream),
+                 "quasar_checkpoint_backward")
+
+
+def linear_weight_grad(dy, q, exponent, *, dw_dtype="fp32", out=None, stream=None):
+    """``dw`` [out, in] = dy^T k, the gradient of a linear layer's weight, with k
+    [tokens, in] the input that ``checkpoint_rows`` kept and dy [tokens, out]
+    (fp32 or bf16) its output's gradient; in fp32, or rounded once to bf16."""
+    return _done((_binding or _load()).linear_weight_grad(dy, q, exponent, _dtype(dw_dtype, "dw_dtype"), out, stream),
+                 "quasar_linear_weight_grad")

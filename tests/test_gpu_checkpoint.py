@@ -1,0 +1,316 @@
+"""Activations kept in 8 bits: checkpoint_rows bit for bit against its definition,
+the activations' gradients and the linear layer's weight gradient against theirs
+in 64 bits.
+
+Tolerances, u = 2^-24, v = 2^-8.  GELU's tail at |x| = t is off by its fit and a
+dozen roundings (16 u) and by the rounding of the exponential's argument t^2 / 2
+(1.2 t^2 u); SiLU by 8 u.  Their derivatives: each term as much, and its products.
+The hardware's exponential gives 0 for results below 2^-126 (at -87.5, say, where
+it is 9.98e-39): what it is multiplied by there, |x| at most, is lost with it.
+The weight gradient: its products are exact, a sum of n terms is off by n steps
+of 2 u at most, however a matrix instruction adds them."""
+import math
+
+import pytest
+import torch
+
+from paper_2608_13966_amd import ops as O
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+U, V = 2.0 ** -24, 2.0 ** -8
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+E4M3 = torch.float8_e4m3fn
+INF, NAN = float("inf"), float("nan")
+
+
+def gen(shape, dtype, seed, scale=1.0, pad=0, off=0):
+    """Normal values with rows and columns of other sizes among them, in rows of a wider buffer."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    t = torch.randn(shape, generator=g, device=DEV) * scale
+    t *= torch.exp2(torch.randint(-6, 7, (shape[0], 1), generator=g, device=DEV).float())
+    t *= torch.where(torch.rand(1, shape[1], generator=g, device=DEV) < 0.05, 30.0, 1.0)
+    buf = torch.empty(shape[0] * (shape[1] + pad) + off, device=DEV, dtype=dtype)
+    v = buf[off:].view(shape[0], shape[1] + pad)[:, :shape[1]]
+    v.copy_(t)
+    return v
+
+
+def rnd(dtype):
+    return V if dtype is torch.bfloat16 else U
+
+
+def kept_ref(x):
+    """(q as numbers, exponents) by the definition, in 64 bits."""
+    rows, cols = x.shape
+    n = -(-cols // 128)
+    b = torch.nn.functional.pad(x.double(), (0, n * 128 - cols)).view(rows, n, 128)
+    top = torch.where(b.isfinite(), b.abs(), 0.0).amax(2)
+    m, e = torch.frexp(top / 448)
+    e = torch.where(m == 0.5, e - 1, e)
+    e = torch.where(top == 0, -120, e).clamp(-120, 120)
+    v = b * torch.exp2(-e.double())[:, :, None]
+    step = torch.exp2(v.abs().clamp_min(2.0 ** -6).log2().floor() - 3)
+    q = torch.where(v.isfinite(), torch.round(v / step) * step, NAN)
+    q = torch.where((e == 120)[:, :, None], q.clamp(-240, 240), q)  # 256 * 2^120 would not be finite
+    return q.view(rows, n * 128)[:, :cols], (e + 127).to(torch.uint8)
+
+
+def back(q, e):
+    return q.double() * torch.exp2(e.double() - 127).repeat_interleave(128, 1)[:, :q.shape[1]]
+
+
+def lost(x):
+    """What an exponential below 2^-126 that is given as 0 takes away."""
+    return (x.abs() + 1) * 2.0 ** -126
+
+
+def act_ref(act, x):
+    """act(x) and how far the kernels' may be from it."""
+    x = x.double()
+    if act == "relu":
+        return torch.where(x < 0, 0.0, x), torch.zeros_like(x)
+    if act == "silu":
+        y = x * torch.sigmoid(x)
+        return y, 8 * U * y.abs() + lost(x)
+    tail = 0.5 * torch.special.erfc(x.abs() / math.sqrt(2))
+    y = torch.where(x > 0, x - x * tail, x * tail)
+    return y, (x.abs() * tail) * (16 + 1.2 * x * x) * U + 2 * U * y.abs() + lost(x)
+
+
+def grad_ref(act, x):
+    if act == "relu":
+        return (x > 0).double(), torch.zeros_like(x)
+    if act == "silu":
+        s, r = torch.sigmoid(x), torch.sigmoid(-x)
+        return s + x * s * r, (10 * s + 16 * x.abs() * s * r) * U + lost(x)
+    tail = 0.5 * torch.special.erfc(x.abs() / math.sqrt(2))
+    dens = x * torch.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+    cdf = torch.where(x > 0, 1 - tail, tail)
+    return cdf + dens, (tail * (16 + 1.2 * x * x) + dens.abs() * (8 + 1.2 * x * x) + 4 * cdf) * U + lost(x)
+
+
+SHAPES = [(1, 1), (3, 7), (2, 127), (5, 128), (4, 129), (17, 300), (33, 1000), (8, 4096), (3, 14337), (1, 40000), (70000, 3)]
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("xt,yt,act", [("bf16", None, "none"), ("fp32", None, "gelu"), ("bf16", None, "gelu"), ("bf16", "fp32", "silu"),
+                                       ("fp32", "bf16", "relu")])
+def test_rows(shape, xt, yt, act):
+    x = gen(shape, DT[xt], 1, pad=shape[1] % 4, off=shape[1] % 3)
+    o = O.checkpoint_rows(x, act=act, y_dtype=yt)
+    q, e = kept_ref(x)
+    assert o["q"].dtype is E4M3 and torch.equal(o["exponent"], e)
+    assert torch.equal(o["q"].double(), q)
+    k = back(o["q"], e)  # four significant bits, or 2^-10 of the stretch's scale
+    f = torch.exp2(e.double() - 127).repeat_interleave(128, 1)[:, :shape[1]]
+    assert ((k - x.double()).abs() <= torch.maximum(x.double().abs() * 2.0 ** -4, f * 2.0 ** -10)).all()
+    if act == "none":
+        assert o["y"] is None
+        same = O.checkpoint_rows(x, want_y=True)
+        assert torch.equal(same["y"], x) and torch.equal(same["q"].view(torch.uint8), o["q"].view(torch.uint8))
+    else:
+        y, tol = act_ref(act, x)
+        assert o["y"].dtype is DT[yt or xt]
+        assert ((o["y"].double() - y).abs() <= tol + rnd(o["y"].dtype) * (y.abs() + tol)).all()
+
+
+def test_rows_at_the_edges():
+    """The exponent where the largest value is 448 times a power of two or next to it, at both ends of the range, and in
+    stretches of zeros; halfway values go to the even code."""
+    tops = []
+    for p in (-149, -126, -125, -113, -112, -111, -20, 0, 1, 100, 127):
+        for m in (1.0, 1.75, 1.75 - 2.0 ** -23, 1.75 + 2.0 ** -23, 2 - 2.0 ** -23):
+            v = math.ldexp(m, p)
+            tops.append(v)
+    tops.append(0.0)
+    x = torch.zeros(len(tops), 256, device=DEV)
+    x[:, 77] = torch.tensor(tops, dtype=torch.float64).float().to(DEV)
+    x[:, 78] = -x[:, 77] / 3
+    x[:, 200] = 1.0 + 2.0 ** -4                                  # between 1 and 1.125
+    x[:, 201] = 1.0 + 3 * 2.0 ** -4
+    x[:, 202] = -448.0
+    o = O.checkpoint_rows(x)
+    q, e = kept_ref(x)
+    assert torch.equal(o["exponent"], e) and torch.equal(o["q"].double(), q)
+    assert (o["exponent"][-1, 0] == 7) and (e[:, 1] == 127).all()
+    assert (o["q"][:, 200].float() == 1.0).all() and (o["q"][:, 201].float() == 1.25).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_what_is_not_finite_stays_by_itself(dtype):
+    x = gen((5, 400), dtype, 1)
+    x[0, 3], x[1, 130], x[2, 399], x[3, :128] = NAN, INF, -INF, NAN
+    x[4, 256:384] = INF
+    o = O.checkpoint_rows(x, act="relu")
+    q, e = kept_ref(x)
+    assert torch.equal(o["exponent"], e)
+    bad = ~x.isfinite()
+    assert o["q"].float()[bad].isnan().all() and torch.equal(o["q"].double()[~bad], q[~bad])
+    assert torch.equal(o["y"].isnan(), x.isnan()) and o["y"][1, 130] == INF and o["y"][2, 399] == 0
+
+
+def test_outputs_in_wider_buffers_and_in_place():
+    x = gen((9, 300), torch.bfloat16, 1, pad=3, off=1)
+    want = O.checkpoint_rows(x, act="gelu")
+    qb, eb = torch.full((9, 307), 7, device=DEV, dtype=torch.uint8), torch.full((9, 5), 9, device=DEV, dtype=torch.uint8)
+    y = x.clone()
+    o = O.checkpoint_rows(y, act="gelu", out={"q": qb[:, 2:302].view(E4M3), "exponent": eb[:, 1:4], "y": y})
+    assert o["y"] is y and torch.equal(y, want["y"])
+    assert torch.equal(qb[:, 2:302], want["q"].view(torch.uint8)) and torch.equal(eb[:, 1:4], want["exponent"])
+    assert (qb[:, :2] == 7).all() and (qb[:, 302:] == 7).all() and (eb[:, [0, 4]] == 9).all()
+    dy = gen((9, 300), torch.bfloat16, 2)
+    dx = O.checkpoint_backward(dy, o["q"], o["exponent"], act="gelu")["dx"]
+    assert torch.equal(dx, O.checkpoint_backward(dy, want["q"], want["exponent"], act="gelu")["dx"])
+    g = dy.clone()
+    assert O.checkpoint_backward(g, o["q"], o["exponent"], act="gelu", out={"dx": g})["dx"] is g and torch.equal(g, dx)
+
+
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+@pytest.mark.parametrize("gt,xt,act", [("bf16", None, "gelu"), ("fp32", None, "gelu"), ("bf16", "fp32", "silu"), ("fp32", "bf16", "relu"),
+                                       ("fp32", None, "silu")])
+def test_backward(shape, gt, xt, act):
+    kept = O.checkpoint_rows(gen(shape, torch.float32, 1, 0.3))
+    dy = gen(shape, DT[gt], 2, pad=shape[1] % 4, off=shape[1] % 3)
+    o = O.checkpoint_backward(dy, kept["q"], kept["exponent"], act=act, dx_dtype=xt)
+    assert o["dx"].dtype is DT[xt or gt]
+    d, tol = grad_ref(act, back(kept["q"], kept["exponent"]))
+    want, tol = dy.double() * d, dy.double().abs() * (tol + 2 * U * d.abs())
+    assert ((o["dx"].double() - want).abs() <= tol + rnd(o["dx"].dtype) * (want.abs() + tol) + 1e-37).all()
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu"])
+def test_derivatives_over_the_whole_range(act):
+    """Every E4M3 number at every exponent, as far as it is finite in fp32: the derivative is finite, and NaN only for the
+    NaN codes."""
+    codes = torch.arange(256, device=DEV, dtype=torch.uint8).repeat(241, 1)
+    e = torch.arange(7, 248, device=DEV, dtype=torch.uint8)[:, None].repeat(1, 2)
+    q = codes.view(E4M3)
+    dx = O.checkpoint_backward(torch.ones(241, 256, device=DEV), q, e, act=act)["dx"].double()
+    x = back(q, e)
+    nan, kept = x.isnan(), ~(x.abs() >= 2.0 ** 128)
+    assert torch.equal(dx.isnan()[kept], nan[kept])
+    nan |= ~kept
+    assert dx[~nan].isfinite().all()
+    d, tol = grad_ref(act, torch.where(nan, 0.0, x.clamp(-1e4, 1e4)))
+    assert ((dx - d).abs() <= tol + 2 * U * d.abs())[~nan].all()
+
+
+def test_derivatives_against_differences():
+    x = torch.linspace(-6, 6, 241, dtype=torch.float64)
+    for act in ("silu", "gelu"):
+        d, _ = grad_ref(act, x)
+        diff = (act_ref(act, x + 1e-5)[0] - act_ref(act, x - 1e-5)[0]) / 2e-5
+        assert (d - diff).abs().max() < 1e-9, act  # h^2 of the third derivative, 1e-16 / h
+
+
+# ---- the weight gradient ------------------------------------------------------------
+
+def check_weight(dy, q, e, dw):
+    k, g = back(q, e), dy.double()
+    want, size = g.t().contiguous() @ k, g.abs().t().contiguous() @ k.abs()
+    n = dy.shape[0] * (3 if dy.dtype is torch.float32 else 1) + 4
+    tol = 2 * n * U * size
+    assert dw.shape == want.shape
+    bad = ~((dw.double() - want).abs() <= tol + rnd(dw.dtype) * (want.abs() + tol) + 1e-37)
+    assert not bad.any(), (int(bad.sum()), float((dw.double() - want).abs().max()))
+
+
+TNK = [(1, 1, 1), (1, 64, 64), (3, 7, 5), (63, 64, 129), (64, 65, 64), (65, 200, 300), (130, 128, 128), (200, 129, 72), (777, 100, 1544),
+       (1000, 256, 256), (4097, 64, 40), (256, 1030, 520)]
+
+
+@pytest.mark.parametrize("t,n,k", TNK)
+@pytest.mark.parametrize("gt,wt", [("bf16", "fp32"), ("fp32", "fp32"), ("bf16", "bf16"), ("fp32", "bf16")])
+def test_weight_grad(t, n, k, gt, wt):
+    kept = O.checkpoint_rows(gen((t, k), torch.bfloat16, 1))
+    dy = gen((t, n), DT[gt], 2, 1e-3, pad=n % 4, off=n % 3)
+    out = {"dw": torch.full((n, k), NAN, device=DEV, dtype=DT[wt])}
+    o = O.linear_weight_grad(dy, kept["q"], kept["exponent"], dw_dtype=wt, out=out)
+    assert o["dw"] is out["dw"]
+    check_weight(dy, kept["q"], kept["exponent"], o["dw"])
+    again = O.linear_weight_grad(dy, kept["q"], kept["exponent"], dw_dtype=wt)
+    assert torch.equal(again["dw"], o["dw"])
+
+
+@pytest.mark.parametrize("t,n,k", [(300, 2048, 4096), (1, 4096, 4096), (513, 4096, 4104), (1025, 2056, 8192), (4100, 1000, 2000),
+                                   (127, 5000, 3333)])
+@pytest.mark.parametrize("gt", ["bf16", "fp32"])
+def test_large_weight_grad(t, n, k, gt):
+    kept = O.checkpoint_rows(gen((t, k), torch.bfloat16, 1))
+    dy = gen((t, n), DT[gt], 2, 1e-3)
+    check_weight(dy, kept["q"], kept["exponent"], O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"])
+
+
+@pytest.mark.parametrize("t,n,k", [(100, 72, 136), (700, 4096, 4096)])
+@pytest.mark.parametrize("pads", [(1, 3, 1), (8, 8, 0), (13, 5, 2)])
+def test_weight_grad_strides(t, n, k, pads):
+    """Rows of wider buffers, which hold NaN; what is beside the result stays."""
+    gp, qp, ep = pads
+    kept = O.checkpoint_rows(gen((t, k), torch.bfloat16, 1))
+    blocks = -(-k // 128)
+    dyb = torch.full((t, n + gp), NAN, device=DEV, dtype=torch.bfloat16)
+    qb, eb = torch.full((t, k + qp), 0x7f, device=DEV, dtype=torch.uint8), torch.full((t, blocks + ep), 255, device=DEV, dtype=torch.uint8)
+    dyb[:, :n], qb[:, :k], eb[:, :blocks] = gen((t, n), torch.bfloat16, 2), kept["q"].view(torch.uint8), kept["exponent"]
+    dwb = torch.full((n, k + gp), 7.0, device=DEV)
+    dy, q, e, dw = dyb[:, :n], qb[:, :k].view(E4M3), eb[:, :blocks], dwb[:, :k]
+    O.linear_weight_grad(dy, q, e, out={"dw": dw})
+    check_weight(dy, q, e, dw)
+    assert (dwb[:, k:] == 7).all()
+
+
+@pytest.mark.parametrize("gt", ["bf16", "fp32"])
+@pytest.mark.parametrize("n,k", [(300, 200), (4096, 4096)])
+def test_one_hot_tokens_read_what_was_kept(gt, n, k):
+    """dy with one 1 a row: the gradient's rows are the activations that were kept, bit for bit."""
+    t = 130
+    kept = O.checkpoint_rows(gen((t, k), torch.bfloat16, 1))
+    dy = torch.zeros(t, n, device=DEV, dtype=DT[gt])
+    at = torch.randperm(n, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV)[:t]
+    dy[torch.arange(t, device=DEV), at] = 1.0
+    dw = O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"]
+    assert torch.equal(dw[at].double(), back(kept["q"], kept["exponent"]))
+    assert int(dw.count_nonzero()) == int((kept["q"].float() != 0).sum())
+
+
+@pytest.mark.parametrize("n,k", [(300, 200), (4096, 4096)])
+def test_fp32_gradients_are_taken_whole(n, k):
+    """One token, x = 1: dweight is dy itself, all 24 bits of it; and infinity and NaN."""
+    x = torch.ones(1, k, device=DEV)
+    kept = O.checkpoint_rows(x)
+    dy = gen((1, n), torch.float32, 1)
+    dy[0, 5], dy[0, 6], dy[0, 7], dy[0, 8] = INF, NAN, 3.4028234663852886e38, -1e-30
+    dw = O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"]
+    assert torch.equal(dw.nan_to_num(12.5), dy.nan_to_num(12.5)[0][:, None].expand(n, k))
+
+
+@pytest.mark.parametrize("gt", ["bf16", "fp32"])
+@pytest.mark.parametrize("t,n,k", [(70, 200, 300), (191, 4096, 4096)])
+def test_what_is_not_finite_reaches_its_row_and_column(gt, t, n, k):
+    x = gen((t, k), torch.bfloat16, 1)
+    x[x == 0] = 1.0
+    kept = O.checkpoint_rows(x)
+    dy = gen((t, n), DT[gt], 2)
+    want = O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"]
+    dy[t - 1, n - 2] = INF
+    x[3, k - 1] = NAN
+    kept = O.checkpoint_rows(x)
+    dw = O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"]
+    q = kept["q"].float()[t - 1]
+    row = torch.where(q == 0, NAN, torch.copysign(torch.full_like(q, INF), q))
+    row[k - 1] = NAN
+    assert torch.equal(dw[n - 2].nan_to_num(0.5), row.nan_to_num(0.5)) and dw[:, k - 1].isnan().all()
+    rest = torch.ones(n, device=DEV, dtype=torch.bool)
+    rest[n - 2] = False
+    assert torch.equal(dw[rest, :k - 1], want[rest, :k - 1])
+
+
+def test_no_tokens():
+    q, e = torch.empty(0, 300, device=DEV, dtype=torch.uint8).view(E4M3), torch.empty(0, 3, device=DEV, dtype=torch.uint8)
+    out = {"dw": torch.full((40, 300), 7.0, device=DEV)}
+    dw = O.linear_weight_grad(torch.empty(0, 40, device=DEV), q, e, out=out)["dw"]
+    assert (dw == 0).all()
+    o = O.checkpoint_rows(torch.empty(0, 300, device=DEV), act="gelu")
+    assert o["q"].shape == (0, 300) and o["exponent"].shape == (0, 3) and o["y"].shape == (0, 300)
+    assert O.checkpoint_backward(torch.empty(0, 300, device=DEV), q, e, act="relu")["dx"].shape == (0, 300)

@@ -1,0 +1,166 @@
+"""embed and its gradient against their definitions in 64 bits.
+
+Tolerances, u = 2^-24, v = 2^-8: a looked-up value is a product (u) and its
+rounding; a gradient's row of c terms c additions, a product and its rounding, in
+any order within (c + 1) u of the sum of the terms' sizes."""
+import pytest
+import torch
+
+from paper_2608_13966_amd import ops as O
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda"
+U, V = 2.0 ** -24, 2.0 ** -8
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+def gen(shape, dtype, seed, pad=0, off=0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    buf = torch.full((shape[0] * (shape[1] + pad) + off,), float("nan"), device=DEV, dtype=dtype)
+    t = buf[off:].view(shape[0], shape[1] + pad)[:, :shape[1]]
+    t.copy_(torch.randn(shape, generator=g, device=DEV))
+    return t
+
+
+def draw(n, rows, kind, seed=0, dtype=torch.int64):
+    """Token lists: uniform; a few values; one value; sorted; with tokens that are none; each row once."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    if kind == "once":
+        t = torch.randperm(rows, generator=g, device=DEV)[:n]
+    else:
+        t = torch.randint(0, {"few": min(3, rows), "one": 1}.get(kind, rows), (n,), generator=g, device=DEV)
+    if kind == "one":
+        t += rows - 1
+    if kind == "sorted":
+        t = t.sort()[0]
+    if kind == "none":
+        r = torch.rand(n, generator=g, device=DEV)
+        t = torch.where(r < 0.2, -1, torch.where(r < 0.3, rows, torch.where(r < 0.35, 2 ** 31 - 1, t)))
+        t = torch.where(r > 0.98, -2 ** 31, t)
+    return t.to(dtype)
+
+
+def rnd(dtype):
+    return V if dtype is torch.bfloat16 else U
+
+
+def check_lookup(tok, w, scale, y):
+    ok = (tok >= 0) & (tok < w.shape[0])
+    want = torch.where(ok[:, None], w.double()[torch.where(ok, tok, 0).long()] * scale, 0.0)
+    assert y.shape == want.shape
+    assert ((y.double() - want).abs() <= want.abs() * (rnd(y.dtype) + 1.01 * U) + 1e-38).all()
+    assert (y[~ok] == 0).all()
+
+
+@pytest.mark.parametrize("rows,cols,n", [(1, 1, 1), (5, 3, 17), (300, 64, 40), (77, 65, 9), (50, 128, 33), (40, 200, 5), (40, 257, 6),
+                                         (99, 1000, 70), (64, 1025, 3), (31, 4096, 50), (9, 5001, 11)])
+@pytest.mark.parametrize("wt,yt,it", [("bf16", None, torch.int64), ("fp32", "bf16", torch.int32), ("bf16", "fp32", torch.int32),
+                                      ("fp32", None, torch.int64)])
+def test_lookup(rows, cols, n, wt, yt, it):
+    w = gen((rows, cols), DT[wt], 1, pad=cols % 5, off=cols % 3)
+    for kind in ("uniform", "none"):
+        tok = draw(n, rows, kind, 2, it)
+        o = O.embed(tok, w, scale=1.5, y_dtype=yt)
+        assert o["y"].dtype is DT[yt or wt]
+        check_lookup(tok, w, 1.5, o["y"])
+
+
+def test_lookup_into_a_wider_buffer():
+    w, tok = gen((20, 300), torch.bfloat16, 1), draw(37, 20, "none", 3)
+    buf = torch.full((37 * 311 + 5,), 7.0, device=DEV)
+    y = buf[5:].view(37, 311)[:, :300]
+    o = O.embed(tok, w, scale=-2.0, y_dtype="fp32", out={"y": y})
+    assert o["y"] is y
+    check_lookup(tok, w, -2.0, y)
+    assert (buf[:5] == 7).all() and (buf[5:].view(37, 311)[:, 300:] == 7).all()
+
+
+def check_grad(dy, tok, rows, scale, dw):
+    ok = (tok >= 0) & (tok < rows)
+    idx = tok[ok].long()
+    terms = dy[ok].double() * scale
+    want = torch.zeros(rows, dy.shape[1], device=DEV, dtype=torch.float64).index_add_(0, idx, terms)
+    size = torch.zeros_like(want).index_add_(0, idx, terms.abs())
+    count = torch.bincount(idx, minlength=rows)[:, None]
+    assert dw.shape == want.shape
+    e = (count + 2) * U * size
+    bad = ~((dw.double() - want).abs() <= e + rnd(dw.dtype) * (want.abs() + e) + 1e-38)
+    assert not bad.any(), int(bad.sum())
+    assert (dw[count[:, 0] == 0] == 0).all()
+
+
+KINDS = ["uniform", "few", "one", "sorted", "none", "once"]
+
+
+@pytest.mark.parametrize("rows,cols,n", [(1, 1, 1), (1, 70, 300), (5, 3, 17), (300, 64, 40), (77, 65, 9), (513, 130, 1025),
+                                         (40, 257, 2000), (5000, 100, 4096), (20000, 9, 4100), (700, 1000, 700), (99, 4096, 64)])
+@pytest.mark.parametrize("kind", KINDS)
+def test_grad(rows, cols, n, kind):
+    n = min(n, rows) if kind == "once" else n
+    for i, (gt, wt, it) in enumerate([("bf16", None, torch.int64), ("fp32", "bf16", torch.int32), ("fp32", None, torch.int64),
+                                      ("bf16", "fp32", torch.int32)]):
+        dy = gen((n, cols), DT[gt], i, pad=cols % 5, off=cols % 3)
+        tok = draw(n, rows, kind, 10 + i, it)
+        ok = (tok >= 0) & (tok < rows)
+        dy[~ok] = float("nan")  # reaches nothing
+        out = {"dw": torch.full((rows, cols), float("nan"), device=DEV, dtype=DT[wt or gt])}
+        o = O.embed_backward(dy, tok, rows, scale=1.5, dw_dtype=wt, out=out)
+        assert o["dw"] is out["dw"]
+        check_grad(dy, tok, rows, 1.5, o["dw"])
+        again = O.embed_backward(dy, tok, rows, scale=1.5, dw_dtype=wt)
+        assert torch.equal(again["dw"], o["dw"])
+
+
+@pytest.mark.parametrize("rows,cols,n,kind", [(160000, 16, 70000, "uniform"), (3, 40, 300000, "few"), (131072, 8, 20000, "one"),
+                                              (1 << 20, 2, 300000, "none"), (1 << 19, 3, 17, "once"), (2, 513, 16385, "few")])
+def test_grad_of_long_lists(rows, cols, n, kind):
+    """Several chunks of the sort, two and three passes, rows that thousands of stretches share."""
+    dy, tok = gen((n, cols), torch.float32, 1), draw(n, rows, kind, 2)
+    check_grad(dy, tok, rows, 0.5, O.embed_backward(dy, tok, rows, scale=0.5)["dw"])
+
+
+def test_grad_into_a_wider_buffer_with_a_used_workspace():
+    dy, tok = gen((500, 300), torch.bfloat16, 1), draw(500, 60, "none", 3)
+    dy = dy.nan_to_num()
+    want = O.embed_backward(dy, tok, 60)["dw"]
+    buf = torch.full((60 * 311 + 5,), 7.0, device=DEV, dtype=torch.bfloat16)
+    dw = buf[5:].view(60, 311)[:, :300]
+    from paper_2608_13966_amd import ops
+    ws = torch.full((ops.quasar_embed_backward_workspace_bytes(60, 300, 500),), 255, device=DEV, dtype=torch.uint8)
+    for _ in range(2):
+        o = O.embed_backward(dy, tok, 60, out={"dw": dw, "workspace": ws})
+        assert o["workspace"] is ws and torch.equal(dw, want)
+    assert (buf[:5] == 7).all() and (buf[5:].view(60, 311)[:, 300:] == 7).all()
+
+
+def test_no_tokens():
+    dy, tok = torch.empty(0, 33, device=DEV), torch.empty(0, device=DEV, dtype=torch.int64)
+    assert O.embed(tok, torch.ones(5, 33, device=DEV))["y"].shape == (0, 33)
+    out = {"dw": torch.full((5000, 33), 7.0, device=DEV)}
+    assert (O.embed_backward(dy, tok, 5000, out=out)["dw"] == 0).all()
+
+
+def test_nan_stays_in_its_row():
+    dy, tok = torch.ones(200, 80, device=DEV), torch.arange(200, device=DEV) % 50
+    dy[7, 3], dy[9, 4] = float("nan"), float("inf")
+    dw = O.embed_backward(dy, tok, 64)["dw"]
+    assert dw[7, 3].isnan() and dw[9, 4] == float("inf")
+    dw[7, 3] = dw[9, 4] = 4.0
+    assert (dw[:50] == 4).all() and (dw[50:] == 0).all()
+
+
+def test_rows_past_four_gigabytes():
+    """Offsets of the table's and of the gradient's rows past 2^32 bytes."""
+    rows, cols = (1 << 20) + 5, 2200
+    w = torch.zeros(rows, cols, device=DEV, dtype=torch.bfloat16)
+    w[-3:] = gen((3, cols), torch.bfloat16, 1)
+    tok = torch.tensor([rows - 1, rows - 3, 0, rows - 2, rows - 1, rows], device=DEV)
+    check = O.embed(tok, w, scale=2.0)["y"]
+    assert torch.equal(check[[0, 1, 3, 4]], (w[[rows - 1, rows - 3, rows - 2, rows - 1]].float() * 2).bfloat16())
+    assert (check[[2, 5]] == 0).all()
+    dy = gen((6, cols), torch.bfloat16, 2)
+    w.fill_(7.0)
+    dw = O.embed_backward(dy, tok, rows, out={"dw": w})["dw"]
+    assert torch.equal(dw[rows - 3:], torch.stack([dy[1], dy[3], (dy[0].float() + dy[4].float()).bfloat16()]))
+    assert torch.equal(dw[0], dy[2]) and int(dw[1:rows - 3].count_nonzero()) == 0
