@@ -349,7 +349,9 @@ typedef struct {
 
 int quasar_linear_weight_grad(const quasar_weight_grad* a, void* stream);
 int quasar_linear_weight_grad_check(const quasar_weight_grad* a);
-size_t quasar_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols, int32_t dy_dtype);
+/* Device scratch that this call needs (its workspace fields are not looked at): a copy of dy is part of it where the
+ * alignment of dy, its stride or its type ask for one.  0 where it needs none, or for an invalid call. */
+size_t quasar_linear_weight_grad_workspace_bytes(const quasar_weight_grad* a);
 
 #ifdef __cplusplus
 }

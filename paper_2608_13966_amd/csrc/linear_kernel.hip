@@ -802,26 +802,6 @@ __global__ __launch_bounds__(256) void unpack_kernel(Weights w, quasar_linear a,
   }
 }
 
-// 16 bytes per lane from global memory straight into LDS: lane l's go from
-// from + off to to + 16 l (from and to: the same in every lane).  In assembly
-// because the compiler makes every later LDS read wait for all such loads in
-// flight; the kernel counts them itself (no register is written by them).
-__device__ __forceinline__ void load_lds16(const char* from, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory");
-}
-
-// Tile `b` of a grid as (tm, tn): each of the eight XCDs (workgroup b runs on
-// XCD b % 8) takes a stretch of the tiles, eight tiles of tokens wide, so that
-// what its workgroups read together fits its L2.
-__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
-  const int total = tiles_m * tiles_n, q = total >> 3, r = total & 7, xcd = b & 7;
-  const int t = xcd * q + (xcd < r ? xcd : r) + (b >> 3);
-  const int per = 8 * tiles_n, g = t / per, first = g * 8, wide = tiles_m - first < 8 ? tiles_m - first : 8;
-  const int in = t - g * per;
-  tm = first + in % wide;
-  tn = in / wide;
-}
-
 // A workgroup makes 256 tokens x 256 outputs with 8 wavefronts of 128 x 64.
 // Both operands of a step lie in LDS as two halves each (x0: the first 64
 // tokens of every wavefront's 128, r0: the first 32 outputs of its 64, x1 and

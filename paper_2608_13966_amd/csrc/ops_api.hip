@@ -333,27 +333,27 @@ int quasar_checkpoint_backward(const quasar_checkpoint_grad* a, void* stream) {
   return status_of(quasar::launch_checkpoint_backward(*a, reinterpret_cast<hipStream_t>(stream)));
 }
 
-static bool weight_grad_sizes(int64_t tokens, int64_t rows, int64_t cols) {
-  return tokens >= 0 && tokens <= kMaxTokens && rows >= 1 && rows <= kMaxWeight && cols >= 1 && cols <= kMaxWeight;
-}
-
-size_t quasar_linear_weight_grad_workspace_bytes(int64_t tokens, int64_t rows, int64_t cols, int32_t dy_dtype) {
-  size_t bytes;
-  return weight_grad_sizes(tokens, rows, cols) && f32_or_bf16(dy_dtype) &&
-                 quasar::weight_grad_fits(tokens, rows, cols, dy_dtype, bytes) ? bytes : 0;
-}
-
-int quasar_linear_weight_grad_check(const quasar_weight_grad* a) {
+static int check_weight_grad(const quasar_weight_grad* a, size_t& need) {
   if (a == nullptr) return QUASAR_ERR_ARG;
-  if (!weight_grad_sizes(a->tokens, a->rows, a->cols)) return QUASAR_ERR_SHAPE;
+  if (a->tokens < 0 || a->tokens > kMaxTokens || a->rows < 1 || a->rows > kMaxWeight || a->cols < 1 || a->cols > kMaxWeight)
+    return QUASAR_ERR_SHAPE;
   if (!f32_or_bf16(a->dy_dtype) || !f32_or_bf16(a->dweight_dtype)) return QUASAR_ERR_FORMAT;
-  size_t need;
-  if (!quasar::weight_grad_fits(a->tokens, a->rows, a->cols, a->dy_dtype, need)) return QUASAR_ERR_SHAPE;
+  if (!quasar::weight_grad_fits(*a, need)) return QUASAR_ERR_SHAPE;
   if (!a->dweight || (a->tokens > 0 && (!a->dy || !a->q || !a->exponent))) return QUASAR_ERR_ARG;
   QUASAR_TRY(check_matrix(a->dy, a->tokens, a->rows, a->dy_stride, a->dy_dtype));
   QUASAR_TRY(check_matrix(a->q, a->tokens, a->cols, a->q_stride, QUASAR_E4M3));
   QUASAR_TRY(check_matrix(a->exponent, a->tokens, (a->cols + 127) / 128, a->exponent_stride, QUASAR_E4M3));
-  QUASAR_TRY(check_matrix(a->dweight, a->rows, a->cols, a->dweight_stride, a->dweight_dtype));
+  return check_matrix(a->dweight, a->rows, a->cols, a->dweight_stride, a->dweight_dtype);
+}
+
+size_t quasar_linear_weight_grad_workspace_bytes(const quasar_weight_grad* a) {
+  size_t need;
+  return check_weight_grad(a, need) == QUASAR_OK ? need : 0;
+}
+
+int quasar_linear_weight_grad_check(const quasar_weight_grad* a) {
+  size_t need;
+  QUASAR_TRY(check_weight_grad(a, need));
   if (misaligned(a->workspace, 16)) return QUASAR_ERR_ALIGN;
   return need > 0 && (a->workspace == nullptr || a->workspace_bytes < need) ? QUASAR_ERR_WORKSPACE : QUASAR_OK;
 }

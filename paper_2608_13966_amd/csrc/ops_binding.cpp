@@ -621,17 +621,17 @@ py::object linear_weight_grad(const Tensor& dy, const Tensor& q, const Tensor& e
   a.dy_dtype = code(dy, "dy");
   a.dweight_dtype = dw_dtype < 0 ? QUASAR_F32 : dw_dtype;
   const Tensor dw = result(out, "dw", {a.rows, a.cols}, type_of(a.dweight_dtype), dev);
-  a.workspace_bytes = quasar_linear_weight_grad_workspace_bytes(a.tokens, a.rows, a.cols, a.dy_dtype);
-  const Maybe ws = workspace(out, a.workspace_bytes, dev);
   a.dy = ptr(dy);
   a.q = static_cast<uint8_t*>(ptr(q));
   a.exponent = static_cast<uint8_t*>(ptr(e));
   a.dweight = ptr(dw);
-  a.workspace = ptr(ws);
   a.dy_stride = dy.stride(0);
   a.q_stride = q.stride(0);
   a.exponent_stride = e.stride(0);
   a.dweight_stride = dw.stride(0);
+  a.workspace_bytes = quasar_linear_weight_grad_workspace_bytes(&a);
+  const Maybe ws = workspace(out, a.workspace_bytes, dev);
+  a.workspace = ptr(ws);
   const int s = quasar_linear_weight_grad(&a, on.handle(dy));
   if (s != QUASAR_OK) return py::int_(s);
   py::dict o;

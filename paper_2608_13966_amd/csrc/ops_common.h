@@ -360,4 +360,25 @@ __device__ __forceinline__ void activate(float (&v)[N], int act) {
   }
 }
 
+// ---- tiles of large products ----------------------------------------------------
+// 16 bytes per lane from global memory straight into LDS: lane l's go from
+// from + off to to + 16 l (from and to: the same in every lane).  In assembly
+// because the compiler makes every later LDS read wait for all such loads in
+// flight; the kernel counts them itself (no register is written by them).
+__device__ __forceinline__ void load_lds16(const char* from, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory");
+}
+
+// Tile `b` of a grid as (tm, tn): each of the eight XCDs (workgroup b runs on
+// XCD b % 8) takes a stretch of the tiles, eight tiles of tokens wide, so that
+// what its workgroups read together fits its L2.
+__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int total = tiles_m * tiles_n, q = total >> 3, r = total & 7, xcd = b & 7;
+  const int t = xcd * q + (xcd < r ? xcd : r) + (b >> 3);
+  const int per = 8 * tiles_n, g = t / per, first = g * 8, wide = tiles_m - first < 8 ? tiles_m - first : 8;
+  const int in = t - g * per;
+  tm = first + in % wide;
+  tn = in / wide;
+}
+
 }  // namespace quasar

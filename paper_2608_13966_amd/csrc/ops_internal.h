@@ -56,7 +56,7 @@ hipError_t launch_checkpoint(const quasar_checkpoint& a, hipStream_t stream);
 hipError_t launch_checkpoint_backward(const quasar_checkpoint_grad& a, hipStream_t stream);
 
 // weight_grad_kernel.hip
-bool weight_grad_fits(int64_t tokens, int64_t rows, int64_t cols, int dy_dtype, size_t& workspace);
+bool weight_grad_fits(const quasar_weight_grad& a, size_t& workspace);
 hipError_t launch_weight_grad(const quasar_weight_grad& a, hipStream_t stream);
 
 }  // namespace quasar

@@ -162,7 +162,7 @@ def lib():
                 ("quasar_checkpoint_rows", [kp, _vp], C.c_int), ("quasar_checkpoint_rows_check", [kp], C.c_int),
                 ("quasar_checkpoint_backward", [kg, _vp], C.c_int), ("quasar_checkpoint_backward_check", [kg], C.c_int),
                 ("quasar_linear_weight_grad", [wg, _vp], C.c_int), ("quasar_linear_weight_grad_check", [wg], C.c_int),
-                ("quasar_linear_weight_grad_workspace_bytes", [_i64, _i64, _i64, _i32], _sz)):
+                ("quasar_linear_weight_grad_workspace_bytes", [wg], _sz)):
             f = getattr(L, name)
             f.argtypes, f.restype = args, res
         _lib = L
@@ -285,8 +285,8 @@ def quasar_linear_weight_grad_check(a: WeightGrad) -> int:
     return lib().quasar_linear_weight_grad_check(C.byref(a))
 
 
-def quasar_linear_weight_grad_workspace_bytes(tokens: int, rows: int, cols: int, dy_dtype: int) -> int:
-    return int(lib().quasar_linear_weight_grad_workspace_bytes(int(tokens), int(rows), int(cols), int(dy_dtype)))
+def quasar_linear_weight_grad_workspace_bytes(a: WeightGrad) -> int:
+    return int(lib().quasar_linear_weight_grad_workspace_bytes(C.byref(a)))
 
 
 # ---- the calls --------------------------------------------------------------------

@@ -167,13 +167,19 @@ def test_checkpoint_backward_arguments(kw, status):
     assert _checkpoint_backward(**kw) == status
 
 
-def _weight(**kw):
-    t, n, k, dt = kw.get("tokens", 777), kw.get("rows", 200), kw.get("cols", 300), kw.get("dy_dtype", Q.BF16)
-    p = dict(tokens=t, rows=n, cols=k, dy=A, q=A, exponent=A, dweight=A, workspace=A,
-             workspace_bytes=O.quasar_linear_weight_grad_workspace_bytes(t, n, k, dt), dy_stride=n, q_stride=k,
-             exponent_stride=(k + 127) // 128, dweight_stride=k, dy_dtype=dt, dweight_dtype=Q.F32)
+def _weight_args(**kw):
+    t, n, k = kw.get("tokens", 777), kw.get("rows", 200), kw.get("cols", 300)
+    p = dict(tokens=t, rows=n, cols=k, dy=A, q=A, exponent=A, dweight=A, workspace=A, dy_stride=n, q_stride=k,
+             exponent_stride=(k + 127) // 128, dweight_stride=k, dy_dtype=Q.BF16, dweight_dtype=Q.F32)
     p.update(kw)
-    return O.quasar_linear_weight_grad_check(O.WeightGrad(**p))
+    a = O.WeightGrad(**p)
+    if "workspace_bytes" not in kw:
+        a.workspace_bytes = O.quasar_linear_weight_grad_workspace_bytes(a)
+    return a
+
+
+def _weight(**kw):
+    return O.quasar_linear_weight_grad_check(_weight_args(**kw))
 
 
 @pytest.mark.parametrize("kw,status", [
@@ -192,17 +198,26 @@ def test_weight_grad_arguments(kw, status):
 @pytest.mark.parametrize("dt", [Q.BF16, Q.F32])
 def test_weight_grad_workspace(dt):
     some = 0
-    for t, n, k in ((1, 1, 1), (64, 64, 64), (5000, 200, 300), (8192, 14336, 4096), (16384, 256, 256), (333, 4000, 4100)):
-        need = O.quasar_linear_weight_grad_workspace_bytes(t, n, k, dt)
+    for t, n, k in ((1, 1, 1), (64, 64, 64), (5000, 200, 300), (8192, 14336, 4096), (16384, 256, 256), (2000, 4000, 4100)):
         kw = dict(tokens=t, rows=n, cols=k, dy_dtype=dt)
+        need = _weight_args(**kw).workspace_bytes
         assert _weight(**kw) == Q.OK
         if need:
             some += 1
             assert _weight(workspace_bytes=need - 1, **kw) == Q.ERR_WORKSPACE
             assert _weight(workspace=None, **kw) == Q.ERR_WORKSPACE
     assert some > 0
-    assert O.quasar_linear_weight_grad_workspace_bytes(-1, 4, 4, dt) == 0
-    assert O.quasar_linear_weight_grad_workspace_bytes(5, 4, 4, O.E4M3) == 0
+    assert _weight_args(tokens=-1).workspace_bytes == 0 and _weight_args(dy_dtype=O.E4M3).workspace_bytes == 0
+
+
+def test_weight_grad_copies_dy_only_where_it_has_to():
+    kw = dict(tokens=8192, rows=14336, cols=4096)
+    plain, whole = _weight_args(**kw).workspace_bytes, 8192 * 14336 * 2
+    assert plain < whole
+    for more in (dict(dy=A + 2), dict(dy_stride=14337), dict(dy_dtype=Q.F32)):
+        need = _weight_args(**kw, **more).workspace_bytes
+        assert need >= plain + whole
+        assert _weight(**kw, **more) == Q.OK and _weight(**kw, **more, workspace_bytes=plain) == Q.ERR_WORKSPACE
 
 
 def test_wrappers_refuse_before_launch():
