@@ -369,16 +369,23 @@ __device__ __forceinline__ void load_lds16(const char* from, uint32_t off, uint3
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from) : "memory");
 }
 
-// Tile `b` of a grid as (tm, tn): each of the eight XCDs (workgroup b runs on
-// XCD b % 8) takes a stretch of the tiles, eight tiles of tokens wide, so that
-// what its workgroups read together fits its L2.
-__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
-  const int total = tiles_m * tiles_n, q = total >> 3, r = total & 7, xcd = b & 7;
-  const int t = xcd * q + (xcd < r ? xcd : r) + (b >> 3);
+// The place of workgroup b among `total` that are handed out in stretches: each of
+// the eight XCDs (workgroup b runs on XCD b % 8) takes neighbours.
+__device__ __forceinline__ int stretch_of(int b, int total) {
+  const int q = total >> 3, r = total & 7, xcd = b & 7;
+  return xcd * q + (xcd < r ? xcd : r) + (b >> 3);
+}
+// Tile t of tiles_m x tiles_n, counted eight tiles of tokens wide, so that what
+// an XCD's workgroups read together fits its L2.
+__device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int& tm, int& tn) {
   const int per = 8 * tiles_n, g = t / per, first = g * 8, wide = tiles_m - first < 8 ? tiles_m - first : 8;
   const int in = t - g * per;
   tm = first + in % wide;
   tn = in / wide;
+}
+// Tile `b` of a grid as (tm, tn).
+__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
+  tile_at(stretch_of(b, tiles_m * tiles_n), tiles_m, tiles_n, tm, tn);
 }
 
 }  // namespace quasar

@@ -166,42 +166,64 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
 }
 
 // ---- large weights ----------------------------------------------------------------
-// x in bf16 [padded tokens, kp], rows past the last token zero; and what the tile
-// kernel cannot load of dy as it is: all of it in bf16 [padded tokens, np] (fp32: its
-// three parts one after the other, which the products then run through as through
-// three times the tokens), or the last, incomplete step's rows alone.
+// x in bf16 with the tokens of a step side by side, [padded tokens / 64, kp, 64], 0 past
+// the last token: a transposing load has half the rate of a plain one, so what is
+// written out anyway is turned on the way.  And what the tile kernel cannot load of dy
+// as it is: all of it in bf16 [padded tokens, np] (fp32: its three parts one after the
+// other, which the products then run through as through three times the tokens), or the
+// last, incomplete step's rows alone.
 struct Spread {
   uint16_t *x, *dy;
-  int64_t x_pieces, dy_pieces;  // of eight elements
-  int64_t padded, first;        // tokens; the first that dy holds
-  Divide kp8, np8;              // pieces of a row
+  int64_t dy_pieces;  // of eight elements
+  int64_t first;      // the first token that dy holds
+  int steps, kp;
+  unsigned x_groups;  // workgroups that write x: 64 tokens and 128 columns each
+  Divide np8;         // pieces of a row
 };
 
 template <int GT>
 __global__ __launch_bounds__(256) void spread_kernel(quasar_weight_grad a, Spread s) {
-  const int64_t all = s.x_pieces + s.dy_pieces, step = (int64_t)gridDim.x * 256;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += step) {
-    if (i < s.x_pieces) {
-      const int64_t t = i / s.kp8.by;
-      const int k = (int)(i - t * s.kp8.by) * 8;
-      const bool has = t < a.tokens;
-      const uint2 q = load_bytes(has ? a.q + t * a.q_stride + k : a.q, has ? (int)a.cols - k : 0);
-      const uint32_t e = has ? a.exponent[t * a.exponent_stride + (k >> 7)] : 127u;
-      st128(s.x + i * 8, kept_bf16(q, as_f32(e << 23)));
-    } else {
-      const int64_t j = i - s.x_pieces, r = j / s.np8.by, t = r + s.first;
-      const int n = (int)(j - r * s.np8.by) * 8;
-      const bool has = t < a.tokens;
-      Piece<GT> g;
-      g.load(a.dy, has ? t * a.dy_stride + n : 0, has ? (int)a.rows - n : 0);
-      if constexpr (GT == kElemF32) {
-        uint4 p[3];
-        split3(g.f, p);
+  if (blockIdx.x < s.x_groups) {
+    __shared__ __align__(16) uint16_t lds[kStep * 128];
+    const int step = blockIdx.x % (unsigned)s.steps, block = blockIdx.x / (unsigned)s.steps, c = (threadIdx.x & 15) * 8;
+    const int left = (int)a.cols - block * 128 - c;
+    uint2 q[4];
+    uint32_t e[4];
 #pragma unroll
-        for (int q = 0; q < 3; q++) st128(s.dy + (q * s.dy_pieces + j) * 8, p[q]);
-      } else {
-        st128(s.dy + j * 8, make_uint4(g.d[0], g.d[1], g.d[2], g.d[3]));
-      }
+    for (int i = 0; i < 4; i++) {
+      const int64_t t = (int64_t)step * kStep + (threadIdx.x >> 4) + 16 * i;
+      const bool has = t < a.tokens;
+      q[i] = load_bytes(has ? a.q + t * a.q_stride + block * 128 + c : a.q, has ? left : 0);
+      e[i] = has ? a.exponent[t * a.exponent_stride + block] : 127u;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      *reinterpret_cast<uint4*>(lds + spot<128>((threadIdx.x >> 4) + 16 * i, c)) = kept_bf16(q[i], as_f32(e[i] << 23));
+    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = wave_index();
+    uint16_t* const out = s.x + ((int64_t)step * s.kp + block * 128) * kStep;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      const int tile = wave * 2 + (i >> 1), k = tile * 16 + (lane & 15), t0 = (i & 1) * 32;
+      const bf16x8 v = read_tile<128>(lds, t0, tile * 16, lane);
+      if (block * 128 + k < s.kp) st128(out + k * kStep + t0 + 8 * (lane >> 4), __builtin_bit_cast(uint4, v));
+    }
+    return;
+  }
+  const int64_t step = (int64_t)(gridDim.x - s.x_groups) * 256;
+  for (int64_t j = (int64_t)(blockIdx.x - s.x_groups) * 256 + threadIdx.x; j < s.dy_pieces; j += step) {
+    const int64_t r = j / s.np8.by, t = r + s.first;
+    const int n = (int)(j - r * s.np8.by) * 8;
+    const bool has = t < a.tokens;
+    Piece<GT> g;
+    g.load(a.dy, has ? t * a.dy_stride + n : 0, has ? (int)a.rows - n : 0);
+    if constexpr (GT == kElemF32) {
+      uint4 p[3];
+      split3(g.f, p);
+#pragma unroll
+      for (int q = 0; q < 3; q++) st128(s.dy + (q * s.dy_pieces + j) * 8, p[q]);
+    } else {
+      st128(s.dy + j * 8, make_uint4(g.d[0], g.d[1], g.d[2], g.d[3]));
     }
   }
 }
@@ -214,109 +236,130 @@ struct Operands {
   int whole, period, steps;
 };
 
-// A workgroup makes 256 x 256 values of dweight with 8 wavefronts of 128 rows x 64
-// columns, 64 tokens a step.  Both operands of a step lie in LDS as two halves each
-// (g0: the first 64 rows of every wavefront's 128, x0: the first 32 columns of its
-// 64, x1 and g1 the rest), and a step has two phases, each with 32 matrix
-// instructions a wavefront: g0 (x0 x1), g1 (x0 x1).  Two stages; a half is filled again
-// as soon as both halves of the workgroup have read it.
+// In LDS, 16-byte chunk c of x's column m lies at chunk c ^ (m / 2 % 8) of the
+// column's 128 bytes: the 16 columns that an operand read or a store touches at one
+// chunk then lie in 16 different groups of four banks.
+__device__ __forceinline__ int chunk_at(int m, int c) { return m * kStep + 8 * (c ^ ((m >> 1) & 7)); }
+
+// A workgroup makes 256 x 256 values of dweight with 8 wavefronts of 64 rows x 128
+// columns, 64 tokens a step.  Both operands of a step lie in LDS as two halves each, g0
+// and x0 the first 128 rows and columns (of dy whole lines of memory), 32 and 64 of
+// them a wavefront's, g1 and x1 the rest; and a step has two phases, each with 32
+// matrix instructions a wavefront: x0 (g0 g1), x1 (g0 g1).  dy is read by transposing loads,
+// twice as dear as plain ones, hence the wavefront's shape, and the reads are spread
+// evenly: phase 0 reads x0 and g1, phase 1 x1 and the next step's g0.  (Both operands
+// through transposing loads, in tiles of 128 x 64: 862 us, not @; LDS was busy all the
+// time.)  Two stages; a half is filled again as soon as all have read it.
 //
-// The wavefronts of a SIMD work in turn: those of wm = 1 run one barrier behind, so
+// The wavefronts of a SIMD work in turn: those of wk = 1 run one barrier behind, so
 // that while one multiplies the other reads its next operands.  Barriers 2p and 2p + 1
-// end the reading and the multiplying of phase p for wm = 0, 2p + 1 and 2p + 2 for wm
+// end the reading and the multiplying of phase p for wk = 0, 2p + 1 and 2p + 2 for wk
 // = 1; a wavefront has its operands before it comes to the barrier that ends the
 // reading.  Hence
-//  - a half filled in phase p may be one whose last reads were in phase p - 1
-//    (g0, x0 and x1, read in a step's phase 0, are filled for the step after the
-//    next in its phase 1; g1 in the next step's phase 0);
-//  - what phase p reads has to have landed for every wavefront's own loads
-//    before the barrier that ends its reading of phase p - 1: with two loads a
-//    half, "at most 8 outstanding" then, either phase.
+//  - a half filled in phase p may be one whose last reads were in phase p - 1: x0 and
+//    g1, read in a step's phase 0, are filled for the step after the next in its phase
+//    1; x1 in the next step's phase 0; g0, read in the phase 1 before, in phase 0;
+//  - what phase p reads has to have landed for every wavefront's own loads before the
+//    barrier that ends its reading of phase p - 1: it was filled in phase p - 3, and
+//    p - 2 and p - 1 have issued four loads each since: "at most 8 outstanding".
 // Past the last step the loads repeat it, so that the counts hold.
-constexpr int kSlabPitch = 64 + 4, kSlab = 32 * kSlabPitch;
+constexpr int kSlabPitch = 128 + 4, kSlab = 16 * kSlabPitch;
 __global__ __launch_bounds__(512, 2) void weight_grad_tile_kernel(quasar_weight_grad a, Operands op, int tiles_n, int tiles_k,
-                                                                  int steps_per, float* part) {
-  constexpr int kHalf = kStep * 128, kStage = 4 * kHalf;  // elements; halves g0, x0, x1, g1
+                                                                  int whole, int shared, int splits, int steps_per, float* part) {
+  constexpr int kHalf = kStep * 128, kStage = 4 * kHalf;  // elements; halves g0, g1, x0, x1
   __shared__ __align__(16) uint16_t lds[2 * kStage];
   static_assert(8 * kSlab * 4 <= (int)sizeof(lds), "the epilogue's stage fits");
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void*)lds;
   const int lane = threadIdx.x & 63, wave = wave_index();
-  const int wm = wave >> 2, wn = wave & 3;
-  int tn, tk;
-  const int split = blockIdx.x / (unsigned)(tiles_n * tiles_k);
-  tile_of(blockIdx.x - split * tiles_n * tiles_k, tiles_n, tiles_k, tn, tk);
-  const int n0 = tn * 256, k0 = tk * 256;
+  const int wk = wave >> 2, wn = wave & 3;
+  // the first `whole` tiles are a workgroup's each, the last `shared` ones that of `splits`
+  int tile, split = 0, tn, tk;
+  if ((int)blockIdx.x < whole) {
+    tile = stretch_of(blockIdx.x, whole);
+    steps_per = op.steps;
+    part = nullptr;
+  } else {
+    const int u = stretch_of(blockIdx.x - whole, shared * splits);
+    split = u / shared;
+    tile = whole + (u - split * shared);
+    if (part) part += ((int64_t)(tile - whole) * splits + split) * (256 * 256);
+  }
+  tile_at(tile, tiles_n, tiles_k, tn, tk);
+  const int64_t n0 = (int64_t)tn * 256, k0 = (int64_t)tk * 256;
   const int first = split * steps_per, left = op.steps - first, steps = left < steps_per ? left : steps_per;
 
-  // each wavefront loads 8 rows of a half, 4 an instruction; columns past the matrix repeat its last ones
-  uint32_t col[4][2], row[2];
+  // each wavefront loads 8 rows of a half of dy, 4 an instruction, and 16 columns of a half of x, 8 an
+  // instruction; rows and columns past the matrix repeat its last ones
+  uint32_t row[2], g_col[2][2], x_at[2][2];
 #pragma unroll
   for (int i = 0; i < 2; i++) {
     const int t = wave * 8 + i * 4 + (lane >> 4);
     const int f = (t & 3) | ((t >> 1) & 4), c = ((((lane & 15) >> 1) ^ f) << 4) + (lane & 1) * 8;
+    const int m = wave * 16 + i * 8 + (lane >> 3);
     row[i] = (uint32_t)t;
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-      const int n = n0 + (c >> 6) * 128 + h * 64 + (c & 63), k = k0 + (c >> 5) * 64 + h * 32 + (c & 31);
-      col[h == 0 ? 0 : 3][i] = 2u * (uint32_t)(n < op.np - 8 ? n : op.np - 8);
-      col[h == 0 ? 1 : 2][i] = 2u * (uint32_t)(k < op.kp - 8 ? k : op.kp - 8);
+      const int n = (int)n0 + h * 128 + c, k = (int)k0 + h * 128 + m;
+      g_col[h][i] = 2u * (uint32_t)(n < op.np - 8 ? n : op.np - 8);
+      x_at[h][i] = 2u * (uint32_t)((k < op.kp ? k : op.kp - 1) * kStep + 8 * ((lane & 7) ^ ((m >> 1) & 7)));
     }
   }
-  const auto fill = [&](int h, int step) {
+  const auto fill_g = [&](int h, int step) {
     const uint32_t to = lds0 + ((step & 1) * kStage + h * kHalf + wave * 8 * 128) * 2;
     const int s = first + (step < steps ? step : steps - 1);
-    const char* from;
-    uint32_t pitch;
-    if (h == 0 || h == 3) {
-      const bool rest = s >= op.whole;
-      pitch = 2u * (uint32_t)(rest ? op.rest_stride : op.dy_stride);
-      from = reinterpret_cast<const char*>(rest ? op.rest : op.dy) + (int64_t)(rest ? s - op.whole : s) * kStep * pitch;
-    } else {
-      int sx = s;
-      if (sx >= op.period) sx -= op.period;
-      if (sx >= op.period) sx -= op.period;
-      pitch = 2u * (uint32_t)op.kp;
-      from = reinterpret_cast<const char*>(op.x) + (int64_t)sx * kStep * pitch;
-    }
+    const bool rest = s >= op.whole;
+    const uint32_t pitch = 2u * (uint32_t)(rest ? op.rest_stride : op.dy_stride);
+    const char* const from = reinterpret_cast<const char*>(rest ? op.rest : op.dy) + (int64_t)(rest ? s - op.whole : s) * kStep * pitch;
 #pragma unroll
-    for (int i = 0; i < 2; i++) load_lds16(from, __umul24(row[i], pitch) + col[h][i], to + i * 4 * 128 * 2);
+    for (int i = 0; i < 2; i++) load_lds16(from, __umul24(row[i], pitch) + g_col[h][i], to + i * 4 * 128 * 2);
   };
-  f32x4 acc[8][4];
+  const auto fill_x = [&](int h, int step) {
+    const uint32_t to = lds0 + ((step & 1) * kStage + (2 + h) * kHalf + wave * 16 * kStep) * 2;
+    int s = first + (step < steps ? step : steps - 1);
+    if (s >= op.period) s -= op.period;
+    if (s >= op.period) s -= op.period;
+    const char* const from = reinterpret_cast<const char*>(op.x) + (int64_t)s * op.kp * (2 * kStep);
 #pragma unroll
-  for (int i = 0; i < 8; i++)
+    for (int i = 0; i < 2; i++) load_lds16(from, x_at[h][i], to + i * 8 * kStep * 2);
+  };
+  f32x4 acc[4][8];
 #pragma unroll
-    for (int j = 0; j < 4; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  bf16x8 fg[4][2], fx[2][2][2];
-  const auto read_g = [&](int h, int stage) {
-    const uint16_t* p = lds + stage * kStage + (h ? 3 : 0) * kHalf;
+  for (int i = 0; i < 4; i++)
 #pragma unroll
-    for (int i = 0; i < 4; i++)
+    for (int j = 0; j < 8; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  bf16x8 fg[2][2][2], next[2][2], fx[4][2];
+  const auto read_g = [&](int h, int stage, bf16x8 (&to)[2][2]) {
+    const uint16_t* p = lds + stage * kStage + h * kHalf;
 #pragma unroll
-      for (int k = 0; k < 2; k++) fg[i][k] = read_tile<128>(p, 32 * k, wm * 64 + 16 * i, lane);
+    for (int i = 0; i < 2; i++)
+#pragma unroll
+      for (int k = 0; k < 2; k++) to[i][k] = read_tile<128>(p, 32 * k, wn * 32 + 16 * i, lane);
   };
   const auto read_x = [&](int h, int stage) {
-    const uint16_t* p = lds + stage * kStage + (h ? 2 : 1) * kHalf;
+    const uint16_t* p = lds + stage * kStage + (2 + h) * kHalf;
 #pragma unroll
-    for (int j = 0; j < 2; j++)
+    for (int j = 0; j < 4; j++)
 #pragma unroll
-      for (int k = 0; k < 2; k++) fx[h][j][k] = read_tile<128>(p, 32 * k, wn * 32 + 16 * j, lane);
+      for (int k = 0; k < 2; k++)
+        fx[j][k] = __builtin_bit_cast(
+            bf16x8, *reinterpret_cast<const uint4*>(p + chunk_at(wk * 64 + 16 * j + (lane & 15), 4 * k + (lane >> 4))));
   };
-  // ends the phase's reading, multiplies by both halves of x, ends the phase
-  const auto multiply = [&](int hg) {
+  // ends the phase's reading, multiplies by both halves of dy, ends the phase
+  const auto multiply = [&](int hx) {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int hx = 0; hx < 2; hx++)
+    for (int hg = 0; hg < 2; hg++)
 #pragma unroll
       for (int k = 0; k < 2; k++)
 #pragma unroll
-        for (int i = 0; i < 4; i++)
+        for (int i = 0; i < 2; i++)
 #pragma unroll
-          for (int j = 0; j < 2; j++)
-            acc[hg * 4 + i][hx * 2 + j] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(fg[i][k], fx[hx][j][k], acc[hg * 4 + i][hx * 2 + j], 0, 0, 0);
+          for (int j = 0; j < 4; j++)
+            acc[hg * 2 + i][hx * 4 + j] =
+                __builtin_amdgcn_mfma_f32_16x16x32_bf16(fg[hg][i][k], fx[j][k], acc[hg * 2 + i][hx * 4 + j], 0, 0, 0);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_barrier();
@@ -324,66 +367,96 @@ __global__ __launch_bounds__(512, 2) void weight_grad_tile_kernel(quasar_weight_
   };
   const auto landed8 = [] { asm volatile("s_waitcnt vmcnt(8)" ::: "memory"); };
 
-  fill(0, 0);
-  fill(1, 0);
-  fill(2, 0);
-  fill(3, 0);
-  fill(0, 1);
-  fill(1, 1);
-  fill(2, 1);
+  fill_g(0, 0);
+  fill_x(0, 0);
+  fill_g(1, 0);
+  fill_x(1, 0);
+  fill_g(0, 1);
+  fill_x(0, 1);
+  fill_g(1, 1);
   landed8();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
-  if (wm == 1) __builtin_amdgcn_s_barrier();
+  read_g(0, 0, fg[0]);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();  // g0 may be filled again
+  asm volatile("" ::: "memory");
+  if (wk == 1) __builtin_amdgcn_s_barrier();
   for (int s = 0; s < steps; s++) {
     const int stage = s & 1;
-    read_g(0, stage);
     read_x(0, stage);
-    read_x(1, stage);
-    fill(3, s + 1);
+    read_g(1, stage, fg[1]);
+    fill_x(1, s + 1);
+    fill_g(0, s + 2);
     landed8();
     multiply(0);
-    read_g(1, stage);
-    fill(0, s + 2);
-    fill(1, s + 2);
-    fill(2, s + 2);
+    read_x(1, stage);
+    read_g(0, stage ^ 1, next);
+    fill_x(0, s + 2);
+    fill_g(1, s + 2);
     landed8();
     multiply(1);
-  }
-  if (wm == 0) __builtin_amdgcn_s_barrier();
-  // LDS is the epilogue's once every wavefront's loads have landed
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-  __syncthreads();
-  // 32 rows at a time through the wavefront's part of LDS, so that a lane stores eight neighbours
-  float* const st = reinterpret_cast<float*>(lds) + wave * kSlab;
-  const int c = (lane & 7) * 8;
-  const int64_t k = k0 + wn * 64 + c, nw = n0 + wm * 128;
-  const int some = (int)(a.cols - k < 0 ? 0 : a.cols - k < 8 ? a.cols - k : 8);
-#pragma unroll
-  for (int s = 0; s < 4; s++) {
 #pragma unroll
     for (int i = 0; i < 2; i++)
 #pragma unroll
-      for (int j = 0; j < 4; j++)
+      for (int k = 0; k < 2; k++) fg[0][i][k] = next[i][k];
+  }
+  if (wk == 0) __builtin_amdgcn_s_barrier();
+  // LDS is the epilogue's once every wavefront's loads have landed
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  // 16 rows at a time through the wavefront's part of LDS, so that a lane stores eight neighbours
+  float* const st = reinterpret_cast<float*>(lds) + wave * kSlab;
+  const int c = (lane & 15) * 8;
+  const int64_t k = k0 + (c >> 6) * 128 + wk * 64 + (c & 63);
+  const int some = (int)(a.cols - k < 0 ? 0 : a.cols - k < 8 ? a.cols - k : 8);
 #pragma unroll
-        for (int e = 0; e < 4; e++)
-          st[(16 * i + 4 * (lane >> 4) + e) * kSlabPitch + 16 * j + (lane & 15)] = acc[2 * s + i][j][e];
+  for (int i = 0; i < 4; i++) {
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+#pragma unroll
+      for (int e = 0; e < 4; e++) st[(4 * (lane >> 4) + e) * kSlabPitch + 16 * j + (lane & 15)] = acc[i][j][e];
     wave_lds_fence();
 #pragma unroll
-    for (int p = 0; p < 32; p += 8) {
-      const int r = p + (lane >> 3);
-      const int64_t n = nw + 32 * s + r;
+    for (int p = 0; p < 16; p += 4) {
+      const int r = p + (lane >> 4);
+      const int n = (i >> 1) * 128 + wn * 32 + (i & 1) * 16 + r;
       float v[8];
 #pragma unroll
       for (int q = 0; q < 8; q++) v[q] = st[r * kSlabPitch + c + q];
-      if (n >= a.rows) continue;
       if (part)
-        store_piece<false>(part, ((int64_t)split * a.rows + n) * part_pitch(a.cols) + k, v, some);
-      else
-        store_piece(a.dweight, n * a.dweight_stride + k, v, some, a.dweight_dtype == QUASAR_BF16);
+        store_piece<false>(part, n * 256 + (k - k0), v, 8);
+      else if (n0 + n < a.rows)
+        store_piece(a.dweight, (n0 + n) * a.dweight_stride + k, v, some, a.dweight_dtype == QUASAR_BF16);
     }
     wave_lds_fence();
   }
+}
+
+// dweight from the shares of the tiles from `whole` on, [tiles][splits][256][256], 32 workgroups a tile.
+__global__ __launch_bounds__(256) void weight_grad_tile_join_kernel(quasar_weight_grad a, const float* part, int tiles_n, int tiles_k,
+                                                                    int whole, int splits) {
+  const int tile = blockIdx.x >> 5, i = (blockIdx.x & 31) * 256 + threadIdx.x;
+  int tn, tk;
+  tile_at(whole + tile, tiles_n, tiles_k, tn, tk);
+  const int64_t n = (int64_t)tn * 256 + (i >> 5), k = (int64_t)tk * 256 + (i & 31) * 8;
+  const int left = (int)(a.cols - k < 8 ? a.cols - k : 8);
+  if (n >= a.rows || left <= 0) return;
+  part += (int64_t)tile * splits * (256 * 256) + i * 8;
+  float v[8] = {};
+  for (int s = 0; s < splits; s += 8) {  // eight shares in flight at once
+    Piece<kElemF32> p[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+      if (s + j < splits) p[j].load(part, (int64_t)(s + j) * (256 * 256), 8);
+#pragma unroll
+    for (int j = 0; j < 8; j++)
+      if (s + j < splits) {
+#pragma unroll
+        for (int q = 0; q < 8; q++) v[q] += p[j].get(q);
+      }
+  }
+  store_piece(a.dweight, n * a.dweight_stride + k, v, left, a.dweight_dtype == QUASAR_BF16);
 }
 
 // dweight from the sums of `splits` shares of the tokens, eight values a thread.
@@ -418,6 +491,7 @@ struct Choice {
   int64_t tiles_n, tiles;
   int64_t padded, np, kp, parts;   // the tile kernel's tokens and columns, and the parts of dy
   int64_t rest;                    // the tokens from here on are copied
+  int64_t whole;                   // the tiles of one workgroup each
   size_t x_bytes, dy_bytes, bytes;  // workspace: x, dy, and all of it with the shares' sums
 };
 
@@ -439,7 +513,19 @@ Choice choose(const quasar_weight_grad& a) {
     c.rest = direct(a) ? tokens / kStep * kStep : 0;
     c.dy_bytes = (size_t)(c.parts * (c.padded - c.rest) * c.np * 2);
     all = c.parts * steps;
-    while (c.splits < 32 && 2 * c.tiles * c.splits <= kCUs && all >= 2 * c.splits * 16) c.splits *= 2;
+    // tiles for whole rounds of the CUs are a workgroup's each; those past them are shared out where that takes less
+    // time, of a step (1.55 us), a round (5) and the shares' sums, written and read at 5.2 TB/s (and 6 for the launch)
+    c.whole = c.tiles / kCUs * kCUs;
+    const int64_t rest = c.tiles - c.whole;
+    double least = 0.0;
+    for (int s = 1; rest > 0 && s <= 32 && s <= all; s++) {
+      const int64_t rounds = (rest * s + kCUs - 1) / kCUs;
+      const double us = rounds * (5.0 + (double)((all + s - 1) / s) * 1.55) + (s == 1 ? 0.0 : 6.0 + (double)(rest * s) * (2 * 256 * 256 * 4 / 5.2e6));
+      if (s == 1 || us < least) {
+        least = us;
+        c.splits = s;
+      }
+    }
   } else {
     c.tile = tiles_of(128) >= kCUs && a.dy_dtype == QUASAR_BF16 ? 128 : 64;
     c.tiles = tiles_of(c.tile);
@@ -449,7 +535,8 @@ Choice choose(const quasar_weight_grad& a) {
   c.steps = (int)((all + c.splits - 1) / c.splits);
   c.splits = (int)((all + c.steps - 1) / c.steps);
   c.bytes = c.x_bytes + c.dy_bytes;
-  if (c.splits > 1) c.bytes += (size_t)c.splits * (size_t)rows * (size_t)part_pitch(cols) * 4;
+  if (c.splits > 1)
+    c.bytes += (size_t)c.splits * (c.tile == 256 ? (size_t)(c.tiles - c.whole) * 256 * 256 : (size_t)rows * (size_t)part_pitch(cols)) * 4;
   return c;
 }
 
@@ -463,20 +550,25 @@ hipError_t launch_large(const quasar_weight_grad& a, const Choice& c, float* par
   char* const ws = reinterpret_cast<char*>(a.workspace);
   const int steps = (int)(c.padded / kStep);
   const int64_t copied = c.padded - c.rest;
-  Spread s{reinterpret_cast<uint16_t*>(ws), reinterpret_cast<uint16_t*>(ws + c.x_bytes), c.padded * (c.kp / 8), copied * (c.np / 8),
-           c.padded, c.rest, Divide((uint32_t)(c.kp / 8)), Divide((uint32_t)(c.np / 8))};
-  const int64_t groups = (s.x_pieces + s.dy_pieces + 255) / 256, most = 32 * kCUs;
-  const dim3 grid((unsigned)(groups < most ? groups : most));
+  const int64_t x_groups = steps * ((c.kp + 127) / 128), pieces = copied * (c.np / 8), most = 32 * kCUs;
+  Spread s{reinterpret_cast<uint16_t*>(ws), reinterpret_cast<uint16_t*>(ws + c.x_bytes), pieces, c.rest, steps, (int)c.kp,
+           (unsigned)x_groups, Divide((uint32_t)(c.np / 8))};
+  const int64_t dy_groups = (pieces + 255) / 256;
+  const dim3 grid((unsigned)(x_groups + (dy_groups < most ? dy_groups : most)));
   if (a.dy_dtype == QUASAR_F32)
     spread_kernel<kElemF32><<<grid, dim3(256), 0, stream>>>(a, s);
   else
     spread_kernel<kElemBF16><<<grid, dim3(256), 0, stream>>>(a, s);
-  const hipError_t e = hipGetLastError();
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   Operands op{reinterpret_cast<const uint16_t*>(a.dy), s.dy, s.x, (int)(c.rest > 0 ? a.dy_stride : 0), (int)c.np, (int)c.kp,
               (int)c.np, (int)(c.rest / kStep), steps, (int)c.parts * steps};
-  weight_grad_tile_kernel<<<dim3((unsigned)(c.tiles * c.splits)), dim3(512), 0, stream>>>(
-      a, op, (int)c.tiles_n, (int)(c.tiles / c.tiles_n), c.steps, part);
+  const int tiles_n = (int)c.tiles_n, tiles_k = (int)(c.tiles / c.tiles_n), whole = (int)c.whole, shared = (int)(c.tiles - c.whole);
+  weight_grad_tile_kernel<<<dim3((unsigned)(whole + shared * c.splits)), dim3(512), 0, stream>>>(a, op, tiles_n, tiles_k, whole, shared,
+                                                                                                 c.splits, c.steps, part);
+  e = hipGetLastError();
+  if (e != hipSuccess || !part) return e;
+  weight_grad_tile_join_kernel<<<dim3((unsigned)shared * 32), dim3(256), 0, stream>>>(a, part, tiles_n, tiles_k, whole, c.splits);
   return hipGetLastError();
 }
 
@@ -485,22 +577,22 @@ hipError_t launch_large(const quasar_weight_grad& a, const Choice& c, float* par
 bool weight_grad_fits(const quasar_weight_grad& a, size_t& workspace) {
   const Choice c = choose(a);
   workspace = c.bytes;
-  return c.tiles * c.splits <= most_groups(c.tile == 256 ? 512 : 256) && (c.splits == 1 || a.rows * (part_pitch(a.cols) / 8) <= 256 * most_groups(256));
+  if (c.tile == 256 && c.padded / kStep * ((c.kp + 127) / 128) + 32 * kCUs > most_groups(256)) return false;
+  if (c.tile == 256) return c.tiles <= most_groups(512) - 32 * kCUs;
+  return c.tiles * c.splits <= most_groups(256) && (c.splits == 1 || a.rows * (part_pitch(a.cols) / 8) <= 256 * most_groups(256));
 }
 
 hipError_t launch_weight_grad(const quasar_weight_grad& a, hipStream_t stream) {
   const Choice c = choose(a);
   float* const part = c.splits > 1 ? reinterpret_cast<float*>(reinterpret_cast<char*>(a.workspace) + c.x_bytes + c.dy_bytes) : nullptr;
-  hipError_t e = hipSuccess;
-  if (c.tile == 256)
-    e = launch_large(a, c, part, stream);
-  else if (a.dy_dtype == QUASAR_F32)
+  if (c.tile == 256) return launch_large(a, c, part, stream);
+  if (a.dy_dtype == QUASAR_F32)
     launch_tiles<kElemF32, 64>(a, c, part, stream);
   else if (c.tile == 64)
     launch_tiles<kElemBF16, 64>(a, c, part, stream);
   else
     launch_tiles<kElemBF16, 128>(a, c, part, stream);
-  if (e == hipSuccess) e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !part) return e;
   const int64_t n = a.rows * (part_pitch(a.cols) / 8);
   weight_grad_join_kernel<<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream>>>(a, part, c.splits);
