@@ -60,10 +60,11 @@ struct Sort {
   const uint2* from;     // later ones (token, position) pairs
   uint2* to;
   uint32_t* counts;      // [chunks][bins]
+  uint32_t* next;        // the same of the next pass, or NULL
   uint8_t* touched;      // [rows], 1 where a token has the row
   int index_bits, tokens, chunk;
   uint32_t rows;
-  int shift, bins;
+  int shift, width, bins;
 };
 
 __device__ __forceinline__ uint2 pair_at(const Sort& s, int i) {
@@ -71,15 +72,22 @@ __device__ __forceinline__ uint2 pair_at(const Sort& s, int i) {
   return make_uint2(token_at(s.index, s.index_bits, i, s.rows), (uint32_t)i);
 }
 
-// How often each digit occurs in a chunk; and on the first pass all rows are marked as untouched.
-__global__ __launch_bounds__(kThreads) void count_kernel(Sort s) {
+// n pieces of 16 zeros, by thread i of `all`
+__device__ __forceinline__ void clear(void* p, int64_t n, int64_t i, int64_t all) {
+  for (; i < n; i += all) reinterpret_cast<uint4*>(p)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// How often each digit of the first pass occurs in a chunk.  All rows are marked as
+// untouched, and the counts of the later passes (`later` of them) are cleared: the
+// pass before counts its keys where it brings them, by integer atomics, whose order
+// does not matter.
+__global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int later) {
   __shared__ uint32_t bin[kMaxBins];
   for (int i = threadIdx.x; i < s.bins; i += kThreads) bin[i] = 0;
-  if (!s.from) {
-    const uint32_t quads = (s.rows + 15) / 16;  // the array is whole pieces of 16
-    for (uint32_t i = blockIdx.x * kThreads + threadIdx.x; i < quads; i += gridDim.x * kThreads)
-      reinterpret_cast<uint4*>(s.touched)[i] = make_uint4(0u, 0u, 0u, 0u);
-  }
+  const int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
+  const int64_t each = (int64_t)gridDim.x * s.bins;
+  clear(s.touched, ((int64_t)s.rows + 15) / 16, i0, all);  // the array is whole pieces of 16
+  for (int64_t i = i0; i < later * each; i += all) s.counts[each + i] = 0;
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * s.chunk;
   const int end = (int)(first + s.chunk < s.tokens ? first + s.chunk : s.tokens);
@@ -89,10 +97,46 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Sort s) {
   for (int i = threadIdx.x; i < s.bins; i += kThreads) s.counts[(int64_t)blockIdx.x * s.bins + i] = bin[i];
 }
 
+// How many of the wavefront's keys so far have this lane's digit, those of lower
+// lanes among them; `count` has them by digit.
+__device__ __forceinline__ uint32_t rank_of(uint32_t key, int bins, bool has, uint32_t* count) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t d = has ? key & (bins - 1) : 0;
+  uint64_t same = __ballot(has);  // the lanes with the same digit
+  for (int b = 1; b < bins; b *= 2) {
+    const uint64_t set = __ballot((d & b) != 0);
+    same &= (d & b) ? set : ~set;
+  }
+  const uint32_t below = __popcll(same & (((uint64_t)1 << lane) - 1));
+  const uint32_t rank = has ? count[d] + below : 0;
+  wave_lds_fence();
+  if (has && below == 0) count[d] += __popcll(same);
+  wave_lds_fence();
+  return rank;
+}
+
+// The sum of n over the lower lanes of a workgroup of WAVES wavefronts (s: WAVES
+// numbers of LDS).
+template <int WAVES>
+__device__ __forceinline__ uint32_t sum_before(uint32_t n, uint32_t* s) {
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  uint32_t run = n;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) {
+    const uint32_t up = __shfl_up(run, o);
+    if (lane >= o) run += up;
+  }
+  if (lane == 63) s[wave] = run;
+  __syncthreads();
+  run -= n;
+  for (int w = 0; w < wave; w++) run += s[w];
+  return run;
+}
+
 // Brings the keys of a chunk to their places: those of smaller digits come first,
 // then those of the same digit in earlier chunks, then in earlier wavefronts and
 // rounds of this one.
-__global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
+__device__ __forceinline__ void place(const Sort& s, int chunks) {
   constexpr int kWaves = kThreads / 64, kKeys = kRound / kThreads;  // keys a lane holds
   __shared__ uint32_t base[kMaxBins], count[kWaves][kMaxBins], sums[kWaves];
   const int lane = threadIdx.x & 63, wave = wave_index(), bins = s.bins;
@@ -105,7 +149,7 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
     before[j] = all[j] = 0;
     if (d < bins) {
 #pragma unroll 8
-      for (int c = 0; c < (int)gridDim.x; c++) {
+      for (int c = 0; c < chunks; c++) {
         const uint32_t n = s.counts[(int64_t)c * bins + d];
         before[j] += c < (int)blockIdx.x ? n : 0;
         all[j] += n;
@@ -113,17 +157,7 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
     }
     mine += all[j];
   }
-  // digits before this thread's: over the wavefront, then the wavefronts
-  uint32_t run = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const uint32_t up = __shfl_up(run, o);
-    if (lane >= o) run += up;
-  }
-  if (lane == 63) sums[wave] = run;
-  __syncthreads();
-  uint32_t at = run - mine;
-  for (int w = 0; w < wave; w++) at += sums[w];
+  uint32_t at = sum_before<kWaves>(mine, sums);
 #pragma unroll
   for (int j = 0; j < kOwn; j++) {
     const int d = threadIdx.x * kOwn + j;
@@ -145,18 +179,7 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
         key[j] = pair_at(s, (int)i);
         if (!s.from && key[j].x < s.rows) s.touched[key[j].x] = 1;
       }
-      const uint32_t d = has ? (key[j].x >> s.shift) & (bins - 1) : 0;
-      // the lanes with the same digit
-      uint64_t same = __ballot(has);
-      for (int b = 1; b < bins; b *= 2) {
-        const uint64_t set = __ballot((d & b) != 0);
-        same &= (d & b) ? set : ~set;
-      }
-      const uint32_t below = __popcll(same & (((uint64_t)1 << lane) - 1));
-      rank[j] = has ? count[wave][d] + below : 0;
-      wave_lds_fence();
-      if (has && below == 0) count[wave][d] += __popcll(same);
-      wave_lds_fence();
+      rank[j] = rank_of(key[j].x >> s.shift, bins, has, count[wave]);
     }
     __syncthreads();
     // count: the keys of the wavefronts before; base: past this round
@@ -174,9 +197,74 @@ __global__ __launch_bounds__(kThreads) void place_kernel(Sort s) {
 #pragma unroll
     for (int j = 0; j < kKeys; j++) {
       const int64_t i = i0 + wave * (64 * kKeys) + j * 64 + lane;
-      if (i < end) s.to[count[wave][(key[j].x >> s.shift) & (bins - 1)] + rank[j]] = key[j];
+      if (i < end) {
+        const uint32_t to = count[wave][(key[j].x >> s.shift) & (bins - 1)] + rank[j];
+        s.to[to] = key[j];
+        if (s.next) atomicAdd(s.next + (int64_t)(to / (uint32_t)s.chunk) * bins + ((key[j].x >> (s.shift + s.width)) & (bins - 1)), 1u);
+      }
     }
     __syncthreads();
+  }
+}
+
+// All passes at once, for a list that one workgroup holds.
+constexpr int kSmall = 4096, kSmallRows = 1 << 18;
+__global__ __launch_bounds__(1024) void sort_small_kernel(Sort s, int passes) {
+  constexpr int kWaves = 16, kKeys = kSmall / 1024;
+  __shared__ uint2 list[kSmall];
+  __shared__ uint32_t count[kWaves][kMaxBins], sums[kWaves];
+  const int lane = threadIdx.x & 63, wave = wave_index(), bins = s.bins;
+  uint2 key[kKeys];
+#pragma unroll
+  for (int j = 0; j < kKeys; j++) {
+    const int i = wave * (64 * kKeys) + j * 64 + lane;
+    key[j] = i < s.tokens ? pair_at(s, i) : make_uint2(0u, 0u);
+  }
+  clear(s.touched, ((int64_t)s.rows + 15) / 16, threadIdx.x, 1024);
+  __syncthreads();
+  for (int p = 0; p < passes; p++) {
+    const int shift = p * s.width;
+    for (int i = threadIdx.x; i < kWaves * kMaxBins; i += 1024) (&count[0][0])[i] = 0;
+    __syncthreads();
+    uint32_t rank[kKeys];
+#pragma unroll
+    for (int j = 0; j < kKeys; j++) {
+      const bool has = wave * (64 * kKeys) + j * 64 + lane < s.tokens;
+      rank[j] = rank_of(key[j].x >> shift, bins, has, count[wave]);
+    }
+    __syncthreads();
+    uint32_t all = 0;
+    if (threadIdx.x < kMaxBins) {
+#pragma unroll
+      for (int w = 0; w < kWaves; w++) {
+        const uint32_t n = count[w][threadIdx.x];
+        count[w][threadIdx.x] = all;
+        all += n;
+      }
+    }
+    const uint32_t at = sum_before<kWaves>(all, sums);
+    if (threadIdx.x < kMaxBins) {
+#pragma unroll
+      for (int w = 0; w < kWaves; w++) count[w][threadIdx.x] += at;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kKeys; j++) {
+      if (wave * (64 * kKeys) + j * 64 + lane < s.tokens) list[count[wave][(key[j].x >> shift) & (bins - 1)] + rank[j]] = key[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kKeys; j++) {
+      const int i = wave * (64 * kKeys) + j * 64 + lane;
+      if (i < s.tokens) key[j] = list[i];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < kKeys; j++) {
+    const int i = wave * (64 * kKeys) + j * 64 + lane;
+    if (i >= s.tokens) continue;
+    s.to[i] = key[j];
+    if (key[j].x < s.rows) s.touched[key[j].x] = 1;
   }
 }
 
@@ -188,7 +276,8 @@ struct Grad {
   const uint8_t* touched;
   float* part;            // [stretches][2][pitch]: a stretch's sums for a row begun before it, and for one that goes on
   int64_t dy_stride, dw_stride;
-  int64_t sum_groups;     // workgroups that sum; the rest write zeros
+  int64_t sum_groups, sum_sets;    // workgroups that sum; the rest write zeros, from this set of rows on
+  int64_t join_groups, join_sets;  // likewise of the last launch
   int tokens, stretch, stretches, cols, pitch;
   uint32_t rows;
   float scale;
@@ -209,26 +298,48 @@ __device__ __forceinline__ void put_row(const Grad& g, uint32_t row, int c, cons
     put_row<false>(g, row, c, v);
 }
 
-constexpr int kZeroRows = 8;  // rows that L lanes look at for zeros
+constexpr int kZeroRows = 8;  // rows that a wavefront looks at for zeros at a time
+
+// Zeros in the rows of set `set` of kZeroRows that no token has, by a wavefront: 16 bytes a lane, neighbours.
+__device__ __forceinline__ void zero_rows(const Grad& g, int64_t set, int64_t end) {
+  if (set >= end) return;
+  const int lane = threadIdx.x & 63, size = g.dw_bf16 ? 2 : 4, bytes = g.cols * size;
+  const int64_t r0 = set * kZeroRows;
+  if (r0 >= g.rows) return;
+  const uint2 t = *reinterpret_cast<const uint2*>(g.touched + r0);  // whole pieces of 16 are there
+#pragma unroll 1
+  for (int i = 0; i < kZeroRows; i++) {
+    if (((i < 4 ? t.x : t.y) >> (8 * (i & 3)) & 0xffu) || r0 + i >= g.rows) continue;
+    char* const p = reinterpret_cast<char*>(g.dw) + (r0 + i) * g.dw_stride * size;
+    for (int b = lane * 16; b < bytes; b += 1024) {
+      if (b + 16 <= bytes) {
+        st16_any(p + b, make_uint4(0u, 0u, 0u, 0u));
+      } else {
+        for (int e = b; e < bytes; e += size) {
+          if (size == 2)
+            *reinterpret_cast<uint16_t*>(p + e) = 0;
+          else
+            *reinterpret_cast<uint32_t*>(p + e) = 0u;
+        }
+      }
+    }
+  }
+}
+
+// Workgroups past the first `chunks` write zeros, up to set g.sum_sets.
+__global__ __launch_bounds__(kThreads) void place_kernel(Sort s, int chunks, Grad g) {
+  if ((int)blockIdx.x < chunks)
+    place(s, chunks);
+  else
+    zero_rows(g, (int64_t)(blockIdx.x - chunks) * (kThreads / 64) + wave_index(), g.sum_sets);
+}
 
 // L lanes (8 columns each) take a stretch of the sorted list; the next rows are in flight meanwhile.
 template <int GT, int L>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per) {
   const int lane = threadIdx.x & (L - 1);
   if (blockIdx.x >= g.sum_groups) {
-    const int64_t u = (blockIdx.x - g.sum_groups) * (kThreads / L) + threadIdx.x / L;
-    const uint32_t set = per.of((uint32_t)u), part = (uint32_t)u - set * per.by;
-    const int64_t r0 = (int64_t)set * kZeroRows;
-    const int c = (int)part * (8 * L) + lane * 8;
-    const float zero[8] = {};
-    if (c >= g.cols) return;
-    if (r0 >= g.rows) return;
-    uint2 t = *reinterpret_cast<const uint2*>(g.touched + r0);  // whole pieces of 16 are there
-#pragma unroll
-    for (int i = 0; i < kZeroRows; i++) {
-      const uint32_t has = (i < 4 ? t.x : t.y) >> (8 * (i & 3)) & 0xffu;
-      if (!has && r0 + i < g.rows) put_row(g, (uint32_t)r0 + i, c, zero);
-    }
+    zero_rows(g, g.sum_sets + (blockIdx.x - g.sum_groups) * (kThreads / 64) + wave_index(), g.join_sets);
     return;
   }
   const int64_t u = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
@@ -283,23 +394,41 @@ template <int L>
 __global__ __launch_bounds__(kThreads) void embed_join_kernel(Grad g, Divide per) {
   constexpr int kShares = kThreads / L;
   __shared__ float lds[kShares > 1 ? (kShares - 1) * L * 8 : 1];
+  if (blockIdx.x >= g.join_groups) {
+    zero_rows(g, g.join_sets + (blockIdx.x - g.join_groups) * (kThreads / 64) + wave_index(), (int64_t)g.rows);
+    return;
+  }
   const int lane = threadIdx.x & (L - 1), share = threadIdx.x / L;
   const uint32_t st = per.of(blockIdx.x), part = blockIdx.x - st * per.by;
   const int c = (int)part * (8 * L) + lane * 8;
   const int64_t p0 = (int64_t)st * g.stretch, p1 = p0 + g.stretch;
   if (p1 >= g.tokens) return;
-  const uint32_t key = g.sorted[p1].x;
-  if (key >= g.rows || g.sorted[p1 - 1].x != key) return;                     // none goes on
-  if (g.sorted[p0].x == key && p0 > 0 && g.sorted[p0 - 1].x == key) return;  // it began before
+  const uint32_t key = g.sorted[p1].x, last = g.sorted[p1 - 1].x, first = g.sorted[p0].x, before = p0 > 0 ? g.sorted[p0 - 1].x : g.rows;
+  if (key >= g.rows || last != key) return;         // none goes on
+  if (first == key && before == key) return;        // it began before
+  // how many stretches follow that begin with it: 64 looked at together
+  int more = 1;
+  for (int64_t s = (int64_t)st + 1; ; s += 64) {
+    const int64_t mine = s + (threadIdx.x & 63);
+    const uint64_t same = __ballot(mine < g.stretches && g.sorted[mine * g.stretch].x == key);
+    const int run = ~same ? __builtin_ctzll(~same) : 64;
+    more += run;
+    if (run < 64) break;
+  }
   float sum[8] = {};
-  const auto add = [&](int64_t stretch, int slot) {
-    float v[8];
-    load_floats(g.part, (stretch * 2 + slot) * g.pitch + c, g.pitch - c, false, v);
+  constexpr int kAhead = 4;
+  for (int i = share; i < more; i += kShares * kAhead) {  // its sums: slot 1 of the stretch where it begins, slot 0 of the others
+    Piece<kElemF32> v[kAhead];
 #pragma unroll
-    for (int i = 0; i < 8; i++) sum[i] += v[i];
-  };
-  if (share == 0) add(st, 1);
-  for (int64_t s = (int64_t)st + 1 + share; s < g.stretches && g.sorted[s * g.stretch].x == key; s += kShares) add(s, 0);
+    for (int j = 0; j < kAhead; j++) {
+      const int at = i + j * kShares;
+      v[j].load(g.part, (((int64_t)st + at) * 2 + (at == 0)) * g.pitch + c, at < more ? g.pitch - c : 0);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; j++)
+#pragma unroll
+      for (int k = 0; k < 8; k++) sum[k] += v[j].get(k);
+  }
   if (share > 0) {
 #pragma unroll
     for (int i = 0; i < 8; i++) lds[((share - 1) * 8 + i) * L + lane] = sum[i];
@@ -322,6 +451,9 @@ hipError_t with_lanes(int64_t cols, F f) {
   return f(integral_constant<int, 64>());
 }
 
+constexpr int64_t kPlaceZeros = 48 << 20, kJoinZeros = 32 << 20;  // bytes
+
+int64_t least_of(int64_t a, int64_t b) { return a < b ? a : b; }
 int64_t round16(int64_t n) { return (n + 15) & ~(int64_t)15; }
 
 // The sort's passes and where the scratch memory's parts lie.
@@ -345,22 +477,26 @@ struct Plan {
     a = 0;
     b = a + round16(tokens * 8);
     counts = b + round16(tokens * 8);
-    touched = counts + round16((int64_t)chunks * 4 << bits);
+    touched = counts + round16(((int64_t)chunks * 4 << bits) * passes);
     part = touched + round16(rows);
     bytes = part + (int64_t)stretches * 2 * pitch * 4;
   }
 };
 
+constexpr int kWaves = kThreads / 64;
+int64_t sets_of(int64_t rows) { return (rows + kZeroRows - 1) / kZeroRows; }
+
 template <int GT, int L>
 hipError_t launch_sum(Grad g, hipStream_t stream) {
   const int64_t per = (g.cols + 8 * L - 1) / (8 * L), each = kThreads / L;
-  const int64_t units = g.stretches * per, zeros = ((int64_t)g.rows + kZeroRows - 1) / kZeroRows * per;
-  g.sum_groups = (units + each - 1) / each;
-  const int64_t groups = g.sum_groups + (zeros + each - 1) / each;
+  g.sum_groups = (g.stretches * per + each - 1) / each;
+  const int64_t groups = g.sum_groups + (g.join_sets - g.sum_sets + kWaves - 1) / kWaves;
   embed_sum_kernel<GT, L><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.stretches < 2) return e;
-  embed_join_kernel<L><<<dim3((unsigned)((g.stretches - 1) * per)), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
+  g.join_groups = (g.stretches - 1) * per;
+  const int64_t joins = g.join_groups + (sets_of(g.rows) - g.join_sets + kWaves - 1) / kWaves;
+  embed_join_kernel<L><<<dim3((unsigned)joins), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
   return hipGetLastError();
 }
 
@@ -399,10 +535,9 @@ bool embed_backward_fits(int64_t rows, int64_t cols, int64_t tokens, size_t& wor
   workspace = (size_t)p.bytes;
   bool fits = true;
   (void)with_lanes(cols, [&](auto lanes) {
-    constexpr int L = decltype(lanes)::value, each = kThreads / L;
-    const int64_t per = (cols + 8 * L - 1) / (8 * L), zeros = (rows + kZeroRows - 1) / kZeroRows * per;
-    fits = p.stretches * per <= most_groups(kThreads) && zeros < (int64_t)1 << 31 &&
-           (p.stretches * per + each - 1) / each + (zeros + each - 1) / each <= most_groups(kThreads);
+    constexpr int L = decltype(lanes)::value;
+    const int64_t per = (cols + 8 * L - 1) / (8 * L), zeros = sets_of(rows) / kWaves + 2;
+    fits = p.stretches * per + zeros <= most_groups(kThreads);
     return hipSuccess;
   });
   return fits;
@@ -421,21 +556,11 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   s.chunk = p.chunk;
   s.rows = (uint32_t)a.rows;
   s.bins = 1 << p.bits;
-  for (int i = 0; i < p.passes; i++) {
-    s.from = i == 0 ? nullptr : bufs[(i - 1) & 1];
-    s.to = bufs[i & 1];
-    s.shift = i * p.bits;
-    count_kernel<<<dim3(p.chunks), dim3(kThreads), 0, stream>>>(s);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    place_kernel<<<dim3(p.chunks), dim3(kThreads), 0, stream>>>(s);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
+  s.width = p.bits;
   Grad g{};
   g.dy = a.dy;
   g.dw = a.dweight;
-  g.sorted = s.to;
+  g.sorted = bufs[(p.passes - 1) & 1];
   g.touched = s.touched;
   g.part = reinterpret_cast<float*>(ws + p.part);
   g.dy_stride = a.dy_stride;
@@ -448,6 +573,30 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   g.rows = s.rows;
   g.scale = a.scale;
   g.dw_bf16 = a.dweight_dtype == QUASAR_BF16;
+  // what the launches that wait most write of the zeros beside: the last pass of the sort, and the join
+  const int64_t sets = sets_of(a.rows), set_bytes = a.cols * size_of(a.dweight_dtype) * kZeroRows;
+  const bool small = a.tokens <= kSmall && a.rows <= kSmallRows;
+  g.sum_sets = p.passes > 1 && !small ? least_of(kPlaceZeros / set_bytes, sets) : 0;
+  g.join_sets = p.stretches > 1 ? sets - least_of(kJoinZeros / set_bytes, sets - g.sum_sets) : sets;
+  if (small) {
+    s.to = bufs[(p.passes - 1) & 1];
+    sort_small_kernel<<<dim3(1), dim3(1024), 0, stream>>>(s, p.passes);
+  } else {
+    count_kernel<<<dim3(p.chunks), dim3(kThreads), 0, stream>>>(s, p.passes - 1);
+  }
+  hipError_t e = hipGetLastError();
+  for (int i = 0; i < p.passes && e == hipSuccess && !small; i++) {
+    const bool last = i == p.passes - 1;
+    s.from = i == 0 ? nullptr : bufs[(i - 1) & 1];
+    s.to = bufs[i & 1];
+    s.shift = i * p.bits;
+    s.next = last ? nullptr : s.counts + ((int64_t)p.chunks << p.bits);
+    const int64_t zeros = last ? (g.sum_sets + kWaves - 1) / kWaves : 0;
+    place_kernel<<<dim3((unsigned)(p.chunks + zeros)), dim3(kThreads), 0, stream>>>(s, p.chunks, g);
+    e = hipGetLastError();
+    s.counts = s.next;
+  }
+  if (e != hipSuccess) return e;
   return with_lanes(a.cols, [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
     return a.dy_dtype == QUASAR_BF16 ? launch_sum<kElemBF16, L>(g, stream) : launch_sum<kElemF32, L>(g, stream);
