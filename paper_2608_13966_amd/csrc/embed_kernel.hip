@@ -6,9 +6,13 @@
 // order; then stretches of the sorted list of the same length are summed, however
 // the tokens are distributed: a stretch writes the rows of the table whose tokens
 // lie in it whole, and leaves what it has of the others (its first and its last
-// at most) to a last launch that joins them.  Rows that no token has are written as
-// zeros by further workgroups of the summing launch.  No float atomics: the order
-// of every sum follows from the tokens.
+// at most) to a last launch that joins them.  No float atomics: the order of every
+// sum follows from the tokens.
+//
+// Rows that no token has are zeros.  Where there are few tokens for the table, all of
+// it is filled with zeros beside the sort, whose few workgroups mostly wait; else the
+// sort marks the rows that tokens have, and further workgroups of the summing launch
+// write zeros into the others.
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -61,7 +65,7 @@ struct Sort {
   uint2* to;
   uint32_t* counts;      // [chunks][bins]
   uint32_t* next;        // the same of the next pass, or NULL
-  uint8_t* touched;      // [rows], 1 where a token has the row
+  uint8_t* touched;      // [rows], 1 where a token has the row; or NULL
   int index_bits, tokens, chunk;
   uint32_t rows;
   int shift, width, bins;
@@ -72,21 +76,46 @@ __device__ __forceinline__ uint2 pair_at(const Sort& s, int i) {
   return make_uint2(token_at(s.index, s.index_bits, i, s.rows), (uint32_t)i);
 }
 
-// n pieces of 16 zeros, by thread i of `all`
-__device__ __forceinline__ void clear(void* p, int64_t n, int64_t i, int64_t all) {
-  for (; i < n; i += all) reinterpret_cast<uint4*>(p)[i] = make_uint4(0u, 0u, 0u, 0u);
+// A table to be filled with zeros, in units of 16 bytes a thread.  A fill of 1 GiB
+// takes 157 us in workgroups of 4 KB, 173 of 8 KB, 190 of 32 KB.
+struct Fill {
+  char* p;
+  int64_t bytes;
+  int size;  // of an element
+};
+// Units a .. b - 1, by the workgroups from `group` on, `groups` in all.
+template <int THREADS>
+__device__ __forceinline__ void fill_units(const Fill& f, int64_t a, int64_t b, int64_t group, int64_t groups) {
+  for (int64_t u = a + group; u < b; u += groups) {
+    int64_t at = (u * THREADS + threadIdx.x) * 16;
+    if (at + 16 <= f.bytes) {
+      st16_any(f.p + at, make_uint4(0u, 0u, 0u, 0u));
+    } else {
+      for (; at < f.bytes; at += f.size) {
+        if (f.size == 2)
+          *reinterpret_cast<uint16_t*>(f.p + at) = 0;
+        else
+          *reinterpret_cast<uint32_t*>(f.p + at) = 0u;
+      }
+    }
+  }
 }
 
-// How often each digit of the first pass occurs in a chunk.  All rows are marked as
-// untouched, and the counts of the later passes (`later` of them) are cleared: the
-// pass before counts its keys where it brings them, by integer atomics, whose order
-// does not matter.
-__global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int later) {
+// All rows are marked as untouched, by thread i of `all`.
+__device__ __forceinline__ void clear_marks(const Sort& s, int64_t i, int64_t all) {
+  if (!s.touched) return;
+  for (; i < ((int64_t)s.rows + 15) / 16; i += all)  // the array is whole pieces of 16
+    reinterpret_cast<uint4*>(s.touched)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// How often each digit of the first pass occurs in a chunk.  The counts of the later
+// passes (`later` of them) are cleared: the pass before counts its keys where it brings
+// them, by integer atomics, whose order does not matter.
+__device__ __forceinline__ void count(const Sort& s, int chunks, int later) {
   __shared__ uint32_t bin[kMaxBins];
   for (int i = threadIdx.x; i < s.bins; i += kThreads) bin[i] = 0;
-  const int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)gridDim.x * kThreads;
-  const int64_t each = (int64_t)gridDim.x * s.bins;
-  clear(s.touched, ((int64_t)s.rows + 15) / 16, i0, all);  // the array is whole pieces of 16
+  const int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)chunks * kThreads, each = (int64_t)chunks * s.bins;
+  clear_marks(s, i0, all);
   for (int64_t i = i0; i < later * each; i += all) s.counts[each + i] = 0;
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * s.chunk;
@@ -95,6 +124,14 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int later) {
     atomicAdd(&bin[(pair_at(s, (int)i).x >> s.shift) & (s.bins - 1)], 1u);
   __syncthreads();
   for (int i = threadIdx.x; i < s.bins; i += kThreads) s.counts[(int64_t)blockIdx.x * s.bins + i] = bin[i];
+}
+
+// In both kernels the workgroups past the first `chunks` fill units a .. b - 1.
+__global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int chunks, int later, Fill f, int64_t a, int64_t b) {
+  if ((int)blockIdx.x < chunks)
+    count(s, chunks, later);
+  else
+    fill_units<kThreads>(f, a, b, blockIdx.x - chunks, gridDim.x - chunks);
 }
 
 // How many of the wavefront's keys so far have this lane's digit, those of lower
@@ -177,7 +214,7 @@ __device__ __forceinline__ void place(const Sort& s, int chunks) {
       const bool has = i < end;
       if (has) {
         key[j] = pair_at(s, (int)i);
-        if (!s.from && key[j].x < s.rows) s.touched[key[j].x] = 1;
+        if (s.touched && !s.from && key[j].x < s.rows) s.touched[key[j].x] = 1;
       }
       rank[j] = rank_of(key[j].x >> s.shift, bins, has, count[wave]);
     }
@@ -207,9 +244,20 @@ __device__ __forceinline__ void place(const Sort& s, int chunks) {
   }
 }
 
-// All passes at once, for a list that one workgroup holds.
+__global__ __launch_bounds__(kThreads) void place_kernel(Sort s, int chunks, Fill f, int64_t a, int64_t b) {
+  if ((int)blockIdx.x < chunks)
+    place(s, chunks);
+  else
+    fill_units<kThreads>(f, a, b, blockIdx.x - chunks, gridDim.x - chunks);
+}
+
+// All passes at once, for a list that one workgroup holds; the others fill.
 constexpr int kSmall = 4096, kSmallRows = 1 << 18;
-__global__ __launch_bounds__(1024) void sort_small_kernel(Sort s, int passes) {
+__global__ __launch_bounds__(1024) void sort_small_kernel(Sort s, int passes, Fill f, int64_t fills) {
+  if (blockIdx.x > 0) {
+    fill_units<1024>(f, 0, fills, blockIdx.x - 1, gridDim.x - 1);
+    return;
+  }
   constexpr int kWaves = 16, kKeys = kSmall / 1024;
   __shared__ uint2 list[kSmall];
   __shared__ uint32_t count[kWaves][kMaxBins], sums[kWaves];
@@ -220,7 +268,7 @@ __global__ __launch_bounds__(1024) void sort_small_kernel(Sort s, int passes) {
     const int i = wave * (64 * kKeys) + j * 64 + lane;
     key[j] = i < s.tokens ? pair_at(s, i) : make_uint2(0u, 0u);
   }
-  clear(s.touched, ((int64_t)s.rows + 15) / 16, threadIdx.x, 1024);
+  clear_marks(s, threadIdx.x, 1024);
   __syncthreads();
   for (int p = 0; p < passes; p++) {
     const int shift = p * s.width;
@@ -264,7 +312,7 @@ __global__ __launch_bounds__(1024) void sort_small_kernel(Sort s, int passes) {
     const int i = wave * (64 * kKeys) + j * 64 + lane;
     if (i >= s.tokens) continue;
     s.to[i] = key[j];
-    if (key[j].x < s.rows) s.touched[key[j].x] = 1;
+    if (s.touched && key[j].x < s.rows) s.touched[key[j].x] = 1;
   }
 }
 
@@ -276,8 +324,7 @@ struct Grad {
   const uint8_t* touched;
   float* part;            // [stretches][2][pitch]: a stretch's sums for a row begun before it, and for one that goes on
   int64_t dy_stride, dw_stride;
-  int64_t sum_groups, sum_sets;    // workgroups that sum; the rest write zeros, from this set of rows on
-  int64_t join_groups, join_sets;  // likewise of the last launch
+  int64_t sum_groups;     // workgroups that sum; the rest write zeros
   int tokens, stretch, stretches, cols, pitch;
   uint32_t rows;
   float scale;
@@ -298,17 +345,15 @@ __device__ __forceinline__ void put_row(const Grad& g, uint32_t row, int c, cons
     put_row<false>(g, row, c, v);
 }
 
-constexpr int kZeroRows = 8;  // rows that a wavefront looks at for zeros at a time
-
-// Zeros in the rows of set `set` of kZeroRows that no token has, by a wavefront: 16 bytes a lane, neighbours.
-__device__ __forceinline__ void zero_rows(const Grad& g, int64_t set, int64_t end) {
-  if (set >= end) return;
-  const int lane = threadIdx.x & 63, size = g.dw_bf16 ? 2 : 4, bytes = g.cols * size;
-  const int64_t r0 = set * kZeroRows;
+// Zeros in set `set` of eight rows, where no token has them, by a wavefront: 16 bytes a lane.
+constexpr int kSet = 8;
+__device__ __forceinline__ void zero_rows(const Grad& g, int64_t set) {
+  const int64_t r0 = set * kSet;
   if (r0 >= g.rows) return;
+  const int lane = threadIdx.x & 63, size = g.dw_bf16 ? 2 : 4, bytes = g.cols * size;
   const uint2 t = *reinterpret_cast<const uint2*>(g.touched + r0);  // whole pieces of 16 are there
 #pragma unroll 1
-  for (int i = 0; i < kZeroRows; i++) {
+  for (int i = 0; i < kSet; i++) {
     if (((i < 4 ? t.x : t.y) >> (8 * (i & 3)) & 0xffu) || r0 + i >= g.rows) continue;
     char* const p = reinterpret_cast<char*>(g.dw) + (r0 + i) * g.dw_stride * size;
     for (int b = lane * 16; b < bytes; b += 1024) {
@@ -326,20 +371,15 @@ __device__ __forceinline__ void zero_rows(const Grad& g, int64_t set, int64_t en
   }
 }
 
-// Workgroups past the first `chunks` write zeros, up to set g.sum_sets.
-__global__ __launch_bounds__(kThreads) void place_kernel(Sort s, int chunks, Grad g) {
-  if ((int)blockIdx.x < chunks)
-    place(s, chunks);
-  else
-    zero_rows(g, (int64_t)(blockIdx.x - chunks) * (kThreads / 64) + wave_index(), g.sum_sets);
-}
+constexpr int kMaxStretch = 32;
 
-// L lanes (8 columns each) take a stretch of the sorted list; the next rows are in flight meanwhile.
+// L lanes (8 columns each) take a stretch of the sorted list.
 template <int GT, int L>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per) {
   const int lane = threadIdx.x & (L - 1);
   if (blockIdx.x >= g.sum_groups) {
-    zero_rows(g, g.sum_sets + (blockIdx.x - g.sum_groups) * (kThreads / 64) + wave_index(), g.join_sets);
+    for (int64_t u = blockIdx.x - g.sum_groups; u * (kThreads / 64 * kSet) < g.rows; u += gridDim.x - g.sum_groups)
+      zero_rows(g, u * (kThreads / 64) + wave_index());
     return;
   }
   const int64_t u = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
@@ -351,17 +391,33 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
   const uint2* const list = g.sorted + p0;
   // the row that the stretch begins in the middle of, and the one that goes on past it
   const uint32_t none = g.rows, head = p0 > 0 ? list[-1].x : none, tail = p0 + n < g.tokens ? list[n].x : none;
-  constexpr int kAhead = 4;
-  Piece<GT> row[kAhead];
-  uint2 key[kAhead];
-  const auto fetch = [&](int j, int i) {
-    key[j] = i < n ? list[i] : make_uint2(none, 0u);
-    row[j].load(g.dy, key[j].x < none ? key[j].y * g.dy_stride + c : 0, key[j].x < none ? left : 0);
-  };
+  // The list goes through LDS: a load of it from memory between those of dy's rows would wait for all of them.
+  __shared__ uint2 pairs[kThreads / L][kMaxStretch];
+  uint2* const mine = pairs[threadIdx.x / L];
+  for (int i = lane; i < n; i += L) mine[i] = list[i];
+  wave_lds_fence();
+  constexpr int kAhead = 4;  // rows of a batch; the next one is in flight while one is summed
+  struct Batch {
+    uint32_t key[kAhead];
+    Piece<GT> row[kAhead];
+  } batch[2];
+  const auto fetch = [&](Batch& b, int i) {
+    uint2 p[kAhead];
 #pragma unroll
-  for (int j = 0; j < kAhead; j++) fetch(j, j);
+    for (int j = 0; j < kAhead; j++) p[j] = i + j < n ? mine[i + j] : make_uint2(none, 0u);
+#pragma unroll
+    for (int j = 0; j < kAhead; j++) {
+      if constexpr (L == 64) {
+        p[j].x = __builtin_amdgcn_readfirstlane(p[j].x);
+        p[j].y = __builtin_amdgcn_readfirstlane(p[j].y);
+      }
+      b.key[j] = p[j].x;
+      b.row[j].load(g.dy, p[j].x < none ? p[j].y * g.dy_stride + c : 0, p[j].x < none ? left : 0);
+    }
+  };
+  fetch(batch[0], 0);
   float sum[8] = {};
-  uint32_t now = key[0].x;
+  uint32_t now = batch[0].key[0];
   bool begun = now == head;  // before this stretch
   const auto flush = [&](bool goes_on) {
     if (now >= none) return;
@@ -370,20 +426,26 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
     else
       put_row(g, now, c, sum);
   };
-  for (int i = 0; i < n; i += kAhead) {
+  const auto add = [&](const Batch& b) {
 #pragma unroll
     for (int j = 0; j < kAhead; j++) {
-      if (key[j].x != now) {
+      if (b.key[j] != now) {
         flush(false);
-        now = key[j].x;
+        now = b.key[j];
         begun = false;
 #pragma unroll
         for (int k = 0; k < 8; k++) sum[k] = 0.0f;
       }
 #pragma unroll
-      for (int k = 0; k < 8; k++) sum[k] += row[j].get(k);
-      fetch(j, i + kAhead + j);
+      for (int k = 0; k < 8; k++) sum[k] += b.row[j].get(k);
     }
+  };
+  for (int i = 0; i < n; i += 2 * kAhead) {
+    fetch(batch[1], i + kAhead);
+    add(batch[0]);
+    if (i + kAhead >= n) break;
+    fetch(batch[0], i + 2 * kAhead);
+    add(batch[1]);
   }
   flush(now == tail);
 }
@@ -394,10 +456,6 @@ template <int L>
 __global__ __launch_bounds__(kThreads) void embed_join_kernel(Grad g, Divide per) {
   constexpr int kShares = kThreads / L;
   __shared__ float lds[kShares > 1 ? (kShares - 1) * L * 8 : 1];
-  if (blockIdx.x >= g.join_groups) {
-    zero_rows(g, g.join_sets + (blockIdx.x - g.join_groups) * (kThreads / 64) + wave_index(), (int64_t)g.rows);
-    return;
-  }
   const int lane = threadIdx.x & (L - 1), share = threadIdx.x / L;
   const uint32_t st = per.of(blockIdx.x), part = blockIdx.x - st * per.by;
   const int c = (int)part * (8 * L) + lane * 8;
@@ -451,7 +509,7 @@ hipError_t with_lanes(int64_t cols, F f) {
   return f(integral_constant<int, 64>());
 }
 
-constexpr int64_t kPlaceZeros = 48 << 20, kJoinZeros = 32 << 20;  // bytes
+constexpr int64_t kCountFill = 8 << 10, kPlaceFill = 12 << 10;  // units
 
 int64_t least_of(int64_t a, int64_t b) { return a < b ? a : b; }
 int64_t round16(int64_t n) { return (n + 15) & ~(int64_t)15; }
@@ -483,20 +541,18 @@ struct Plan {
   }
 };
 
-constexpr int kWaves = kThreads / 64;
-int64_t sets_of(int64_t rows) { return (rows + kZeroRows - 1) / kZeroRows; }
+int64_t zero_groups(int64_t rows) { return least_of((rows + 4 * kSet - 1) / (4 * kSet), most_groups(kThreads) / 2); }
+unsigned with_fill(int64_t others, int64_t units) { return (unsigned)(others + least_of(units, most_groups(kThreads) - others)); }
 
 template <int GT, int L>
 hipError_t launch_sum(Grad g, hipStream_t stream) {
   const int64_t per = (g.cols + 8 * L - 1) / (8 * L), each = kThreads / L;
   g.sum_groups = (g.stretches * per + each - 1) / each;
-  const int64_t groups = g.sum_groups + (g.join_sets - g.sum_sets + kWaves - 1) / kWaves;
-  embed_sum_kernel<GT, L><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
-  hipError_t e = hipGetLastError();
+  const int64_t groups = g.sum_groups + (g.touched ? zero_groups(g.rows) : 0);
+  if (groups > 0) embed_sum_kernel<GT, L><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.stretches < 2) return e;
-  g.join_groups = (g.stretches - 1) * per;
-  const int64_t joins = g.join_groups + (sets_of(g.rows) - g.join_sets + kWaves - 1) / kWaves;
-  embed_join_kernel<L><<<dim3((unsigned)joins), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
+  embed_join_kernel<L><<<dim3((unsigned)((g.stretches - 1) * per)), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
   return hipGetLastError();
 }
 
@@ -536,8 +592,7 @@ bool embed_backward_fits(int64_t rows, int64_t cols, int64_t tokens, size_t& wor
   bool fits = true;
   (void)with_lanes(cols, [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
-    const int64_t per = (cols + 8 * L - 1) / (8 * L), zeros = sets_of(rows) / kWaves + 2;
-    fits = p.stretches * per + zeros <= most_groups(kThreads);
+    fits = p.stretches * ((cols + 8 * L - 1) / (8 * L)) <= most_groups(kThreads) / 2;
     return hipSuccess;
   });
   return fits;
@@ -561,7 +616,6 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   g.dy = a.dy;
   g.dw = a.dweight;
   g.sorted = bufs[(p.passes - 1) & 1];
-  g.touched = s.touched;
   g.part = reinterpret_cast<float*>(ws + p.part);
   g.dy_stride = a.dy_stride;
   g.dw_stride = a.dweight_stride;
@@ -573,28 +627,43 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   g.rows = s.rows;
   g.scale = a.scale;
   g.dw_bf16 = a.dweight_dtype == QUASAR_BF16;
-  // what the launches that wait most write of the zeros beside: the last pass of the sort, and the join
-  const int64_t sets = sets_of(a.rows), set_bytes = a.cols * size_of(a.dweight_dtype) * kZeroRows;
-  const bool small = a.tokens <= kSmall && a.rows <= kSmallRows;
-  g.sum_sets = p.passes > 1 && !small ? least_of(kPlaceZeros / set_bytes, sets) : 0;
-  g.join_sets = p.stretches > 1 ? sets - least_of(kJoinZeros / set_bytes, sets - g.sum_sets) : sets;
-  if (small) {
+  // Filling all of the table is the faster where no more than a quarter of its rows can be touched (131072 x 4096 in
+  // bf16: 8 tokens @ us against @, 32768 @ against @): they are written twice, but the rest without a look at the marks,
+  // and beside the sort.
+  const int64_t bytes = a.rows * a.cols * size_of(a.dweight_dtype);
+  const Fill f{reinterpret_cast<char*>(a.dweight), bytes, (int)size_of(a.dweight_dtype)};
+  const bool fill = a.tokens <= a.rows / 4 && (a.rows == 1 || a.dweight_stride == a.cols);
+  if (fill) s.touched = nullptr;
+  g.touched = s.touched;
+  hipError_t e;
+  if (a.tokens <= kSmall && a.rows <= kSmallRows) {
+    const int64_t units = fill ? (bytes + 1024 * 16 - 1) / (1024 * 16) : 0;
     s.to = bufs[(p.passes - 1) & 1];
-    sort_small_kernel<<<dim3(1), dim3(1024), 0, stream>>>(s, p.passes);
-  } else {
-    count_kernel<<<dim3(p.chunks), dim3(kThreads), 0, stream>>>(s, p.passes - 1);
-  }
-  hipError_t e = hipGetLastError();
-  for (int i = 0; i < p.passes && e == hipSuccess && !small; i++) {
-    const bool last = i == p.passes - 1;
-    s.from = i == 0 ? nullptr : bufs[(i - 1) & 1];
-    s.to = bufs[i & 1];
-    s.shift = i * p.bits;
-    s.next = last ? nullptr : s.counts + ((int64_t)p.chunks << p.bits);
-    const int64_t zeros = last ? (g.sum_sets + kWaves - 1) / kWaves : 0;
-    place_kernel<<<dim3((unsigned)(p.chunks + zeros)), dim3(kThreads), 0, stream>>>(s, p.chunks, g);
+    sort_small_kernel<<<dim3((unsigned)(1 + least_of(units, most_groups(1024) - 1))), dim3(1024), 0, stream>>>(s, p.passes, f, units);
     e = hipGetLastError();
-    s.counts = s.next;
+  } else {
+    // shares of the fill that take about as long as the sort's part
+    const int64_t units = fill ? (bytes + kThreads * 16 - 1) / (kThreads * 16) : 0;
+    int64_t done = 0;
+    const auto share = [&](int64_t n) {
+      const int64_t a0 = done;
+      done = least_of(done + n, units);
+      return a0;
+    };
+    int64_t from = share(kCountFill);
+    count_kernel<<<dim3(with_fill(p.chunks, done - from)), dim3(kThreads), 0, stream>>>(s, p.chunks, p.passes - 1, f, from, done);
+    e = hipGetLastError();
+    for (int i = 0; i < p.passes && e == hipSuccess; i++) {
+      const bool last = i == p.passes - 1;
+      s.from = i == 0 ? nullptr : bufs[(i - 1) & 1];
+      s.to = bufs[i & 1];
+      s.shift = i * p.bits;
+      s.next = last ? nullptr : s.counts + ((int64_t)p.chunks << p.bits);
+      from = share(last ? units : kPlaceFill);
+      place_kernel<<<dim3(with_fill(p.chunks, done - from)), dim3(kThreads), 0, stream>>>(s, p.chunks, f, from, done);
+      e = hipGetLastError();
+      s.counts = s.next;
+    }
   }
   if (e != hipSuccess) return e;
   return with_lanes(a.cols, [&](auto lanes) {

@@ -137,8 +137,11 @@ def test_grad_into_a_wider_buffer_with_a_used_workspace():
 def test_no_tokens():
     dy, tok = torch.empty(0, 33, device=DEV), torch.empty(0, device=DEV, dtype=torch.int64)
     assert O.embed(tok, torch.ones(5, 33, device=DEV))["y"].shape == (0, 33)
-    out = {"dw": torch.full((5000, 33), 7.0, device=DEV)}
-    assert (O.embed_backward(dy, tok, 5000, out=out)["dw"] == 0).all()
+    for rows in (1, 5000, 300000):
+        out = {"dw": torch.full((rows, 33), 7.0, device=DEV)}
+        assert (O.embed_backward(dy, tok, rows, out=out)["dw"] == 0).all()
+    out = {"dw": torch.full((300000, 2), 7.0, device=DEV)}
+    assert (O.embed_backward(dy[:, :2], tok, 300000, out=out)["dw"] == 0).all()
 
 
 def test_nan_stays_in_its_row():
