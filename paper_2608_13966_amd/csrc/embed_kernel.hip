@@ -82,6 +82,7 @@ struct Fill {
   char* p;
   int64_t bytes;
   int size;  // of an element
+  bool nt;   // past the caches: more than twice what the last level holds
 };
 // Units a .. b - 1, by the workgroups from `group` on, `groups` in all.
 template <int THREADS>
@@ -89,7 +90,10 @@ __device__ __forceinline__ void fill_units(const Fill& f, int64_t a, int64_t b, 
   for (int64_t u = a + group; u < b; u += groups) {
     int64_t at = (u * THREADS + threadIdx.x) * 16;
     if (at + 16 <= f.bytes) {
-      st16_any(f.p + at, make_uint4(0u, 0u, 0u, 0u));
+      if (f.nt)
+        st16_any_nt(f.p + at, make_uint4(0u, 0u, 0u, 0u));
+      else
+        st16_any(f.p + at, make_uint4(0u, 0u, 0u, 0u));
     } else {
       for (; at < f.bytes; at += f.size) {
         if (f.size == 2)
@@ -412,7 +416,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
         p[j].y = __builtin_amdgcn_readfirstlane(p[j].y);
       }
       b.key[j] = p[j].x;
-      b.row[j].load(g.dy, p[j].x < none ? p[j].y * g.dy_stride + c : 0, p[j].x < none ? left : 0);
+      // read once: kept in no cache, where the lines of dw that are still to be written out are (118 us, so 80)
+      b.row[j].template load<true>(g.dy, p[j].x < none ? p[j].y * g.dy_stride + c : 0, p[j].x < none ? left : 0);
     }
   };
   fetch(batch[0], 0);
@@ -631,7 +636,7 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   // bf16: 8 tokens @ us against @, 32768 @ against @): they are written twice, but the rest without a look at the marks,
   // and beside the sort.
   const int64_t bytes = a.rows * a.cols * size_of(a.dweight_dtype);
-  const Fill f{reinterpret_cast<char*>(a.dweight), bytes, (int)size_of(a.dweight_dtype)};
+  const Fill f{reinterpret_cast<char*>(a.dweight), bytes, (int)size_of(a.dweight_dtype), bytes > (int64_t)512 << 20};
   const bool fill = a.tokens <= a.rows / 4 && (a.rows == 1 || a.dweight_stride == a.cols);
   if (fill) s.touched = nullptr;
   g.touched = s.touched;

@@ -21,6 +21,14 @@ __device__ __forceinline__ uint4 ld16_any(const void* p) {
   return v;
 }
 __device__ __forceinline__ void st16_any(void* p, uint4 v) { __builtin_memcpy(p, &v, 16); }
+// ... non-temporal: for what is read or written once and is too much for the caches to keep
+typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+__device__ __forceinline__ uint4 ld16_any_nt(const void* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p)));
+}
+__device__ __forceinline__ void st16_any_nt(void* p, uint4 v) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4_any, v), reinterpret_cast<u32x4_any*>(p));
+}
 __device__ __forceinline__ uint2 ld8_any(const void* p) {
   uint2 v;
   __builtin_memcpy(&v, p, 8);
@@ -47,10 +55,11 @@ struct Piece;
 template <>
 struct Piece<kElemBF16> {
   uint32_t d[4];
+  template <bool NT = false>
   __device__ __forceinline__ void load(const void* base, int64_t e, int n) {
     const uint16_t* p = reinterpret_cast<const uint16_t*>(base) + e;
     if (n >= 8) {
-      const uint4 t = ld16_any(p);
+      const uint4 t = NT ? ld16_any_nt(p) : ld16_any(p);
       d[0] = t.x; d[1] = t.y; d[2] = t.z; d[3] = t.w;
     } else {
 #pragma unroll
@@ -70,10 +79,11 @@ struct Piece<kElemBF16> {
 template <>
 struct Piece<kElemF32> {
   float f[8];
+  template <bool NT = false>
   __device__ __forceinline__ void load(const void* base, int64_t e, int n) {
     const float* p = reinterpret_cast<const float*>(base) + e;
     if (n >= 8) {
-      const uint4 a = ld16_any(p), b = ld16_any(p + 4);
+      const uint4 a = NT ? ld16_any_nt(p) : ld16_any(p), b = NT ? ld16_any_nt(p + 4) : ld16_any(p + 4);
       f[0] = as_f32(a.x); f[1] = as_f32(a.y); f[2] = as_f32(a.z); f[3] = as_f32(a.w);
       f[4] = as_f32(b.x); f[5] = as_f32(b.y); f[6] = as_f32(b.z); f[7] = as_f32(b.w);
     } else {
