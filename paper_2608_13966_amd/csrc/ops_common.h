@@ -123,13 +123,21 @@ __device__ __forceinline__ void load_floats(const void* base, int64_t e, int n, 
   for (int i = 0; i < 8; i++) v[i] = vs[0][i];
 }
 
+template <bool NT>
+__device__ __forceinline__ void st16_as(void* p, uint4 v) {
+  if constexpr (NT)
+    st16_any_nt(p, v);
+  else
+    st16_any(p, v);
+}
+
 // Eight values to a tensor of fp32 or bf16 elements (nearest even), the first n of them.
-template <bool BF16>
+template <bool BF16, bool NT = false>
 __device__ __forceinline__ void store_piece(void* base, int64_t e, const float (&v)[8], int n) {
   if constexpr (BF16) {
     uint16_t* p = reinterpret_cast<uint16_t*>(base) + e;
     if (n >= 8) {
-      st16_any(p, make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+      st16_as<NT>(p, make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
                              pack_bf16x2(v[6], v[7])));
     } else {
 #pragma unroll
@@ -139,8 +147,8 @@ __device__ __forceinline__ void store_piece(void* base, int64_t e, const float (
   } else {
     float* p = reinterpret_cast<float*>(base) + e;
     if (n >= 8) {
-      st16_any(p, make_uint4(as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])));
-      st16_any(p + 4, make_uint4(as_u32(v[4]), as_u32(v[5]), as_u32(v[6]), as_u32(v[7])));
+      st16_as<NT>(p, make_uint4(as_u32(v[0]), as_u32(v[1]), as_u32(v[2]), as_u32(v[3])));
+      st16_as<NT>(p + 4, make_uint4(as_u32(v[4]), as_u32(v[5]), as_u32(v[6]), as_u32(v[7])));
     } else {
 #pragma unroll
       for (int i = 0; i < 8; i++)
@@ -148,11 +156,12 @@ __device__ __forceinline__ void store_piece(void* base, int64_t e, const float (
     }
   }
 }
+template <bool NT = false>
 __device__ __forceinline__ void store_piece(void* base, int64_t e, const float (&v)[8], int n, bool bf16) {
   if (bf16)
-    store_piece<true>(base, e, v, n);
+    store_piece<true, NT>(base, e, v, n);
   else
-    store_piece<false>(base, e, v, n);
+    store_piece<false, NT>(base, e, v, n);
 }
 
 // Eight elements at byte `at` of a wavefront's buffer (wave_buffer in

@@ -11,6 +11,7 @@
 namespace quasar {
 
 constexpr int kCUs = 256;  // compute units of the card
+constexpr int64_t kLastLevel = (int64_t)256 << 20;  // bytes of its last-level cache
 
 // Workgroups of a launch: HIP takes fewer than 2^32 threads in a grid.  A call
 // with more rows than that many take is launched in pieces of its rows.
