@@ -224,6 +224,7 @@ constexpr int kDppXor1 = 0xB1;        // quad_perm [1,0,3,2]
 constexpr int kDppXor2 = 0x4E;        // quad_perm [2,3,0,1]
 constexpr int kDppHalfMirror = 0x141; // lane i <-> 7 - i inside each 8
 constexpr int kDppMirror = 0x140;     // lane i <-> 15 - i inside each 16
+constexpr int kDppHalf = 0x128;       // lane i <-> (i + 8) % 16 inside each 16
 
 // x of the lane that DPP control CTRL names, 0 where it names none (bound_ctrl:
 // no old value to set up first)

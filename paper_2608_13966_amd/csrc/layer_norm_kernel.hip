@@ -17,7 +17,7 @@ __host__ __device__ constexpr int ln_pitch(int cols) { return (cols + 3) & ~3; }
 namespace {
 
 // Threads of a workgroup, and the rows that it works on at once, where TPR
-// threads (16 lanes, a wavefront, or a workgroup) work on one row.
+// threads (8, 16 or 32 lanes, a wavefront, or a workgroup) work on one row.
 template <int TPR>
 struct Shape {
   static constexpr int kThreads = TPR < 256 ? 256 : TPR, kRows = kThreads / TPR;
@@ -29,11 +29,13 @@ struct Shape {
 // several wavefronts.
 template <int TPR, typename Op>
 __device__ __forceinline__ float row_reduce(float x, float* s, Op op) {
-  if constexpr (TPR == 16) {
+  if constexpr (TPR < 64) {
     x = op(x, dpp_f32<kDppXor1>(x));
     x = op(x, dpp_f32<kDppXor2>(x));
     x = op(x, dpp_f32<kDppHalfMirror>(x));
-    return op(x, dpp_f32<kDppMirror>(x));
+    if constexpr (TPR >= 16) x = op(x, dpp_f32<kDppMirror>(x));
+    if constexpr (TPR == 32) x = pair_rows<16>(x, op);
+    return x;
   } else {
     return group_reduce<TPR / 64>(x, s, op);
   }
@@ -146,8 +148,9 @@ hipError_t with_shape(int64_t cols, F f) {
   using std::integral_constant;
 #define QUASAR_SHAPE(T, N) \
   if (cols <= 8 * T * N) return f(integral_constant<int, T>(), integral_constant<int, N>())
+  QUASAR_SHAPE(8, 1);
   QUASAR_SHAPE(16, 1);
-  QUASAR_SHAPE(16, 2);
+  QUASAR_SHAPE(32, 1);
   QUASAR_SHAPE(64, 1);
   QUASAR_SHAPE(64, 2);
   QUASAR_SHAPE(64, 4);
@@ -203,11 +206,20 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_backward_kern
   __shared__ float shares[kShares > 1 ? (kShares - 1) * kWide * NV * 8 : 1];
   const int t = Shape<TPR>::lane(), cols = (int)a.cols;
   const float rcols = 1.0f / (float)cols;
-  float w[NV][8], dw[NV][8] = {}, db[NV][8] = {};
-#pragma unroll
-  for (int v = 0; v < NV; v++) {
+  constexpr bool kKeep = NV < 4;  // the weight stays in registers
+  float w[kKeep ? NV : 1][8], dw[NV][8] = {}, db[NV][8] = {};
+  const auto weight = [&](int v) -> float (&)[8] {
     const int c = (v * TPR + t) * 8;
-    load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w[v]);
+    if constexpr (kKeep) return w[v];
+    load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w[0]);
+    return w[0];
+  };
+  if constexpr (kKeep) {
+#pragma unroll
+    for (int v = 0; v < NV; v++) {
+      const int c = (v * TPR + t) * 8;
+      load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w[v]);
+    }
   }
   int flip = 0;
   for (int64_t row = (int64_t)blockIdx.x * kRows + Shape<TPR>::row(); row < a.rows; row += (int64_t)gridDim.x * kRows) {
@@ -221,8 +233,8 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_backward_kern
       ph[v].load(a.h, eh + c, cols - c);
     }
     // dh is asked for with the rest where there are registers for it
-    constexpr bool kEarly = TPR <= 256;
-    float dh[NV][8];
+    constexpr bool kEarly = TPR <= 512 || NV == 1;
+    float dh[kEarly ? NV : 1][8];
     if (kEarly && a.dh) {
 #pragma unroll
       for (int v = 0; v < NV; v++) {
@@ -233,16 +245,18 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_backward_kern
     const float rstd = a.rstd[row], mean = a.mean[row];
     float dot = 0.0f, sum = 0.0f;
 #pragma unroll
-    for (int v = 0; v < NV; v++)
+    for (int v = 0; v < NV; v++) {
+      float(&wv)[8] = weight(v);
 #pragma unroll
       for (int i = 0; i < 8; i++) {
         // past the row's end g and w are 0
-        const float n = (ph[v].get(i) - mean) * rstd, g = pg[v].get(i), u = g * w[v][i];
+        const float n = (ph[v].get(i) - mean) * rstd, g = pg[v].get(i), u = g * wv[i];
         sum += u;
         dot = __builtin_fmaf(u, n, dot);
         dw[v][i] = __builtin_fmaf(g, n, dw[v][i]);
         db[v][i] += g;
       }
+    }
     // two LDS rows in turn: a wavefront may be a row ahead of another's read
     if constexpr (TPR <= 64) {
       sum = row_reduce<TPR>(sum, nullptr, SumOp());
@@ -269,26 +283,33 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_backward_kern
     for (int v = 0; v < NV; v++) {
       const int c = (v * TPR + t) * 8, n8 = cols - c;
       float dx[8];
+      float(&wv)[8] = weight(v);
 #pragma unroll
       for (int i = 0; i < 8; i++) {
         const float n = (ph[v].get(i) - mean) * rstd;
-        dx[i] = rstd * __builtin_fmaf(-m, n, __builtin_fmaf(pg[v].get(i), w[v][i], -mu));
+        dx[i] = rstd * __builtin_fmaf(-m, n, __builtin_fmaf(pg[v].get(i), wv[i], -mu));
       }
       if (a.dh) {
-        if constexpr (!kEarly) load_floats(a.dh, ed + c, n8, a.dx_dtype == QUASAR_BF16, dh[v]);
+        float(&d)[8] = dh[kEarly ? v : 0];
+        if constexpr (!kEarly) load_floats(a.dh, ed + c, n8, a.dx_dtype == QUASAR_BF16, d);
 #pragma unroll
-        for (int i = 0; i < 8; i++) dx[i] += dh[v][i];
+        for (int i = 0; i < 8; i++) dx[i] += d[i];
       }
       store_piece(a.dx, ex + c, dx, n8, a.dx_dtype == QUASAR_BF16);
     }
   }
   // the groups of a wavefront, then the wavefronts
   const auto meet = [&](float (&s)[NV][8], float* out) {
-    if constexpr (TPR == 16) {
+    if constexpr (TPR < 64) {
 #pragma unroll
       for (int v = 0; v < NV; v++)
 #pragma unroll
-        for (int i = 0; i < 8; i++) s[v][i] = pair_rows<32>(pair_rows<16>(s[v][i], SumOp()), SumOp());
+        for (int i = 0; i < 8; i++) {
+          float x = s[v][i];
+          if constexpr (TPR == 8) x += dpp_f32<kDppHalf>(x);
+          if constexpr (TPR <= 16) x = pair_rows<16>(x, SumOp());
+          s[v][i] = pair_rows<32>(x, SumOp());
+        }
     }
     if constexpr (kShares > 1) {
       const int wave = wave_index();
@@ -353,17 +374,37 @@ __global__ __launch_bounds__(256) void ln_parts_kernel(const float* parts, int n
   }
 }
 
+// f(TPR, NV): as few pieces a thread as there are threads for, since dweight's and dbias' shares take registers too.
+template <typename F>
+hipError_t with_backward_shape(int64_t cols, F f) {
+  using std::integral_constant;
+#define QUASAR_SHAPE(T, N) \
+  if (cols <= 8 * T * N) return f(integral_constant<int, T>(), integral_constant<int, N>())
+  QUASAR_SHAPE(8, 1);
+  QUASAR_SHAPE(16, 1);
+  QUASAR_SHAPE(32, 1);
+  QUASAR_SHAPE(64, 1);
+  QUASAR_SHAPE(64, 2);
+  QUASAR_SHAPE(256, 1);
+  QUASAR_SHAPE(512, 1);
+  QUASAR_SHAPE(1024, 1);
+  QUASAR_SHAPE(1024, 2);
+  QUASAR_SHAPE(1024, 4);
+#undef QUASAR_SHAPE
+  return hipErrorInvalidValue;
+}
+
 // workgroups of the backward pass, each with its shares of dweight and dbias
 int backward_groups(int64_t rows, int64_t cols) {
-  const int64_t per = cols <= 256 ? 16 : cols <= 2048 ? 4 : 1;  // rows a workgroup takes at once
-  const int64_t most = (cols <= 8192 ? 4 : 2) * kCUs;          // what runs at once (of 1024 threads: two a CU)
+  const int64_t per = cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1;  // rows a workgroup takes at once
+  const int64_t most = (cols <= 2048 ? 4 : cols <= 4096 ? 2 : 1) * kCUs;  // what runs at once
   const int64_t groups = (rows + per - 1) / per, rounds = groups <= most ? 1 : (groups + most - 1) / most;
   return (int)((groups + rounds - 1) / rounds);  // no more parts than that many rounds need
 }
 
 template <int GT, int HT>
 hipError_t launch_backward_types(const quasar_layer_norm_backward& a, hipStream_t stream) {
-  return with_shape(a.cols, [&](auto tpr, auto nv) {
+  return with_backward_shape(a.cols, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
     const int n = backward_groups(a.rows, a.cols), pitch = ln_pitch((int)a.cols);
     float* const parts = n == 1 ? nullptr : reinterpret_cast<float*>(a.workspace);
