@@ -79,11 +79,13 @@ __device__ __forceinline__ bf16x8 read_tile(const uint16_t* lds, int t0, int col
   return __builtin_bit_cast(bf16x8, r);
 }
 
-// A workgroup makes B x B values of dweight (or of its share's sums in part) from
-// its share of the tokens, 64 at a time: the next 64 come to registers while these
-// are multiplied.  Four wavefronts of B/2 x B/2.
-template <int GT, int B>
+// A workgroup makes 64 x 64 values of dweight (or of its share's sums in part) from
+// its share of the tokens, 64 at a time: the next two steps' pieces come to registers
+// while one is multiplied (with one step's, 777 tokens, 1000 x 1544 took 20.6 us, not
+// 13.7).  Four wavefronts of 32 x 32.
+template <int GT>
 __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, int tiles_n, int splits, int steps_per, float* part) {
+  constexpr int B = 64;
   constexpr int kParts = GT == kElemF32 ? 3 : 1, kPieces = kStep * B / 8 / 256, T = B / 32;
   __shared__ __align__(16) uint16_t lds[(kParts + 1) * kStep * B];
   uint16_t* const xs = lds + kParts * kStep * B;
@@ -97,17 +99,47 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
   constexpr int kWide = B / 8, kRound = 256 / kWide;
   const int c = (tid % kWide) * 8, tr = tid / kWide;
   const int ln = (int)(a.rows - n0 - c < 8 ? a.rows - n0 - c : 8), lk = (int)(a.cols - k0 - c < 8 ? a.cols - k0 - c : 8);
-  Piece<GT> g[kPieces];
-  uint2 q[kPieces];
-  uint32_t e[kPieces];
-  const auto fetch = [&](int64_t t) {
+  struct Fetched {
+    Piece<GT> g[kPieces];
+    uint2 q[kPieces];
+    uint32_t e[kPieces];
+  } f[2];
+  // Whole pieces without a branch (the compiler would wait for all of them where a branch ends): past a row's end is the
+  // next row, and columns past the matrix reach nothing that is stored; those of a thread without any are the first ones.
+  const int64_t gn = ln > 0 ? n0 + c : 0, qk = lk > 0 ? k0 + c : 0;
+  const auto fetch = [&](Fetched& o, int64_t t) {
+#pragma unroll
+    for (int i = 0; i < kPieces; i++) {
+      const int64_t r = t + tr + i * kRound;
+      o.g[i].load(a.dy, r * a.dy_stride + gn, 8);
+      o.q[i] = ld8_any(a.q + r * a.q_stride + qk);
+      o.e[i] = a.exponent[r * a.exponent_stride + (qk >> 7)];
+    }
+  };
+  // near the last token: nothing past it
+  const auto fetch_some = [&](Fetched& o, int64_t t) {
 #pragma unroll
     for (int i = 0; i < kPieces; i++) {
       const int64_t r = t + tr + i * kRound;
       const bool has = r < t1;
-      g[i].load(a.dy, has ? r * a.dy_stride + n0 + c : 0, has ? ln : 0);
-      q[i] = load_bytes(has ? a.q + r * a.q_stride + k0 + c : a.q, has ? lk : 0);
-      e[i] = has && lk > 0 ? a.exponent[r * a.exponent_stride + ((k0 + c) >> 7)] : 127u;
+      o.g[i].load(a.dy, has ? r * a.dy_stride + n0 + c : 0, has ? ln : 0);
+      o.q[i] = load_bytes(has ? a.q + r * a.q_stride + k0 + c : a.q, has ? lk : 0);
+      o.e[i] = has && lk > 0 ? a.exponent[r * a.exponent_stride + ((k0 + c) >> 7)] : 127u;
+    }
+  };
+  const auto stage = [&](const Fetched& o) {
+#pragma unroll
+    for (int i = 0; i < kPieces; i++) {
+      const int at = spot<B>(tr + i * kRound, c);
+      if constexpr (GT == kElemF32) {
+        uint4 p[3];
+        split3(o.g[i].f, p);
+#pragma unroll
+        for (int j = 0; j < 3; j++) *reinterpret_cast<uint4*>(lds + j * kStep * B + at) = p[j];
+      } else {
+        *reinterpret_cast<uint4*>(lds + at) = make_uint4(o.g[i].d[0], o.g[i].d[1], o.g[i].d[2], o.g[i].d[3]);
+      }
+      *reinterpret_cast<uint4*>(xs + at) = kept_bf16(o.q[i], as_f32(o.e[i] << 23));
     }
   };
   f32x4 acc[T][T];
@@ -116,24 +148,13 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
 #pragma unroll
     for (int j = 0; j < T; j++) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const int wn = (wave >> 1) * (B / 2), wk = (wave & 1) * (B / 2);
-  if (t0 < t1) fetch(t0);
-  for (int64_t t = t0; t < t1; t += kStep) {
-    __syncthreads();  // the last step's reads are done
-#pragma unroll
-    for (int i = 0; i < kPieces; i++) {
-      const int at = spot<B>(tr + i * kRound, c);
-      if constexpr (GT == kElemF32) {
-        uint4 p[3];
-        split3(g[i].f, p);
-#pragma unroll
-        for (int j = 0; j < 3; j++) *reinterpret_cast<uint4*>(lds + j * kStep * B + at) = p[j];
-      } else {
-        *reinterpret_cast<uint4*>(lds + at) = make_uint4(g[i].d[0], g[i].d[1], g[i].d[2], g[i].d[3]);
-      }
-      *reinterpret_cast<uint4*>(xs + at) = kept_bf16(q[i], as_f32(e[i] << 23));
-    }
-    if (t + kStep < t1) fetch(t + kStep);
-    __syncthreads();
+  const auto meet = [&] {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+  const auto multiply = [&] {
+    meet();
 #pragma unroll
     for (int k = 0; k < kStep; k += 32) {
       bf16x8 mx[T];
@@ -148,6 +169,43 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
           for (int j = 0; j < T; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mg, mx[j], acc[i][j], 0, 0, 0);
         }
     }
+    meet();  // every wavefront is done with the step
+  };
+  // the steps whose pieces, eight elements past a row's end too, lie before the last token's row
+  const int64_t safe = a.tokens - 8 < t1 ? a.tokens - 8 : t1;
+  const int whole = safe > t0 ? (int)((safe - t0) / kStep) : 0;
+  int64_t t = t0;
+  if (whole >= 2) {
+    fetch(f[0], t);
+    fetch(f[1], t + kStep);
+    int s = 0;
+    for (; s + 3 < whole; s += 2, t += 2 * kStep) {
+      stage(f[0]);
+      fetch(f[0], t + 2 * kStep);
+      multiply();
+      stage(f[1]);
+      fetch(f[1], t + 3 * kStep);
+      multiply();
+    }
+    const bool three = s + 2 < whole;
+    stage(f[0]);
+    if (three) fetch(f[0], t + 2 * kStep);
+    multiply();
+    stage(f[1]);
+    multiply();
+    if (three) {
+      stage(f[0]);
+      multiply();
+    }
+  } else if (whole == 1) {
+    fetch(f[0], t);
+    stage(f[0]);
+    multiply();
+  }
+  for (t = t0 + (int64_t)whole * kStep; t < t1; t += kStep) {
+    fetch_some(f[0], t);
+    stage(f[0]);
+    multiply();
   }
   // acc[i][j][e]: row 16 i + 4 (lane / 16) + e, column 16 j + lane % 16
 #pragma unroll
@@ -488,62 +546,79 @@ bool direct(const quasar_weight_grad& a) {
 
 struct Choice {
   int tile, splits, steps;  // values a side; shares of the tokens, and the steps of each
-  int64_t tiles_n, tiles;
+  int64_t tiles_n, tiles;           // tiles a column of them, and all
   int64_t padded, np, kp, parts;   // the tile kernel's tokens and columns, and the parts of dy
   int64_t rest;                    // the tokens from here on are copied
   int64_t whole;                   // the tiles of one workgroup each
   size_t x_bytes, dy_bytes, bytes;  // workspace: x, dy, and all of it with the shares' sums
 };
 
+// The least time of both kernels over the shares that the tokens can be cut into, from what was measured of their parts
+// (us).  A step of the 64 x 64 kernel takes 0.25, and 0.23 for each workgroup that a CU has, up to four (fp32: 0.7 and
+// 0.58), a round of workgroups 2.5 more.  A step of the tile kernel takes 1.3, in full rounds at the clock that the card
+// then holds 1.5; a round 2 and what its tiles write at 5.2 TB/s; the launch that spreads its operands 10 and what it moves.
+// Shares cost a join of 5, and what they and it move.  (bf16, the better against the other kernel at its best: 777 tokens,
+// 1000 x 1544 13.7, 29; 4096, 256 x 256 11.2, 21; 8192, 1024 x 1024 45.2, 46.9; 2048, 2048 x 2048 41.5, 46.3; 8192, 2048 x
+// 2048 85.5, 147; 200, 4096 x 4096 29.2, 31.0; 1000 48.1, 78.1.  A 128 x 128 form of the first was never better by more
+// than a tenth.)
+constexpr double kMoved = 5.2e6;  // bytes a us
 Choice choose(const quasar_weight_grad& a) {
-  const int64_t tokens = a.tokens, rows = a.rows, cols = a.cols;
+  const int64_t steps = a.tokens > 0 ? (a.tokens + kStep - 1) / kStep : 1;
+  const int64_t out = a.rows * part_pitch(a.cols) * 4;
+  const bool wide = a.dy_dtype == QUASAR_F32;
   Choice c{};
-  const auto tiles_of = [&](int b) { return ((rows + b - 1) / b) * ((cols + b - 1) / b); };
-  const int64_t steps = tokens > 0 ? (tokens + kStep - 1) / kStep : 1;
-  c.splits = 1;
-  c.parts = a.dy_dtype == QUASAR_F32 ? 3 : 1;
-  int64_t all = steps;
-  if (tiles_of(256) >= 128 && steps >= 8 && rows <= kMaxPitch && cols <= kMaxPitch) {
-    c.tile = 256;
-    c.tiles = tiles_of(256);
-    c.padded = steps * kStep;
-    c.np = (rows + 7) & ~(int64_t)7;
-    c.kp = (cols + 7) & ~(int64_t)7;
-    c.x_bytes = (size_t)(c.padded * c.kp * 2);
-    c.rest = direct(a) ? tokens / kStep * kStep : 0;
-    c.dy_bytes = (size_t)(c.parts * (c.padded - c.rest) * c.np * 2);
-    all = c.parts * steps;
-    // tiles for whole rounds of the CUs are a workgroup's each; those past them are shared out where that takes less
-    // time, of a step (1.55 us), a round (5) and the shares' sums, written and read at 5.2 TB/s (and 6 for the launch)
-    c.whole = c.tiles / kCUs * kCUs;
-    const int64_t rest = c.tiles - c.whole;
-    double least = 0.0;
-    for (int s = 1; rest > 0 && s <= 32 && s <= all; s++) {
-      const int64_t rounds = (rest * s + kCUs - 1) / kCUs;
-      const double us = rounds * (5.0 + (double)((all + s - 1) / s) * 1.55) + (s == 1 ? 0.0 : 6.0 + (double)(rest * s) * (2 * 256 * 256 * 4 / 5.2e6));
-      if (s == 1 || us < least) {
-        least = us;
-        c.splits = s;
-      }
-    }
-  } else {
-    c.tile = tiles_of(128) >= kCUs && a.dy_dtype == QUASAR_BF16 ? 128 : 64;
-    c.tiles = tiles_of(c.tile);
-    while (c.splits < 32 && 2 * c.tiles * c.splits <= 4 * kCUs && steps >= 2 * c.splits * 4) c.splits *= 2;
+  double least = 0.0;
+  const auto take = [&](double us, int tile, int64_t splits) {
+    if (c.tile != 0 && us >= least) return;
+    least = us;
+    c.tile = tile;
+    c.splits = (int)splits;
+  };
+  const int64_t small = ((a.rows + 63) / 64) * ((a.cols + 63) / 64);
+  for (int64_t s = 1, last = 0; s <= 32 && s <= steps && (s == 1 || small * s <= 16 * kCUs); s++) {
+    const int64_t per = (steps + s - 1) / s, groups = small * s;
+    if (per == last) continue;  // as many steps a share
+    last = per;
+    const int64_t full = groups / (4 * kCUs), rest = (groups % (4 * kCUs) + kCUs - 1) / kCUs;
+    const auto round = [&](double n) { return n == 0 ? 0.0 : 2.5 + (double)per * (wide ? 0.7 + 0.58 * n : 0.25 + 0.23 * n); };
+    take((double)full * round(4) + round((double)rest) + (s == 1 ? 0.0 : 5.0 + (double)(out * 2 * s) / kMoved), 64, s);
   }
-  c.tiles_n = (rows + c.tile - 1) / c.tile;
-  c.steps = (int)((all + c.splits - 1) / c.splits);
-  c.splits = (int)((all + c.steps - 1) / c.steps);
+  const int64_t tiles = ((a.rows + 255) / 256) * ((a.cols + 255) / 256), whole = tiles / kCUs * kCUs, rest = tiles - whole;
+  const int64_t parts = wide ? 3 : 1, all = parts * steps, padded = steps * kStep;
+  const int64_t np = (a.rows + 7) & ~(int64_t)7, kp = (a.cols + 7) & ~(int64_t)7, from = direct(a) ? a.tokens / kStep * kStep : 0;
+  if (a.rows <= kMaxPitch && a.cols <= kMaxPitch && all < (int64_t)1 << 24) {
+    constexpr double kTile = 256 * 256 * 4 / kMoved;
+    const auto round = [&](int64_t groups, int64_t per) {
+      return 2.0 + (double)per * (1.3 + 0.2 * (double)groups / kCUs) + (double)groups * kTile;
+    };
+    const double spread = 10.0 + (double)(padded * kp * 3 + (padded - from) * np * (wide ? 10 : 4)) / kMoved +
+                          (double)(whole / kCUs) * round(kCUs, all);
+    if (rest == 0) take(spread, 256, 1);
+    for (int64_t s = 1; rest > 0 && s <= 32 && s <= all; s++) {
+      const int64_t per = (all + s - 1) / s, groups = rest * s, full = groups / kCUs, last = groups % kCUs;
+      take(spread + (double)full * round(kCUs, per) + (last == 0 ? 0.0 : round(last, per)) +
+               (s == 1 ? 0.0 : 5.0 + (double)groups * kTile),
+           256, s);
+    }
+  }
+  const int64_t b = c.tile, total = c.tile == 256 ? all : steps;
+  c.tiles_n = (a.rows + b - 1) / b;
+  c.tiles = c.tiles_n * ((a.cols + b - 1) / b);
+  c.steps = (int)((total + c.splits - 1) / c.splits);
+  c.splits = (int)((total + c.steps - 1) / c.steps);
+  if (c.tile == 256) {
+    c.parts = parts;
+    c.padded = padded;
+    c.np = np;
+    c.kp = kp;
+    c.rest = from;
+    c.whole = whole;
+    c.x_bytes = (size_t)(padded * kp * 2);
+    c.dy_bytes = (size_t)(parts * (padded - from) * np * 2);
+  }
   c.bytes = c.x_bytes + c.dy_bytes;
-  if (c.splits > 1)
-    c.bytes += (size_t)c.splits * (c.tile == 256 ? (size_t)(c.tiles - c.whole) * 256 * 256 : (size_t)rows * (size_t)part_pitch(cols)) * 4;
+  if (c.splits > 1) c.bytes += (size_t)c.splits * (size_t)(c.tile == 256 ? rest * 256 * 256 * 4 : out);
   return c;
-}
-
-template <int GT, int B>
-void launch_tiles(const quasar_weight_grad& a, const Choice& c, float* part, hipStream_t stream) {
-  weight_grad_kernel<GT, B><<<dim3((unsigned)(c.tiles * c.splits)), dim3(256), 0, stream>>>(a, (int)c.tiles_n, c.splits, c.steps,
-                                                                                            part);
 }
 
 hipError_t launch_large(const quasar_weight_grad& a, const Choice& c, float* part, hipStream_t stream) {
@@ -586,12 +661,11 @@ hipError_t launch_weight_grad(const quasar_weight_grad& a, hipStream_t stream) {
   const Choice c = choose(a);
   float* const part = c.splits > 1 ? reinterpret_cast<float*>(reinterpret_cast<char*>(a.workspace) + c.x_bytes + c.dy_bytes) : nullptr;
   if (c.tile == 256) return launch_large(a, c, part, stream);
+  const dim3 grid((unsigned)(c.tiles * c.splits));
   if (a.dy_dtype == QUASAR_F32)
-    launch_tiles<kElemF32, 64>(a, c, part, stream);
-  else if (c.tile == 64)
-    launch_tiles<kElemBF16, 64>(a, c, part, stream);
+    weight_grad_kernel<kElemF32><<<grid, dim3(256), 0, stream>>>(a, (int)c.tiles_n, c.splits, c.steps, part);
   else
-    launch_tiles<kElemBF16, 128>(a, c, part, stream);
+    weight_grad_kernel<kElemBF16><<<grid, dim3(256), 0, stream>>>(a, (int)c.tiles_n, c.splits, c.steps, part);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !part) return e;
   const int64_t n = a.rows * (part_pitch(a.cols) / 8);
