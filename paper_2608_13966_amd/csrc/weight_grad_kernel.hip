@@ -24,11 +24,10 @@ __host__ __device__ constexpr int64_t part_pitch(int64_t cols) { return (cols + 
 
 // Eight E4M3 bytes times a power of two as packed bf16, exact.
 __device__ __forceinline__ uint4 kept_bf16(uint2 q, float f) {
-  float v[8];
-  unpack_e4m3x8(q, v);
-#pragma unroll
-  for (int i = 0; i < 8; i++) v[i] *= f;
-  return make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+  return make_uint4(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.x, f, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.x, f, true)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.y, f, false)),
+                    __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(q.y, f, true)));
 }
 
 // Eight fp32 values as the sum of three bf16 ones each: cut off after eight
@@ -82,13 +81,14 @@ __device__ __forceinline__ bf16x8 read_tile(const uint16_t* lds, int t0, int col
 // A workgroup makes 64 x 64 values of dweight (or of its share's sums in part) from
 // its share of the tokens, 64 at a time: the next two steps' pieces come to registers
 // while one is multiplied (with one step's, 777 tokens, 1000 x 1544 took 20.6 us, not
-// 13.7).  Four wavefronts of 32 x 32.
+// 14; four steps' were no faster).  Four wavefronts of 32 x 32.
 template <int GT>
 __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, int tiles_n, int splits, int steps_per, float* part) {
   constexpr int B = 64;
   constexpr int kParts = GT == kElemF32 ? 3 : 1, kPieces = kStep * B / 8 / 256, T = B / 32;
-  __shared__ __align__(16) uint16_t lds[(kParts + 1) * kStep * B];
-  uint16_t* const xs = lds + kParts * kStep * B;
+  // two stages where they are small: the next step is written while one is read (fp32's would leave fewer workgroups)
+  constexpr int kStages = GT == kElemF32 ? 1 : 2, kStage = (kParts + 1) * kStep * B, kX = kParts * kStep * B;
+  __shared__ __align__(16) uint16_t lds[kStages * kStage];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
   const int split = blockIdx.x % (unsigned)splits, tile = blockIdx.x / (unsigned)splits;
   const int64_t n0 = (int64_t)(tile % tiles_n) * B, k0 = (int64_t)(tile / tiles_n) * B;
@@ -106,14 +106,25 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
   } f[2];
   // Whole pieces without a branch (the compiler would wait for all of them where a branch ends): past a row's end is the
   // next row, and columns past the matrix reach nothing that is stored; those of a thread without any are the first ones.
+  // A thread's places in a step are 32-bit offsets from the step's first row.
   const int64_t gn = ln > 0 ? n0 + c : 0, qk = lk > 0 ? k0 + c : 0;
+  constexpr int kSize = elem_size<GT>();
+  uint32_t g_at[kPieces], q_at[kPieces], e_at[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; i++) {
+    const int64_t r = tr + i * kRound;
+    g_at[i] = (uint32_t)((r * a.dy_stride + gn) * kSize);
+    q_at[i] = (uint32_t)(r * a.q_stride + qk);
+    e_at[i] = (uint32_t)(r * a.exponent_stride + (qk >> 7));
+  }
   const auto fetch = [&](Fetched& o, int64_t t) {
+    const char* const g = reinterpret_cast<const char*>(a.dy) + t * a.dy_stride * kSize;
+    const uint8_t *const q = a.q + t * a.q_stride, *const e = a.exponent + t * a.exponent_stride;
 #pragma unroll
     for (int i = 0; i < kPieces; i++) {
-      const int64_t r = t + tr + i * kRound;
-      o.g[i].load(a.dy, r * a.dy_stride + gn, 8);
-      o.q[i] = ld8_any(a.q + r * a.q_stride + qk);
-      o.e[i] = a.exponent[r * a.exponent_stride + (qk >> 7)];
+      o.g[i].load(g + g_at[i], 0, 8);
+      o.q[i] = ld8_any(q + q_at[i]);
+      o.e[i] = e[e_at[i]];
     }
   };
   // near the last token: nothing past it
@@ -127,19 +138,20 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
       o.e[i] = has && lk > 0 ? a.exponent[r * a.exponent_stride + ((k0 + c) >> 7)] : 127u;
     }
   };
-  const auto stage = [&](const Fetched& o) {
+  const auto stage = [&](const Fetched& o, int to) {
+    uint16_t* const p = lds + to * kStage;
 #pragma unroll
     for (int i = 0; i < kPieces; i++) {
       const int at = spot<B>(tr + i * kRound, c);
       if constexpr (GT == kElemF32) {
-        uint4 p[3];
-        split3(o.g[i].f, p);
+        uint4 v[3];
+        split3(o.g[i].f, v);
 #pragma unroll
-        for (int j = 0; j < 3; j++) *reinterpret_cast<uint4*>(lds + j * kStep * B + at) = p[j];
+        for (int j = 0; j < 3; j++) *reinterpret_cast<uint4*>(p + j * kStep * B + at) = v[j];
       } else {
-        *reinterpret_cast<uint4*>(lds + at) = make_uint4(o.g[i].d[0], o.g[i].d[1], o.g[i].d[2], o.g[i].d[3]);
+        *reinterpret_cast<uint4*>(p + at) = make_uint4(o.g[i].d[0], o.g[i].d[1], o.g[i].d[2], o.g[i].d[3]);
       }
-      *reinterpret_cast<uint4*>(xs + at) = kept_bf16(o.q[i], as_f32(o.e[i] << 23));
+      *reinterpret_cast<uint4*>(p + kX + at) = kept_bf16(o.q[i], as_f32(o.e[i] << 23));
     }
   };
   f32x4 acc[T][T];
@@ -153,59 +165,76 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
-  const auto multiply = [&] {
-    meet();
+  const auto multiply = [&](int from) {
+    const uint16_t* const p = lds + from * kStage;
 #pragma unroll
     for (int k = 0; k < kStep; k += 32) {
       bf16x8 mx[T];
 #pragma unroll
-      for (int j = 0; j < T; j++) mx[j] = read_tile<B>(xs, k, wk + 16 * j, lane);
+      for (int j = 0; j < T; j++) mx[j] = read_tile<B>(p + kX, k, wk + 16 * j, lane);
 #pragma unroll
-      for (int p = 0; p < kParts; p++)
+      for (int q = 0; q < kParts; q++)
 #pragma unroll
         for (int i = 0; i < T; i++) {
-          const bf16x8 mg = read_tile<B>(lds + p * kStep * B, k, wn + 16 * i, lane);
+          const bf16x8 mg = read_tile<B>(p + q * kStep * B, k, wn + 16 * i, lane);
 #pragma unroll
           for (int j = 0; j < T; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mg, mx[j], acc[i][j], 0, 0, 0);
         }
     }
-    meet();  // every wavefront is done with the step
   };
   // the steps whose pieces, eight elements past a row's end too, lie before the last token's row
   const int64_t safe = a.tokens - 8 < t1 ? a.tokens - 8 : t1;
-  const int whole = safe > t0 ? (int)((safe - t0) / kStep) : 0;
-  int64_t t = t0;
-  if (whole >= 2) {
-    fetch(f[0], t);
-    fetch(f[1], t + kStep);
-    int s = 0;
-    for (; s + 3 < whole; s += 2, t += 2 * kStep) {
-      stage(f[0]);
-      fetch(f[0], t + 2 * kStep);
-      multiply();
-      stage(f[1]);
-      fetch(f[1], t + 3 * kStep);
-      multiply();
+  const bool near = a.dy_stride < kMaxPitch && a.q_stride < kMaxPitch && a.exponent_stride < kMaxPitch;  // offsets fit
+  const int whole = near && safe > t0 ? (int)((safe - t0) / kStep) : 0;
+  const auto step_at = [&](int s) { return t0 + (int64_t)(s < whole ? s : whole - 1) * kStep; };  // past the last: it again
+  if (whole > 0) {
+    fetch(f[0], step_at(0));
+    fetch(f[1], step_at(1));
+    if constexpr (kStages == 2) {
+      stage(f[0], 0);
+      fetch(f[0], step_at(2));
     }
-    const bool three = s + 2 < whole;
-    stage(f[0]);
-    if (three) fetch(f[0], t + 2 * kStep);
-    multiply();
-    stage(f[1]);
-    multiply();
-    if (three) {
-      stage(f[0]);
-      multiply();
+    // step s, the next one in o
+    const auto step = [&](int s, Fetched& o) {
+      if constexpr (kStages == 2) {
+        meet();  // the step is written, and all are done with the one before
+        const uint16_t* const p = lds + (s & 1) * kStage;
+        bf16x8 mx[2][T], mg[2][T];
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+          for (int j = 0; j < T; j++) {
+            mx[k][j] = read_tile<B>(p + kX, 32 * k, wk + 16 * j, lane);
+            mg[k][j] = read_tile<B>(p, 32 * k, wn + 16 * j, lane);
+          }
+        stage(o, (s + 1) & 1);
+        fetch(o, step_at(s + 3));
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+          for (int i = 0; i < T; i++)
+#pragma unroll
+            for (int j = 0; j < T; j++) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mg[k][i], mx[k][j], acc[i][j], 0, 0, 0);
+      } else {
+        stage(o, 0);
+        fetch(o, step_at(s + 2));
+        meet();
+        multiply(0);
+        meet();
+      }
+    };
+    for (int s = 0; s < whole; s += 2) {
+      step(s, f[kStages == 2 ? 1 : 0]);
+      if (s + 1 < whole) step(s + 1, f[kStages == 2 ? 0 : 1]);
     }
-  } else if (whole == 1) {
-    fetch(f[0], t);
-    stage(f[0]);
-    multiply();
+    meet();
   }
-  for (t = t0 + (int64_t)whole * kStep; t < t1; t += kStep) {
+  for (int64_t t = t0 + (int64_t)whole * kStep; t < t1; t += kStep) {
     fetch_some(f[0], t);
-    stage(f[0]);
-    multiply();
+    stage(f[0], 0);
+    meet();
+    multiply(0);
+    meet();
   }
   // acc[i][j][e]: row 16 i + 4 (lane / 16) + e, column 16 j + lane % 16
 #pragma unroll
@@ -554,13 +583,12 @@ struct Choice {
 };
 
 // The least time of both kernels over the shares that the tokens can be cut into, from what was measured of their parts
-// (us).  A step of the 64 x 64 kernel takes 0.25, and 0.23 for each workgroup that a CU has, up to four (fp32: 0.7 and
-// 0.58), a round of workgroups 2.5 more.  A step of the tile kernel takes 1.3, in full rounds at the clock that the card
-// then holds 1.5; a round 2 and what its tiles write at 5.2 TB/s; the launch that spreads its operands 10 and what it moves.
-// Shares cost a join of 5, and what they and it move.  (bf16, the better against the other kernel at its best: 777 tokens,
-// 1000 x 1544 13.7, 29; 4096, 256 x 256 11.2, 21; 8192, 1024 x 1024 45.2, 46.9; 2048, 2048 x 2048 41.5, 46.3; 8192, 2048 x
-// 2048 85.5, 147; 200, 4096 x 4096 29.2, 31.0; 1000 48.1, 78.1.  A 128 x 128 form of the first was never better by more
-// than a tenth.)
+// (us).  A step of the 64 x 64 kernel takes 0.2, and 0.23 for each workgroup that a CU has, up to four (fp32: 0.6 and 0.52),
+// a round of workgroups 2, and 0.8 for each, more.  A step of the tile kernel takes 1.3, in full rounds at the clock that
+// the card then holds 1.5; a round 2 and what its tiles write at 5.2 TB/s; the launch that spreads its operands 10 and what
+// it moves.  Shares cost a join of 5, and what they and it move.  (bf16, 64 x 64 against tiles, each at its best: 777 tokens,
+// 1000 x 1544 14, 29; 4096, 256 x 256 11, 21; 8192, 1024 x 1024 47, 45; 2048, 2048 x 2048 41, 46; 8192, 2048 x 2048 147, 86;
+// 200, 4096 x 4096 36, 29; 1000 78, 48.  A 128 x 128 form of the first was never better by more than a tenth.)
 constexpr double kMoved = 5.2e6;  // bytes a us
 Choice choose(const quasar_weight_grad& a) {
   const int64_t steps = a.tokens > 0 ? (a.tokens + kStep - 1) / kStep : 1;
@@ -580,7 +608,7 @@ Choice choose(const quasar_weight_grad& a) {
     if (per == last) continue;  // as many steps a share
     last = per;
     const int64_t full = groups / (4 * kCUs), rest = (groups % (4 * kCUs) + kCUs - 1) / kCUs;
-    const auto round = [&](double n) { return n == 0 ? 0.0 : 2.5 + (double)per * (wide ? 0.7 + 0.58 * n : 0.25 + 0.23 * n); };
+    const auto round = [&](double n) { return n == 0 ? 0.0 : 2.0 + 0.8 * n + (double)per * (wide ? 0.6 + 0.52 * n : 0.2 + 0.23 * n); };
     take((double)full * round(4) + round((double)rest) + (s == 1 ? 0.0 : 5.0 + (double)(out * 2 * s) / kMoved), 64, s);
   }
   const int64_t tiles = ((a.rows + 255) / 256) * ((a.cols + 255) / 256), whole = tiles / kCUs * kCUs, rest = tiles - whole;
