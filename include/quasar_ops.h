@@ -331,8 +331,9 @@ int quasar_checkpoint_backward_check(const quasar_checkpoint_grad* a);
 /*
  * The weight gradient of a linear layer whose input was kept:
  *   dweight[n, k] = sum over t of dy[t, n] * q[t, k] * 2^e
- * Products are exact in fp32 (dy in fp32 is taken in three parts of bf16, of
- * which values under 2^-126 in size are lost), sums are in fp32 in a fixed order.
+ * Products are exact in fp32 (dy in fp32 is taken in three parts of bf16; values
+ * under 2^-126 in size, of a part or of q * 2^e, may be lost), sums are in fp32 in
+ * a fixed order.
  */
 typedef struct {
   int64_t tokens;            /* 0 <= tokens <= 2^28: none gives 0 */

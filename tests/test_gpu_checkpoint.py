@@ -286,6 +286,33 @@ def test_fp32_gradients_are_taken_whole(n, k):
 
 
 @pytest.mark.parametrize("gt", ["bf16", "fp32"])
+@pytest.mark.parametrize("t,n,k", [(150, 200, 300), (700, 4096, 4096)])
+@pytest.mark.parametrize("x_size,dy_size", [(2.0 ** -100, 2.0 ** 90), (2.0 ** 120, 2.0 ** -100)])
+def test_weight_grad_at_the_ends_of_the_range(gt, t, n, k, x_size, dy_size):
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = (torch.rand(t, k, generator=g, device=DEV) + 0.5) * x_size
+    dy = ((torch.randn(t, n, generator=g, device=DEV) + 3) * dy_size).to(DT[gt])
+    kept = O.checkpoint_rows(x)
+    assert (back(kept["q"], kept["exponent"]) != 0).all()
+    check_weight(dy, kept["q"], kept["exponent"], O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"])
+
+
+@pytest.mark.parametrize("n,k", [(64, 200), (4096, 2048)])
+def test_weight_grad_with_far_apart_rows(n, k):
+    """Strides past what 32-bit offsets of a step take."""
+    t, stride = 100, (1 << 22) + 24
+    kept = O.checkpoint_rows(gen((t, k), torch.bfloat16, 1))
+    buf = torch.empty(t * stride, device=DEV, dtype=torch.bfloat16)
+    dy = buf.view(t, stride)[:, :n]
+    dy.copy_(gen((t, n), torch.bfloat16, 2))
+    check_weight(dy, kept["q"], kept["exponent"], O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"])
+    qb = torch.empty(t * stride, device=DEV, dtype=torch.uint8)
+    q = qb.view(t, stride)[:, :k]
+    q.copy_(kept["q"].view(torch.uint8))
+    check_weight(dy, q.view(E4M3), kept["exponent"], O.linear_weight_grad(dy, q.view(E4M3), kept["exponent"])["dw"])
+
+
+@pytest.mark.parametrize("gt", ["bf16", "fp32"])
 @pytest.mark.parametrize("t,n,k", [(70, 200, 300), (191, 4096, 4096)])
 def test_what_is_not_finite_reaches_its_row_and_column(gt, t, n, k):
     x = gen((t, k), torch.bfloat16, 1)

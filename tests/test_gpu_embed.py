@@ -144,6 +144,19 @@ def test_no_tokens():
     assert (O.embed_backward(dy[:, :2], tok, 300000, out=out)["dw"] == 0).all()
 
 
+@pytest.mark.parametrize("n", [1, 700, 5000])
+@pytest.mark.parametrize("rows", [3, 1000, 100000])
+def test_tokens_that_are_none(n, rows):
+    """Padding alone: no row is read, and the gradient is 0 whatever dy holds."""
+    tok = torch.full((n,), -1, device=DEV)
+    tok[::2] = rows
+    assert (O.embed(tok, torch.full((rows, 20), float("nan"), device=DEV))["y"] == 0).all()
+    for stride in (20, 24):
+        dw = torch.full((rows, stride), 7.0, device=DEV)[:, :20]
+        dy = torch.full((n, 20), float("nan"), device=DEV)
+        assert (O.embed_backward(dy, tok, rows, out={"dw": dw})["dw"] == 0).all()
+
+
 def test_nan_stays_in_its_row():
     dy, tok = torch.ones(200, 80, device=DEV), torch.arange(200, device=DEV) % 50
     dy[7, 3], dy[9, 4] = float("nan"), float("inf")
