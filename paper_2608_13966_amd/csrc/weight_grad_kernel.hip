@@ -391,23 +391,40 @@ __global__ __launch_bounds__(512, 2) void weight_grad_tile_kernel(quasar_weight_
       x_at[h][i] = 2u * (uint32_t)((k < op.kp ? k : op.kp - 1) * kStep + 8 * ((lane & 7) ^ ((m >> 1) & 7)));
     }
   }
-  const auto fill_g = [&](int h, int step) {
-    const uint32_t to = lds0 + ((step & 1) * kStage + h * kHalf + wave * 8 * 128) * 2;
-    const int s = first + (step < steps ? step : steps - 1);
-    const bool rest = s >= op.whole;
-    const uint32_t pitch = 2u * (uint32_t)(rest ? op.rest_stride : op.dy_stride);
-    const char* const from = reinterpret_cast<const char*>(rest ? op.rest : op.dy) + (int64_t)(rest ? s - op.whole : s) * kStep * pitch;
-#pragma unroll
-    for (int i = 0; i < 2; i++) load_lds16(from, __umul24(row[i], pitch) + g_col[h][i], to + i * 4 * 128 * 2);
+  // where the next step to be filled lies, a step on at a time; past the last step it stays
+  int g_step = first, x_step = first;
+  const bool in_rest = first >= op.whole;
+  uint32_t pitch = 2u * (uint32_t)(in_rest ? op.rest_stride : op.dy_stride);
+  const char* g_from = reinterpret_cast<const char*>(in_rest ? op.rest : op.dy) + (int64_t)(first - (in_rest ? op.whole : 0)) * kStep * pitch;
+  const int64_t g_pace = (int64_t)kStep * pitch, x_pace = (int64_t)op.kp * (2 * kStep);
+  const char* x_from = reinterpret_cast<const char*>(op.x) + (int64_t)(first % op.period) * x_pace;
+  int x_left = op.period - 1 - first % op.period;  // steps until x begins again
+  const auto next_g = [&] {
+    if (g_step + 1 >= first + steps) return;
+    g_from += g_pace;
+    if (++g_step == op.whole) {
+      g_from = reinterpret_cast<const char*>(op.rest);
+      pitch = 2u * (uint32_t)op.rest_stride;
+    }
   };
-  const auto fill_x = [&](int h, int step) {
-    const uint32_t to = lds0 + ((step & 1) * kStage + (2 + h) * kHalf + wave * 16 * kStep) * 2;
-    int s = first + (step < steps ? step : steps - 1);
-    if (s >= op.period) s -= op.period;
-    if (s >= op.period) s -= op.period;
-    const char* const from = reinterpret_cast<const char*>(op.x) + (int64_t)s * op.kp * (2 * kStep);
+  const auto next_x = [&] {
+    if (x_step + 1 >= first + steps) return;
+    x_step++;
+    x_from += x_pace;
+    if (x_left-- == 0) {
+      x_from = reinterpret_cast<const char*>(op.x);
+      x_left = op.period - 1;
+    }
+  };
+  const auto fill_g = [&](int h, int stage) {
+    const uint32_t to = lds0 + (stage * kStage + h * kHalf + wave * 8 * 128) * 2;
 #pragma unroll
-    for (int i = 0; i < 2; i++) load_lds16(from, x_at[h][i], to + i * 8 * kStep * 2);
+    for (int i = 0; i < 2; i++) load_lds16(g_from, __umul24(row[i], pitch) + g_col[h][i], to + i * 4 * 128 * 2);
+  };
+  const auto fill_x = [&](int h, int stage) {
+    const uint32_t to = lds0 + (stage * kStage + (2 + h) * kHalf + wave * 16 * kStep) * 2;
+#pragma unroll
+    for (int i = 0; i < 2; i++) load_lds16(x_from, x_at[h][i], to + i * 8 * kStep * 2);
   };
   f32x4 acc[4][8];
 #pragma unroll
@@ -458,9 +475,12 @@ __global__ __launch_bounds__(512, 2) void weight_grad_tile_kernel(quasar_weight_
   fill_x(0, 0);
   fill_g(1, 0);
   fill_x(1, 0);
+  next_g();
+  next_x();
   fill_g(0, 1);
   fill_x(0, 1);
   fill_g(1, 1);
+  next_g();
   landed8();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -473,14 +493,16 @@ __global__ __launch_bounds__(512, 2) void weight_grad_tile_kernel(quasar_weight_
     const int stage = s & 1;
     read_x(0, stage);
     read_g(1, stage, fg[1]);
-    fill_x(1, s + 1);
-    fill_g(0, s + 2);
+    fill_x(1, stage ^ 1);
+    fill_g(0, stage);
+    next_x();
     landed8();
     multiply(0);
     read_x(1, stage);
     read_g(0, stage ^ 1, next);
-    fill_x(0, s + 2);
-    fill_g(1, s + 2);
+    fill_x(0, stage);
+    fill_g(1, stage);
+    next_g();
     landed8();
     multiply(1);
 #pragma unroll
