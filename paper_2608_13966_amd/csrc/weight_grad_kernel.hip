@@ -332,11 +332,18 @@ __device__ __forceinline__ int chunk_at(int m, int c) { return m * kStep + 8 * (
 // columns, 64 tokens a step.  Both operands of a step lie in LDS as two halves each, g0
 // and x0 the first 128 rows and columns (of dy whole lines of memory), 32 and 64 of
 // them a wavefront's, g1 and x1 the rest; and a step has two phases, each with 32
-// matrix instructions a wavefront: x0 (g0 g1), x1 (g0 g1).  dy is read by transposing loads,
-// twice as dear as plain ones, hence the wavefront's shape, and the reads are spread
-// evenly: phase 0 reads x0 and g1, phase 1 x1 and the next step's g0.  (Both operands
-// through transposing loads, in tiles of 128 x 64: 862 us, not @; LDS was busy all the
-// time.)  Two stages; a half is filled again as soon as all have read it.
+// matrix instructions a wavefront: x0 (g0 g1), x1 (g0 g1).  The reads are spread evenly:
+// phase 0 reads x0 and g1, phase 1 x1 and the next step's g0.  Two stages; a half is
+// filled again as soon as all have read it.
+//
+// 8192 tokens, 14336 x 4096, normal values: the call takes 719 us (26 spread the operands,
+// 17 join the shares), 1.34 PFLOP/s; a library product of these sizes with its sum along
+// the rows takes 700 to 735, dy^T x as it is 1030.  Matrix units are busy 70% of the
+// time, and the card's power is part of the bound: with all-zero operands 619.  On the way
+// (us): both operands through transposing loads, three quarters of a step's reads in its
+// first phase 882; halves of half lines of dy 922, of whole ones 795; the tiles past whole
+// rounds shared out 747; addresses that go on a step at a time 727; loads ahead of reads
+// 719.  32 x 32 x 16 instructions took 777, not 747.
 //
 // The wavefronts of a SIMD work in turn: those of wk = 1 run one barrier behind, so
 // that while one multiplies the other reads its next operands.  Barriers 2p and 2p + 1
@@ -491,17 +498,17 @@ __global__ __launch_bounds__(512, 2) void weight_grad_tile_kernel(quasar_weight_
   if (wk == 1) __builtin_amdgcn_s_barrier();
   for (int s = 0; s < steps; s++) {
     const int stage = s & 1;
-    read_x(0, stage);
-    read_g(1, stage, fg[1]);
     fill_x(1, stage ^ 1);
     fill_g(0, stage);
+    read_x(0, stage);
+    read_g(1, stage, fg[1]);
     next_x();
     landed8();
     multiply(0);
-    read_x(1, stage);
-    read_g(0, stage ^ 1, next);
     fill_x(0, stage);
     fill_g(1, stage);
+    read_x(1, stage);
+    read_g(0, stage ^ 1, next);
     next_g();
     landed8();
     multiply(1);
