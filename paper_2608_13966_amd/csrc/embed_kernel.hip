@@ -13,6 +13,11 @@
 // it is filled with zeros beside the sort, whose few workgroups mostly wait; else the
 // sort marks the rows that tokens have, and further workgroups of the summing launch
 // write zeros into the others.
+//
+// All of it is bound by memory but for the launches.  32768 tokens of 131072 x 4096 in
+// bf16: lookup 64 us; gradient 260 (count 6, place 24 and 150 with the fill, sum 70, join
+// 9; the bytes at a copy's rate 259, a fill of the table alone 157).  8 tokens, lookup
+// 2.7; 1999 of 50021 x 1537 in fp32, gradient 62 (47, 9 and 5).
 #include "ops_common.h"
 #include "ops_internal.h"
 
