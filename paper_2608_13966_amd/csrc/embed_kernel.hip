@@ -71,7 +71,6 @@ struct Sort {
   const uint2* from;     // later ones (token, position) pairs
   uint2* to;
   uint32_t* counts;      // [chunks][bins]
-  uint32_t* next;        // the same of the next pass, or NULL
   uint8_t* touched;      // [rows], 1 where a token has the row; or NULL
   int index_bits, tokens, chunk;
   uint32_t rows;
@@ -119,15 +118,11 @@ __device__ __forceinline__ void clear_marks(const Sort& s, int64_t i, int64_t al
     reinterpret_cast<uint4*>(s.touched)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// How often each digit of the first pass occurs in a chunk.  The counts of the later
-// passes (`later` of them) are cleared: the pass before counts its keys where it brings
-// them, by integer atomics, whose order does not matter.
-__device__ __forceinline__ void count(const Sort& s, int chunks, int later) {
+// How often each digit of a pass occurs in a chunk.
+__device__ __forceinline__ void count(const Sort& s, int chunks) {
   __shared__ uint32_t bin[kMaxBins];
   for (int i = threadIdx.x; i < s.bins; i += kThreads) bin[i] = 0;
-  const int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x, all = (int64_t)chunks * kThreads, each = (int64_t)chunks * s.bins;
-  clear_marks(s, i0, all);
-  for (int64_t i = i0; i < later * each; i += all) s.counts[each + i] = 0;
+  if (!s.from) clear_marks(s, (int64_t)blockIdx.x * kThreads + threadIdx.x, (int64_t)chunks * kThreads);
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * s.chunk;
   const int end = (int)(first + s.chunk < s.tokens ? first + s.chunk : s.tokens);
@@ -138,9 +133,9 @@ __device__ __forceinline__ void count(const Sort& s, int chunks, int later) {
 }
 
 // In both kernels the workgroups past the first `chunks` fill units a .. b - 1.
-__global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int chunks, int later, Fill f, int64_t a, int64_t b) {
+__global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int chunks, Fill f, int64_t a, int64_t b) {
   if ((int)blockIdx.x < chunks)
-    count(s, chunks, later);
+    count(s, chunks);
   else
     fill_units<kThreads>(f, a, b, blockIdx.x - chunks, gridDim.x - chunks);
 }
@@ -192,19 +187,21 @@ __device__ __forceinline__ void place(const Sort& s, int chunks) {
   constexpr int kOwn = kMaxBins / kThreads;
   uint32_t before[kOwn], all[kOwn], mine = 0;
 #pragma unroll
-  for (int j = 0; j < kOwn; j++) {
-    const int d = threadIdx.x * kOwn + j;
-    before[j] = all[j] = 0;
-    if (d < bins) {
-#pragma unroll 8
-      for (int c = 0; c < chunks; c++) {
-        const uint32_t n = s.counts[(int64_t)c * bins + d];
-        before[j] += c < (int)blockIdx.x ? n : 0;
-        all[j] += n;
-      }
+  for (int j = 0; j < kOwn; j++) before[j] = all[j] = 0;
+  if ((int)threadIdx.x * kOwn < bins) {
+    static_assert(kOwn == 2, "a pair of digits");
+    const uint2* const own = reinterpret_cast<const uint2*>(s.counts) + threadIdx.x;
+#pragma unroll 16
+    for (int c = 0; c < chunks; c++) {
+      const uint2 n = own[(int64_t)c * (bins / 2)];
+      before[0] += c < (int)blockIdx.x ? n.x : 0;
+      before[1] += c < (int)blockIdx.x ? n.y : 0;
+      all[0] += n.x;
+      all[1] += n.y;
     }
-    mine += all[j];
   }
+#pragma unroll
+  for (int j = 0; j < kOwn; j++) mine += all[j];
   uint32_t at = sum_before<kWaves>(mine, sums);
 #pragma unroll
   for (int j = 0; j < kOwn; j++) {
@@ -245,11 +242,7 @@ __device__ __forceinline__ void place(const Sort& s, int chunks) {
 #pragma unroll
     for (int j = 0; j < kKeys; j++) {
       const int64_t i = i0 + wave * (64 * kKeys) + j * 64 + lane;
-      if (i < end) {
-        const uint32_t to = count[wave][(key[j].x >> s.shift) & (bins - 1)] + rank[j];
-        s.to[to] = key[j];
-        if (s.next) atomicAdd(s.next + (int64_t)(to / (uint32_t)s.chunk) * bins + ((key[j].x >> (s.shift + s.width)) & (bins - 1)), 1u);
-      }
+      if (i < end) s.to[count[wave][(key[j].x >> s.shift) & (bins - 1)] + rank[j]] = key[j];
     }
     __syncthreads();
   }
@@ -526,6 +519,7 @@ constexpr int64_t kCountFill = 8 << 10, kPlaceFill = 12 << 10;  // units
 int64_t least_of(int64_t a, int64_t b) { return a < b ? a : b; }
 int64_t round16(int64_t n) { return (n + 15) & ~(int64_t)15; }
 
+constexpr int64_t kFull = 2048;  // wavefronts that sum at once
 // The sort's passes and where the scratch memory's parts lie.
 struct Plan {
   int passes, bits;          // digits of so many bits
@@ -540,14 +534,15 @@ struct Plan {
     const int64_t rounds = tokens > 0 ? (tokens + kRound - 1) / kRound : 1, each = (rounds + kMaxChunks - 1) / kMaxChunks;
     chunk = (int)(each * kRound);
     chunks = (int)((rounds + each - 1) / each);
-    // short stretches where there are few tokens, so that enough of them run at once
-    stretch = tokens >= 16384 ? 32 : tokens >= 4096 ? 16 : 8;
+    // short stretches where there are few wavefronts' worth of them, so that enough run at once
+    const int64_t lanes = cols <= 64 ? 8 : cols <= 128 ? 16 : cols <= 256 ? 32 : (cols + 511) / 512 * 64, waves = tokens * lanes / 64;
+    stretch = waves >= 32 * kFull ? 32 : waves >= 16 * kFull ? 16 : 8;
     stretches = (int)((tokens + stretch - 1) / stretch);
     pitch = (int)((cols + 7) & ~(int64_t)7);
     a = 0;
     b = a + round16(tokens * 8);
     counts = b + round16(tokens * 8);
-    touched = counts + round16(((int64_t)chunks * 4 << bits) * passes);
+    touched = counts + round16((int64_t)chunks * 4 << bits);
     part = touched + round16(rows);
     bytes = part + (int64_t)stretches * 2 * pitch * 4;
   }
@@ -666,19 +661,18 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
       done = least_of(done + n, units);
       return a0;
     };
-    int64_t from = share(kCountFill);
-    count_kernel<<<dim3(with_fill(p.chunks, done - from)), dim3(kThreads), 0, stream>>>(s, p.chunks, p.passes - 1, f, from, done);
-    e = hipGetLastError();
+    e = hipSuccess;
     for (int i = 0; i < p.passes && e == hipSuccess; i++) {
-      const bool last = i == p.passes - 1;
       s.from = i == 0 ? nullptr : bufs[(i - 1) & 1];
       s.to = bufs[i & 1];
       s.shift = i * p.bits;
-      s.next = last ? nullptr : s.counts + ((int64_t)p.chunks << p.bits);
-      from = share(last ? units : kPlaceFill);
+      int64_t from = share(kCountFill);
+      count_kernel<<<dim3(with_fill(p.chunks, done - from)), dim3(kThreads), 0, stream>>>(s, p.chunks, f, from, done);
+      e = hipGetLastError();
+      if (e != hipSuccess) break;
+      from = share(i == p.passes - 1 ? units : kPlaceFill);
       place_kernel<<<dim3(with_fill(p.chunks, done - from)), dim3(kThreads), 0, stream>>>(s, p.chunks, f, from, done);
       e = hipGetLastError();
-      s.counts = s.next;
     }
   }
   if (e != hipSuccess) return e;
