@@ -12,12 +12,12 @@
 // Rows that no token has are zeros.  Where there are few tokens for the table, all of
 // it is filled with zeros beside the sort, whose few workgroups mostly wait; else the
 // sort marks the rows that tokens have, and further workgroups of the summing launch
-// write zeros into the others.
+// write zeros into the others.  Short lists and small tables take one launch, in which
+// each workgroup sorts for itself.
 //
 // All of it is bound by memory but for the launches.  32768 tokens of 131072 x 4096 in
-// bf16: lookup 64 us; gradient 260 (count 6, place 24 and 150 with the fill, sum 70, join
-// 9; the bytes at a copy's rate 259, a fill of the table alone 157).  8 tokens, lookup
-// 2.7; 1999 of 50021 x 1537 in fp32, gradient 62 (47, 9 and 5).
+// bf16: lookup 64 us; gradient 247 (@; the bytes at a copy's rate 259, a fill of the table
+// alone 157).  8 tokens, lookup 2.7; 1999 of 50021 x 1537 in fp32, gradient 62 (47, 9 and 5).
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -349,29 +349,34 @@ __device__ __forceinline__ void put_row(const Grad& g, uint32_t row, int c, cons
     put_row<false>(g, row, c, v);
 }
 
-// Zeros in set `set` of eight rows, where no token has them, by a wavefront: 16 bytes a lane.
+// Zeros in a row by `lanes` lanes: 16 bytes each.
+__device__ __forceinline__ void zero_row(const Grad& g, int64_t row, int lanes = 64) {
+  const int lane = threadIdx.x & (lanes - 1), size = g.dw_bf16 ? 2 : 4, bytes = g.cols * size;
+  char* const p = reinterpret_cast<char*>(g.dw) + row * g.dw_stride * size;
+  for (int b = lane * 16; b < bytes; b += lanes * 16) {
+    if (b + 16 <= bytes) {
+      st16_any(p + b, make_uint4(0u, 0u, 0u, 0u));
+    } else {
+      for (int e = b; e < bytes; e += size) {
+        if (size == 2)
+          *reinterpret_cast<uint16_t*>(p + e) = 0;
+        else
+          *reinterpret_cast<uint32_t*>(p + e) = 0u;
+      }
+    }
+  }
+}
+
+// Zeros in set `set` of eight rows, where no token has them, by a wavefront.
 constexpr int kSet = 8;
 __device__ __forceinline__ void zero_rows(const Grad& g, int64_t set) {
   const int64_t r0 = set * kSet;
   if (r0 >= g.rows) return;
-  const int lane = threadIdx.x & 63, size = g.dw_bf16 ? 2 : 4, bytes = g.cols * size;
   const uint2 t = *reinterpret_cast<const uint2*>(g.touched + r0);  // whole pieces of 16 are there
 #pragma unroll 1
   for (int i = 0; i < kSet; i++) {
     if (((i < 4 ? t.x : t.y) >> (8 * (i & 3)) & 0xffu) || r0 + i >= g.rows) continue;
-    char* const p = reinterpret_cast<char*>(g.dw) + (r0 + i) * g.dw_stride * size;
-    for (int b = lane * 16; b < bytes; b += 1024) {
-      if (b + 16 <= bytes) {
-        st16_any(p + b, make_uint4(0u, 0u, 0u, 0u));
-      } else {
-        for (int e = b; e < bytes; e += size) {
-          if (size == 2)
-            *reinterpret_cast<uint16_t*>(p + e) = 0;
-          else
-            *reinterpret_cast<uint32_t*>(p + e) = 0u;
-        }
-      }
-    }
+    zero_row(g, r0 + i);
   }
 }
 
@@ -504,6 +509,181 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(Grad g, Divide per
   put_row(g, key, c, sum);
 }
 
+// ---- gradient, one launch -----------------------------------------------------------
+// For lists and tables so small that launches would take most of the time: the first
+// `sum_groups` workgroups sort the whole list, each for itself, and sum the rows whose
+// tokens begin in their share of it (8 L columns of them); the others write the zeros.
+// Up to kFew tokens are sorted by counting the smaller keys of each: 221 of 10136 x 16
+// 9 us, 13 by digits (for up to 512 counting takes as long as digits).
+constexpr int kFew = 256;
+constexpr int kOnceBits = 10;   // of a position: a key is row and position in 32 bits
+constexpr int kOnceTokens = 1 << kOnceBits, kOnceRows = 1 << 18;
+
+// The first of list[0 .. n - 1], ascending, that is not below v.
+__device__ __forceinline__ int lower_bound(const uint32_t* list, int n, uint32_t v) {
+  int at = 0;
+  for (; n > 0;) {
+    const int half = n >> 1;
+    if (list[at + half] < v) {
+      at += half + 1;
+      n -= half + 1;
+    } else {
+      n = half;
+    }
+  }
+  return at;
+}
+
+template <int GT, int L>
+__global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int passes, int parts, int each, int zero_rows_each) {
+  constexpr int kWaves = 16, kShares = 1024 / L;
+  __shared__ __align__(16) uint32_t list[kOnceTokens];
+  __shared__ uint32_t sums[kWaves];
+  // first the digits' counts (or the rows that tokens have, one bit each), then the shares' sums
+  __shared__ union {
+    uint32_t count[kWaves][kMaxBins];
+    uint32_t bits[kOnceRows / 32];
+    float part[kShares][2][8][L];
+  } u;
+  const int tid = threadIdx.x, wave = wave_index();
+  const bool has = tid < s.tokens;
+  uint32_t key = has ? token_at(s.index, s.index_bits, tid, s.rows) << kOnceBits | (uint32_t)tid : ~0u;
+  if ((int)blockIdx.x >= g.sum_groups) {
+    const int r0 = (int)(blockIdx.x - g.sum_groups) * zero_rows_each, left = (int)s.rows - r0, n = left < zero_rows_each ? left : zero_rows_each;
+    if (n <= 0) return;
+    for (int i = tid; i < (n + 31) / 32; i += 1024) u.bits[i] = 0;
+    __syncthreads();
+    const uint32_t own = (key >> kOnceBits) - (uint32_t)r0;
+    if (has && own < (uint32_t)n) atomicOr(&u.bits[own >> 5], 1u << (own & 31));
+    __syncthreads();
+    const int lanes = L == 64 || g.dw_bf16 ? L : 2 * L;
+    for (int r = tid / lanes; r < n; r += 1024 / lanes)
+      if (!(u.bits[r >> 5] >> (r & 31) & 1u)) zero_row(g, r0 + r, lanes);
+    return;
+  }
+  if (s.tokens <= kFew) {
+    // a place is the number of smaller keys, each key's in shares
+    constexpr int kOwn = kFew * kFew / 4096;  // pieces of four keys
+    if (tid < kFew) {
+      list[tid] = key;
+      u.bits[tid] = 0;
+    }
+    __syncthreads();
+    const uint32_t mine = list[tid & (kFew - 1)];
+    uint32_t below = 0;
+    const uint4* const from = reinterpret_cast<const uint4*>(list) + (tid / kFew) * kOwn;
+    for (int j = 0; j < kOwn; j++) {
+      const uint4 v = from[j];
+      below += (v.x < mine) + (v.y < mine) + (v.z < mine) + (v.w < mine);
+    }
+    atomicAdd(&u.bits[tid & (kFew - 1)], below);
+    __syncthreads();
+    if (tid < s.tokens) list[u.bits[tid]] = mine;
+    __syncthreads();
+  } else {
+    const int bins = s.bins;
+    for (int p = 0; p < passes; p++) {
+      const int shift = kOnceBits + p * s.width;
+      for (int i = tid; i < kWaves * kMaxBins; i += 1024) (&u.count[0][0])[i] = 0;
+      __syncthreads();
+      const uint32_t rank = rank_of(key >> shift, bins, has, u.count[wave]);
+      __syncthreads();
+      uint32_t all = 0;
+      if (tid < kMaxBins) {
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) {
+          const uint32_t n = u.count[w][tid];
+          u.count[w][tid] = all;
+          all += n;
+        }
+      }
+      const uint32_t at = sum_before<kWaves>(all, sums);
+      if (tid < kMaxBins) {
+#pragma unroll
+        for (int w = 0; w < kWaves; w++) u.count[w][tid] += at;
+      }
+      __syncthreads();
+      if (has) list[u.count[wave][(key >> shift) & (bins - 1)] + rank] = key;
+      __syncthreads();
+      if (has) key = list[tid];
+    }
+  }
+  // the tokens a .. b - 1 of the rows that begin in this workgroup's share
+  const int n = lower_bound(list, s.tokens, s.rows << kOnceBits);
+  const int share = tid / L, col = tid & (L - 1), group = (int)blockIdx.x / parts;
+  const int c = ((int)blockIdx.x - group * parts) * (8 * L) + col * 8, left = g.cols - c;
+  const auto row_at = [&](int i) { return list[i] >> kOnceBits; };
+  const auto from_row = [&](int i) {  // i, or where the row that goes on there ends
+    if (i >= n) return n;
+    return i > 0 && row_at(i) == row_at(i - 1) ? lower_bound(list, n, (row_at(i) + 1) << kOnceBits) : i;
+  };
+  const int a = from_row(group * each), b = from_row((group + 1) * each), q = (b - a + kShares - 1) / kShares;
+  const int p0 = a + share * q, p1 = p0 + q < b ? p0 + q : b;
+  const bool any = p0 < p1, begun = any && p0 > a && row_at(p0) == row_at(p0 - 1), goes_on = any && p1 < b && row_at(p1) == row_at(p1 - 1);
+  if (any) {
+    constexpr int kAhead = 4;
+    struct Batch {
+      uint32_t key[kAhead];
+      Piece<GT> row[kAhead];
+    } batch[2];
+    const auto fetch = [&](Batch& o, int i) {
+#pragma unroll
+      for (int j = 0; j < kAhead; j++) {
+        const uint32_t v = i + j < p1 ? list[i + j] : ~0u;
+        o.key[j] = v >> kOnceBits;
+        o.row[j].load(g.dy, i + j < p1 ? (int64_t)(v & (kOnceTokens - 1)) * g.dy_stride + c : 0, i + j < p1 ? left : 0);
+      }
+    };
+    fetch(batch[0], p0);
+    float sum[8] = {};
+    uint32_t now = batch[0].key[0];
+    bool before = begun;
+    const auto flush = [&](bool on) {
+      if (before || on) {
+#pragma unroll
+        for (int k = 0; k < 8; k++) u.part[share][before ? 0 : 1][k][col] = sum[k];
+      } else if (left > 0) {
+        put_row(g, now, c, sum);
+      }
+    };
+    const auto add = [&](const Batch& o, int i) {
+#pragma unroll
+      for (int j = 0; j < kAhead; j++) {
+        if (i + j >= p1) break;
+        if (o.key[j] != now) {
+          flush(false);
+          now = o.key[j];
+          before = false;
+#pragma unroll
+          for (int k = 0; k < 8; k++) sum[k] = 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; k++) sum[k] += o.row[j].get(k);
+      }
+    };
+    for (int i = p0; i < p1; i += 2 * kAhead) {
+      fetch(batch[1], i + kAhead);
+      add(batch[0], i);
+      fetch(batch[0], i + 2 * kAhead);
+      add(batch[1], i + kAhead);
+    }
+    flush(goes_on);
+  }
+  __syncthreads();
+  // the rows that several shares have sums of, by the one in which they begin
+  if (!goes_on || left <= 0 || (begun && row_at(p0) == row_at(p1 - 1))) return;
+  const uint32_t row = row_at(p1);
+  float sum[8];
+#pragma unroll
+  for (int k = 0; k < 8; k++) sum[k] = u.part[share][1][k][col];
+  const int last = (lower_bound(list, n, (row + 1) << kOnceBits) - 1 - a) / q;  // the share in which it ends
+#pragma unroll 4
+  for (int t = share + 1; t <= last; t++)
+#pragma unroll
+    for (int k = 0; k < 8; k++) sum[k] += u.part[t][0][k][col];
+  put_row(g, row, c, sum);
+}
+
 // f(L) for the lanes that a row of so many columns takes
 template <typename F>
 hipError_t with_lanes(int64_t cols, F f) {
@@ -560,6 +740,21 @@ hipError_t launch_sum(Grad g, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.stretches < 2) return e;
   embed_join_kernel<L><<<dim3((unsigned)((g.stretches - 1) * per)), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
+  return hipGetLastError();
+}
+
+template <int GT, int L>
+hipError_t launch_once(const Grad& from, const Sort& s, int passes, hipStream_t stream) {
+  Grad g = from;
+  // about four tokens a share, and no more workgroups than run at once
+  const int64_t parts = (g.cols + 8 * L - 1) / (8 * L), most = parts < kCUs / 2 ? kCUs / 2 / parts : 1;
+  int64_t groups = (g.tokens + 4 * (1024 / L) - 1) / (4 * (1024 / L));
+  groups = groups < 1 ? 1 : least_of(groups, most);
+  const int64_t bytes = (int64_t)g.rows * g.cols * (g.dw_bf16 ? 2 : 4);
+  const int64_t zeros = least_of((bytes + 16383) / 16384, 2 * kCUs);
+  g.sum_groups = groups * parts;
+  embed_once_kernel<GT, L><<<dim3((unsigned)(g.sum_groups + zeros)), dim3(1024), 0, stream>>>(
+      g, s, passes, (int)parts, (int)((g.tokens + groups - 1) / groups), (int)((g.rows + zeros - 1) / zeros));
   return hipGetLastError();
 }
 
@@ -638,10 +833,19 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   g.rows = s.rows;
   g.scale = a.scale;
   g.dw_bf16 = a.dweight_dtype == QUASAR_BF16;
+  const int64_t bytes = a.rows * a.cols * size_of(a.dweight_dtype);
+  // One launch (us, against three): 221 tokens of 10136 x 16 9, 22; 1000 of 1000 x 1024 15, 19; 1024 of 10000 x 8192 25, 34;
+  // 512 of 32000 x 4096 35, 43.  In tables of which the last-level cache holds less than half, the fill past it decides: 8 of
+  // 131072 x 2048 in fp32 101, 94.  With all tokens the same 1000 of 1000 x 1024 take 25, 22; longer lists 2762 x 598 115, 47.
+  if (a.tokens <= kOnceTokens && a.rows <= kOnceRows && bytes <= 2 * kLastLevel) {
+    return with_lanes(a.cols, [&](auto lanes) {
+      constexpr int L = decltype(lanes)::value;
+      return a.dy_dtype == QUASAR_BF16 ? launch_once<kElemBF16, L>(g, s, p.passes, stream) : launch_once<kElemF32, L>(g, s, p.passes, stream);
+    });
+  }
   // Filling all of the table is the faster where no more than half of its rows can be touched: they are written twice, but
   // the rest without a look at the marks, and beside the sort (131072 x 4096 in bf16, us: 8 tokens 183 against 196, 32768
   // 260 against 293, 60000 317 against 358; 65536 tokens of 50000 x 2048 130 against 126).
-  const int64_t bytes = a.rows * a.cols * size_of(a.dweight_dtype);
   const Fill f{reinterpret_cast<char*>(a.dweight), bytes, (int)size_of(a.dweight_dtype), bytes > 2 * kLastLevel};
   const bool fill = a.tokens <= a.rows / 2 && (a.rows == 1 || a.dweight_stride == a.cols);
   if (fill) s.touched = nullptr;

@@ -120,6 +120,23 @@ def test_grad_of_long_lists(rows, cols, n, kind):
     check_grad(dy, tok, rows, 0.5, O.embed_backward(dy, tok, rows, scale=0.5)["dw"])
 
 
+@pytest.mark.parametrize("rows,cols,n,kinds", [
+    (60, 33, 255, KINDS), (60, 33, 256, KINDS), (600, 72, 257, KINDS), (90, 300, 1023, KINDS), (3000, 130, 1024, KINDS),
+    (1500, 513, 1025, KINDS), (2000, 20, 4096, KINDS), (600, 33, 4097, KINDS), (1 << 18, 8, 1000, ["uniform", "one", "none"]),
+    ((1 << 18) + 1, 8, 1000, ["uniform", "one", "none"]), (2, 1, 1000, KINDS), (7, 9000, 40, KINDS), (3, 65536, 90, ["few", "none"]),
+    (140000, 1000, 5, ["uniform", "one"])])
+def test_grad_of_short_lists(rows, cols, n, kinds):
+    """Around the ends of the forms: lists that each workgroup sorts, that one workgroup sorts, and longer ones;
+    tables of more rows or bytes than the first form takes."""
+    for kind in kinds:
+        m = min(n, rows) if kind == "once" else n
+        for i, (gt, wt, it) in enumerate([("bf16", "fp32", torch.int32), ("fp32", None, torch.int64)]):
+            dy, tok = gen((m, cols), DT[gt], i, pad=cols % 5, off=cols % 3), draw(m, rows, kind, 20 + i, it)
+            dy[(tok < 0) | (tok >= rows)] = float("nan")
+            out = {"dw": torch.full((rows, cols), float("nan"), device=DEV, dtype=DT[wt or gt])}
+            check_grad(dy, tok, rows, -0.75, O.embed_backward(dy, tok, rows, scale=-0.75, dw_dtype=wt, out=out)["dw"])
+
+
 def test_grad_into_a_wider_buffer_with_a_used_workspace():
     dy, tok = gen((500, 300), torch.bfloat16, 1), draw(500, 60, "none", 3)
     dy = dy.nan_to_num()
