@@ -90,8 +90,12 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
   constexpr int kStages = GT == kElemF32 ? 1 : 2, kStage = (kParts + 1) * kStep * B, kX = kParts * kStep * B;
   __shared__ __align__(16) uint16_t lds[kStages * kStage];
   const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
-  const int split = blockIdx.x % (unsigned)splits, tile = blockIdx.x / (unsigned)splits;
-  const int64_t n0 = (int64_t)(tile % tiles_n) * B, k0 = (int64_t)(tile / tiles_n) * B;
+  // neighbouring tiles on an XCD, whose L2 then holds what they read: 10308 tokens, 6825 x 216 109 us, else 165; 12011, 1743 x
+  // 1459 171, 269; 777, 1000 x 1544 14, 14
+  const int tiles = (int)(gridDim.x / (unsigned)splits), u = stretch_of(blockIdx.x, gridDim.x), split = u / tiles;
+  int tn, tk;
+  tile_at(u - split * tiles, tiles_n, tiles / tiles_n, tn, tk);
+  const int64_t n0 = (int64_t)tn * B, k0 = (int64_t)tk * B;
   const int64_t t0 = (int64_t)split * steps_per * kStep;
   const int64_t t1 = t0 + (int64_t)steps_per * kStep < a.tokens ? t0 + (int64_t)steps_per * kStep : a.tokens;
 
@@ -614,10 +618,11 @@ struct Choice {
 // The least time of both kernels over the shares that the tokens can be cut into, from what was measured of their parts
 // (us).  A step of the 64 x 64 kernel takes 0.2, and 0.23 for each workgroup that a CU has, up to four (fp32: 0.6 and 0.52),
 // a round of workgroups 2, and 0.8 for each, more.  A step of the tile kernel takes 1.3, in full rounds at the clock that
-// the card then holds 1.5; a round 2 and what its tiles write at 5.2 TB/s; the launch that spreads its operands 10 and what
-// it moves.  Shares cost a join of 5, and what they and it move.  (bf16, 64 x 64 against tiles, each at its best: 777 tokens,
-// 1000 x 1544 14, 29; 4096, 256 x 256 11, 21; 8192, 1024 x 1024 47, 45; 2048, 2048 x 2048 41, 46; 8192, 2048 x 2048 147, 86;
-// 200, 4096 x 4096 36, 29; 1000 78, 48.  A 128 x 128 form of the first was never better by more than a tenth.)
+// the card then holds 1.5; a round 2 and what its tiles write at 6.9 TB/s; the launch that spreads its operands 7 and what
+// it moves.  Shares cost a join of 5 and 3, and what they and it move.  (bf16, 64 x 64 against tiles, each at its best: 777
+// tokens, 1000 x 1544 14, 30; 4096, 256 x 256 11, 24; 8192, 1024 x 1024 48, 48; 2048, 2048 x 2048 41, 45; 8192, 2048 x 2048
+// 161, 86; 200, 4096 x 4096 38, 29; 1000 78, 47; 10308, 6824 x 216 101, 58, 6825 x 216 107, 101.  A 128 x 128 form of the
+// first was never better by more than a tenth.)
 constexpr double kMoved = 5.2e6;  // bytes a us
 Choice choose(const quasar_weight_grad& a) {
   const int64_t steps = a.tokens > 0 ? (a.tokens + kStep - 1) / kStep : 1;
@@ -644,17 +649,17 @@ Choice choose(const quasar_weight_grad& a) {
   const int64_t parts = wide ? 3 : 1, all = parts * steps, padded = steps * kStep;
   const int64_t np = (a.rows + 7) & ~(int64_t)7, kp = (a.cols + 7) & ~(int64_t)7, from = direct(a) ? a.tokens / kStep * kStep : 0;
   if (a.rows <= kMaxPitch && a.cols <= kMaxPitch && all < (int64_t)1 << 24) {
-    constexpr double kTile = 256 * 256 * 4 / kMoved;
+    constexpr double kTile = 256 * 256 * 4 / 6.9e6;
     const auto round = [&](int64_t groups, int64_t per) {
       return 2.0 + (double)per * (1.3 + 0.2 * (double)groups / kCUs) + (double)groups * kTile;
     };
-    const double spread = 10.0 + (double)(padded * kp * 3 + (padded - from) * np * (wide ? 10 : 4)) / kMoved +
+    const double spread = 7.0 + (double)(padded * kp * 3 + (padded - from) * np * (wide ? 10 : 4)) / kMoved +
                           (double)(whole / kCUs) * round(kCUs, all);
     if (rest == 0) take(spread, 256, 1);
     for (int64_t s = 1; rest > 0 && s <= 32 && s <= all; s++) {
       const int64_t per = (all + s - 1) / s, groups = rest * s, full = groups / kCUs, last = groups % kCUs;
       take(spread + (double)full * round(kCUs, per) + (last == 0 ? 0.0 : round(last, per)) +
-               (s == 1 ? 0.0 : 5.0 + (double)groups * kTile),
+               (s == 1 ? 0.0 : 3.0 + (double)groups * kTile),
            256, s);
     }
   }
