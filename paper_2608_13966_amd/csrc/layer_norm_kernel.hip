@@ -401,13 +401,14 @@ hipError_t with_backward_shape(int64_t cols, F f) {
 // Workgroups of the backward pass, each with its shares of dweight and dbias: what runs at once, in whole rounds of rows.
 // Where one or two rounds would do, fewer may be better, since their shares are written and summed too: a round is reckoned
 // 1.1 us, a workgroup's shares 6.2e-6 us a column.  (777 x 1537 fp32: 256 workgroups 11.7 us, 96 14.9, 777 16.6; 1000 x 4096
-// bf16: 256 16.0, 96 20.6, 512 18.5; 300 x 4096: 128 10.4, 300 13.7.)
+// bf16: 256 16.0, 96 20.6, 512 18.5; 300 x 4096: 128 10.4, 300 13.7.)  One workgroup's need no second launch, 3.4 (fp32: 4 x
+// 4096 6.1, else 7.5; 6 7.4, 7.5; past 8192 columns a round takes longer: 3 x 16384 11.4, 9.1).
 int backward_groups(int64_t rows, int64_t cols) {
   const int64_t per = cols <= 64 ? 32 : cols <= 128 ? 16 : cols <= 256 ? 8 : cols <= 1024 ? 4 : 1;  // rows a workgroup takes at once
   const int64_t most = (cols <= 2048 ? 4 : cols <= 4096 ? 2 : 1) * kCUs;
   const int64_t units = (rows + per - 1) / per, first = (units + most - 1) / most;
   int64_t groups = (units + first - 1) / first;
-  const auto time = [&](int64_t n) { return (double)((units + n - 1) / n) * 1.1 + (double)(n * cols) * 6.2e-6; };
+  const auto time = [&](int64_t n) { return (double)((units + n - 1) / n) * 1.1 + (double)(n * cols) * 6.2e-6 + (n == 1 && cols <= 8192 ? 0.0 : 3.4); };
   for (int64_t rounds = first + 1; first <= 2 && rounds <= 8 && rounds <= units; rounds++) {
     const int64_t n = (units + rounds - 1) / rounds;
     if (time(n) < time(groups)) groups = n;
