@@ -66,10 +66,10 @@ __device__ __forceinline__ int spot(int t, int col) {
 }
 
 // The operand of a 16 x 16 x 32 matrix instruction: columns col .. col + 15 of the
-// 32 rows from t0 on.
-template <int W>
+// 32 rows from t0 on.  (APART: its groups of four columns lie so far apart.)
+template <int W, int APART = 4>
 __device__ __forceinline__ bf16x8 read_tile(const uint16_t* lds, int t0, int col, int lane) {
-  const int t = t0 + 8 * (lane >> 4) + ((lane & 15) >> 2), c = col + 4 * (lane & 3);
+  const int t = t0 + 8 * (lane >> 4) + ((lane & 15) >> 2), c = col + APART * (lane & 3);
   typedef __attribute__((address_space(3))) s16x4 lds4;
   const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + spot<W>(t, c)));
   const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(lds + spot<W>(t + 4, c)));
@@ -254,6 +254,145 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
         else
           put_elem(a.dweight, n * a.dweight_stride + k, acc[i][j][r], a.dweight_dtype == QUASAR_BF16);
       }
+}
+
+// ---- few tokens ---------------------------------------------------------------------
+// Up to 128 tokens: one step is all there is, and writing dweight is what takes the time.  A workgroup makes 128 rows x
+// 256 columns (128 past 64 tokens) from operands that it stages once; a wavefront keeps its columns of x in registers,
+// reads 16 rows of dy at a time and stores from where the products are: x is the first operand, so that a lane has
+// neighbours of a row.  bf16, us (a fill of dweight's bytes; the other kernels): 16 tokens, 8192 x 8192 in fp32 42 (40;
+// 65), in bf16 22 (20; 44); 4, 14336 x 4096 37 (35; 62); 96, 4096 x 4096 15 (10; 25).  Past the caches 73, not 42.
+template <int GT, int KS>
+struct Few {
+  static constexpr int P = KS > 2 ? 1 : 2;                          // 32-column parts of a wavefront
+  static constexpr int N = GT == kElemF32 && KS > 2 ? 64 : 128, K = 128 * P;  // rows and columns of a workgroup
+};
+template <int GT, int KS, bool WB>
+__global__ __launch_bounds__(256) void weight_grad_few_kernel(quasar_weight_grad a, int tiles_k) {
+  constexpr int N = Few<GT, KS>::N, K = Few<GT, KS>::K, P = Few<GT, KS>::P, R = 32 * KS, kParts = GT == kElemF32 ? 3 : 1;
+  constexpr int kXRow = K / 8, kXRows = 256 / kXRow, kX = R / kXRows, kGRow = N / 8, kGRows = 256 / kGRow, kG = R / kGRows;
+  __shared__ __align__(16) uint16_t lds[R * K + kParts * R * N];
+  uint16_t* const lds_g = lds + R * K;
+  const int tid = threadIdx.x, lane = tid & 63, wave = wave_index();
+  const int u = stretch_of(blockIdx.x, gridDim.x), tn = u / tiles_k;
+  const int64_t n0 = (int64_t)tn * N, k0 = (int64_t)(u - tn * tiles_k) * K;
+  // this thread's pieces: eight columns of a row of each round.  Whole ones without a branch: a row past the last
+  // token is the last one's and becomes 0, a piece past a row's end is the row's last (nothing of it is stored)
+  const int xc = (tid % kXRow) * 8, xr = tid / kXRow, gc = (tid % kGRow) * 8, gr = tid / kGRow, last = (int)a.tokens - 1;
+  const int lk = (int)(a.cols - k0 - xc < 8 ? a.cols - k0 - xc : 8), ln = (int)(a.rows - n0 - gc < 8 ? a.rows - n0 - gc : 8);
+  const int64_t xk = lk < 8 ? a.cols - 8 : k0 + xc, gn = ln < 8 ? a.rows - 8 : n0 + gc;
+  const int64_t block = (lk > 0 ? k0 + xc : a.cols - 1) >> 7;
+  uint2 q[kX];
+  uint32_t e[kX];
+  Piece<GT> g[kG];
+#pragma unroll
+  for (int i = 0; i < kX; i++) {
+    const int t = xr + kXRows * i < last ? xr + kXRows * i : last;
+    q[i] = ld8_any(a.q + t * a.q_stride + xk);
+    e[i] = a.exponent[t * a.exponent_stride + block];
+  }
+#pragma unroll
+  for (int i = 0; i < kG; i++) {
+    const int t = gr + kGRows * i < last ? gr + kGRows * i : last;
+    g[i].load(a.dy, t * a.dy_stride + gn, 8);
+  }
+  // a piece that the row's end cuts: its elements one by one
+  if (lk > 0 && lk < 8) {
+#pragma unroll
+    for (int i = 0; i < kX; i++) {
+      const int t = xr + kXRows * i < last ? xr + kXRows * i : last;
+      const uint8_t* const p = a.q + t * a.q_stride + k0 + xc;
+      uint32_t b[8];
+#pragma unroll
+      for (int j = 0; j < 8; j++) b[j] = p[j < lk ? j : 0];
+      q[i] = make_uint2(b[0] | b[1] << 8 | b[2] << 16 | b[3] << 24, b[4] | b[5] << 8 | b[6] << 16 | b[7] << 24);
+    }
+  }
+  if (ln > 0 && ln < 8) {
+#pragma unroll
+    for (int i = 0; i < kG; i++) {
+      const int t = gr + kGRows * i < last ? gr + kGRows * i : last;
+      const int64_t at = t * a.dy_stride + n0 + gc;
+      if constexpr (GT == kElemF32) {
+#pragma unroll
+        for (int j = 0; j < 8; j++) g[i].f[j] = reinterpret_cast<const float*>(a.dy)[at + (j < ln ? j : 0)];
+      } else {
+        const uint16_t* const p = reinterpret_cast<const uint16_t*>(a.dy) + at;
+#pragma unroll
+        for (int j = 0; j < 4; j++) g[i].d[j] = p[2 * j < ln ? 2 * j : 0] | (uint32_t)p[2 * j + 1 < ln ? 2 * j + 1 : 0] << 16;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kX; i++) {
+    const int t = xr + kXRows * i;
+    const uint4 v = kept_bf16(q[i], as_f32(e[i] << 23));
+    *reinterpret_cast<uint4*>(lds + spot<K>(t, xc)) = t <= last ? v : make_uint4(0u, 0u, 0u, 0u);
+  }
+#pragma unroll
+  for (int i = 0; i < kG; i++) {
+    const int t = gr + kGRows * i;
+    uint4 v[kParts];
+    if constexpr (GT == kElemF32)
+      split3(g[i].f, v);
+    else
+      v[0] = make_uint4(g[i].d[0], g[i].d[1], g[i].d[2], g[i].d[3]);
+#pragma unroll
+    for (int p = 0; p < kParts; p++)
+      *reinterpret_cast<uint4*>(lds_g + p * R * N + spot<N>(t, gc)) = t <= last ? v[p] : make_uint4(0u, 0u, 0u, 0u);
+  }
+  __syncthreads();
+  // Instruction h of part p has columns 32 p + 8 (0 .. 3) + 4 h + (0 .. 3), with an output in fp32 32 p + 16 h + (0 .. 15):
+  // four lanes then store 64 neighbouring bytes
+  constexpr int kApart = WB ? 8 : 4, kNext = WB ? 4 : 16;
+  const int w0 = wave * (32 * P);
+  bf16x8 mx[P][2][KS];
+#pragma unroll
+  for (int p = 0; p < P; p++)
+#pragma unroll
+    for (int h = 0; h < 2; h++)
+#pragma unroll
+      for (int k = 0; k < KS; k++) mx[p][h][k] = read_tile<K, kApart>(lds, 32 * k, w0 + 32 * p + kNext * h, lane);
+  for (int s = 0; s < N && n0 + s < a.rows; s += 16) {
+    f32x4 acc[P][2];
+#pragma unroll
+    for (int p = 0; p < P; p++)
+#pragma unroll
+      for (int h = 0; h < 2; h++) acc[p][h] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < KS; k++)
+#pragma unroll
+      for (int z = 0; z < kParts; z++) {
+        const bf16x8 mg = read_tile<N>(lds_g + z * R * N, 32 * k, s, lane);
+#pragma unroll
+        for (int p = 0; p < P; p++)
+#pragma unroll
+          for (int h = 0; h < 2; h++) acc[p][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx[p][h][k], mg, acc[p][h], 0, 0, 0);
+      }
+    // acc[p][h][i]: row s + lane % 16, column 32 p + kNext h + kApart (lane / 16) + i
+    const int64_t n = n0 + s + (lane & 15), k = k0 + w0 + kApart * (lane >> 4), at = n * a.dweight_stride + k;
+    if (n >= a.rows) continue;
+#pragma unroll
+    for (int p = 0; p < P; p++) {
+      if constexpr (WB) {
+        const float v[8] = {acc[p][0][0], acc[p][0][1], acc[p][0][2], acc[p][0][3], acc[p][1][0], acc[p][1][1], acc[p][1][2], acc[p][1][3]};
+        store_piece<true>(a.dweight, at + 32 * p, v, (int)(a.cols - k - 32 * p));
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+          const int left = (int)(a.cols - k) - 32 * p - 16 * h;
+          float* const to = reinterpret_cast<float*>(a.dweight) + at + 32 * p + 16 * h;
+          if (left >= 4) {
+            st16_any(to, __builtin_bit_cast(uint4, acc[p][h]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 3; i++)
+              if (i < left) to[i] = acc[p][h][i];
+          }
+        }
+      }
+    }
+  }
 }
 
 // ---- large weights ----------------------------------------------------------------
@@ -607,7 +746,7 @@ bool direct(const quasar_weight_grad& a) {
 }
 
 struct Choice {
-  int tile, splits, steps;  // values a side; shares of the tokens, and the steps of each
+  int tile, splits, steps;  // values a side, 0: the kernel for few tokens; shares of the tokens, and the steps of each
   int64_t tiles_n, tiles;           // tiles a column of them, and all
   int64_t padded, np, kp, parts;   // the tile kernel's tokens and columns, and the parts of dy
   int64_t rest;                    // the tokens from here on are copied
@@ -624,7 +763,35 @@ struct Choice {
 // 161, 86; 200, 4096 x 4096 38, 29; 1000 78, 47; 10308, 6824 x 216 101, 58, 6825 x 216 107, 101.  A 128 x 128 form of the
 // first was never better by more than a tenth.)
 constexpr double kMoved = 5.2e6;  // bytes a us
+
+// f(type of dy, steps of 32 tokens)
+template <typename F>
+auto with_few(const quasar_weight_grad& a, F f) {
+  using std::integral_constant;
+  const auto steps = [&](auto gt) {
+    if (a.tokens <= 32) return f(gt, integral_constant<int, 1>());
+    if (a.tokens <= 64) return f(gt, integral_constant<int, 2>());
+    if (a.tokens <= 96) return f(gt, integral_constant<int, 3>());
+    return f(gt, integral_constant<int, 4>());
+  };
+  return a.dy_dtype == QUASAR_F32 ? steps(integral_constant<int, kElemF32>()) : steps(integral_constant<int, kElemBF16>());
+}
+
 Choice choose(const quasar_weight_grad& a) {
+  // The kernel for few tokens where it has workgroups for half of the CUs (us, against the others: 64 tokens of 2048 x 2048
+  // in 128 of them 8.4, 8.1, with dweight in bf16 5.9, 6.6; in 256 of 2048 x 4096 9.1, 12.8; 43 of 1347 x 2606 in 121 8.8, 8.3;
+  // 33 of 1000 x 1000 in 32 6.2, 5.1).
+  if (a.tokens >= 1 && a.tokens <= 128 && a.rows >= 8 && a.cols >= 8) {
+    Choice few{};
+    few.splits = few.steps = 1;
+    (void)with_few(a, [&](auto gt, auto ks) {
+      using Form = Few<decltype(gt)::value, decltype(ks)::value>;
+      few.tiles_n = (a.rows + Form::N - 1) / Form::N;
+      few.tiles = few.tiles_n * ((a.cols + Form::K - 1) / Form::K);
+      return 0;
+    });
+    if (few.tiles >= kCUs / 2 && few.tiles <= most_groups(256)) return few;
+  }
   const int64_t steps = a.tokens > 0 ? (a.tokens + kStep - 1) / kStep : 1;
   const int64_t out = a.rows * part_pitch(a.cols) * 4;
   const bool wide = a.dy_dtype == QUASAR_F32;
@@ -716,12 +883,25 @@ bool weight_grad_fits(const quasar_weight_grad& a, size_t& workspace) {
   workspace = c.bytes;
   if (c.tile == 256 && c.padded / kStep * ((c.kp + 127) / 128) + 32 * kCUs > most_groups(256)) return false;
   if (c.tile == 256) return c.tiles <= most_groups(512) - 32 * kCUs;
+  if (c.tile == 0) return true;
   return c.tiles * c.splits <= most_groups(256) && (c.splits == 1 || a.rows * (part_pitch(a.cols) / 8) <= 256 * most_groups(256));
+}
+
+template <int GT, int KS>
+hipError_t launch_few(const quasar_weight_grad& a, const Choice& c, hipStream_t stream) {
+  const dim3 grid((unsigned)c.tiles);
+  const int tiles_k = (int)(c.tiles / c.tiles_n);
+  if (a.dweight_dtype == QUASAR_BF16)
+    weight_grad_few_kernel<GT, KS, true><<<grid, dim3(256), 0, stream>>>(a, tiles_k);
+  else
+    weight_grad_few_kernel<GT, KS, false><<<grid, dim3(256), 0, stream>>>(a, tiles_k);
+  return hipGetLastError();
 }
 
 hipError_t launch_weight_grad(const quasar_weight_grad& a, hipStream_t stream) {
   const Choice c = choose(a);
   float* const part = c.splits > 1 ? reinterpret_cast<float*>(reinterpret_cast<char*>(a.workspace) + c.x_bytes + c.dy_bytes) : nullptr;
+  if (c.tile == 0) return with_few(a, [&](auto gt, auto ks) { return launch_few<decltype(gt)::value, decltype(ks)::value>(a, c, stream); });
   if (c.tile == 256) return launch_large(a, c, part, stream);
   const dim3 grid((unsigned)(c.tiles * c.splits));
   if (a.dy_dtype == QUASAR_F32)

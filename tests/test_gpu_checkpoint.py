@@ -260,6 +260,42 @@ def test_weight_grad_strides(t, n, k, pads):
     assert (dwb[:, k:] == 7).all()
 
 
+FEW = [(1, 3126, 4372), (2, 8, 33000), (3, 16400, 9), (31, 1500, 2700), (32, 2047, 2049), (33, 2049, 2047), (64, 2061, 2560), (65, 1281, 1803),
+       (96, 1030, 3001), (97, 2056, 1416), (128, 1999, 1289)]
+
+
+@pytest.mark.parametrize("t,n,k", FEW)
+@pytest.mark.parametrize("gt,wt", [("bf16", "fp32"), ("fp32", "fp32"), ("bf16", "bf16"), ("fp32", "bf16")])
+def test_weight_grad_of_few_tokens(t, n, k, gt, wt):
+    """Rows of wider buffers, which hold NaN, as does what lies before and after them; what is beside the result stays."""
+    kept, blocks = O.checkpoint_rows(gen((t, k), torch.bfloat16, 1)), -(-k // 128)
+    dyb = torch.full((t + 2, n + 3), NAN, device=DEV, dtype=DT[gt])
+    qb = torch.full((t + 2, k + 5), 0x7f, device=DEV, dtype=torch.uint8)
+    eb = torch.full((t + 2, blocks + 1), 255, device=DEV, dtype=torch.uint8)
+    dwb = torch.full((n + 2, k + 5), 7.0, device=DEV, dtype=DT[wt])
+    dy, q, e, dw = dyb[1:-1, 1:n + 1], qb[1:-1, 1:k + 1], eb[1:-1, 1:], dwb[1:-1, 3:k + 3]
+    dy.copy_(gen((t, n), DT[gt], 2, 1e-3)), q.copy_(kept["q"].view(torch.uint8)), e.copy_(kept["exponent"])
+    assert O.linear_weight_grad(dy, q.view(E4M3), e, dw_dtype=wt, out={"dw": dw})["workspace"] is None
+    check_weight(dy, q.view(E4M3), e, dw)
+    again = O.linear_weight_grad(dy.contiguous(), kept["q"], kept["exponent"], dw_dtype=wt)["dw"]
+    assert torch.equal(again, dw)
+    dw.fill_(7.0)
+    assert (dwb == 7).all()
+
+
+@pytest.mark.parametrize("gt", ["bf16", "fp32"])
+@pytest.mark.parametrize("t,n,k", [(1, 2050, 3001), (70, 3001, 1030)])
+def test_what_is_not_finite_among_few_tokens(gt, t, n, k):
+    kept, dy = O.checkpoint_rows(gen((t, k), torch.bfloat16, 1).clamp_min(0.5)), gen((t, n), DT[gt], 2)
+    want = O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"].clone()
+    dy[t - 1, n - 2], dy[0, 0] = INF, NAN
+    kept["q"].view(torch.uint8)[t - 1, k - 1] = 0x7f
+    dw = O.linear_weight_grad(dy, kept["q"], kept["exponent"])["dw"]
+    assert (dw[n - 2, :k - 1] == INF).all() and dw[0].isnan().all() and dw[:, k - 1].isnan().all()
+    rows = [i for i in range(n) if i not in (0, n - 2)]
+    assert torch.equal(dw[rows, :k - 1], want[rows, :k - 1])
+
+
 @pytest.mark.parametrize("gt", ["bf16", "fp32"])
 @pytest.mark.parametrize("n,k", [(300, 200), (4096, 4096)])
 def test_one_hot_tokens_read_what_was_kept(gt, n, k):
