@@ -183,6 +183,27 @@ __device__ __forceinline__ void place(const Sort& s, int chunks) {
   constexpr int kWaves = kThreads / 64, kKeys = kRound / kThreads;  // keys a lane holds
   __shared__ uint32_t base[kMaxBins], count[kWaves][kMaxBins], sums[kWaves];
   const int lane = threadIdx.x & 63, wave = wave_index(), bins = s.bins;
+  const int64_t first = (int64_t)blockIdx.x * s.chunk;
+  const int end = (int)(first + s.chunk < s.tokens ? first + s.chunk : s.tokens);
+  uint2 key[kKeys];
+  const auto fetch = [&](int64_t i0) {
+    int at[kKeys];
+#pragma unroll
+    for (int j = 0; j < kKeys; j++) {  // past the end the last, without a branch: the loads then run side by side
+      const int64_t i = i0 + wave * (64 * kKeys) + j * 64 + lane;
+      at[j] = (int)(i < end ? i : end - 1);
+    }
+    if (s.from) {
+#pragma unroll
+      for (int j = 0; j < kKeys; j++) key[j] = s.from[at[j]];
+    } else if (s.index_bits == 64) {
+#pragma unroll
+      for (int j = 0; j < kKeys; j++) key[j] = make_uint2(token_at(s.index, 64, at[j], s.rows), (uint32_t)at[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kKeys; j++) key[j] = make_uint2(token_at(s.index, 32, at[j], s.rows), (uint32_t)at[j]);
+    }
+  };
   // of two digits a thread: their number before this chunk, and in all
   constexpr int kOwn = kMaxBins / kThreads;
   uint32_t before[kOwn], all[kOwn], mine = 0;
@@ -209,21 +230,16 @@ __device__ __forceinline__ void place(const Sort& s, int chunks) {
     base[d] = at + before[j];
     at += all[j];
   }
-  const int64_t first = (int64_t)blockIdx.x * s.chunk;
-  const int end = (int)(first + s.chunk < s.tokens ? first + s.chunk : s.tokens);
   for (int64_t i0 = first; i0 < end; i0 += kRound) {
+    fetch(i0);
     for (int i = threadIdx.x; i < kWaves * kMaxBins; i += kThreads) (&count[0][0])[i] = 0;
     __syncthreads();
-    uint2 key[kKeys];
     uint32_t rank[kKeys];
 #pragma unroll
     for (int j = 0; j < kKeys; j++) {
       const int64_t i = i0 + wave * (64 * kKeys) + j * 64 + lane;
       const bool has = i < end;
-      if (has) {
-        key[j] = pair_at(s, (int)i);
-        if (s.touched && !s.from && key[j].x < s.rows) s.touched[key[j].x] = 1;
-      }
+      if (has && s.touched && !s.from && key[j].x < s.rows) s.touched[key[j].x] = 1;
       rank[j] = rank_of(key[j].x >> s.shift, bins, has, count[wave]);
     }
     __syncthreads();
@@ -516,7 +532,7 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(Grad g, Divide per
 // Up to kFew tokens are sorted by counting the smaller keys of each: 221 of 10136 x 16
 // 9 us, 13 by digits (for up to 512 counting takes as long as digits).
 constexpr int kFew = 256;
-constexpr int kOnceBits = 10;   // of a position: a key is row and position in 32 bits
+constexpr int kOnceBits = 11;   // of a position: a key is row and position in 32 bits
 constexpr int kOnceTokens = 1 << kOnceBits, kOnceRows = 1 << 18;
 
 // The first of list[0 .. n - 1], ascending, that is not below v.
@@ -534,10 +550,11 @@ __device__ __forceinline__ int lower_bound(const uint32_t* list, int n, uint32_t
   return at;
 }
 
-template <int GT, int L>
+// KEYS tokens a thread (a wavefront's follow one another).
+template <int GT, int L, int KEYS>
 __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int passes, int parts, int each, int zero_rows_each) {
   constexpr int kWaves = 16, kShares = 1024 / L;
-  __shared__ __align__(16) uint32_t list[kOnceTokens];
+  __shared__ __align__(16) uint32_t list[KEYS * 1024];
   __shared__ uint32_t sums[kWaves];
   // first the digits' counts (or the rows that tokens have, one bit each), then the shares' sums
   __shared__ union {
@@ -545,27 +562,34 @@ __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int pa
     uint32_t bits[kOnceRows / 32];
     float part[kShares][2][8][L];
   } u;
-  const int tid = threadIdx.x, wave = wave_index();
-  const bool has = tid < s.tokens;
-  uint32_t key = has ? token_at(s.index, s.index_bits, tid, s.rows) << kOnceBits | (uint32_t)tid : ~0u;
+  const int tid = threadIdx.x, wave = wave_index(), first = wave * (64 * KEYS) + (tid & 63);  // and every 64th on
+  uint32_t key[KEYS];
+#pragma unroll
+  for (int j = 0; j < KEYS; j++) {
+    const int i = first + j * 64;
+    key[j] = i < s.tokens ? token_at(s.index, s.index_bits, i, s.rows) << kOnceBits | (uint32_t)i : ~0u;
+  }
   if ((int)blockIdx.x >= g.sum_groups) {
     const int r0 = (int)(blockIdx.x - g.sum_groups) * zero_rows_each, left = (int)s.rows - r0, n = left < zero_rows_each ? left : zero_rows_each;
     if (n <= 0) return;
     for (int i = tid; i < (n + 31) / 32; i += 1024) u.bits[i] = 0;
     __syncthreads();
-    const uint32_t own = (key >> kOnceBits) - (uint32_t)r0;
-    if (has && own < (uint32_t)n) atomicOr(&u.bits[own >> 5], 1u << (own & 31));
+#pragma unroll
+    for (int j = 0; j < KEYS; j++) {
+      const uint32_t own = (key[j] >> kOnceBits) - (uint32_t)r0;  // no token: past every row
+      if (own < (uint32_t)n) atomicOr(&u.bits[own >> 5], 1u << (own & 31));
+    }
     __syncthreads();
     const int lanes = L == 64 || g.dw_bf16 ? L : 2 * L;
     for (int r = tid / lanes; r < n; r += 1024 / lanes)
       if (!(u.bits[r >> 5] >> (r & 31) & 1u)) zero_row(g, r0 + r, lanes);
     return;
   }
-  if (s.tokens <= kFew) {
+  if (KEYS == 1 && s.tokens <= kFew) {
     // a place is the number of smaller keys, each key's in shares
     constexpr int kOwn = kFew * kFew / 4096;  // pieces of four keys
     if (tid < kFew) {
-      list[tid] = key;
+      list[tid] = key[0];
       u.bits[tid] = 0;
     }
     __syncthreads();
@@ -586,7 +610,9 @@ __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int pa
       const int shift = kOnceBits + p * s.width;
       for (int i = tid; i < kWaves * kMaxBins; i += 1024) (&u.count[0][0])[i] = 0;
       __syncthreads();
-      const uint32_t rank = rank_of(key >> shift, bins, has, u.count[wave]);
+      uint32_t rank[KEYS];
+#pragma unroll
+      for (int j = 0; j < KEYS; j++) rank[j] = rank_of(key[j] >> shift, bins, first + j * 64 < s.tokens, u.count[wave]);
       __syncthreads();
       uint32_t all = 0;
       if (tid < kMaxBins) {
@@ -603,9 +629,13 @@ __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int pa
         for (int w = 0; w < kWaves; w++) u.count[w][tid] += at;
       }
       __syncthreads();
-      if (has) list[u.count[wave][(key >> shift) & (bins - 1)] + rank] = key;
+#pragma unroll
+      for (int j = 0; j < KEYS; j++)
+        if (first + j * 64 < s.tokens) list[u.count[wave][(key[j] >> shift) & (bins - 1)] + rank[j]] = key[j];
       __syncthreads();
-      if (has) key = list[tid];
+#pragma unroll
+      for (int j = 0; j < KEYS; j++)
+        if (first + j * 64 < s.tokens) key[j] = list[first + j * 64];
     }
   }
   // the tokens a .. b - 1 of the rows that begin in this workgroup's share
@@ -743,7 +773,7 @@ hipError_t launch_sum(Grad g, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int GT, int L>
+template <int GT, int L, int KEYS>
 hipError_t launch_once(const Grad& from, const Sort& s, int passes, hipStream_t stream) {
   Grad g = from;
   // about four tokens a share, and no more workgroups than run at once
@@ -753,7 +783,7 @@ hipError_t launch_once(const Grad& from, const Sort& s, int passes, hipStream_t 
   const int64_t bytes = (int64_t)g.rows * g.cols * (g.dw_bf16 ? 2 : 4);
   const int64_t zeros = least_of((bytes + 16383) / 16384, 2 * kCUs);
   g.sum_groups = groups * parts;
-  embed_once_kernel<GT, L><<<dim3((unsigned)(g.sum_groups + zeros)), dim3(1024), 0, stream>>>(
+  embed_once_kernel<GT, L, KEYS><<<dim3((unsigned)(g.sum_groups + zeros)), dim3(1024), 0, stream>>>(
       g, s, passes, (int)parts, (int)((g.tokens + groups - 1) / groups), (int)((g.rows + zeros - 1) / zeros));
   return hipGetLastError();
 }
@@ -835,12 +865,17 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   g.dw_bf16 = a.dweight_dtype == QUASAR_BF16;
   const int64_t bytes = a.rows * a.cols * size_of(a.dweight_dtype);
   // One launch (us, against three): 221 tokens of 10136 x 16 9, 22; 1000 of 1000 x 1024 15, 19; 1024 of 10000 x 8192 25, 34;
-  // 512 of 32000 x 4096 35, 43.  In tables of which the last-level cache holds less than half, the fill past it decides: 8 of
-  // 131072 x 2048 in fp32 101, 94.  With all tokens the same 1000 of 1000 x 1024 take 25, 22; longer lists 2762 x 598 115, 47.
+  // 512 of 32000 x 4096 35, 43; 2048 of 10000 x 8192 29, 39; 1076 of 38447 x 128 16, 22; 1999 of 50021 x 1537 in fp32 57, 57.  In tables of which the last-level cache holds less than half, the fill past it decides: 8 of
+  // 131072 x 2048 in fp32 101, 94.  With all tokens the same 1000 of 1000 x 1024 take 25, 22, 2048 41, 28.
   if (a.tokens <= kOnceTokens && a.rows <= kOnceRows && bytes <= 2 * kLastLevel) {
     return with_lanes(a.cols, [&](auto lanes) {
       constexpr int L = decltype(lanes)::value;
-      return a.dy_dtype == QUASAR_BF16 ? launch_once<kElemBF16, L>(g, s, p.passes, stream) : launch_once<kElemF32, L>(g, s, p.passes, stream);
+      const auto keys = [&](auto n) {
+        constexpr int KEYS = decltype(n)::value;
+        return a.dy_dtype == QUASAR_BF16 ? launch_once<kElemBF16, L, KEYS>(g, s, p.passes, stream)
+                                         : launch_once<kElemF32, L, KEYS>(g, s, p.passes, stream);
+      };
+      return a.tokens <= 1024 ? keys(std::integral_constant<int, 1>()) : keys(std::integral_constant<int, 2>());
     });
   }
   // Filling all of the table is the faster where no more than half of its rows can be touched: they are written twice, but
