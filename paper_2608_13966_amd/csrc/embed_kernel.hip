@@ -16,8 +16,9 @@
 // each workgroup sorts for itself.
 //
 // All of it is bound by memory but for the launches.  32768 tokens of 131072 x 4096 in
-// bf16: lookup 64 us; gradient 247 (@; the bytes at a copy's rate 259, a fill of the table
-// alone 157).  8 tokens, lookup 2.7; 1999 of 50021 x 1537 in fp32, gradient 62 (47, 9 and 5).
+// bf16: lookup 64 us; gradient 244 (the bytes at a copy's rate 259, a fill of the table
+// alone 157).  8 tokens, lookup 2.7; 1999 of 50021 x 1537 in fp32, gradient 57 (a fill
+// 45); 46151 of 538 x 1130 in bf16 57 (its bytes 21), half of it the sort's four launches.
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -40,7 +41,9 @@ __device__ __forceinline__ uint32_t token_at(const void* index, int bits, int64_
 // L lanes (8 columns each) a row, NV pieces a lane.  An output that the last-level
 // cache does not hold goes past it: 32768 tokens of 4096 in bf16 65 us, else 76 (four
 // pieces a lane 66, one 100).
-template <int WT, int L, int NV, bool NT>
+// WHOLE: a row has eight columns or more, and the lane that its end cuts moves the last eight, some of them the lane's
+// before too.
+template <int WT, int L, int NV, bool NT, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void embed_kernel(quasar_embedding a, int64_t units, Divide per) {
   const int lane = threadIdx.x & (L - 1);
   const int64_t u = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
@@ -50,12 +53,21 @@ __global__ __launch_bounds__(kThreads) void embed_kernel(quasar_embedding a, int
   Piece<WT> p[NV];
 #pragma unroll
   for (int v = 0; v < NV; v++) {
-    const int c = ((int)part * NV + v) * (8 * L) + lane * 8;
-    p[v].load(a.weight, row < rows ? row * a.weight_stride + c : 0, row < rows ? (int)a.cols - c : 0);
+    int c = ((int)part * NV + v) * (8 * L) + lane * 8;
+    if constexpr (WHOLE) {
+      c = c < (int)a.cols - 8 ? c : (int)a.cols - 8;
+      p[v].load(a.weight, (row < rows ? row : 0) * a.weight_stride + c, 8);
+    } else {
+      p[v].load(a.weight, row < rows ? row * a.weight_stride + c : 0, row < rows ? (int)a.cols - c : 0);
+    }
   }
 #pragma unroll
   for (int v = 0; v < NV; v++) {
-    const int c = ((int)part * NV + v) * (8 * L) + lane * 8;
+    int c = ((int)part * NV + v) * (8 * L) + lane * 8;
+    if (WHOLE) {
+      if (c >= (int)a.cols) continue;
+      c = c < (int)a.cols - 8 ? c : (int)a.cols - 8;
+    }
     float f[8];
 #pragma unroll
     for (int i = 0; i < 8; i++) f[i] = row < rows ? p[v].get(i) * a.scale : 0.0f;
@@ -398,8 +410,10 @@ __device__ __forceinline__ void zero_rows(const Grad& g, int64_t set) {
 
 constexpr int kMaxStretch = 32;
 
-// L lanes (8 columns each) take a stretch of the sorted list.
-template <int GT, int L>
+// L lanes (8 columns each) take a stretch of the sorted list.  WHOLE: a row has eight columns or more, and the lane
+// that its end cuts takes its last eight, some of them the lane's before too (the same sums), so that no load has a
+// branch and all of a batch run side by side.
+template <int GT, int L, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per) {
   const int lane = threadIdx.x & (L - 1);
   if (blockIdx.x >= g.sum_groups) {
@@ -410,7 +424,9 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
   const int64_t u = (int64_t)blockIdx.x * (kThreads / L) + threadIdx.x / L;
   const uint32_t st = per.of((uint32_t)u), part = (uint32_t)u - st * per.by;
   if (st >= (uint32_t)g.stretches) return;
-  const int c = (int)part * (8 * L) + lane * 8, left = g.cols - c;
+  int c = (int)part * (8 * L) + lane * 8;
+  const int left = g.cols - c;
+  if (WHOLE && left < 8) c = g.cols - 8;
   const int64_t p0 = (int64_t)st * g.stretch;
   const int n = (int)(g.tokens - p0 < g.stretch ? g.tokens - p0 : g.stretch);
   const uint2* const list = g.sorted + p0;
@@ -421,6 +437,8 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
   uint2* const mine = pairs[threadIdx.x / L];
   for (int i = lane; i < n; i += L) mine[i] = list[i];
   wave_lds_fence();
+  if (mine[0].x >= none) return;  // and all that follow
+  const uint32_t at0 = mine[0].y;
   constexpr int kAhead = 4;  // rows of a batch; the next one is in flight while one is summed
   struct Batch {
     uint32_t key[kAhead];
@@ -429,7 +447,10 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
   const auto fetch = [&](Batch& b, int i) {
     uint2 p[kAhead];
 #pragma unroll
-    for (int j = 0; j < kAhead; j++) p[j] = i + j < n ? mine[i + j] : make_uint2(none, 0u);
+    for (int j = 0; j < kAhead; j++) {
+      p[j] = mine[i + j < n ? i + j : n - 1];
+      if (i + j >= n) p[j].x = none;
+    }
 #pragma unroll
     for (int j = 0; j < kAhead; j++) {
       if constexpr (L == 64) {
@@ -438,7 +459,10 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
       }
       b.key[j] = p[j].x;
       // read once: kept in no cache, where the lines of dw that are still to be written out are (118 us, so 80)
-      b.row[j].template load<true>(g.dy, p[j].x < none ? p[j].y * g.dy_stride + c : 0, p[j].x < none ? left : 0);
+      if constexpr (WHOLE)  // a row that is none, or past the stretch: its first one again, whose sum nothing reads
+        b.row[j].template load<true>(g.dy, (p[j].x < none ? p[j].y : at0) * g.dy_stride + c, 8);
+      else
+        b.row[j].template load<true>(g.dy, p[j].x < none ? p[j].y * g.dy_stride + c : 0, p[j].x < none ? left : 0);
     }
   };
   fetch(batch[0], 0);
@@ -446,9 +470,9 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
   uint32_t now = batch[0].key[0];
   bool begun = now == head;  // before this stretch
   const auto flush = [&](bool goes_on) {
-    if (now >= none) return;
+    if (now >= none || left <= 0) return;
     if (begun || goes_on)
-      store_piece<false>(g.part, ((int64_t)st * 2 + (begun ? 0 : 1)) * g.pitch + c, sum, g.pitch - c);
+      store_piece<false>(g.part, ((int64_t)st * 2 + (begun ? 0 : 1)) * g.pitch + c, sum, WHOLE ? 8 : g.pitch - c);
     else
       put_row(g, now, c, sum);
   };
@@ -466,13 +490,16 @@ __global__ __launch_bounds__(kThreads) void embed_sum_kernel(Grad g, Divide per)
       for (int k = 0; k < 8; k++) sum[k] += b.row[j].get(k);
     }
   };
-  for (int i = 0; i < n; i += 2 * kAhead) {
+  int i = 0;
+  for (; i + 2 * kAhead < n; i += 2 * kAhead) {
     fetch(batch[1], i + kAhead);
     add(batch[0]);
-    if (i + kAhead >= n) break;
     fetch(batch[0], i + 2 * kAhead);
     add(batch[1]);
   }
+  fetch(batch[1], i + kAhead);
+  add(batch[0]);
+  add(batch[1]);
   flush(now == tail);
 }
 
@@ -505,13 +532,13 @@ __global__ __launch_bounds__(kThreads) void embed_join_kernel(Grad g, Divide per
     Piece<kElemF32> v[kAhead];
 #pragma unroll
     for (int j = 0; j < kAhead; j++) {
-      const int at = i + j * kShares;
-      v[j].load(g.part, (((int64_t)st + at) * 2 + (at == 0)) * g.pitch + c, at < more ? g.pitch - c : 0);
+      const int at = i + j * kShares < more ? i + j * kShares : i;  // without a branch, as above
+      v[j].load(g.part, (((int64_t)st + at) * 2 + (at == 0)) * g.pitch + (c < g.pitch ? c : 0), 8);
     }
 #pragma unroll
     for (int j = 0; j < kAhead; j++)
 #pragma unroll
-      for (int k = 0; k < 8; k++) sum[k] += v[j].get(k);
+      for (int k = 0; k < 8; k++) sum[k] += i + j * kShares < more ? v[j].get(k) : 0.0f;
   }
   if (share > 0) {
 #pragma unroll
@@ -551,7 +578,7 @@ __device__ __forceinline__ int lower_bound(const uint32_t* list, int n, uint32_t
 }
 
 // KEYS tokens a thread (a wavefront's follow one another).
-template <int GT, int L, int KEYS>
+template <int GT, int L, int KEYS, bool WHOLE>
 __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int passes, int parts, int each, int zero_rows_each) {
   constexpr int kWaves = 16, kShares = 1024 / L;
   __shared__ __align__(16) uint32_t list[KEYS * 1024];
@@ -641,7 +668,9 @@ __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int pa
   // the tokens a .. b - 1 of the rows that begin in this workgroup's share
   const int n = lower_bound(list, s.tokens, s.rows << kOnceBits);
   const int share = tid / L, col = tid & (L - 1), group = (int)blockIdx.x / parts;
-  const int c = ((int)blockIdx.x - group * parts) * (8 * L) + col * 8, left = g.cols - c;
+  int c = ((int)blockIdx.x - group * parts) * (8 * L) + col * 8;
+  const int left = g.cols - c;
+  if (WHOLE && left < 8) c = g.cols - 8;  // as in embed_sum_kernel
   const auto row_at = [&](int i) { return list[i] >> kOnceBits; };
   const auto from_row = [&](int i) {  // i, or where the row that goes on there ends
     if (i >= n) return n;
@@ -659,9 +688,9 @@ __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int pa
     const auto fetch = [&](Batch& o, int i) {
 #pragma unroll
       for (int j = 0; j < kAhead; j++) {
-        const uint32_t v = i + j < p1 ? list[i + j] : ~0u;
+        const uint32_t v = list[i + j < p1 ? i + j : p1 - 1];
         o.key[j] = v >> kOnceBits;
-        o.row[j].load(g.dy, i + j < p1 ? (int64_t)(v & (kOnceTokens - 1)) * g.dy_stride + c : 0, i + j < p1 ? left : 0);
+        o.row[j].load(g.dy, (int64_t)(v & (kOnceTokens - 1)) * g.dy_stride + (WHOLE || left > 0 ? c : 0), WHOLE ? 8 : left);
       }
     };
     fetch(batch[0], p0);
@@ -691,12 +720,16 @@ __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int pa
         for (int k = 0; k < 8; k++) sum[k] += o.row[j].get(k);
       }
     };
-    for (int i = p0; i < p1; i += 2 * kAhead) {
+    int i = p0;
+    for (; i + 2 * kAhead < p1; i += 2 * kAhead) {
       fetch(batch[1], i + kAhead);
       add(batch[0], i);
       fetch(batch[0], i + 2 * kAhead);
       add(batch[1], i + kAhead);
     }
+    if (i + kAhead < p1) fetch(batch[1], i + kAhead);
+    add(batch[0], i);
+    add(batch[1], i + kAhead);
     flush(goes_on);
   }
   __syncthreads();
@@ -766,7 +799,12 @@ hipError_t launch_sum(Grad g, hipStream_t stream) {
   const int64_t per = (g.cols + 8 * L - 1) / (8 * L), each = kThreads / L;
   g.sum_groups = (g.stretches * per + each - 1) / each;
   const int64_t groups = g.sum_groups + (g.touched ? zero_groups(g.rows) : 0);
-  if (groups > 0) embed_sum_kernel<GT, L><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
+  if (groups > 0) {
+    if (g.cols >= 8)
+      embed_sum_kernel<GT, L, true><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
+    else
+      embed_sum_kernel<GT, L, false><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || g.stretches < 2) return e;
   embed_join_kernel<L><<<dim3((unsigned)((g.stretches - 1) * per)), dim3(kThreads), 0, stream>>>(g, Divide((uint32_t)per));
@@ -783,8 +821,12 @@ hipError_t launch_once(const Grad& from, const Sort& s, int passes, hipStream_t 
   const int64_t bytes = (int64_t)g.rows * g.cols * (g.dw_bf16 ? 2 : 4);
   const int64_t zeros = least_of((bytes + 16383) / 16384, 2 * kCUs);
   g.sum_groups = groups * parts;
-  embed_once_kernel<GT, L, KEYS><<<dim3((unsigned)(g.sum_groups + zeros)), dim3(1024), 0, stream>>>(
-      g, s, passes, (int)parts, (int)((g.tokens + groups - 1) / groups), (int)((g.rows + zeros - 1) / zeros));
+  const dim3 grid((unsigned)(g.sum_groups + zeros));
+  const int each = (int)((g.tokens + groups - 1) / groups), zeros_each = (int)((g.rows + zeros - 1) / zeros);
+  if (g.cols >= 8)
+    embed_once_kernel<GT, L, KEYS, true><<<grid, dim3(1024), 0, stream>>>(g, s, passes, (int)parts, each, zeros_each);
+  else
+    embed_once_kernel<GT, L, KEYS, false><<<grid, dim3(1024), 0, stream>>>(g, s, passes, (int)parts, each, zeros_each);
   return hipGetLastError();
 }
 
@@ -803,10 +845,16 @@ hipError_t launch_lookup(const quasar_embedding& a, hipStream_t stream) {
         s.index = reinterpret_cast<const char*>(a.index) + t * (a.index_bits / 8);
         s.y = rows_on(a.y, t, a.y_stride, size_of(a.y_dtype));
         const int64_t units = s.tokens * per, groups = (units + each - 1) / each;
-        if (nt)
-          embed_kernel<WT, L, NV, true><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(s, units, Divide((uint32_t)per));
+        const auto run = [&](auto past, auto whole) {
+          embed_kernel<WT, L, NV, decltype(past)::value, decltype(whole)::value>
+              <<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(s, units, Divide((uint32_t)per));
+        };
+        if (a.cols < 8)
+          run(std::false_type(), std::false_type());
+        else if (nt)
+          run(std::true_type(), std::true_type());
         else
-          embed_kernel<WT, L, NV, false><<<dim3((unsigned)groups), dim3(kThreads), 0, stream>>>(s, units, Divide((uint32_t)per));
+          run(std::false_type(), std::true_type());
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
       }
@@ -864,9 +912,10 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   g.scale = a.scale;
   g.dw_bf16 = a.dweight_dtype == QUASAR_BF16;
   const int64_t bytes = a.rows * a.cols * size_of(a.dweight_dtype);
-  // One launch (us, against three): 221 tokens of 10136 x 16 9, 22; 1000 of 1000 x 1024 15, 19; 1024 of 10000 x 8192 25, 34;
-  // 512 of 32000 x 4096 35, 43; 2048 of 10000 x 8192 29, 39; 1076 of 38447 x 128 16, 22; 1999 of 50021 x 1537 in fp32 57, 57.  In tables of which the last-level cache holds less than half, the fill past it decides: 8 of
-  // 131072 x 2048 in fp32 101, 94.  With all tokens the same 1000 of 1000 x 1024 take 25, 22, 2048 41, 28.
+  // One launch (us, against three): 221 tokens of 10136 x 16 9, 22; 1000 of 1545 x 654 13, 19; 1024 of 10000 x 8192 25, 34;
+  // 1076 of 38447 x 128 14, 20; 2048 of 10000 x 8192 28, 38; 1999 of 50021 x 1537 in fp32 57, 57.  In tables of which the
+  // last-level cache holds less than half, the fill past it decides: 8 of 131072 x 2048 in fp32 101, 94.  With all tokens the
+  // same 1000 of 1000 x 1024 take 19, 22, 2048 32, 26; and more lists longer than that.
   if (a.tokens <= kOnceTokens && a.rows <= kOnceRows && bytes <= 2 * kLastLevel) {
     return with_lanes(a.cols, [&](auto lanes) {
       constexpr int L = decltype(lanes)::value;

@@ -151,6 +151,27 @@ def test_grad_into_a_wider_buffer_with_a_used_workspace():
     assert (buf[:5] == 7).all() and (buf[5:].view(60, 311)[:, 300:] == 7).all()
 
 
+@pytest.mark.parametrize("cols", [7, 8, 9, 15, 65, 513, 519, 1025])
+@pytest.mark.parametrize("n", [40, 2047, 2048, 2049, 6000])
+@pytest.mark.parametrize("gt", ["bf16", "fp32"])
+def test_widths_that_cut_a_piece(cols, n, gt):
+    """Rows whose last piece is short, between values that stay."""
+    rows = 500
+    for kind in ("uniform", "few", "none"):
+        tok = draw(n, rows, kind, cols)
+        table = gen((rows, cols), DT[gt], 1, pad=3, off=1)
+        yb = torch.full((n + 2, cols + 5), 7.0, device=DEV, dtype=DT[gt])
+        O.embed(tok, table, scale=3.0, out={"y": yb[1:-1, 2:cols + 2]})
+        check_lookup(tok, table, 3.0, yb[1:-1, 2:cols + 2])
+        dy = gen((n, cols), DT[gt], 2, pad=3, off=1)
+        dy[(tok < 0) | (tok >= rows)] = float("nan")
+        wb = torch.full((rows + 2, cols + 5), 7.0, device=DEV, dtype=DT[gt])
+        O.embed_backward(dy, tok, rows, scale=0.5, out={"dw": wb[1:-1, 2:cols + 2]})
+        check_grad(dy, tok, rows, 0.5, wb[1:-1, 2:cols + 2])
+        yb[1:-1, 2:cols + 2], wb[1:-1, 2:cols + 2] = 7.0, 7.0
+        assert (yb == 7).all() and (wb == 7).all()
+
+
 def test_no_tokens():
     dy, tok = torch.empty(0, 33, device=DEV), torch.empty(0, device=DEV, dtype=torch.int64)
     assert O.embed(tok, torch.ones(5, 33, device=DEV))["y"].shape == (0, 33)
