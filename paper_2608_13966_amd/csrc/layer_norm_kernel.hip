@@ -6,9 +6,9 @@
 // and step: the mean, then the squares of the deviations from it (two sums, since
 // sum(h^2) - cols mean^2 cancels where the mean is large), the row's largest |y| and
 // the outputs all come from one read.  67 M elements in bf16 with a residual, rows of
-// 64 to 16384 columns: forward 92 to 100 us, 5.4 to 5.8 TB/s (a copy of 1 GiB: 5.1);
-// gradients 101 to 118, 4.5 to 5.3.  Odd widths cost more (1537 columns: 106 and 147),
-// as do gradients past 16384 columns, whose shares spill (32768: 378).  One row of 4096
+// 64 to 16384 columns: forward 92 to 98 us, 5.4 to 5.8 TB/s (a copy of 1 GiB: 5.0);
+// gradients 101 to 118, 4.5 to 5.3.  Odd widths cost more (1537 columns: 108 and 137),
+// as do gradients past 16384 columns, whose shares spill (32768: 364).  One row of 4096
 // takes 3.9 us.
 #include "ops_common.h"
 #include "ops_internal.h"
@@ -52,25 +52,40 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_kernel(quasar
   const int t = Shape<TPR>::lane(), cols = (int)a.cols;
   const int64_t row = (int64_t)blockIdx.x * Shape<TPR>::kRows + Shape<TPR>::row();
   if (row >= a.rows) return;  // whole rows of 16 lanes; no barrier follows where there are several rows
+  // us, element by element and cut: 500000 x 60 bf16 71, 60; 29626 x 198 15.4, 12.6; 4000 x 5313 27, 24.5; fp32 100000 x 129
+  // 21, 24
+  constexpr int kMode = TPR == 1024 && NV == 2 ? kCutNone : TPR >= 64 ? kCutAll : kCutBF16 | (TPR == 8 ? kCutTiny : 0);
   float h[NV][8];
+  int col[NV];
   Piece<XT> px[NV];
   Piece<RT == kElemNone ? XT : RT> pr[NV];
   const int64_t ex = row * a.x_stride, er = row * a.residual_stride;
 #pragma unroll
   for (int v = 0; v < NV; v++) {
-    const int c = (v * TPR + t) * 8;
-    px[v].load(a.x, ex + c, cols - c);
-    if constexpr (RT != kElemNone) pr[v].load(a.residual, er + c, cols - c);
+    col[v] = (v * TPR + t) * 8;
+    load_cut<kMode>(px[v], a.x, ex, col[v], cols);
+    if constexpr (RT != kElemNone) load_cut<kMode>(pr[v], a.residual, er, col[v], cols);
   }
+  // weight and bias are asked for beside the row where there are registers for them
+  constexpr bool kEarly = NV <= 2 && TPR <= 256;
+  float w[NV][8], b[NV][8] = {};
+  const auto affine = [&] {
+    load_cut_floats<kMode>(a.weight, 0, col, cols, a.weight_dtype == QUASAR_BF16, w);
+    if (a.bias) load_cut_floats<kMode>(a.bias, 0, col, cols, a.bias_dtype == QUASAR_BF16, b);
+  };
+  if constexpr (kEarly) affine();
   float sum = 0.0f;
 #pragma unroll
-  for (int v = 0; v < NV; v++)
+  for (int v = 0; v < NV; v++) {
+    cut<kMode>(px[v], col[v], cols);
+    if constexpr (RT != kElemNone) cut<kMode>(pr[v], col[v], cols);
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       h[v][i] = px[v].get(i);
       if constexpr (RT != kElemNone) h[v][i] += pr[v].get(i);
       sum += h[v][i];
     }
+  }
   const float mean = row_reduce<TPR>(sum, red[0], SumOp()) / (float)cols;
   if constexpr (RT != kElemNone) {
     if (a.h) {
@@ -102,16 +117,13 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_kernel(quasar
     if (a.mean) a.mean[row] = mean;
     if (a.rstd) a.rstd[row] = rstd;
   }
+  if constexpr (!kEarly) affine();
   float top = 0.0f;
 #pragma unroll
   for (int v = 0; v < NV; v++) {
-    const int c = (v * TPR + t) * 8;
-    float w[8], b[8] = {};
-    load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w);
-    if (a.bias) load_floats(a.bias, c, cols - c, a.bias_dtype == QUASAR_BF16, b);
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      h[v][i] = __builtin_fmaf(h[v][i] * rstd, w[i], b[i]);
+      h[v][i] = __builtin_fmaf(h[v][i] * rstd, w[v][i], b[v][i]);
       top = fmaxf(top, fabsf(h[v][i]));
     }
   }
@@ -209,22 +221,25 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_backward_kern
   __shared__ float red[2][2][kWaves];
   __shared__ float shares[kShares > 1 ? (kShares - 1) * kWide * NV * 8 : 1];
   const int t = Shape<TPR>::lane(), cols = (int)a.cols;
+  // us, element by element and cut: 500000 x 60 bf16 92, 60; 29626 x 198 26, 18; 777 x 1537 fp32 11.9, 12.8; 65536 x 1024 bf16
+  // 106, 125; past 4096 columns 4000 x 5313 45, 42, but 8192 x 8192 114, 116
+  constexpr int kMode = TPR == 8 ? kCutBF16 | kCutTiny : TPR < 64 || TPR == 256 || TPR == 512 ? kCutBF16 : kCutNone;
   const float rcols = 1.0f / (float)cols;
   constexpr bool kKeep = NV < 4;  // the weight stays in registers
   float w[kKeep ? NV : 1][8], dw[NV][8] = {}, db[NV][8] = {};
   const auto weight = [&](int v) -> float (&)[8] {
-    const int c = (v * TPR + t) * 8;
-    if constexpr (kKeep) return w[v];
-    load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w[0]);
-    return w[0];
-  };
-  if constexpr (kKeep) {
-#pragma unroll
-    for (int v = 0; v < NV; v++) {
-      const int c = (v * TPR + t) * 8;
-      load_floats(a.weight, c, cols - c, a.weight_dtype == QUASAR_BF16, w[v]);
+    if constexpr (kKeep) {
+      return w[v];
+    } else {
+      const int c[1] = {(v * TPR + t) * 8};
+      load_cut_floats<kMode>(a.weight, 0, c, cols, a.weight_dtype == QUASAR_BF16, w);
+      return w[0];
     }
-  }
+  };
+  int col[NV];
+#pragma unroll
+  for (int v = 0; v < NV; v++) col[v] = (v * TPR + t) * 8;
+  if constexpr (kKeep) load_cut_floats<kMode>(a.weight, 0, col, cols, a.weight_dtype == QUASAR_BF16, w);
   int flip = 0;
   for (int64_t row = (int64_t)blockIdx.x * kRows + Shape<TPR>::row(); row < a.rows; row += (int64_t)gridDim.x * kRows) {
     Piece<GT> pg[NV];
@@ -233,23 +248,21 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_backward_kern
 #pragma unroll
     for (int v = 0; v < NV; v++) {
       const int c = (v * TPR + t) * 8;
-      pg[v].load(a.dy, eg + c, cols - c);
-      ph[v].load(a.h, eh + c, cols - c);
+      load_cut<kMode>(pg[v], a.dy, eg, c, cols);
+      load_cut<kMode>(ph[v], a.h, eh, c, cols);
     }
     // dh is asked for with the rest where there are registers for it
     constexpr bool kEarly = TPR <= 512 || NV == 1;
     float dh[kEarly ? NV : 1][8];
-    if (kEarly && a.dh) {
-#pragma unroll
-      for (int v = 0; v < NV; v++) {
-        const int c = (v * TPR + t) * 8;
-        load_floats(a.dh, ed + c, cols - c, a.dx_dtype == QUASAR_BF16, dh[v]);
-      }
+    if constexpr (kEarly) {
+      if (a.dh) load_cut_floats<kMode>(a.dh, ed, col, cols, a.dx_dtype == QUASAR_BF16, dh);
     }
     const float rstd = a.rstd[row], mean = a.mean[row];
     float dot = 0.0f, sum = 0.0f;
 #pragma unroll
     for (int v = 0; v < NV; v++) {
+      cut<kMode>(pg[v], (v * TPR + t) * 8, cols);
+      cut<kMode>(ph[v], (v * TPR + t) * 8, cols);
       float(&wv)[8] = weight(v);
 #pragma unroll
       for (int i = 0; i < 8; i++) {
@@ -295,7 +308,10 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_backward_kern
       }
       if (a.dh) {
         float(&d)[8] = dh[kEarly ? v : 0];
-        if constexpr (!kEarly) load_floats(a.dh, ed + c, n8, a.dx_dtype == QUASAR_BF16, d);
+        if constexpr (!kEarly) {
+          const int at[1] = {c};
+          load_cut_floats<kMode>(a.dh, ed, at, cols, a.dx_dtype == QUASAR_BF16, dh);
+        }
 #pragma unroll
         for (int i = 0; i < 8; i++) dx[i] += d[i];
       }

@@ -69,6 +69,18 @@ struct Piece<kElemBF16> {
       }
     }
   }
+  // The first `gone` elements (1 to 8) go, the rest move up, 0 behind them.
+  __device__ __forceinline__ void drop(int gone) {
+    const uint32_t odd = (uint32_t)(gone & 1) * 16u;
+#pragma unroll
+    for (int i = 0; i < 4; i++) d[i] = __builtin_amdgcn_alignbit(i < 3 ? d[i + 1] : 0u, d[i], odd);
+#pragma unroll
+    for (int by = 1; by <= 4; by *= 2)
+      if (gone & (2 * by)) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) d[i] = i + by < 4 ? d[i + by] : 0u;
+      }
+  }
   __device__ __forceinline__ float get(int i) const {
     return (i & 1) ? as_f32(d[i >> 1] & 0xffff0000u) : as_f32(d[i >> 1] << 16);
   }
@@ -91,9 +103,58 @@ struct Piece<kElemF32> {
       for (int i = 0; i < 8; i++) f[i] = i < n ? p[i] : 0.0f;
     }
   }
+  __device__ __forceinline__ void drop(int gone) {
+#pragma unroll
+    for (int by = 1; by <= 8; by *= 2)
+      if (gone & by) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = i + by < 8 ? f[i + by] : 0.0f;
+      }
+  }
   __device__ __forceinline__ float get(int i) const { return f[i]; }
   __device__ __forceinline__ void refresh() {}
 };
+
+// Eight elements of a row (it begins at element `row` and has `cols`) from column c on, the rest 0.  Where MODE says
+// cut, a piece that the row's end cuts comes as the row's last eight, without a branch, so that the loads of several
+// pieces run side by side (element by element each is waited for); cut() then moves what there is to its place.
+enum CutMode : int { kCutNone = 0, kCutBF16 = 1, kCutAll = 2, kCutTiny = 4 };  // of elements so wide; rows of less than eight occur
+template <int MODE, int T>
+constexpr bool cuts() { return (MODE & 3) >= (T == kElemBF16 ? 1 : 2); }
+template <int MODE, int T>
+__device__ __forceinline__ void load_cut(Piece<T>& p, const void* base, int64_t row, int c, int cols) {
+  if (!cuts<MODE, T>() || ((MODE & kCutTiny) && cols < 8))
+    p.load(base, row + c, cols - c);
+  else
+    p.load(base, row + (c < cols - 8 ? c : cols - 8), 8);
+}
+template <int MODE, int T>
+__device__ __forceinline__ void cut(Piece<T>& p, int c, int cols) {
+  if constexpr (cuts<MODE, T>()) {
+    const int left = cols - c;
+    if (left < 8 && !((MODE & kCutTiny) && cols < 8)) p.drop(left > 0 ? 8 - left : 8);
+  }
+}
+// The same, widened, N pieces at once.
+template <int MODE, int N>
+__device__ __forceinline__ void load_cut_floats(const void* base, int64_t row, const int (&c)[N], int cols, bool bf16,
+                                                float (&v)[N][8]) {
+  const auto load = [&](auto piece) {
+    decltype(piece) p[N];
+#pragma unroll
+    for (int j = 0; j < N; j++) load_cut<MODE>(p[j], base, row, c[j], cols);
+#pragma unroll
+    for (int j = 0; j < N; j++) {
+      cut<MODE>(p[j], c[j], cols);
+#pragma unroll
+      for (int i = 0; i < 8; i++) v[j][i] = p[j].get(i);
+    }
+  };
+  if (bf16)
+    load(Piece<kElemBF16>());
+  else
+    load(Piece<kElemF32>());
+}
 
 // Eight elements from each of N places on, the first n[i] of which exist (the
 // others 0).  All loads are issued before the first is waited for.

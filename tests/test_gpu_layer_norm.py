@@ -221,3 +221,31 @@ def test_gradient_against_differences():
             up, down = dict(args, **{name: t + e.view_as(t)}), dict(args, **{name: t - e.view_as(t)})
             got.view(-1)[i] = (loss(**up) - loss(**down)) / 2e-5
         assert (got - want[name]).abs().max() < 1e-8  # differences: h^2 of the third derivative and 1e-16 / h
+
+
+@pytest.mark.parametrize("cols", [1, 5, 7, 8, 9, 15, 60, 65, 70, 127, 131, 198, 260, 511, 700, 1027, 1537, 2047, 3333, 4099, 8191, 9001, 16383])
+@pytest.mark.parametrize("typ", ["bf16", "fp32"])
+def test_widths_that_cut_a_piece(cols, typ):
+    """Rows whose last piece is short, between NaN on the way in and values that stay on the way out."""
+    def inside(seed, rows=9, scale=1.0):
+        buf = torch.full((rows + 2, cols + 5), float("nan"), device=DEV, dtype=DT[typ])
+        buf[1:-1, 2:cols + 2] = gen((rows, cols), DT[typ], seed, scale)
+        return buf[1:-1, 2:cols + 2]
+
+    def around(dtype=DT[typ]):
+        buf = torch.full((11, cols + 5), 7.0, device=DEV, dtype=dtype)
+        return buf, buf[1:-1, 2:cols + 2]
+
+    x, res, w, b = inside(1), inside(2), inside(3, 1)[0], inside(4, 1)[0]
+    (yb, y), (hb, h) = around(), around()
+    o = O.add_layer_norm(x, w, b, res, eps=EPS, out={"y": y, "h": h, "mean": torch.empty(9, device=DEV), "rstd": torch.empty(9, device=DEV)})
+    check_forward(x, w, b, res, o)
+    dy, dh, (dxb, dx) = inside(5), inside(6), around()
+    out = O.add_layer_norm_backward(dy.contiguous(), h.contiguous(), w.contiguous(), o["mean"], o["rstd"], dh.contiguous())
+    kept = {k: out[k].clone() for k in ("dw", "db")}
+    got = O.add_layer_norm_backward(dy, h, w, o["mean"], o["rstd"], dh, out={**kept, "dx": dx})
+    check_backward(dy, h, w, o["mean"], o["rstd"], dh, got)
+    assert all(torch.equal(got[k], out[k]) for k in ("dx", "dw", "db"))
+    for buf, t in ((yb, y), (hb, h), (dxb, dx)):
+        t.fill_(7.0)
+        assert (buf == 7).all()
