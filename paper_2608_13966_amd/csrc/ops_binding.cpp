@@ -80,6 +80,24 @@ Tensor result(const py::object& out, const char* name, at::IntArrayRef shape, at
   return t;
 }
 
+// New vectors of n fp32 elements, `count` at most, in one allocation (five allocations are 2.4 of the 6.7 us that a call
+// for one row takes on the host).  Each is a tensor of its own, no view of another.
+class Vectors {
+ public:
+  Vectors(int64_t n, int count, const at::Device& dev) : n_(n), all_(fresh({count, n}, at::kFloat, dev)) {}
+  Tensor next() {
+    auto t = c10::make_intrusive<at::TensorImpl>(c10::Storage(all_.storage()), all_.key_set(), all_.dtype());
+    t->set_storage_offset(n_ * taken_++);
+    t->set_sizes_contiguous({n_});
+    return Tensor(std::move(t));
+  }
+
+ private:
+  int64_t n_;
+  int taken_ = 0;
+  Tensor all_;
+};
+
 Maybe workspace(const py::object& out, size_t bytes, const at::Device& dev) {
   if (bytes == 0) return std::nullopt;
   if (!out.is_none()) {
@@ -375,13 +393,15 @@ py::object add_layer_norm(const Tensor& x, const Tensor& weight, const Maybe& bi
   if (residual) a.residual_dtype = code(matrix(*residual, "residual", rows, cols, dev), "residual");
   Maybe h, y, q, scale;
   if (residual) h = result(out, "h", {rows, cols}, residual->scalar_type(), dev);
-  const Tensor mean = result(out, "mean", {rows}, at::kFloat, dev);
-  const Tensor rstd = result(out, "rstd", {rows}, at::kFloat, dev);
+  std::optional<Vectors> vectors;
+  if (out.is_none()) vectors.emplace(rows, quantize ? 3 : 2, dev);
+  const auto vector_of_rows = [&](const char* name) { return vectors ? vectors->next() : result(out, name, {rows}, at::kFloat, dev); };
+  const Tensor mean = vector_of_rows("mean"), rstd = vector_of_rows("rstd");
   a.y_dtype = y_dtype < 0 ? a.x_dtype : y_dtype;
   if (want_y) y = result(out, "y", {rows, cols}, type_of(a.y_dtype), dev);
   if (quantize) {
     q = result(out, "q", {rows, cols}, at::kFloat8_e4m3fn, dev);
-    scale = result(out, "scale", {rows}, at::kFloat, dev);
+    scale = vector_of_rows("scale");
   }
   a.x = ptr(x);
   a.residual = ptr(residual);
