@@ -17,8 +17,8 @@
 //
 // All of it is bound by memory but for the launches.  32768 tokens of 131072 x 4096 in
 // bf16: lookup 64 us; gradient 244 (the bytes at a copy's rate 259, a fill of the table
-// alone 157).  8 tokens, lookup 2.7; 1999 of 50021 x 1537 in fp32, gradient 57 (a fill
-// 45); 46151 of 538 x 1130 in bf16 57 (its bytes 21), half of it the sort's four launches.
+// alone 157).  8 tokens, lookup 2.7; 1999 of 50021 x 1537 in fp32, gradient 68 into
+// three tables in turn, 57 into one (a fill 45); 46151 of 538 x 1130 in bf16 57 (its bytes 21), half of it the sort's four launches.
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -100,7 +100,7 @@ struct Fill {
   char* p;
   int64_t bytes;
   int size;  // of an element
-  bool nt;   // past the caches: more than twice what the last level holds
+  bool nt;   // past the caches: more than half of what the last level holds (10000 tokens of 40000 x 4096, bf16 87 us, else 97)
 };
 // Units a .. b - 1, by the workgroups from `group` on, `groups` in all.
 template <int THREADS>
@@ -361,6 +361,7 @@ struct Grad {
   uint32_t rows;
   float scale;
   int dw_bf16;
+  bool nt;                // the one launch's zeros go past the caches
 };
 
 template <bool BF16>
@@ -377,13 +378,16 @@ __device__ __forceinline__ void put_row(const Grad& g, uint32_t row, int c, cons
     put_row<false>(g, row, c, v);
 }
 
-// Zeros in a row by `lanes` lanes: 16 bytes each.
-__device__ __forceinline__ void zero_row(const Grad& g, int64_t row, int lanes = 64) {
+// Zeros in a row by `lanes` lanes: 16 bytes each, past the caches with nt.
+__device__ __forceinline__ void zero_row(const Grad& g, int64_t row, int lanes = 64, bool nt = false) {
   const int lane = threadIdx.x & (lanes - 1), size = g.dw_bf16 ? 2 : 4, bytes = g.cols * size;
   char* const p = reinterpret_cast<char*>(g.dw) + row * g.dw_stride * size;
   for (int b = lane * 16; b < bytes; b += lanes * 16) {
     if (b + 16 <= bytes) {
-      st16_any(p + b, make_uint4(0u, 0u, 0u, 0u));
+      if (nt)
+        st16_any_nt(p + b, make_uint4(0u, 0u, 0u, 0u));
+      else
+        st16_any(p + b, make_uint4(0u, 0u, 0u, 0u));
     } else {
       for (int e = b; e < bytes; e += size) {
         if (size == 2)
@@ -609,7 +613,7 @@ __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int pa
     __syncthreads();
     const int lanes = L == 64 || g.dw_bf16 ? L : 2 * L;
     for (int r = tid / lanes; r < n; r += 1024 / lanes)
-      if (!(u.bits[r >> 5] >> (r & 31) & 1u)) zero_row(g, r0 + r, lanes);
+      if (!(u.bits[r >> 5] >> (r & 31) & 1u)) zero_row(g, r0 + r, lanes, g.nt);
     return;
   }
   if (KEYS == 1 && s.tokens <= kFew) {
@@ -916,7 +920,11 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   // 1076 of 38447 x 128 14, 20; 2048 of 10000 x 8192 28, 38; 1999 of 50021 x 1537 in fp32 57, 57.  In tables of which the
   // last-level cache holds less than half, the fill past it decides: 8 of 131072 x 2048 in fp32 101, 94.  With all tokens the
   // same 1000 of 1000 x 1024 take 19, 22, 2048 32, 26; and more lists longer than that.
+  // Its zeros go past the caches where they would take the room of a longer list's rows (into three tables in turn, 2048 of
+  // 10000 x 8192 29, else 44; of 32000 x 4096 49, 54; but 8 of 40000 x 4096 65, 63, and lines that rows share 80, 68).
   if (a.tokens <= kOnceTokens && a.rows <= kOnceRows && bytes <= 2 * kLastLevel) {
+    const int64_t row_bytes = a.dweight_stride * size_of(a.dweight_dtype);
+    g.nt = a.tokens > kFew && bytes > kLastLevel / 2 && row_bytes % 64 == 0 && (reinterpret_cast<uintptr_t>(a.dweight) & 63) == 0;
     return with_lanes(a.cols, [&](auto lanes) {
       constexpr int L = decltype(lanes)::value;
       const auto keys = [&](auto n) {
@@ -930,7 +938,7 @@ hipError_t launch_embed_backward(const quasar_embedding_backward& a, hipStream_t
   // Filling all of the table is the faster where no more than half of its rows can be touched: they are written twice, but
   // the rest without a look at the marks, and beside the sort (131072 x 4096 in bf16, us: 8 tokens 183 against 196, 32768
   // 260 against 293, 60000 317 against 358; 65536 tokens of 50000 x 2048 130 against 126).
-  const Fill f{reinterpret_cast<char*>(a.dweight), bytes, (int)size_of(a.dweight_dtype), bytes > 2 * kLastLevel};
+  const Fill f{reinterpret_cast<char*>(a.dweight), bytes, (int)size_of(a.dweight_dtype), bytes > kLastLevel / 2};
   const bool fill = a.tokens <= a.rows / 2 && (a.rows == 1 || a.dweight_stride == a.cols);
   if (fill) s.touched = nullptr;
   g.touched = s.touched;
