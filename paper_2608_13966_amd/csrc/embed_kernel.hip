@@ -17,8 +17,9 @@
 //
 // All of it is bound by memory but for the launches.  32768 tokens of 131072 x 4096 in
 // bf16: lookup 64 us; gradient 244 (the bytes at a copy's rate 259, a fill of the table
-// alone 157).  8 tokens, lookup 2.7; 1999 of 50021 x 1537 in fp32, gradient 68 into
-// three tables in turn, 57 into one (a fill 45); 46151 of 538 x 1130 in bf16 57 (its bytes 21), half of it the sort's four launches.
+// alone 157).  8 tokens, lookup 2.7; 1999 of 50021 x 1537 in fp32, gradient 68 into three
+// tables in turn, 57 into one (a fill 45); 46151 of 538 x 1130 in bf16 56 (its bytes 21),
+// nearly half of it the sort's four launches.
 #include "ops_common.h"
 #include "ops_internal.h"
 
@@ -89,11 +90,6 @@ struct Sort {
   int shift, width, bins;
 };
 
-__device__ __forceinline__ uint2 pair_at(const Sort& s, int i) {
-  if (s.from) return s.from[i];
-  return make_uint2(token_at(s.index, s.index_bits, i, s.rows), (uint32_t)i);
-}
-
 // A table to be filled with zeros, in units of 16 bytes a thread.  A fill of 1 GiB
 // takes 157 us in workgroups of 4 KB, 173 of 8 KB, 190 of 32 KB.
 struct Fill {
@@ -130,6 +126,29 @@ __device__ __forceinline__ void clear_marks(const Sort& s, int64_t i, int64_t al
     reinterpret_cast<uint4*>(s.touched)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
+// A lane's keys of the round from i0 on, one in 64 of its wavefront's; past the end the last one, without a branch: the
+// loads then run side by side.
+constexpr int kKeys = kRound / kThreads;
+__device__ __forceinline__ int place_in_round(int j) { return wave_index() * (64 * kKeys) + j * 64 + (int)(threadIdx.x & 63); }
+__device__ __forceinline__ void round_of(const Sort& s, int64_t i0, int end, uint2 (&key)[kKeys]) {
+  int at[kKeys];
+#pragma unroll
+  for (int j = 0; j < kKeys; j++) {
+    const int64_t i = i0 + place_in_round(j);
+    at[j] = (int)(i < end ? i : end - 1);
+  }
+  if (s.from) {
+#pragma unroll
+    for (int j = 0; j < kKeys; j++) key[j] = s.from[at[j]];
+  } else if (s.index_bits == 64) {
+#pragma unroll
+    for (int j = 0; j < kKeys; j++) key[j] = make_uint2(token_at(s.index, 64, at[j], s.rows), (uint32_t)at[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kKeys; j++) key[j] = make_uint2(token_at(s.index, 32, at[j], s.rows), (uint32_t)at[j]);
+  }
+}
+
 // How often each digit of a pass occurs in a chunk.
 __device__ __forceinline__ void count(const Sort& s, int chunks) {
   __shared__ uint32_t bin[kMaxBins];
@@ -138,8 +157,13 @@ __device__ __forceinline__ void count(const Sort& s, int chunks) {
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * s.chunk;
   const int end = (int)(first + s.chunk < s.tokens ? first + s.chunk : s.tokens);
-  for (int64_t i = first + threadIdx.x; i < end; i += kThreads)
-    atomicAdd(&bin[(pair_at(s, (int)i).x >> s.shift) & (s.bins - 1)], 1u);
+  for (int64_t i0 = first; i0 < end; i0 += kRound) {
+    uint2 key[kKeys];
+    round_of(s, i0, end, key);
+#pragma unroll
+    for (int j = 0; j < kKeys; j++)
+      if (i0 + place_in_round(j) < end) atomicAdd(&bin[(key[j].x >> s.shift) & (s.bins - 1)], 1u);
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < s.bins; i += kThreads) s.counts[(int64_t)blockIdx.x * s.bins + i] = bin[i];
 }
@@ -152,22 +176,33 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Sort s, int chunks, Fil
     fill_units<kThreads>(f, a, b, blockIdx.x - chunks, gridDim.x - chunks);
 }
 
-// How many of the wavefront's keys so far have this lane's digit, those of lower
-// lanes among them; `count` has them by digit.
-__device__ __forceinline__ uint32_t rank_of(uint32_t key, int bins, bool has, uint32_t* count) {
+// For K keys a lane, one after the other: how many of the wavefront's keys so far have the key's digit, those of lower
+// lanes among them; `count` has them by digit.  The lanes of the same digit are found for all K side by side.
+template <int K>
+__device__ __forceinline__ void ranks_of(const uint32_t (&key)[K], int bins, const bool (&has)[K], uint32_t* count, uint32_t (&rank)[K]) {
   const int lane = threadIdx.x & 63;
-  const uint32_t d = has ? key & (bins - 1) : 0;
-  uint64_t same = __ballot(has);  // the lanes with the same digit
-  for (int b = 1; b < bins; b *= 2) {
-    const uint64_t set = __ballot((d & b) != 0);
-    same &= (d & b) ? set : ~set;
+  uint32_t d[K];
+  uint64_t same[K];
+#pragma unroll
+  for (int j = 0; j < K; j++) {
+    d[j] = has[j] ? key[j] & (bins - 1) : 0;
+    same[j] = __ballot(has[j]);
   }
-  const uint32_t below = __popcll(same & (((uint64_t)1 << lane) - 1));
-  const uint32_t rank = has ? count[d] + below : 0;
-  wave_lds_fence();
-  if (has && below == 0) count[d] += __popcll(same);
-  wave_lds_fence();
-  return rank;
+  for (int b = 1; b < bins; b *= 2) {
+#pragma unroll
+    for (int j = 0; j < K; j++) {
+      const uint64_t set = __ballot((d[j] & b) != 0);
+      same[j] &= (d[j] & b) ? set : ~set;
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < K; j++) {
+    const uint32_t below = __popcll(same[j] & (((uint64_t)1 << lane) - 1));
+    rank[j] = has[j] ? count[d[j]] + below : 0;
+    wave_lds_fence();
+    if (has[j] && below == 0) count[d[j]] += __popcll(same[j]);
+    wave_lds_fence();
+  }
 }
 
 // The sum of n over the lower lanes of a workgroup of WAVES wavefronts (s: WAVES
@@ -192,30 +227,12 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t n, uint32_t* s) {
 // then those of the same digit in earlier chunks, then in earlier wavefronts and
 // rounds of this one.
 __device__ __forceinline__ void place(const Sort& s, int chunks) {
-  constexpr int kWaves = kThreads / 64, kKeys = kRound / kThreads;  // keys a lane holds
+  constexpr int kWaves = kThreads / 64;
   __shared__ uint32_t base[kMaxBins], count[kWaves][kMaxBins], sums[kWaves];
-  const int lane = threadIdx.x & 63, wave = wave_index(), bins = s.bins;
+  const int wave = wave_index(), bins = s.bins;
   const int64_t first = (int64_t)blockIdx.x * s.chunk;
   const int end = (int)(first + s.chunk < s.tokens ? first + s.chunk : s.tokens);
   uint2 key[kKeys];
-  const auto fetch = [&](int64_t i0) {
-    int at[kKeys];
-#pragma unroll
-    for (int j = 0; j < kKeys; j++) {  // past the end the last, without a branch: the loads then run side by side
-      const int64_t i = i0 + wave * (64 * kKeys) + j * 64 + lane;
-      at[j] = (int)(i < end ? i : end - 1);
-    }
-    if (s.from) {
-#pragma unroll
-      for (int j = 0; j < kKeys; j++) key[j] = s.from[at[j]];
-    } else if (s.index_bits == 64) {
-#pragma unroll
-      for (int j = 0; j < kKeys; j++) key[j] = make_uint2(token_at(s.index, 64, at[j], s.rows), (uint32_t)at[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kKeys; j++) key[j] = make_uint2(token_at(s.index, 32, at[j], s.rows), (uint32_t)at[j]);
-    }
-  };
   // of two digits a thread: their number before this chunk, and in all
   constexpr int kOwn = kMaxBins / kThreads;
   uint32_t before[kOwn], all[kOwn], mine = 0;
@@ -243,17 +260,18 @@ __device__ __forceinline__ void place(const Sort& s, int chunks) {
     at += all[j];
   }
   for (int64_t i0 = first; i0 < end; i0 += kRound) {
-    fetch(i0);
+    round_of(s, i0, end, key);
     for (int i = threadIdx.x; i < kWaves * kMaxBins; i += kThreads) (&count[0][0])[i] = 0;
     __syncthreads();
-    uint32_t rank[kKeys];
+    uint32_t digit[kKeys], rank[kKeys];
+    bool has[kKeys];
 #pragma unroll
     for (int j = 0; j < kKeys; j++) {
-      const int64_t i = i0 + wave * (64 * kKeys) + j * 64 + lane;
-      const bool has = i < end;
-      if (has && s.touched && !s.from && key[j].x < s.rows) s.touched[key[j].x] = 1;
-      rank[j] = rank_of(key[j].x >> s.shift, bins, has, count[wave]);
+      has[j] = i0 + place_in_round(j) < end;
+      digit[j] = key[j].x >> s.shift;
+      if (has[j] && s.touched && !s.from && key[j].x < s.rows) s.touched[key[j].x] = 1;
     }
+    ranks_of(digit, bins, has, count[wave], rank);
     __syncthreads();
     // count: the keys of the wavefronts before; base: past this round
     for (int d = threadIdx.x; d < bins; d += kThreads) {
@@ -269,8 +287,7 @@ __device__ __forceinline__ void place(const Sort& s, int chunks) {
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kKeys; j++) {
-      const int64_t i = i0 + wave * (64 * kKeys) + j * 64 + lane;
-      if (i < end) s.to[count[wave][(key[j].x >> s.shift) & (bins - 1)] + rank[j]] = key[j];
+      if (has[j]) s.to[count[wave][(key[j].x >> s.shift) & (bins - 1)] + rank[j]] = key[j];
     }
     __syncthreads();
   }
@@ -297,8 +314,9 @@ __global__ __launch_bounds__(1024) void sort_small_kernel(Sort s, int passes, Fi
   uint2 key[kKeys];
 #pragma unroll
   for (int j = 0; j < kKeys; j++) {
-    const int i = wave * (64 * kKeys) + j * 64 + lane;
-    key[j] = i < s.tokens ? pair_at(s, i) : make_uint2(0u, 0u);
+    const int i = wave * (64 * kKeys) + j * 64 + lane, at = i < s.tokens ? i : s.tokens - 1;
+    key[j] = make_uint2(0u, (uint32_t)at);
+    if (s.tokens > 0) key[j].x = s.index_bits == 64 ? token_at(s.index, 64, at, s.rows) : token_at(s.index, 32, at, s.rows);
   }
   clear_marks(s, threadIdx.x, 1024);
   __syncthreads();
@@ -306,12 +324,14 @@ __global__ __launch_bounds__(1024) void sort_small_kernel(Sort s, int passes, Fi
     const int shift = p * s.width;
     for (int i = threadIdx.x; i < kWaves * kMaxBins; i += 1024) (&count[0][0])[i] = 0;
     __syncthreads();
-    uint32_t rank[kKeys];
+    uint32_t digit[kKeys], rank[kKeys];
+    bool has[kKeys];
 #pragma unroll
     for (int j = 0; j < kKeys; j++) {
-      const bool has = wave * (64 * kKeys) + j * 64 + lane < s.tokens;
-      rank[j] = rank_of(key[j].x >> shift, bins, has, count[wave]);
+      has[j] = wave * (64 * kKeys) + j * 64 + lane < s.tokens;
+      digit[j] = key[j].x >> shift;
     }
+    ranks_of(digit, bins, has, count[wave], rank);
     __syncthreads();
     uint32_t all = 0;
     if (threadIdx.x < kMaxBins) {
@@ -641,9 +661,14 @@ __global__ __launch_bounds__(1024) void embed_once_kernel(Grad g, Sort s, int pa
       const int shift = kOnceBits + p * s.width;
       for (int i = tid; i < kWaves * kMaxBins; i += 1024) (&u.count[0][0])[i] = 0;
       __syncthreads();
-      uint32_t rank[KEYS];
+      uint32_t digit[KEYS], rank[KEYS];
+      bool has[KEYS];
 #pragma unroll
-      for (int j = 0; j < KEYS; j++) rank[j] = rank_of(key[j] >> shift, bins, first + j * 64 < s.tokens, u.count[wave]);
+      for (int j = 0; j < KEYS; j++) {
+        has[j] = first + j * 64 < s.tokens;
+        digit[j] = key[j] >> shift;
+      }
+      ranks_of(digit, bins, has, u.count[wave], rank);
       __syncthreads();
       uint32_t all = 0;
       if (tid < kMaxBins) {
