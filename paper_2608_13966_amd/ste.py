@@ -11,7 +11,10 @@ product from those (``ops.linear_weight_grad``).
 
 ``embed``, ``add_rms_norm``, ``add_layer_norm``, ``activation`` and
 ``distill_topk_loss`` are the autograd forms of the operators of ``ops`` that
-training uses; their tensors may have any number of leading dimensions.
+training uses; their tensors may have any number of leading dimensions.  A backward
+pass may be captured into a HIP graph; drop what still holds an eager graph of the
+same parameters (a loss that was kept) first: torch accumulates gradients on the
+stream that such a graph was made on, which a capture may not wait for.
 """
 from __future__ import annotations
 
