@@ -16,7 +16,7 @@
 // each workgroup sorts for itself.
 //
 // All of it is bound by memory but for the launches.  32768 tokens of 131072 x 4096 in
-// bf16: lookup 64 us; gradient 244 (the bytes at a copy's rate 259, a fill of the table
+// bf16: lookup 64 us; gradient 243 (the bytes at a copy's rate 259, a fill of the table
 // alone 157).  8 tokens, lookup 2.7; 1999 of 50021 x 1537 in fp32, gradient 68 into three
 // tables in turn, 57 into one (a fill 45); 46151 of 538 x 1130 in bf16 56 (its bytes 21),
 // nearly half of it the sort's four launches.
