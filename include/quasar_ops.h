@@ -192,7 +192,10 @@ size_t quasar_linear_codes_workspace_bytes(const quasar_desc* desc, int64_t toke
  *
  * and, as asked for, h, y and y in 8 bits (q and scale) as quasar_add_rms_norm
  * gives them; a row whose sum of squares is not finite has scale = NaN and
- * every q NaN.  The deviations' squares are summed after the mean is known.
+ * every q NaN.  The deviations' squares are summed after the mean is known, and
+ * the fp32 mean's own error is taken off the deviations.  The mean that is given
+ * out is rounded to fp32: where it is 2^k times the deviations, n of the gradients
+ * below, which take it from there, is off by up to 2^(k - 24).
  * cols is at most QUASAR_NORM_MAX_COLS.
  */
 typedef struct {

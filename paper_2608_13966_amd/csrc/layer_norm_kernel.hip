@@ -3,11 +3,14 @@
 //
 // Both directions are bound by memory.  A row is read once and kept in registers
 // widened to fp32, eight consecutive elements (one 16-byte load in bf16) per lane
-// and step: the mean, then the squares of the deviations from it (two sums, since
-// sum(h^2) - cols mean^2 cancels where the mean is large), the row's largest |y| and
-// the outputs all come from one read.  67 M elements in bf16 with a residual, rows of
-// 64 to 16384 columns: forward 92 to 98 us, 5.4 to 5.8 TB/s (a copy of 1 GiB: 5.0);
-// gradients 101 to 118, 4.5 to 5.3.  Odd widths cost more (1537 columns: 108 and 137),
+// and step: the mean, then the deviations from it and their squares, the row's
+// largest |y| and the outputs all come from one read.  (sum(h^2) - cols mean^2 cancels
+// where the mean is large; and the fp32 mean is itself off by roundings of its own
+// size, so the deviations' mean, which is what it is off by, is taken off again:
+// without that y of rows 1000 +- 2^-8 was off by 2e-2.)  67 M elements in bf16 with a residual, rows of
+// 64 to 16384 columns: forward 94 to 99 us, 5.4 to 5.7 TB/s (a copy of 1 GiB: 5.0),
+// with q beside y 109, q alone 85 at 4096; gradients 101 to 118, 4.5 to 5.3.  Taking
+// the mean's error off costs 0 to 3%.  Odd widths cost more (1537 columns: 110 and 137),
 // as do gradients past 16384 columns, whose shares spill (32768: 364).  One row of 4096
 // takes 3.9 us.
 #include "ops_common.h"
@@ -44,11 +47,34 @@ __device__ __forceinline__ float row_reduce(float x, float* s, Op op) {
     return group_reduce<TPR / 64>(x, s, op);
   }
 }
+// Two sums, through one barrier.
+template <int TPR>
+__device__ __forceinline__ void row_sums(float& x, float& y, float* s, float* t) {
+  if constexpr (TPR <= 64) {
+    x = row_reduce<TPR>(x, s, SumOp());
+    y = row_reduce<TPR>(y, t, SumOp());
+  } else {
+    x = wave_reduce(x, SumOp());
+    y = wave_reduce(y, SumOp());
+    if ((threadIdx.x & 63) == 0) {
+      s[wave_index()] = x;
+      t[wave_index()] = y;
+    }
+    __syncthreads();
+    x = s[0];
+    y = t[0];
+#pragma unroll
+    for (int i = 1; i < TPR / 64; i++) {
+      x += s[i];
+      y += t[i];
+    }
+  }
+}
 
 template <int XT, int RT, int TPR, int NV>
 __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_kernel(quasar_layer_norm a) {
   constexpr int kWaves = TPR < 64 ? 1 : TPR / 64;
-  __shared__ float red[3][kWaves];
+  __shared__ float red[4][kWaves];
   const int t = Shape<TPR>::lane(), cols = (int)a.cols;
   const int64_t row = (int64_t)blockIdx.x * Shape<TPR>::kRows + Shape<TPR>::row();
   if (row >= a.rows) return;  // whole rows of 16 lanes; no barrier follows where there are several rows
@@ -97,7 +123,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_kernel(quasar
       }
     }
   }
-  float ss = 0.0f;
+  float ss = 0.0f, rest = 0.0f;
 #pragma unroll
   for (int v = 0; v < NV; v++) {
     const int left = cols - (v * TPR + t) * 8;
@@ -109,12 +135,19 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_kernel(quasar
         if (i >= left) h[v][i] = 0.0f;
     }
 #pragma unroll
-    for (int i = 0; i < 8; i++) ss = __builtin_fmaf(h[v][i], h[v][i], ss);
+    for (int i = 0; i < 8; i++) {
+      ss = __builtin_fmaf(h[v][i], h[v][i], ss);
+      rest += h[v][i];
+    }
   }
-  ss = row_reduce<TPR>(ss, red[1], SumOp());
-  const float rstd = 1.0f / __builtin_sqrtf(ss / (float)cols + a.eps);
+  row_sums<TPR>(ss, rest, red[1], red[2]);
+  // what the mean is off by (0 where the squares are not finite), and the squares about the better one
+  rest = ss < INFINITY ? rest / (float)cols : 0.0f;
+  float var = __builtin_fmaf(-rest, rest, ss / (float)cols);
+  var = var < 0.0f ? 0.0f : var;  // NaN stays
+  const float rstd = 1.0f / __builtin_sqrtf(var + a.eps);
   if (t == 0) {
-    if (a.mean) a.mean[row] = mean;
+    if (a.mean) a.mean[row] = mean + rest;
     if (a.rstd) a.rstd[row] = rstd;
   }
   if constexpr (!kEarly) affine();
@@ -123,7 +156,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_kernel(quasar
   for (int v = 0; v < NV; v++) {
 #pragma unroll
     for (int i = 0; i < 8; i++) {
-      h[v][i] = __builtin_fmaf(h[v][i] * rstd, w[v][i], b[v][i]);
+      h[v][i] = __builtin_fmaf((h[v][i] - rest) * rstd, w[v][i], b[v][i]);
       top = fmaxf(top, fabsf(h[v][i]));
     }
   }
@@ -136,7 +169,7 @@ __global__ __launch_bounds__(Shape<TPR>::kThreads) void layer_norm_kernel(quasar
     }
   }
   if (!a.q) return;
-  top = row_reduce<TPR>(top, red[2], MaxOp());
+  top = row_reduce<TPR>(top, red[3], MaxOp());
   // NaN for a row that is not finite
   float scale = fmaxf(top / 448.0f, 0x1p-120f);
   if (!(ss < INFINITY)) scale = __builtin_nanf("");

@@ -249,3 +249,49 @@ def test_widths_that_cut_a_piece(cols, typ):
     for buf, t in ((yb, y), (hb, h), (dxb, dx)):
         t.fill_(7.0)
         assert (buf == 7).all()
+
+
+# ---- means that are large against the deviations ----------------------------------------
+# Here the bounds above say nothing: n u of the mean is more than the deviations.  No value of the kernels' sums goes
+# through more than 32 additions in a thread, 6 in a wavefront and 16 between them, so D = 64 takes n's place; and what the
+# mean is off by is known, since all deviations have it: taken off, only the errors of that are left.
+D = 64
+
+
+def about_a_large_mean(h, w, b):
+    """(mean, rstd, y) of fp32 rows in 64 bits, and how far from them a form may be that takes the mean's error off."""
+    hd, wd = h.double(), w.double()
+    mean = hd.mean(1, keepdim=True)
+    d = hd - mean
+    size, var = d.abs().mean(1, keepdim=True), (d * d).mean(1, keepdim=True)
+    rstd = (var + EPS).rsqrt()
+    n = d * rstd
+    y = n * wd + b.double()
+    e_mean = (D + 2) * U * hd.abs().mean(1, keepdim=True)
+    e_dev = U * (d.abs() + e_mean)                           # of a deviation, about the mean that is off
+    e_rest = (D + 3) * U * (size + e_mean)                   # of what it is off by
+    e_var = 2 * (D + 4) * U * (var + e_mean ** 2) + 2 * e_mean * e_rest
+    e_rel = 0.55 * e_var / (var + EPS) + 4 * U               # of rstd
+    e_y = wd.abs() * rstd * (e_rest + e_dev + U * d.abs()) + (n * wd).abs() * (e_rel + 3 * U) + U * y.abs()
+    return (mean[:, 0], rstd[:, 0], y), (U * mean[:, 0].abs() + 1.01 * e_rest[:, 0], rstd[:, 0] * e_rel[:, 0] * 1.1, e_y * 1.1)
+
+
+LARGE_MEANS = [(1000.0, 2.0 ** -8), (-100.0, 2.0 ** -4), (1000.0, 1.0), (12345.678, 0.05), (33333.3, 0.0), (0.0, 1.0)]
+
+
+@pytest.mark.parametrize("cols", [60, 100, 250, 511, 1000, 2047, 4096, 8191, 16384, 32768])
+@pytest.mark.parametrize("mean,size", LARGE_MEANS)
+@pytest.mark.parametrize("typ", ["fp32", "bf16"])
+def test_the_mean_is_taken_off_whole(cols, mean, size, typ):
+    """y, rstd and mean of rows with a large mean: fp32 alone, and the same mean in an fp32 stream that bf16 comes to."""
+    w, b = gen((1, cols), torch.float32, 2, 0.2, mean=1.0)[0], gen((1, cols), torch.float32, 3, 0.1)[0]
+    if typ == "fp32":
+        x, res = gen((9, cols), torch.float32, 1, size, mean=mean), None
+        h = x
+    else:
+        x, res = gen((9, cols), torch.bfloat16, 1, size), gen((9, cols), torch.float32, 4, size, mean=mean)
+        h = x.float() + res
+    o = O.add_layer_norm(x, w, b, res, eps=EPS, y_dtype="fp32")
+    for name, want, tol in zip(("mean", "rstd", "y"), *about_a_large_mean(h, w, b)):
+        assert o[name].isfinite().all(), name
+        close(o[name], want, tol)
