@@ -50,6 +50,7 @@ constexpr uint32_t kInfBits = 0x7f800000u;
 // SiLU's quotient by the hardware's reciprocal and one step of Newton's (within 8 x
 // 2^-24; 8192 x 14336 in bf16 125 us with the division, 104 so), GELU without a
 // selection (past 32 the tail is 0, and infinity times it not a number; 116, 114).
+// GELU of -infinity, which is not a number either, is the caller's to see to: as NaN.
 __device__ __forceinline__ void apply(float (&v)[8], int act) {
   if (act == QUASAR_ACT_RELU) {
 #pragma unroll
@@ -115,7 +116,10 @@ __global__ __launch_bounds__(kThreads) void checkpoint_kernel(quasar_checkpoint 
     if (wild) {
 #pragma unroll
       for (int i = 0; i < 8; i++)
-        if (!(fabsf(v[i]) < INFINITY)) s[i] = __builtin_nanf("");
+        if (!(fabsf(v[i]) < INFINITY)) {
+          s[i] = __builtin_nanf("");
+          if (a.act == QUASAR_ACT_GELU && v[i] < 0.0f) v[i] = s[i];  // -infinity (1 + erf(-infinity)) / 2
+        }
     }
     store_bytes(a.q + row[j] * a.q_stride + c, pack_e4m3x8(s), left);
     if (lane == 0) a.exponent[row[j] * a.exponent_stride + block[j]] = (uint8_t)e;

@@ -151,6 +151,30 @@ def test_what_is_not_finite_stays_by_itself(dtype):
     assert torch.equal(o["y"].isnan(), x.isnan()) and o["y"][1, 130] == INF and o["y"][2, 399] == 0
 
 
+def formula(act, x):
+    """The header's formulas as they stand, in 64 bits."""
+    x = x.double()
+    return {"none": x, "relu": torch.where(x < 0, 0.0, x), "silu": x / (1 + torch.exp(-x)),
+            "gelu": x * (1 + torch.erf(x / math.sqrt(2))) / 2}[act]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu"])
+def test_activations_of_what_is_not_finite(act, dtype):
+    """As IEEE arithmetic takes them through the formulas: SiLU and GELU of -infinity are -infinity times 0.  Neighbours are
+    what they are without them."""
+    clean = gen((5, 400), dtype, 1)
+    x = clean.clone()
+    x[0, 3], x[1, 130], x[2, 399], x[3, :128], x[4, 256:384] = NAN, INF, -INF, NAN, -INF
+    x[1, 131] = -INF
+    bad = ~x.isfinite()
+    y, want = O.checkpoint_rows(x, act=act, want_y=True)["y"], formula(act, x)
+    assert torch.equal(y.isnan()[bad], want.isnan()[bad])
+    there = bad & ~want.isnan()
+    assert torch.equal(y[there].double(), want[there])
+    assert torch.equal(y[~bad], O.checkpoint_rows(clean, act=act, want_y=True)["y"][~bad])
+
+
 def test_outputs_in_wider_buffers_and_in_place():
     x = gen((9, 300), torch.bfloat16, 1, pad=3, off=1)
     want = O.checkpoint_rows(x, act="gelu")
