@@ -43,21 +43,24 @@ class _STELinear(torch.autograd.Function):
 
 
 class _STELinearKept(torch.autograd.Function):
-    """The same, x kept in 8 bits: dL/dr = dL/dy^T of what was kept, in fp32."""
+    """The same, x kept in 8 bits: dL/dr = dL/dy^T of what was kept, in fp32.  Of a frozen weight nothing is kept but r."""
 
     @staticmethod
     def forward(ctx, x, weight, r):
-        kept = ops.checkpoint_rows(_rows(x))
-        ctx.save_for_backward(kept["q"], kept["exponent"], r)
+        kept = ()
+        if ctx.needs_input_grad[1]:
+            o = ops.checkpoint_rows(_rows(x))
+            kept = o["q"], o["exponent"]
+        ctx.save_for_backward(*kept, r)
         return x @ r.to(x.dtype).t()
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, gy):
-        q, exponent, r = ctx.saved_tensors
+        *kept, r = ctx.saved_tensors
         need_x, need_w = ctx.needs_input_grad[:2]
         gx = gy @ r.to(gy.dtype) if need_x else None
-        gw = ops.linear_weight_grad(_rows(gy), q, exponent)["dw"] if need_w else None
+        gw = ops.linear_weight_grad(_rows(gy), *kept)["dw"] if need_w else None
         return gx, gw, None
 
 
@@ -98,7 +101,9 @@ class QuasarLinear(torch.nn.Module):
         self.codes, self.scales, self.zeros = out["codes"], out["scales"], out["zeros"]
 
     def forward(self, x):
-        return (_STELinearKept if self.checkpoint else _STELinear).apply(x, self.weight, self.r)
+        # without gradients the plain form, which keeps nothing then
+        kept = self.checkpoint and torch.is_grad_enabled()
+        return (_STELinearKept if kept else _STELinear).apply(x, self.weight, self.r)
 
     @torch.no_grad()
     def step(self):
