@@ -273,7 +273,8 @@ int quasar_embed(const quasar_embedding* a, void* stream);
 int quasar_embed_check(const quasar_embedding* a);
 
 typedef struct {
-  int64_t rows, cols, tokens;
+  int64_t rows, cols, tokens;  /* as above, with (ceil(tokens / 32) - 1) * ceil(cols / 512) < 2^24, which is more than the
+                                  card's memory holds of dy */
   const void* index;         /* [tokens], contiguous */
   const void* dy;            /* [tokens, cols] */
   void* dweight;             /* [rows, cols] */

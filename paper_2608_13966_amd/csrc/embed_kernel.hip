@@ -905,7 +905,8 @@ bool embed_backward_fits(int64_t rows, int64_t cols, int64_t tokens, size_t& wor
   bool fits = true;
   (void)with_lanes(cols, [&](auto lanes) {
     constexpr int L = decltype(lanes)::value;
-    fits = p.stretches * ((cols + 8 * L - 1) / (8 * L)) <= most_groups(kThreads) / 2;
+    // the join's workgroups; the sums are 256 / L of these to one, and the zeros' at most half a grid
+    fits = ((int64_t)p.stretches - 1) * ((cols + 8 * L - 1) / (8 * L)) <= most_groups(kThreads);
     return hipSuccess;
   });
   return fits;

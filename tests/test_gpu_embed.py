@@ -218,3 +218,15 @@ def test_rows_past_four_gigabytes():
     dw = O.embed_backward(dy, tok, rows, out={"dw": w})["dw"]
     assert torch.equal(dw[rows - 3:], torch.stack([dy[1], dy[3], (dy[0].float() + dy[4].float()).bfloat16()]))
     assert torch.equal(dw[0], dy[2]) and int(dw[1:rows - 3].count_nonzero()) == 0
+
+
+@pytest.mark.parametrize("n", [(1 << 28) - 1000, 1 << 28])
+def test_the_longest_list(n):
+    """Counts in fp32: each token's ones, exact below 2^24, and the tokens that are none."""
+    rows = 1000
+    tok = torch.randint(-1, rows, (n,), device=DEV, dtype=torch.int32, generator=torch.Generator(device=DEV).manual_seed(1))
+    dw = O.embed_backward(torch.ones(n, 1, device=DEV, dtype=torch.bfloat16), tok, rows, dw_dtype="fp32")["dw"]
+    want = torch.zeros(rows, device=DEV, dtype=torch.int64)
+    for part in tok.split(1 << 24):
+        want += torch.bincount(part[part >= 0], minlength=rows)
+    assert torch.equal(dw[:, 0].long(), want) and torch.equal(dw, dw.round())

@@ -133,6 +133,19 @@ def test_embed_backward_workspace():
     assert _embed_backward(**kw) == Q.ERR_SHAPE and O.quasar_embed_backward_workspace_bytes(5, 1 << 20, 1 << 28) == 0
 
 
+def test_embed_backward_takes_the_tokens_that_memory_holds():
+    """Up to 2^28 tokens, where dy in bf16 is at most 288 GB."""
+    for cols, tokens in ((1, 1 << 28), (8, 1 << 28), (257, 1 << 28), (512, 1 << 28), (513, 1 << 28), (520, 270000000), (1025, 1 << 27),
+                         (4096, 35000000), (4097, 35000000), (1 << 20, 137000)):
+        tokens = min(tokens, 1 << 28)
+        kw = dict(rows=1000, cols=cols, tokens=tokens, dy_stride=cols, dweight_stride=cols)
+        assert _embed_backward(**kw) == Q.OK, (cols, tokens)
+        assert O.quasar_embed_backward_workspace_bytes(1000, cols, tokens) > 16 * tokens
+    for cols, tokens, status in ((1024, 1 << 28, Q.OK), (1025, 1 << 28, Q.ERR_SHAPE), (1 << 20, 32 * 8193, Q.ERR_SHAPE)):
+        kw = dict(rows=1000, cols=cols, tokens=tokens, dy_stride=cols, dweight_stride=cols)
+        assert _embed_backward(**kw) == status, (cols, tokens)
+
+
 def _checkpoint(**kw):
     p = dict(rows=4, cols=300, x=A, y=A, q=A, exponent=A, x_stride=300, y_stride=300, q_stride=300, exponent_stride=3,
              x_dtype=Q.BF16, y_dtype=Q.BF16, act=3)
