@@ -345,6 +345,31 @@ def test_fp32_gradients_are_taken_whole(n, k):
     assert torch.equal(dw.nan_to_num(12.5), dy.nan_to_num(12.5)[0][:, None].expand(n, k))
 
 
+@pytest.mark.parametrize("t,n,k,parts", [(100, 4096, 4096, 0), (150, 300, 200, 0), (130, 4096, 4096, 3), (191, 4096, 4096, 3),
+                                         (700, 4096, 4096, 3), (1500, 4099, 4104, 3)])
+def test_all_parts_of_an_fp32_gradient(t, n, k, parts):
+    """One value of 24 significant bits a token, each in a row of dweight of its own, and x a power of two: dweight's rows
+    are those values, scaled, bit for bit, in each form, whichever steps and shares their three parts fall to."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    blocks, rows = -(-k // 128), min(n, t)
+    powers = torch.randint(-20, 20, (t, blocks), generator=g, device=DEV)
+    x = torch.exp2(powers.float()).repeat_interleave(128, 1)[:, :k].contiguous()
+    kept = O.checkpoint_rows(x)
+    assert torch.equal(back(kept["q"], kept["exponent"]), x.double())
+    value = torch.randn(t, generator=g, device=DEV)
+    value = (value.view(torch.int32) | 0x010101).view(torch.float32)  # no part is 0
+    at = torch.randperm(n, generator=g, device=DEV)[:rows]
+    dy = torch.zeros(t, n, device=DEV)
+    tok = torch.randperm(t, generator=g, device=DEV)[:rows]
+    dy[tok, at] = value[tok]
+    o = O.linear_weight_grad(dy, kept["q"], kept["exponent"])
+    if parts:  # the form that spreads dy's parts over its workspace
+        assert o["workspace"].numel() >= parts * -(-t // 64) * 64 * n * 2
+    want = torch.zeros(n, k, device=DEV, dtype=torch.float64)
+    want[at] = value[tok].double()[:, None] * x[tok].double()
+    assert torch.equal(o["dw"].double(), want)
+
+
 @pytest.mark.parametrize("gt", ["bf16", "fp32"])
 @pytest.mark.parametrize("t,n,k", [(150, 200, 300), (700, 4096, 4096)])
 @pytest.mark.parametrize("x_size,dy_size", [(2.0 ** -100, 2.0 ** 90), (2.0 ** 120, 2.0 ** -100)])
