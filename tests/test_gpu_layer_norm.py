@@ -295,3 +295,45 @@ def test_the_mean_is_taken_off_whole(cols, mean, size, typ):
     for name, want, tol in zip(("mean", "rstd", "y"), *about_a_large_mean(h, w, b)):
         assert o[name].isfinite().all(), name
         close(o[name], want, tol)
+
+
+# ---- in place, where a row's end cuts a piece ----------------------------------------------
+# Such a piece comes as the row's last eight elements, some of which another lane, perhaps of another wavefront, owns and
+# writes: they have to be read before that.  Odd widths for each number of threads a row, rows for several rounds.
+
+CUT_WIDTHS = [9, 61, 127, 199, 301, 1023, 1537, 2047, 3333, 4095, 5001, 8191, 16383, 20001]
+
+
+@pytest.mark.parametrize("cols", CUT_WIDTHS)
+@pytest.mark.parametrize("typ", ["bf16", "fp32"])
+def test_forward_in_place_with_a_cut_piece(cols, typ):
+    rows = 600 if cols < 8192 else 300
+    x, res = gen((rows, cols), DT[typ], 1), gen((rows, cols), DT[typ], 2, mean=0.5)
+    w, b = gen((1, cols), DT[typ], 3)[0], gen((1, cols), DT[typ], 4)[0]
+    want = O.add_layer_norm(x, w, b, res, eps=EPS)
+    for turn in range(3):
+        for name in ("x", "res"):
+            t = {"x": x.clone(), "res": res.clone()}
+            out = {"h": t[name], "y": torch.full_like(x, float("nan")), "mean": torch.empty(rows, device=DEV), "rstd": torch.empty(rows, device=DEV)}
+            o = O.add_layer_norm(t["x"], w, b, t["res"], eps=EPS, out=out)
+            assert o["h"] is t[name]
+            for k in ("h", "y", "mean", "rstd"):
+                assert torch.equal(o[k], want[k]), (name, k, turn)
+
+
+@pytest.mark.parametrize("cols", CUT_WIDTHS)
+@pytest.mark.parametrize("typ", ["bf16", "fp32"])
+def test_backward_in_place_with_a_cut_piece(cols, typ):
+    rows = 1500 if cols < 4096 else 600
+    dy, h, dh = gen((rows, cols), DT[typ], 1), gen((rows, cols), DT[typ], 2, 1.3, mean=0.4), gen((rows, cols), DT[typ], 3)
+    w = gen((1, cols), DT[typ], 4)[0]
+    mean, rstd = stats(h)
+    want = O.add_layer_norm_backward(dy, h, w, mean, rstd, dh)
+    for turn in range(3):
+        for name in ("dh", "dy", "h"):
+            t = {"dy": dy.clone(), "h": h.clone(), "dh": dh.clone()}
+            o = O.add_layer_norm_backward(t["dy"], t["h"], w, mean, rstd, t["dh"],
+                                          out={"dx": t[name], "dw": torch.empty(cols, device=DEV), "db": torch.empty(cols, device=DEV)})
+            assert o["dx"] is t[name]
+            for k in ("dx", "dw", "db"):
+                assert torch.equal(o[k], want[k]), (name, k, turn)
