@@ -354,8 +354,9 @@ typedef struct {
 
 int quasar_linear_weight_grad(const quasar_weight_grad* a, void* stream);
 int quasar_linear_weight_grad_check(const quasar_weight_grad* a);
-/* Device scratch that this call needs (its workspace fields are not looked at): a copy of dy is part of it where the
- * alignment of dy, its stride or its type ask for one.  0 where it needs none, or for an invalid call. */
+/* Device scratch that this call needs (its workspace fields are not looked at), 0 where it needs none, or for an invalid
+ * call.  For large weights x in bf16, tokens * cols * 2 bytes, and a copy of dy where its alignment, stride or type ask for
+ * one: tokens * rows * 2 bytes, * 6 from fp32; and the sums of shares of the tokens. */
 size_t quasar_linear_weight_grad_workspace_bytes(const quasar_weight_grad* a);
 
 #ifdef __cplusplus

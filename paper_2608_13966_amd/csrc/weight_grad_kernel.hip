@@ -18,7 +18,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kStep = 64;                    // tokens a step takes
-constexpr int64_t kMaxPitch = (1 << 22) - 1;  // elements of a row whose bytes the tile kernel reckons in 24 bits
+constexpr int64_t kMaxPitch = 1 << 22;       // elements of a row (no weight has more) whose bytes the tile kernel reckons in 24 bits
 
 __host__ __device__ constexpr int64_t part_pitch(int64_t cols) { return (cols + 7) & ~(int64_t)7; }
 
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void weight_grad_kernel(quasar_weight_grad a, 
   };
   // the steps whose pieces, eight elements past a row's end too, lie before the last token's row
   const int64_t safe = a.tokens - 8 < t1 ? a.tokens - 8 : t1;
-  const bool near = a.dy_stride < kMaxPitch && a.q_stride < kMaxPitch && a.exponent_stride < kMaxPitch;  // offsets fit
+  const bool near = a.dy_stride <= kMaxPitch && a.q_stride <= kMaxPitch && a.exponent_stride <= kMaxPitch;  // offsets fit
   const int whole = near && safe > t0 ? (int)((safe - t0) / kStep) : 0;
   const auto step_at = [&](int s) { return t0 + (int64_t)(s < whole ? s : whole - 1) * kStep; };  // past the last: it again
   if (whole > 0) {
@@ -815,7 +815,8 @@ Choice choose(const quasar_weight_grad& a) {
   const int64_t tiles = ((a.rows + 255) / 256) * ((a.cols + 255) / 256), whole = tiles / kCUs * kCUs, rest = tiles - whole;
   const int64_t parts = wide ? 3 : 1, all = parts * steps, padded = steps * kStep;
   const int64_t np = (a.rows + 7) & ~(int64_t)7, kp = (a.cols + 7) & ~(int64_t)7, from = direct(a) ? a.tokens / kStep * kStep : 0;
-  if (a.rows <= kMaxPitch && a.cols <= kMaxPitch && all < (int64_t)1 << 24) {
+  // where its grids take it: the spread's workgroups, and the tiles with up to 32 shares of those past whole rounds
+  if (steps * ((kp + 127) / 128) + 32 * kCUs <= most_groups(256) && tiles + 32 * kCUs <= most_groups(512)) {
     constexpr double kTile = 256 * 256 * 4 / 6.9e6;
     const auto round = [&](int64_t groups, int64_t per) {
       return 2.0 + (double)per * (1.3 + 0.2 * (double)groups / kCUs) + (double)groups * kTile;
@@ -881,9 +882,7 @@ hipError_t launch_large(const quasar_weight_grad& a, const Choice& c, float* par
 bool weight_grad_fits(const quasar_weight_grad& a, size_t& workspace) {
   const Choice c = choose(a);
   workspace = c.bytes;
-  if (c.tile == 256 && c.padded / kStep * ((c.kp + 127) / 128) + 32 * kCUs > most_groups(256)) return false;
-  if (c.tile == 256) return c.tiles <= most_groups(512) - 32 * kCUs;
-  if (c.tile == 0) return true;
+  if (c.tile != 64) return true;
   return c.tiles * c.splits <= most_groups(256) && (c.splits == 1 || a.rows * (part_pitch(a.cols) / 8) <= 256 * most_groups(256));
 }
 

@@ -397,6 +397,18 @@ def test_weight_grad_with_far_apart_rows(n, k):
     check_weight(dy, q.view(E4M3), kept["exponent"], O.linear_weight_grad(dy, q.view(E4M3), kept["exponent"])["dw"])
 
 
+def test_weight_grad_of_the_longest_rows():
+    """dy's rows of 2^22 elements, 64 of them a step, in the form for large weights."""
+    t, n, k = 130, 1 << 22, 264
+    kept = O.checkpoint_rows(gen((t, k), torch.bfloat16, 1))
+    dy = gen((t, n), torch.bfloat16, 2)
+    o = O.linear_weight_grad(dy, kept["q"], kept["exponent"])
+    assert o["workspace"].numel() >= 192 * k * 2
+    some = torch.randperm(n, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV)[:2000]
+    for rows in (slice(0, 600), slice(n - 600, n), some):
+        check_weight(dy[:, rows], kept["q"], kept["exponent"], o["dw"][rows])
+
+
 @pytest.mark.parametrize("gt", ["bf16", "fp32"])
 @pytest.mark.parametrize("t,n,k", [(70, 200, 300), (191, 4096, 4096)])
 def test_what_is_not_finite_reaches_its_row_and_column(gt, t, n, k):

@@ -223,6 +223,24 @@ def test_weight_grad_workspace(dt):
     assert _weight_args(tokens=-1).workspace_bytes == 0 and _weight_args(dy_dtype=O.E4M3).workspace_bytes == 0
 
 
+@pytest.mark.parametrize("dt", [Q.BF16, Q.F32])
+@pytest.mark.parametrize("wt", [Q.BF16, Q.F32])
+def test_weight_grad_takes_what_memory_holds(dt, wt):
+    """Every call whose tensors the card's 288 GB hold, sizes up to the largest; the workspace is x in bf16 and dy's three
+    parts at most, and the shares' sums."""
+    most = 1 << 22
+    for t in (1, 64, 129, 200, 10 ** 4, 10 ** 6, 10 ** 7, 10 ** 8, 1 << 28):
+        for n in (1, 7, 64, 1000, 4096, 10 ** 5, most - 1, most):
+            for k in (1, 7, 64, 1000, 16384, 10 ** 5, most - 1, most):
+                dy, x, dw = t * n * (2 if dt == Q.BF16 else 4), t * k + t * -(-k // 128), n * k * (2 if wt == Q.BF16 else 4)
+                if dy + x + dw > 288e9:
+                    continue
+                a = _weight_args(tokens=t, rows=n, cols=k, dy_dtype=dt, dweight_dtype=wt)
+                assert O.quasar_linear_weight_grad_check(a) == Q.OK, (t, n, k)
+                rows = -(-t // 64) * 64
+                assert a.workspace_bytes <= rows * (2 * (k + 7) + 6 * (n + 7)) + 33 * max(256 * 256 * 4 * 256, n * (k + 7) * 4), (t, n, k)
+
+
 def test_weight_grad_copies_dy_only_where_it_has_to():
     kw = dict(tokens=8192, rows=14336, cols=4096)
     plain, whole = _weight_args(**kw).workspace_bytes, 8192 * 14336 * 2
