@@ -479,14 +479,17 @@ __device__ __forceinline__ int chunk_at(int m, int c) { return m * kStep + 8 * (
 // phase 0 reads x0 and g1, phase 1 x1 and the next step's g0.  Two stages; a half is
 // filled again as soon as all have read it.
 //
-// 8192 tokens, 14336 x 4096, normal values: the call takes 719 us (26 spread the operands,
-// 17 join the shares), 1.34 PFLOP/s; a library product of these sizes with its sum along
-// the rows takes 700 to 735, dy^T x as it is 1030.  Matrix units are busy 70% of the
-// time, and the card's power is part of the bound: with all-zero operands 619.  On the way
-// (us): both operands through transposing loads, three quarters of a step's reads in its
-// first phase 882; halves of half lines of dy 922, of whole ones 795; the tiles past whole
-// rounds shared out 747; addresses that go on a step at a time 727; loads ahead of reads
-// 719.  32 x 32 x 16 instructions took 777, not 747.
+// 8192 tokens, 14336 x 4096, normal values, median of 140 passes on a busy card: the call
+// takes 740 us (26 spread the operands, 18 join the shares), 1.30 PFLOP/s; beside it a
+// library product of bf16 operands that lie along the summed dimension takes 631, of dy
+// and x as they lie here 947.  (Cards differ: 755, 700 to 735 and 1030 on another.  After
+// a rest the first twenty calls of this kernel take 706, up to 966 and 734 as the clocks
+// settle.)  Matrix units are busy 73% of the time, and the card's power is part of the
+// bound.  On the way, on one cool card (us): both operands through transposing loads, three
+// quarters of a step's reads in its first phase 882; halves of half lines of dy 922, of
+// whole ones 795; the tiles past whole rounds shared out 747; addresses that go on a step
+// at a time 727; loads ahead of reads 719, and 619 with all-zero operands.  32 x 32 x 16
+// instructions took 777, not 747.
 //
 // The wavefronts of a SIMD work in turn: those of wk = 1 run one barrier behind, so
 // that while one multiplies the other reads its next operands.  Barriers 2p and 2p + 1
