@@ -397,6 +397,21 @@ def test_weight_grad_with_far_apart_rows(n, k):
     check_weight(dy, q.view(E4M3), kept["exponent"], O.linear_weight_grad(dy, q.view(E4M3), kept["exponent"])["dw"])
 
 
+@pytest.mark.parametrize("t,n,k", TNK + [(128, 2048, 4096), (300, 2048, 4096), (513, 4096, 4104), (1025, 2056, 8192), (4100, 1000, 2000),
+                                         (1500, 4099, 4100), (8191, 2304, 2050), (16385, 300, 77)])
+@pytest.mark.parametrize("gt,wt", [("bf16", "fp32"), ("fp32", "fp32")])
+def test_sums_of_integers_are_exact(t, n, k, gt, wt):
+    """Every product and every sum is an integer below 2^24: no order rounds, and a token that is lost or counted twice
+    shows in any list."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x, dy = torch.randint(-15, 16, (t, k), generator=g, device=DEV), torch.randint(-60, 61, (t, n), generator=g, device=DEV)
+    assert 15 * 60 * t < 2 ** 24
+    kept = O.checkpoint_rows(x.to(torch.bfloat16))
+    assert torch.equal(back(kept["q"], kept["exponent"]).long(), x)
+    dw = O.linear_weight_grad(dy.to(DT[gt]), kept["q"], kept["exponent"], dw_dtype=wt)["dw"]
+    assert torch.equal(dw.double(), dy.double().t().contiguous() @ x.double())
+
+
 def test_weight_grad_of_the_longest_rows():
     """dy's rows of 2^22 elements, 64 of them a step, in the form for large weights."""
     t, n, k = 130, 1 << 22, 264

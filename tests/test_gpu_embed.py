@@ -230,3 +230,17 @@ def test_the_longest_list(n):
     for part in tok.split(1 << 24):
         want += torch.bincount(part[part >= 0], minlength=rows)
     assert torch.equal(dw[:, 0].long(), want) and torch.equal(dw, dw.round())
+
+
+@pytest.mark.parametrize("rows,cols,n", [(1, 1, 700), (5, 3, 1024), (300, 64, 2048), (40, 257, 2049), (5000, 100, 4096), (20000, 9, 4100),
+                                         (700, 1000, 9000), (3, 40, 200000), (538, 130, 46151), (160000, 16, 70000), (2, 513, 16385)])
+@pytest.mark.parametrize("kind", ["uniform", "few", "one", "sorted", "none"])
+@pytest.mark.parametrize("gt", ["bf16", "fp32"])
+def test_sums_of_integers_are_exact(rows, cols, n, kind, gt):
+    """No sum reaches 2^24, so that no order rounds: a token that is lost or counted twice shows in any list."""
+    tok = draw(n, rows, kind, 5)
+    dy = torch.randint(-60, 61, (n, cols), device=DEV, generator=torch.Generator(device=DEV).manual_seed(6))
+    assert 60 * n < 2 ** 24
+    ok = (tok >= 0) & (tok < rows)
+    want = torch.zeros(rows, cols, device=DEV, dtype=torch.int64).index_add_(0, tok[ok], dy[ok])
+    assert torch.equal(O.embed_backward(dy.to(DT[gt]), tok, rows, dw_dtype="fp32")["dw"].long(), want)

@@ -297,6 +297,18 @@ def test_the_mean_is_taken_off_whole(cols, mean, size, typ):
         close(o[name], want, tol)
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 64), (7, 4096), (777, 1537), (3000, 200), (5000, 60), (1030, 4096), (1100, 9000), (300, 20000)])
+@pytest.mark.parametrize("typ", ["bf16", "fp32"])
+def test_sums_over_rows_of_integers_are_exact(rows, cols, typ):
+    """mean 0, rstd 1 and integers: dweight = sum dy h and dbias = sum dy have no rounding, whichever row is lost."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    dy, h = (torch.randint(-9, 10, (rows, cols), generator=g, device=DEV) for _ in range(2))
+    assert 81 * rows < 2 ** 24
+    o = O.add_layer_norm_backward(dy.to(DT[typ]), h.to(DT[typ]), torch.ones(cols, device=DEV), torch.zeros(rows, device=DEV),
+                                  torch.ones(rows, device=DEV))
+    assert torch.equal(o["dw"].long(), (dy * h).sum(0)) and torch.equal(o["db"].long(), dy.sum(0))
+
+
 # ---- in place, where a row's end cuts a piece ----------------------------------------------
 # Such a piece comes as the row's last eight elements, some of which another lane, perhaps of another wavefront, owns and
 # writes: they have to be read before that.  Odd widths for each number of threads a row, rows for several rounds.
